@@ -287,6 +287,75 @@ int monta_combine_staged(const monta_cfg *cfg, const void *y_stage, const float 
 int monta_unregather_combine(const monta_cfg *cfg, const void *y, void *y_stage, const float *gates, void *out,
                              const void *ws, void *stream);
 
+/* ---- 8-bit rows, the norm that writes them, and the expert layer that reads them ----
+ * A row of 8 bits holds hidden e4m3 codes (OCP, largest finite value 448), one after the other, then ceil(hidden / 128) fp32
+ * scales, one for each block of 128 codes (the last block may be shorter), then zeros up to a multiple of 128 bytes; an element is
+ * its code times its block's scale.  hidden has to be a multiple of 16.
+ *
+ * Such rows travel through every entry point that moves rows, bit for bit: monta_fp8_rows (host only) gives the configuration to
+ * call those with (cfg with dtype MONTA_BF16 and half the row's bytes as hidden) and the bytes of a row.  The plan tables do not
+ * depend on hidden or dtype, so a workspace that was routed under either configuration serves both. */
+int monta_fp8_rows(const monta_cfg *cfg, monta_cfg *rows, int64_t *row_bytes);
+
+/* Root-mean-square norm of token rows, with the addition of a residual before it and 8-bit rows behind it:
+ *   s = x + residual, rounded to cfg->dtype (s = x where residual is NULL);  r = 1 / sqrt(mean_h(s^2) + eps)
+ *   v[h] = s[h] * r * weight[h];  out = v rounded once to cfg->dtype;  out_fp8: v with the scale amax / 448 per block, amax the
+ *   largest |v| of the block but at least 2^-40, codes rounded to nearest-even from v (not from out).
+ * x, residual, sum, out [T][H] and weight [H] in cfg->dtype, out_fp8 [T] rows as above, all device pointers, 16-byte aligned.  sum takes s; it
+ * is given if and only if residual is.  out or out_fp8 may be NULL, not both.  sum and out may be x or residual themselves (not
+ * both the same buffer); otherwise nothing may share memory.  Sums are held in fp32: the squares of a row have to add up to a
+ * finite fp32 number; a row with an infinity or a NaN gives NaN in its own outputs and changes no other row.  eps >= 0 (with eps =
+ * 0 a row of zeros gives NaN).  Rows of at most 32 KiB (MONTA_ERR_UNSUPPORTED beyond).  Uses only tokens, hidden and dtype of cfg (all of it is
+ * validated); needs no workspace. */
+int monta_rmsnorm(const monta_cfg *cfg, const void *x, const void *residual, const void *weight, float eps, void *sum, void *out,
+                  void *out_fp8, void *stream);
+
+/* Host only: bytes of the scratch buffer of monta_rmsnorm_backward. */
+int monta_rmsnorm_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
+
+/* Gradient of the norm.  sum: the stored s (x where there was no residual); dout: gradient of out; dsum: gradient that reaches s
+ * by another way (along the residual), or NULL.  With n = s r and g = dout weight:
+ *   dx = r (g - n mean_h(g n)) + dsum, rounded once: the gradient of x and of the residual alike;
+ *   dweight[h] = sum_t dout[t][h] n[t][h], fp32.
+ * The rounding to 8 bits is passed through as if it were not there.  sum, dout, dsum, dx [T][H] and weight [H] in cfg->dtype, 16-byte
+ * aligned; dweight [H] fp32; scratch 16-byte aligned, its contents are of no use afterwards and calls that overlap in time need one
+ * each.  dx may be sum, dout or dsum itself; otherwise nothing may share memory.  The order of the additions is fixed for a shape.
+ * Rows of at most 32 KiB. */
+int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *weight, float eps, const void *dout, const void *dsum,
+                           void *dx, float *dweight, void *scratch, void *stream);
+
+/* The expert layer on 8-bit rows and 8-bit weights:
+ *   y[r][n] = sum_b xs[r][b] * ws[e][n / 128][b] * sum_{h in block b} xc[r][h] * wc[e][n][h]   for every kept row r of expert e,
+ * x_rows [max_rows] rows as above in FINAL order, w_codes [E][out_features][H] e4m3, w_scales [E][ceil(out_features / 128)]
+ * [ceil(H / 128)] fp32, one for each 128 x 128 block of an expert's weights; y [max_rows][out_features] in cfg->dtype.  Device
+ * pointers, 16-byte aligned (w_scales 4-byte); H a multiple of 16, at most 65536; out_features a multiple of 8 (bf16) or 4 (fp32), slice, rows that are not written
+ * and the workspace as in monta_expert_linear.  y, rounded once to cfg->dtype, may share no memory with what is read.  With cfg->dtype
+ * MONTA_BF16 the codes are multiplied by the matrix cores' 8-bit instructions, which drop what lies more than 13 bits below the
+ * largest of a few neighbouring products (1.5e-5 of a block's sum on normal data, a hundredth of the rounding of y); the blocks'
+ * sums are scaled and added in fp32.  With MONTA_FP32 products are exact and all sums fp32, at a lower rate. */
+int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows, const void *w_codes, const float *w_scales, int32_t out_features,
+                            void *y, const void *ws, int slice, void *stream);
+
+/* ---- gradients ---- */
+
+/* Gradient of monta_expert_linear over all kept rows:
+ *   dx_final[r][h] = sum_n dy[r][n] * w_exp[e][n][h]  for every kept row r of expert e,
+ *   dw_exp[e][n][h] = sum over the kept rows r of expert e of dy[r][n] * x_final[r][h]; zero for an expert without rows.
+ * Layouts, types and alignment as in monta_expert_linear, dy like y, dx_final like x_final, dw_exp like w_exp.  Either of dx_final and
+ * dw_exp may be NULL (then w_exp, or x_final, may be, too).  fp32 accumulation, one rounding; the order of the additions is fixed for a
+ * shape and a load.  Rows of no expert are neither read nor written.  No output may share memory with an input or the other output.
+ * hidden and out_features at most 2^20. */
+int monta_expert_linear_backward(const monta_cfg *cfg, const void *dy, const void *x_final, const void *w_exp, int32_t out_features,
+                                 void *dx_final, void *dw_exp, const void *ws, void *stream);
+
+/* Gradient of monta_combine: for every kept choice j of token t, with r = pos_final[t][j],
+ *   dy[r] = gates[t][j] * dout[t], rounded once;  dgates[t][j] = sum_h dout[t][h] * y[r][h], fp32, 0 for a dropped choice.
+ * dout [T][H], y and dy [max_rows][H] in cfg->dtype, 16-byte aligned; gates, dgates [T][k] fp32.  Rows of no choice are neither read
+ * nor written.  No output may share memory with an input or the other output.  Rows of at most 32 KiB.
+ * (The gradient of the dispatch needs no call of its own: a token's is the sum of its rows', monta_combine with gates of one.) */
+int monta_combine_backward(const monta_cfg *cfg, const void *dout, const void *y, const float *gates, void *dy, float *dgates,
+                           const void *ws, void *stream);
+
 /* Pipeline realisations for monta_dispatch_regather:
  *   0  two streams: packs on `stream`, regathers on a library-owned side stream
  *      (default priority), one event per slice, joined back into `stream`;
@@ -371,7 +440,13 @@ enum monta_kernel_id {
     MONTA_K_RETURN = 16,    /* the mirrored return path in one pass           */
     MONTA_K_SCAN = 17,      /* scan of a histogram table too large to rebuild  */
     MONTA_K_SMALL_STEP = 18, /* routing, plan, rows and combine of a small problem in one launch */
-    MONTA_K_COUNT = 19
+    MONTA_K_NORM = 19,          /* root-mean-square norm                      */
+    MONTA_K_NORM_BACKWARD = 20, /* its gradient by the input                  */
+    MONTA_K_NORM_DWEIGHT = 21,  /* the weight's partial sums added            */
+    MONTA_K_EXPERT_SCALED = 22, /* expert layer on 8-bit rows and weights     */
+    MONTA_K_EXPERT_BACKWARD = 23, /* gradients of the expert layer            */
+    MONTA_K_COMBINE_BACKWARD = 24, /* gradients of the combine                */
+    MONTA_K_COUNT = 25
 };
 int monta_profile_enable(int on);
 int monta_profile_reset(void);

@@ -25,7 +25,7 @@ FP32, BF16 = 0, 1
  K_UNREGATHER_COMBINE, K_ALLGATHER, K_GATE, K_EXPERT) = range(13)
 KERNEL_NAMES = ["route_plan", "positions", "pack", "regather", "pack_regather", "combine", "copy", "plan_pack",
                 "unregather", "unregather_combine", "allgather", "gate", "expert", "allgather_regather", "place", "plan_place", "return",
-                "block_scan", "small_step"]
+                "block_scan", "small_step", "norm", "norm_backward", "norm_dweight", "expert_scaled", "expert_backward", "combine_backward"]
 
 
 class MontaError(RuntimeError):
@@ -79,7 +79,9 @@ EXPORTS = ["monta_workspace_bytes", "monta_ws_layout_query", "monta_ws_init", "m
            "monta_unregather_combine", "monta_allgather", "monta_set_pipeline_mode",
            "monta_get_pipeline_mode", "monta_set_plan_mode", "monta_get_plan_mode", "monta_set_cache_policy", "monta_get_cache_policy", "monta_copy", "monta_profile_enable", "monta_profile_reset",
            "monta_profile_read", "monta_plan_chunk_times", "monta_plan_strategy", "monta_strerror",
-           "monta_last_hip_error", "monta_shutdown", "monta_route_dispatch_combine_static", "monta_pipeline_query", "monta_allgather_regather"]
+           "monta_last_hip_error", "monta_shutdown", "monta_route_dispatch_combine_static", "monta_pipeline_query", "monta_allgather_regather",
+           "monta_fp8_rows", "monta_rmsnorm", "monta_rmsnorm_scratch_bytes", "monta_rmsnorm_backward", "monta_combine_backward",
+           "monta_expert_linear_fp8", "monta_expert_linear_backward"]
 
 _lib = None
 
@@ -128,6 +130,13 @@ def lib() -> ctypes.CDLL:
         L.monta_shutdown.argtypes = []
         L.monta_pipeline_query.argtypes = [cfgp] + [ctypes.POINTER(ctypes.c_int32)] * 4
         L.monta_route_dispatch_combine_static.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.monta_fp8_rows.argtypes = [cfgp, cfgp, i64p]
+        L.monta_rmsnorm.argtypes = [cfgp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp]
+        L.monta_rmsnorm_scratch_bytes.argtypes = [cfgp, ctypes.POINTER(ctypes.c_size_t)]
+        L.monta_rmsnorm_backward.argtypes = [cfgp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp, vp]
+        L.monta_combine_backward.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp]
+        L.monta_expert_linear_fp8.argtypes = [cfgp, vp, vp, vp, i32, vp, vp, i32, vp]
+        L.monta_expert_linear_backward.argtypes = [cfgp, vp, vp, vp, i32, vp, vp, vp, vp]
         for name in EXPORTS:
             if name != "monta_strerror":
                 getattr(L, name).restype = ctypes.c_int
@@ -136,7 +145,9 @@ def lib() -> ctypes.CDLL:
 
 
 _HOST_ENTRIES = ["monta_ws_layout_query", "monta_route", "monta_route_dispatch_regather", "monta_route_dispatch_combine_static",
-                 "monta_combine", "monta_unregather_combine", "monta_gate", "monta_expert_linear", "monta_route_dispatch_expert"]
+                 "monta_combine", "monta_unregather_combine", "monta_gate", "monta_expert_linear", "monta_route_dispatch_expert",
+                 "monta_rmsnorm", "monta_rmsnorm_scratch_bytes", "monta_rmsnorm_backward", "monta_combine_backward", "monta_expert_linear_fp8",
+                 "monta_expert_linear_backward"]
 _native = None
 
 
@@ -150,7 +161,7 @@ def _host():
         import torch  # noqa: F401  (its libraries have to be loaded before _host.so)
         from . import _host as native
         L = lib()
-        native.setup(monta_cfg, _ptr, _stream, _current_raw_stream, _check,
+        native.setup(monta_cfg, _ptr, _stream, _current_raw_stream, _check, _current_device,
                      tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _HOST_ENTRIES))
         _native = native
     return _native
@@ -217,6 +228,19 @@ def _current_raw_stream() -> int:
             _raw_stream = (lambda _: torch.cuda.current_stream().cuda_stream), (lambda: None)
     get, device = _raw_stream
     return get(device())
+
+
+_device = None
+
+
+def _current_device() -> int:
+    """The current device's number: the function behind torch.cuda.current_device(), without its own look at whether the
+    runtime is there (a tensor on a device is)."""
+    global _device
+    if _device is None:
+        import torch
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device()
 
 
 def _stream(stream) -> int:
@@ -362,6 +386,39 @@ def monta_route_dispatch_expert(cfg, logits, x, topk_idx, gates, stage, final, w
                                 overlap: int = 1, stream=None):
     (_native or _host()).route_dispatch_expert(cfg, logits, x, topk_idx, gates, stage, final, w_exp, int(out_features), y, ws,
                                               int(overlap), stream)
+
+
+def monta_fp8_rows(cfg):
+    """-> (the configuration under which 8-bit rows are moved, their bytes)."""
+    rows, n = monta_cfg(), ctypes.c_int64(0)
+    _check(lib().monta_fp8_rows(ctypes.byref(cfg), ctypes.byref(rows), ctypes.byref(n)), "monta_fp8_rows")
+    return rows, int(n.value)
+
+
+def monta_rmsnorm(cfg, x, residual, weight, eps: float, sum, out, out_fp8=None, stream=None):
+    (_native or _host()).rmsnorm(cfg, x, residual, weight, eps, sum, out, out_fp8, stream)
+
+
+def monta_rmsnorm_scratch_bytes(cfg) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().monta_rmsnorm_scratch_bytes(ctypes.byref(cfg), ctypes.byref(n)), "monta_rmsnorm_scratch_bytes")
+    return int(n.value)
+
+
+def monta_rmsnorm_backward(cfg, sum, weight, eps: float, dout, dsum, dx, dweight, scratch, stream=None):
+    (_native or _host()).rmsnorm_backward(cfg, sum, weight, eps, dout, dsum, dx, dweight, scratch, stream)
+
+
+def monta_combine_backward(cfg, dout, y, gates, dy, dgates, ws, stream=None):
+    (_native or _host()).combine_backward(cfg, dout, y, gates, dy, dgates, ws, stream)
+
+
+def monta_expert_linear_fp8(cfg, x_rows, w_codes, w_scales, out_features: int, y, ws, slice: int = -1, stream=None):
+    (_native or _host()).expert_linear_fp8(cfg, x_rows, w_codes, w_scales, int(out_features), y, ws, int(slice), stream)
+
+
+def monta_expert_linear_backward(cfg, dy, x_final, w_exp, out_features: int, dx_final, dw_exp, ws, stream=None):
+    (_native or _host()).expert_linear_backward(cfg, dy, x_final, w_exp, int(out_features), dx_final, dw_exp, ws, stream)
 
 
 def monta_copy(dst, src, nbytes: int, stream=None):

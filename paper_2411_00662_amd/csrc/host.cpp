@@ -12,8 +12,8 @@
 
 namespace {
 
-// from binding.py: the cfg class, _ptr, _stream, _current_raw_stream, _check; kept until the process ends
-PyObject *g_cfg_type, *g_ptr, *g_stream, *g_current_stream, *g_check;
+// from binding.py: the cfg class, _ptr, _stream, _current_raw_stream, _check, _current_device; kept until the process ends
+PyObject *g_cfg_type, *g_ptr, *g_stream, *g_current_stream, *g_check, *g_current_device;
 decltype(&monta_ws_layout_query) g_layout;
 decltype(&monta_route) g_route;
 decltype(&monta_route_dispatch_regather) g_route_dispatch_regather;
@@ -23,6 +23,12 @@ decltype(&monta_unregather_combine) g_unregather_combine;
 decltype(&monta_gate) g_gate;
 decltype(&monta_expert_linear) g_expert_linear;
 decltype(&monta_route_dispatch_expert) g_route_dispatch_expert;
+decltype(&monta_rmsnorm) g_rmsnorm;
+decltype(&monta_rmsnorm_scratch_bytes) g_rmsnorm_scratch_bytes;
+decltype(&monta_rmsnorm_backward) g_rmsnorm_backward;
+decltype(&monta_combine_backward) g_combine_backward;
+decltype(&monta_expert_linear_fp8) g_expert_linear_fp8;
+decltype(&monta_expert_linear_backward) g_expert_linear_backward;
 
 // One call: sizes from its cfg, then its arguments in order.  The first failure leaves a Python error and ends the rest.
 struct Call {
@@ -31,6 +37,7 @@ struct Call {
     monta_ws_layout L;
     const char *what;
     bool ok = false;
+    long device = -1;               // of the tensors seen by on_device()
     Size T, E, k, bpe, row;
 
     Call(const char *name, PyObject *const *args, Py_ssize_t n, Py_ssize_t want, bool layout) : what(name)
@@ -75,7 +82,7 @@ struct Call {
     template <typename V = void>
     V *ptr(PyObject *o, Size need, const char *name)
     {
-        if (!ok) return nullptr;
+        if (!ok || o == Py_None) return nullptr;        // the library says what is missing
         if (THPVariable_CheckTypeExact(Py_TYPE(o))) {
             try {
                 const at::Tensor &t = THPVariable_Unpack(o);
@@ -90,6 +97,31 @@ struct Call {
         return static_cast<V *>(p);
     }
 
+    // The same for a buffer that has to lie on the current device, where the kernels will run.
+    template <typename V = void>
+    V *on_device(PyObject *o, Size need, const char *name)
+    {
+        V *p = ptr<V>(o, need, name);
+        if (!ok || o == Py_None || !THPVariable_Check(o)) return p;
+        if (device < 0) {
+            PyObject *d = PyObject_CallNoArgs(g_current_device);
+            if (d) {
+                device = PyLong_AsLong(d);
+                Py_DECREF(d);
+            }
+            if (PyErr_Occurred()) {
+                ok = false;
+                return nullptr;
+            }
+        }
+        const long at = THPVariable_Unpack(o).get_device();
+        if (at != device) {
+            PyErr_Format(PyExc_ValueError, "%s: the tensor is on device %ld, the current device is %ld", name, at, device);
+            ok = false;
+        }
+        return p;
+    }
+
     // an argument that binding.py has turned into a number; as ctypes does, its low 32 bits
     Size number(PyObject *o)
     {
@@ -98,6 +130,13 @@ struct Call {
         const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
         if (PyErr_Occurred()) ok = false;
         return overflow > 0 ? (Size)INT64_MAX : overflow < 0 ? (Size)INT64_MIN : (Size)v;
+    }
+    double real(PyObject *o)
+    {
+        if (!ok) return 0.0;
+        const double v = PyFloat_AsDouble(o);
+        if (PyErr_Occurred()) ok = false;
+        return v;
     }
     static int low32(PyObject *o) { return (int)(uint32_t)PyLong_AsUnsignedLongLongMask(o); }
 
@@ -220,20 +259,96 @@ PyObject *route_dispatch_expert(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// setup(cfg class, _ptr, _stream, _current_raw_stream, _check, address of each entry point in the order below)
+PyObject *rmsnorm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_rmsnorm", a, n, 9, false);
+    if (!c.ok) return nullptr;
+    const Call::Size rows = c.T * c.row, H = c.cfg.hidden;
+    const void *x = c.on_device(a[1], rows, "x"), *residual = c.on_device(a[2], rows, "residual"), *w = c.on_device(a[3], c.row, "weight");
+    const double eps = c.real(a[4]);
+    void *sum = c.on_device(a[5], rows, "sum"), *out = c.on_device(a[6], rows, "out");
+    void *out8 = c.on_device(a[7], c.T * ((H + 4 * ((H + 127) / 128) + 127) / 128 * 128), "out_fp8"), *st = c.stream(a[8]);
+    return c.finish([&] { return g_rmsnorm(&c.cfg, x, residual, w, (float)eps, sum, out, out8, st); });
+}
+
+PyObject *rmsnorm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_rmsnorm_backward", a, n, 10, false);
+    if (!c.ok) return nullptr;
+    const Call::Size rows = c.T * c.row;
+    size_t scratch_bytes = 0;
+    if (const int rc = g_rmsnorm_scratch_bytes(&c.cfg, &scratch_bytes)) return Call::check(rc, c.what);
+    const void *sum = c.on_device(a[1], rows, "sum"), *w = c.on_device(a[2], c.row, "weight");
+    const double eps = c.real(a[3]);
+    const void *dout = c.on_device(a[4], rows, "dout"), *dsum = c.on_device(a[5], rows, "dsum");
+    void *dx = c.on_device(a[6], rows, "dx");
+    float *dw = c.on_device<float>(a[7], (Call::Size)c.cfg.hidden * 4, "dweight");
+    void *scratch = c.on_device(a[8], scratch_bytes, "scratch"), *st = c.stream(a[9]);
+    return c.finish([&] { return g_rmsnorm_backward(&c.cfg, sum, w, (float)eps, dout, dsum, dx, dw, scratch, st); });
+}
+
+PyObject *combine_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_combine_backward", a, n, 8, true);
+    if (!c.ok) return nullptr;
+    const void *dout = c.on_device(a[1], c.T * c.row, "dout"), *y = c.on_device(a[2], c.L.max_rows * c.row, "y");
+    const float *gates = c.on_device<float>(a[3], c.T * c.k * 4, "gates");
+    void *dy = c.on_device(a[4], c.L.max_rows * c.row, "dy");
+    float *dgates = c.on_device<float>(a[5], c.T * c.k * 4, "dgates");
+    const void *ws = c.on_device(a[6], c.L.ws_bytes, "ws");
+    void *st = c.stream(a[7]);
+    return c.finish([&] { return g_combine_backward(&c.cfg, dout, y, gates, dy, dgates, ws, st); });
+}
+
+PyObject *expert_linear_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_expert_linear_fp8", a, n, 9, true);
+    if (!c.ok) return nullptr;
+    const Call::Size N = c.number(a[4]), H = c.cfg.hidden, blocks = (H + 127) / 128;
+    const void *x = c.on_device(a[1], c.L.max_rows * ((H + 4 * blocks + 127) / 128 * 128), "x_rows"), *w = c.on_device(a[2], c.E * N * H, "w_codes");
+    const float *scales = c.on_device<float>(a[3], c.E * ((N + 127) / 128) * blocks * 4, "w_scales");
+    void *y = c.on_device(a[5], c.L.max_rows * N * c.bpe, "y");
+    const void *ws = c.on_device(a[6], c.L.ws_bytes, "ws");
+    void *st = c.stream(a[8]);
+    const int out_features = Call::low32(a[4]), slice = Call::low32(a[7]);
+    return c.finish([&] { return g_expert_linear_fp8(&c.cfg, x, w, scales, out_features, y, ws, slice, st); });
+}
+
+PyObject *expert_linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_expert_linear_backward", a, n, 9, true);
+    if (!c.ok) return nullptr;
+    const Call::Size N = c.number(a[4]), rows = c.L.max_rows;
+    const void *dy = c.on_device(a[1], rows * N * c.bpe, "dy"), *x = c.on_device(a[2], rows * c.row, "x_final"),
+               *w = c.on_device(a[3], c.E * N * c.row, "w_exp");
+    void *dx = c.on_device(a[5], rows * c.row, "dx_final"), *dw = c.on_device(a[6], c.E * N * c.row, "dw_exp");
+    const void *ws = c.on_device(a[7], c.L.ws_bytes, "ws");
+    void *st = c.stream(a[8]);
+    const int out_features = Call::low32(a[4]);
+    return c.finish([&] { return g_expert_linear_backward(&c.cfg, dy, x, w, out_features, dx, dw, ws, st); });
+}
+
+// setup(cfg class, _ptr, _stream, _current_raw_stream, _check, _current_device, address of each entry point in the order below)
 PyObject *setup(PyObject *, PyObject *args)
 {
-    PyObject *cfg, *ptr, *stream, *current, *check;
-    unsigned long long f[9];
-    if (!PyArg_ParseTuple(args, "OOOOO(KKKKKKKKK)", &cfg, &ptr, &stream, &current, &check, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7,
-                          f + 8))
+    PyObject *cfg, *ptr, *stream, *current, *check, *device, *entries;
+    constexpr int kEntries = 15;
+    unsigned long long f[kEntries];
+    if (!PyArg_ParseTuple(args, "OOOOOOO!", &cfg, &ptr, &stream, &current, &check, &device, &PyTuple_Type, &entries)) return nullptr;
+    if (PyTuple_GET_SIZE(entries) != kEntries) {
+        PyErr_SetString(PyExc_TypeError, "setup: another number of entry points");
         return nullptr;
+    }
+    for (int i = 0; i < kEntries; ++i) {
+        f[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(entries, i));
+        if (PyErr_Occurred()) return nullptr;
+    }
     if (!PyType_Check(cfg)) {
         PyErr_SetString(PyExc_TypeError, "setup: the first argument is not a class");
         return nullptr;
     }
-    for (PyObject *o : {cfg, ptr, stream, current, check}) Py_INCREF(o);
-    g_cfg_type = cfg, g_ptr = ptr, g_stream = stream, g_current_stream = current, g_check = check;
+    for (PyObject *o : {cfg, ptr, stream, current, check, device}) Py_INCREF(o);
+    g_cfg_type = cfg, g_ptr = ptr, g_stream = stream, g_current_stream = current, g_check = check, g_current_device = device;
     auto set = [](auto &fn, unsigned long long at) { fn = reinterpret_cast<std::decay_t<decltype(fn)>>((uintptr_t)at); };
     set(g_layout, f[0]);
     set(g_route, f[1]);
@@ -244,6 +359,12 @@ PyObject *setup(PyObject *, PyObject *args)
     set(g_gate, f[6]);
     set(g_expert_linear, f[7]);
     set(g_route_dispatch_expert, f[8]);
+    set(g_rmsnorm, f[9]);
+    set(g_rmsnorm_scratch_bytes, f[10]);
+    set(g_rmsnorm_backward, f[11]);
+    set(g_combine_backward, f[12]);
+    set(g_expert_linear_fp8, f[13]);
+    set(g_expert_linear_backward, f[14]);
     Py_RETURN_NONE;
 }
 
@@ -251,6 +372,7 @@ PyObject *setup(PyObject *, PyObject *args)
 PyMethodDef g_methods[] = {
     {"setup", setup, METH_VARARGS, nullptr}, MONTA_FAST(route), MONTA_FAST(route_dispatch_regather), MONTA_FAST(route_dispatch_combine_static),
     MONTA_FAST(combine), MONTA_FAST(unregather_combine), MONTA_FAST(gate), MONTA_FAST(expert_linear), MONTA_FAST(route_dispatch_expert),
+    MONTA_FAST(rmsnorm), MONTA_FAST(rmsnorm_backward), MONTA_FAST(combine_backward), MONTA_FAST(expert_linear_fp8), MONTA_FAST(expert_linear_backward),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -13,6 +13,7 @@
 #include <mutex>
 #include <vector>
 
+#include "monta_internal.hpp"
 #include "monta_kernels.hpp"
 #include "monta_planner.hpp"
 
@@ -244,8 +245,6 @@ PlanPtrs plan_ptrs(const Geometry &g, const void *ws)
     return p;
 }
 
-inline bool misaligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-
 // ------------------------------------------------------------- profiling
 //
 // One event is recorded after every kernel launch, on the launching stream.  A
@@ -274,45 +273,91 @@ void prof_break_chain(hipStream_t st)
         if (pr.first == st) pr.second = nullptr;
 }
 
-struct ProfScope {
-    hipStream_t st;
-    int kid;
-    hipEvent_t a = nullptr;
-    bool on;
-    ProfScope(int kid_, hipStream_t st_) : st(st_), kid(kid_), on(g_prof_on.load() != 0)
-    {
-        if (!on) return;
-        std::lock_guard<std::mutex> lk(g_prof_mu);
-        for (auto &pr : g_prof_last)
-            if (pr.first == st) a = pr.second;
-        if (!a) {
-            if (hipEventCreate(&a) != hipSuccess) {
-                on = false;
-                a = nullptr;
-                return;
-            }
-            g_prof_events.push_back(a);
-            (void)hipEventRecord(a, st);
+using ProfScope = LaunchTimer;
+
+}  // namespace
+
+namespace monta {
+
+LaunchTimer::LaunchTimer(int kid_, hipStream_t st_) : st(st_), kid(kid_), on(g_prof_on.load() != 0)
+{
+    if (!on) return;
+    std::lock_guard<std::mutex> lk(g_prof_mu);
+    for (auto &pr : g_prof_last)
+        if (pr.first == st) a = pr.second;
+    if (!a) {
+        if (hipEventCreate(&a) != hipSuccess) {
+            on = false;
+            a = nullptr;
+            return;
         }
+        g_prof_events.push_back(a);
+        (void)hipEventRecord(a, st);
     }
-    ~ProfScope()
-    {
-        if (!on) return;
-        hipEvent_t b = nullptr;
-        if (hipEventCreate(&b) != hipSuccess) return;
-        (void)hipEventRecord(b, st);
-        std::lock_guard<std::mutex> lk(g_prof_mu);
-        g_prof_events.push_back(b);
-        g_prof_recs.push_back({kid, a, b});
-        bool found = false;
-        for (auto &pr : g_prof_last)
-            if (pr.first == st) {
-                pr.second = b;
-                found = true;
-            }
-        if (!found) g_prof_last.push_back({st, b});
+}
+
+LaunchTimer::~LaunchTimer()
+{
+    if (!on) return;
+    hipEvent_t b = nullptr;
+    if (hipEventCreate(&b) != hipSuccess) return;
+    (void)hipEventRecord(b, st);
+    std::lock_guard<std::mutex> lk(g_prof_mu);
+    g_prof_events.push_back(b);
+    g_prof_recs.push_back({kid, a, b});
+    bool found = false;
+    for (auto &pr : g_prof_last)
+        if (pr.first == st) {
+            pr.second = b;
+            found = true;
+        }
+    if (!found) g_prof_last.push_back({st, b});
+}
+
+int hip_failed(hipError_t e)
+{
+    g_last_hip = (int)e;
+    (void)hipGetLastError();
+    return MONTA_ERR_HIP;
+}
+
+int open_call(const monta_cfg *cfg, const void *ws, Call *out)
+{
+    Geometry g;
+    if (int rc = validate(cfg, &g)) return rc;
+    out->s = g.s;
+    out->max_rows = g.max_rows;
+    out->kept_bound = std::min<int64_t>((int64_t)g.s.T * g.s.k, (int64_t)g.s.E * g.s.C);
+    out->row_bytes = g.row_bytes;
+    out->ws_bytes = ws_bytes(g);
+    out->H = cfg->hidden;
+    out->bf16 = cfg->dtype == MONTA_BF16;
+    if (ws) out->p = plan_ptrs(g, ws);
+    return MONTA_OK;
+}
+
+void expert_ranges(const Shape &s, const PlanPtrs &p, int slice, ExpertArgs *a)
+{
+    a->lo = slice < 0 ? p.offsets : p.unit_base + (int64_t)slice * s.tp * s.E;
+    if (slice >= 0 && slice + 1 < s.S) {
+        a->hi_base = p.unit_base + (int64_t)(slice + 1) * s.tp * s.E;
+        a->hi_len = nullptr;
+    } else {
+        a->hi_base = p.offsets;
+        a->hi_len = p.kept;
     }
-};
+}
+
+// worst case of the rows in play: every pair of the slice's tokens kept, as far as the capacity lets them (the rows of a
+// padded layout beyond them are never multiplied)
+int64_t slice_kept_bound(const Shape &s, int64_t kept_bound, int slice)
+{
+    return slice < 0 ? kept_bound : std::min<int64_t>(kept_bound, (int64_t)(s.T / s.S) * s.k);
+}
+
+}  // namespace monta
+
+namespace {
 
 int prof_drain()
 {
@@ -443,23 +488,6 @@ int check_act_ptrs(const void *a, const void *b)
 {
     if (!a || !b) return MONTA_ERR_NULL;
     if (misaligned(a, 16) || misaligned(b, 16)) return MONTA_ERR_ALIGN;
-    return MONTA_OK;
-}
-
-// Dynamic LDS above the default limit has to be asked for once per kernel and device.
-struct LdsOptIn {
-    std::atomic<int> done[64];
-};
-
-int opt_in_lds(const void *kernel, int bytes, LdsOptIn &state)
-{
-    int dev = 0;
-    HIP_TRY(hipGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return MONTA_ERR_UNSUPPORTED;
-    if (!state.done[dev].load()) {
-        HIP_TRY(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
-        state.done[dev].store(1);
-    }
     return MONTA_OK;
 }
 
@@ -865,13 +893,6 @@ int launch_route(const Geometry &g, const PlanPtrs &p, const float *logits, int3
     return MONTA_OK;
 }
 
-// Do the bytes [a, a + na) and [b, b + nb) share any?
-bool overlap(const void *a, int64_t na, const void *b, int64_t nb)
-{
-    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-    return pa < pb + (uintptr_t)nb && pb < pa + (uintptr_t)na;
-}
-
 // Lanes per token of small_step_kernel, 0 if the problem is not a small one: all tokens have to be covered by one pass of a
 // workgroup's threads, their choices and the plan by its LDS.  And routing them all in every workgroup must not take longer than
 // routing a share of them and waiting for the others, which grows with tokens x experts and, where each row's workgroup does it, with
@@ -1008,19 +1029,8 @@ int launch_expert_layer(const monta_cfg *cfg, const Geometry &g, const void *x_f
     const double with_rows = s.E * (1.0 - std::pow(1.0 - 1.0 / s.E, (double)kept_bound)), touched = with_rows * out_features * w_row;
     a.stream_from = touched >= kStreamWeightsFrom && w_row % 128 == 0 && !misaligned(w_exp, 128)
                         ? (int64_t)(w_rows * (kCacheableWeights / touched)) : w_rows;
-    // rows of expert e: its whole kept segment [offsets[e], offsets[e] + kept[e]), or the part of it filled by the
-    // slice's units, which starts at unit_base[first unit of the slice][e] and ends where the next slice's starts
-    a.lo = slice < 0 ? p.offsets : p.unit_base + (int64_t)slice * s.tp * s.E;
-    if (slice >= 0 && slice + 1 < s.S) {
-        a.hi_base = p.unit_base + (int64_t)(slice + 1) * s.tp * s.E;
-        a.hi_len = nullptr;
-    } else {
-        a.hi_base = p.offsets;
-        a.hi_len = p.kept;
-    }
-    // worst case of the rows in play: every pair of the slice's tokens kept, as far as the capacity lets them (the rows of a
-    // padded layout beyond them are never multiplied)
-    const int64_t rows_bound = slice < 0 ? kept_bound : std::min<int64_t>(kept_bound, (int64_t)(s.T / s.S) * s.k);
+    expert_ranges(s, p, slice, &a);
+    const int64_t rows_bound = slice_kept_bound(s, kept_bound, slice);
     ProfScope ps(MONTA_K_EXPERT, st);
     if (cfg->dtype == MONTA_BF16) {
         // The offsets inside a direct-to-LDS tile have 31 bits.  The choice of tile looks at the whole problem, not at the slice,

@@ -8,54 +8,13 @@
 // dense contractions and run on the matrix cores; they follow further down.
 #pragma once
 
-#include <hip/hip_runtime.h>
-#include <stdint.h>
-
-#include <type_traits>
+#include "monta_device.hpp"
 
 namespace monta {
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-
-constexpr int kWave = 64;
 // Chosen by measurement on MI355X (128 and 512 threads, 2 and 8 vectors in flight were slower or equal).
 constexpr int kMoverThreads = 256;   // threads per workgroup of the row movers
 constexpr int kVecInFlight = 4;      // 16-byte loads issued by a lane before its first store
-
-// meta[] slots (int32)
-enum { META_R = 0, META_ALIVE = 1, META_C = 2, META_FINAL_ROWS = 4, META_SLOTS = 16 };
-
-struct PlanPtrs {
-    int32_t *meta, *counts, *kept, *offsets, *n, *stage_off, *unit_base, *send_rows, *unit_rows;
-    int32_t *pos_final, *pos_stage, *row_map, *block_counts, *block_base, *local_rank, *kept_prefix;
-};
-
-// n / d for 0 <= n < 2^16 and d < 2^15, by a multiplication: an integer division takes about 40 instructions
-struct FastDiv {
-    uint32_t d, m;
-};
-inline FastDiv fast_div(int d) { return {(uint32_t)d, d > 1 ? (uint32_t)((1ull << 32) / (uint32_t)d + 1) : 0u}; }
-__device__ __forceinline__ int operator/(int n, FastDiv f) { return f.m ? (int)__umulhi((uint32_t)n, f.m) : n; }
-
-struct Shape {
-    int32_t T, E, k, ep, tp, S, U, Tu;
-    int32_t TB;        // tokens per route workgroup
-    int32_t bpu;       // route workgroups per unit
-    int32_t num_blocks;
-    int32_t C;         // per-expert capacity
-    int32_t renorm;
-    int32_t vpr;       // 16-byte vectors per activation row
-    int32_t lpr;       // lanes cooperating on one row in the movers (power of two <= kMoverThreads)
-    int32_t max_rows;  // rows STAGE / FINAL hold; every row index read from a table is checked against it
-    int32_t cache;     // CachePolicy bits: which streams of the movers use non-temporal accesses
-    int32_t padded;    // 1: FINAL is [E][C][H] (expert e at row e*C), 0: compact
-    int32_t lazy;      // 1: the single pass requests a token's row only when it knows that one of its choices is kept
-    int32_t rl;        // lanes that share one token in the route kernel (1, 2, 4 or 8)
-    FastDiv by_E, by_k, by_k1, by_Tu, by_ep;       // for the pairs of a route workgroup (by_k1: k - 1) and for small problems
-    int32_t fast_plan; // 1: every workgroup reduces the histogram table; 0: block_scan_kernel scans it first
-};
 
 // A set bit makes that stream non-temporal (streaming, no reuse expected); a clear bit leaves
 // it cacheable, which pays when the consumer kernel finds the data still in the memory-side cache.
@@ -2087,7 +2046,6 @@ __global__ __launch_bounds__(kMoverThreads) void return_units_kernel(const u32x4
 // carries MT*NT accumulator tiles (element i of lane l = row (i/4)*8 + (l/32)*4 + i%4, column l%32), and the
 // waves' partial tiles are added through LDS in a fixed order at the end, so results are reproducible.
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kGateThreads = 512;
@@ -2510,7 +2468,6 @@ __global__ __launch_bounds__(256) void gate_f32_few_kernel(const float4 *__restr
 
 constexpr int kExpBK = 64;
 constexpr int kExpRowStride = kExpBK * 2 + 16;                                  // bytes in LDS
-constexpr int kXcds = 8;
 
 // BM x BN: the workgroup's tile of y; its WM x WN waves each own (BM/WM) x (BN/WN).  One LDS buffer, two barriers
 // per step.  In use: 128 x 256 with 2 x 2 waves, two workgroups per CU.  Measured and not faster on MI355X (all
@@ -2527,74 +2484,6 @@ struct ExpertTile {
     static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0 && kExpBK == 64 && BM % kRowsPerPass == 0 &&
                       BN % kRowsPerPass == 0, "expert kernel: tile shape");
 };
-
-struct ExpertArgs {
-    const int32_t *lo;      // [E] first row of the expert's range
-    const int32_t *hi_base; // [E] one past its last row is hi_base[e] + hi_len[e] ...
-    const int32_t *hi_len;  // [E] ... or hi_base[e] alone if this is nullptr
-    int16_t E;              // one word for three fields: an argument of its own is one more trip to memory in a chain of them
-    int8_t spread;          // 1: the short tiles' walks along the hidden axis start at different steps (walk_start)
-    int8_t deal;            // the short tiles' numbers go to the XCDs in blocks of 1 << deal
-    int32_t H, N, max_rows;
-    int64_t stream_from;    // first row of all experts' weights (expert * N + column) that is requested as streaming (kStreamLoad)
-                            // where one workgroup reads it
-};
-
-// The expert whose tiles include logical tile number L, found without walking the experts one by one (a walk costs
-// one dependent table read per expert before the workgroup can start): 64 experts at a time, one per lane, a wave
-// scan of their tile counts, a ballot for the first lane whose running total passes L.  Every lane of every wave
-// takes part and gets the same answer.  e == E: no such tile (a surplus workgroup).
-struct ExpertTileHit {
-    int e, lo, hi, tiles;     // expert, its row range [lo, hi), its row tiles
-    uint32_t L;               // tile number inside the expert: at most the number asked for, which is below 2^31, as grids are
-};
-
-// WHOLE: only the whole tiles of a segment count (its ragged last tile is numbered elsewhere); `all` returns the
-// number of tiles counted over all experts when L lies past them.
-template <int BM, bool WHOLE = false>
-__device__ __forceinline__ ExpertTileHit find_expert_tile(const ExpertArgs &a, int nct, int64_t L, int lane,
-                                                          int64_t *all = nullptr)
-{
-    ExpertTileHit h;
-    h.e = a.E;
-    h.lo = h.hi = h.tiles = 0;
-    h.L = 0;
-    int64_t before = 0;                                            // tiles of the experts of earlier rounds
-    for (int e0 = 0; e0 < a.E; e0 += kWave) {
-        const int e = e0 + lane;
-        int lo = 0, hi = 0, tiles = 0;
-        if (e < a.E) {
-            lo = a.lo[e];
-            hi = a.hi_base[e] + (a.hi_len ? a.hi_len[e] : 0);
-            tiles = hi > lo ? (int)(((int64_t)hi - lo + (WHOLE ? 0 : BM - 1)) / BM) : 0;
-        }
-        const int64_t cnt = (int64_t)tiles * nct;
-        int64_t incl = cnt;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int64_t o = __shfl_up(incl, d, kWave);
-            if (lane >= d) incl += o;
-        }
-        // 64 bits, and by a shuffle: from a lane read the compiler knows the tile's number for uniform and divides it in scalar code,
-        // four long chains of which cost every large tile's workgroup about 2 us (128 experts of 1024 x 480, 512 rows each 97 and 94).
-        // The quotients themselves are of 32 bits: those of 64 cost short tiles up to 2 % (fp32, 8 of 512 x 2496, 105 rows 28.9 and 28.3)
-        const int64_t total = __shfl(incl, kWave - 1, kWave);
-        if (L < before + total) {
-            // an expert without tiles repeats its predecessor's running total, so the first lane past L has tiles
-            const unsigned long long past = __ballot(L < before + incl);
-            const int src = __ffsll((long long)past) - 1;
-            h.e = e0 + src;
-            h.lo = __shfl(lo, src, kWave);
-            h.hi = __shfl(hi, src, kWave);
-            h.tiles = __shfl(tiles, src, kWave);
-            h.L = (uint32_t)(L - before - (__shfl(incl, src, kWave) - __shfl(cnt, src, kWave)));
-            return h;
-        }
-        before += total;
-    }
-    if (all) *all = before;
-    return h;
-}
 
 __device__ __forceinline__ unsigned int f32_to_bf16_rne(float f)
 {
@@ -2757,11 +2646,6 @@ constexpr int kBigXBytes = kBigBM * 128, kBigWBytes = kBigBN * 128;       // one
 // two stages of x; of w three, which takes all of a CU's 160 KiB, or two and 512 bytes per wave for the early touches
 constexpr int big_lds_bytes(bool deep_w) { return 2 * kBigXBytes + (deep_w ? 3 * kBigWBytes : 2 * kBigWBytes + 2048); }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *p, uint32_t bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000);
-}
-typedef __attribute__((address_space(3))) void lds_void;
 // Cache bits of a buffer load: `nt`, no reuse expected.  On weights that only one workgroup reads and that would not stay in the
 // memory-side cache until the next call it is worth 10-17 %, as the lines push nothing else out on their way.  Where it is not: on
 // rows that are not whole lines (a line at the seam of two rows is fetched twice), on a tile with a second reader, on weights
@@ -2769,7 +2653,6 @@ typedef __attribute__((address_space(3))) void lds_void;
 // and without).  Three sets of weights in turn, plain and streamed: 64 experts of 7168 x 2048, 16 rows 311 and 277 us; but 16 of
 // 8184 x 2048 112 and 127; 16 of 4096 x 1024 in 32 x 64 tiles, 40 rows 31 and 37; 8 of 2048 x 2048 12.7 and 14.8.
 constexpr int kStreamLoad = 2;
-constexpr uint32_t kOutOfRange = 0x80000000u;                      // a lane offset past every descriptor: no access
 
 // Scalar offset of the 128 bytes that follow those at `at` in every row of a tile of `turn` / 128 steps: from the last step round to the
 // first.  The range check of a buffer load compares the lane's offset with num_records - scalar offset in 32 bits, and the smallest
@@ -2786,7 +2669,6 @@ constexpr bool step_offsets_stay_inside(int nsteps, int start, int past)
 }
 static_assert(step_offsets_stay_inside(1, 0, 8) && step_offsets_stay_inside(2, 1, 8) && step_offsets_stay_inside(7, 5, 8),
               "a one-row tile must refuse the loads of the steps past its end");
-constexpr int kBigMaxHidden = 1 << 20;                             // a tile's 256 rows end far below it
 
 // four fp32 -> four bf16, nearest-even, as 8 bytes
 __device__ __forceinline__ uint2 pack_bf16x4(f32x4 v)
@@ -2795,15 +2677,6 @@ __device__ __forceinline__ uint2 pack_bf16x4(f32x4 v)
     o.x = f32_to_bf16_rne(v[0]) | (f32_to_bf16_rne(v[1]) << 16);
     o.y = f32_to_bf16_rne(v[2]) | (f32_to_bf16_rne(v[3]) << 16);
     return o;
-}
-
-// Where tile number `tile` starts its walk along the hidden axis.  Rows that are a multiple of 4096 bytes apart begin on the same memory
-// channels, so that workgroups which walk in step all wait for a few of them: 256 MiB of weights in rows of 8192 bytes, 64 rows a workgroup,
-// read and nothing else, arrive in 52 us, at 14336 bytes a row in 39 (6.9 TB/s); with the starts spread over the row in 39 and 39.  The
-// multiplier spreads consecutive tiles evenly over any number of steps.  Rows have to be whole steps.
-__device__ __forceinline__ int walk_start(int tile, int nsteps)
-{
-    return (int)(((uint32_t)tile * 40503u & 0xffffu) * (uint32_t)nsteps >> 16);
 }
 
 // A tile of at most XR rows x WR output features: so little arithmetic per step that the step is as long as its loads take
