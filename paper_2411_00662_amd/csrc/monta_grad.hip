@@ -12,7 +12,6 @@ namespace monta {
 namespace {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
@@ -22,25 +21,31 @@ struct GradArgs {
     void *out;
 };
 
+constexpr int kShortTileRows = 64;       // ragged tiles of dx up to this many rows run as short tiles
+
 // What a tile of the output belongs to.
 struct GradTile {
     int e, row0, row_end;   // expert; rows of the tile (dx), or all rows of the expert (dw)
     int rt, ct;             // row tile and column tile inside the expert
+    int side, share;        // row tiles next to one another on one column tile; which of them
 };
 
 // Tile of this workgroup; e < 0: none.  Logical tile numbers go out in blocks of 256, 32 consecutive ones to each XCD (hardware deals
 // consecutive workgroups round robin to the 8 XCDs, each with its own L2); inside an expert the numbering is (panel of 8 row
 // tiles, column tile, row tile), so that an XCD's workgroups share operand tiles.
-template <bool DW, int BR>
-__device__ __forceinline__ GradTile find_grad_tile(const ExpertArgs &a, int nct, int lane)
+// RAGGED_LAST, of dx: the whole tiles of all experts come first and the segments' ragged last tiles after them, the one with the most
+// rows first, so that the last round of workgroups consists of the tiles that cost least.  `scratch`: 257 words of LDS that nothing else uses yet.
+template <bool DW, int BR, bool RAGGED_LAST>
+__device__ __forceinline__ GradTile find_grad_tile(const ExpertArgs &a, int nct, int lane, int *scratch)
 {
     constexpr int P = 8;
+    static_assert(!DW || !RAGGED_LAST, "all tiles of dw are whole walks");
     const int64_t jx = blockIdx.x / kXcds;
     const int64_t L = (jx / 32) * (32 * kXcds) + (int64_t)(blockIdx.x % kXcds) * 32 + jx % 32;
-    GradTile t{-1, 0, 0, 0, 0};
-    int tiles;
-    uint32_t in;
-    int lo, hi;
+    GradTile t{-1, 0, 0, 0, 0, 1, 0};
+    int tiles = 0, lo = 0, hi = 0;
+    uint32_t in = 0;
+    int64_t whole_tiles = 0;
     if constexpr (DW) {
         tiles = (a.N + BR - 1) / BR;
         const int64_t e = L / ((int64_t)tiles * nct);
@@ -50,194 +55,442 @@ __device__ __forceinline__ GradTile find_grad_tile(const ExpertArgs &a, int nct,
         lo = a.lo[e];
         hi = a.hi_base[e] + a.hi_len[e];
     } else {
-        const ExpertTileHit hit = find_expert_tile<BR>(a, nct, L, lane);
-        if (hit.e >= a.E) return t;
-        t.e = hit.e;
-        in = hit.L;
-        tiles = hit.tiles;
-        lo = hit.lo;
-        hi = hit.hi;
+        const ExpertTileHit hit = find_expert_tile<BR, RAGGED_LAST>(a, nct, L, lane, &whole_tiles);
+        if (hit.e < a.E) {
+            t.e = hit.e;
+            in = hit.L;
+            tiles = hit.tiles;
+            lo = hit.lo;
+            hi = hit.hi;
+        }
     }
-    const int full = tiles / P;
-    const bool whole = in < (uint32_t)(full * P) * (uint32_t)nct;
-    const uint32_t rem = whole ? in % (uint32_t)(P * nct) : in - (uint32_t)(full * P) * (uint32_t)nct;
-    const int side = whole ? P : tiles - full * P;
-    t.e = __builtin_amdgcn_readfirstlane(t.e);
-    t.ct = __builtin_amdgcn_readfirstlane((int)(rem / (uint32_t)side));
-    t.rt = __builtin_amdgcn_readfirstlane((whole ? (int)(in / (uint32_t)(P * nct)) : full) * P + (int)(rem % (uint32_t)side));
+    if (t.e >= 0) {
+        const int full = tiles / P;
+        const bool whole = in < (uint32_t)(full * P) * (uint32_t)nct;
+        const uint32_t rem = whole ? in % (uint32_t)(P * nct) : in - (uint32_t)(full * P) * (uint32_t)nct;
+        const int side = whole ? P : tiles - full * P;
+        t.ct = (int)(rem / (uint32_t)side);
+        t.side = side;
+        t.share = (int)(rem % (uint32_t)side);
+        t.rt = (whole ? (int)(in / (uint32_t)(P * nct)) : full) * P + t.share;
+    } else if constexpr (RAGGED_LAST) {
+        // position (L - whole tiles) / nct in the order (rows of the ragged tile, descending; expert, ascending), of the short ones, which are
+        // halves of 128 columns, 2 nct; E <= 256 threads
+        const int64_t Lr = L - whole_tiles;
+        const int tid = threadIdx.x;
+        int mine = 0;
+        if (tid < a.E) {
+            const int first = a.lo[tid], last = a.hi_base[tid] + a.hi_len[tid];
+            mine = last > first ? (last - first) % BR : 0;
+            scratch[tid] = mine;
+        }
+        if (tid == 0) scratch[256] = -1;
+        __syncthreads();
+        int rank = 0, long_ones = 0;
+        for (int o = 0; o < a.E; ++o) {
+            const int other = scratch[o];
+            long_ones += other > kShortTileRows ? 1 : 0;
+            rank += other > mine || (other == mine && o < tid) ? 1 : 0;
+        }
+        const int64_t halves = Lr - (int64_t)long_ones * nct;      // number among the halves
+        if (mine > 0 && rank == (halves < 0 ? Lr / nct : long_ones + halves / (2 * nct))) scratch[256] = tid;
+        __syncthreads();
+        t.e = scratch[256];
+        __syncthreads();                                           // everyone has read it before the stages are laid down
+        if (t.e < 0) return t;
+        lo = a.lo[t.e];
+        hi = a.hi_base[t.e] + a.hi_len[t.e];
+        t.ct = (int)(halves < 0 ? Lr % nct : halves % (2 * nct));
+        t.rt = (hi - lo) / BR;
+    } else {
+        return t;
+    }
     hi = min(hi, a.max_rows);
     lo = max(lo, 0);
-    t.row0 = __builtin_amdgcn_readfirstlane(DW ? lo : lo + t.rt * BR);
-    t.row_end = __builtin_amdgcn_readfirstlane(DW ? max(hi, lo) : min(hi, lo + (t.rt + 1) * BR));
+    t.row0 = DW ? lo : lo + t.rt * BR;
+    t.row_end = DW ? max(hi, lo) : min(hi, lo + (t.rt + 1) * BR);
     if (!DW && t.row0 >= t.row_end) t.e = -1;
     return t;
 }
 
 // --------------------------------------------------------------------------------------------- bf16
 //
-// Steps of 64 elements of the summed axis go straight to LDS.  An operand whose elements lie along that axis ("flat": dy in dx) is
-// stored as rows of 128 bytes, piece c of row r at position c ^ ((r / 2) % 8), and read 16 bytes at a time.  One that lies across it ("deep") is
-// stored as it comes, 64 rows of C elements, and read by the transposing LDS read: 16 lanes hand in 4 rows of 16 elements and get a
-// column of 4 each; two of them are the 8 elements of an MFMA's fragment.  Its swizzle keeps the 8 rows of 32 bytes that half a wave
-// reads (rows 8 g + j, g = 0, 1, j = 0..3) in different banks: the 32-byte segment s of row k sits at segment s ^ f(k).
+// Steps of 64 elements of the summed axis.  An operand whose elements lie along that axis ("flat": dy in dx) is kept in LDS as rows of
+// 128 bytes, piece c of row r at position c ^ ((r / 2) % 8), and read 16 bytes at a time.  One that lies across it ("deep") is kept as it
+// comes, 64 rows of C elements, and read by the transposing LDS read: 16 lanes hand in 4 rows of 16 elements and get a column of 4 each;
+// two of them are the 8 elements of an MFMA's fragment.  Its swizzle keeps the 8 rows of 32 bytes that half a wave reads (rows 8 g + j, g = 0, 1,
+// j = 0..3; rows of 256 bytes or more begin on the same bank, of 128 every second) in different banks: the 32-byte segment s of row k sits at
+// s ^ f(k).
 template <int C>
 __device__ __forceinline__ constexpr int deep_swizzle(int k)
 {
-    if constexpr (C >= 128) return (k & 3) | ((k >> 3) & 1) << 2;          // rows of 256 bytes or more begin on the same bank
-    else if constexpr (C == 64) return ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
-    else return (k >> 3) & 1;
+    static_assert(C == 64 || C >= 128, "deep operand: width");
+    if constexpr (C == 64) return ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
+    else return (k & 3) | ((k >> 3) & 1) << 2;
 }
 
-// BR x BC: tile of the output, rows (of dx) or output features (of dw) x hidden elements; WR x WC waves; NST stages, the loads of NST - 1
-// in flight.
-template <int BR, int BC, int WR, int WC, int NST>
+// Where lane `lane` of the load of chunk c (1 KiB of LDS) of a deep operand of C elements finds its 16 bytes: the position is fixed by the
+// instruction, so the swizzle is applied here.  `exist`: elements of a row from the tile's first on.
+template <int C>
+__device__ __forceinline__ uint32_t deep_at(int c, int lane, uint32_t pitch, int exist)
+{
+    constexpr int per = 2 * C / 16;
+    const int k = (c * 64 + lane) / per, p = lane % per, from = ((p >> 1) ^ deep_swizzle<C>(k)) * 2 + (p & 1);
+    return from * 8 < exist ? (uint32_t)k * pitch + (uint32_t)from * 16 : kOutOfRange;
+}
+
+// Half of the 8 elements along the summed axis of a fragment: rows k .. k+3 of a deep operand, or k+4 .. k+7 (4 rows further on).
+// __restrict__: without alias information on the read the compiler waits for every outstanding load to LDS before it.
+[[maybe_unused]] __device__ __forceinline__ s16x4 read_deep(lds_s16x4 *__restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
+[[maybe_unused]] __device__ __forceinline__ bf16x8 whole_fragment(s16x4 lo, s16x4 hi) { return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)); }
+
+// A tile of 32 RB x 32 CB of the output, rows (of dx) or output features (of dw) x hidden elements, by 2 x 2 waves of 16 RB x 16 CB.
+template <int RB, int CB>
 struct GradShape {
-    static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
-    static constexpr int kStageBytes = (BR + BC) * 128, kLdsBytes = NST * kStageBytes;
-    static constexpr int kCR = BR / 8 / kWaves, kCC = BC / 8 / kWaves, kLoads = kCR + kCC;        // 1 KiB loads per wave and step
-    static constexpr int kRB = BR / WR / 16, kCB = BC / WC / 16;
-    static constexpr int kYounger = (NST - 2) * kLoads;
-    static constexpr int kWait = 0x0070 | (kYounger & 15) | ((kYounger >> 4) << 14);              // vmcnt(kYounger), lgkmcnt(0)
-    static_assert(BR % (8 * kWaves) == 0 && BC % (8 * kWaves) == 0 && BR >= 32 && BC >= 32 && kYounger < 64 && kLdsBytes <= 160 * 1024, "gradient tile: shape");
+    static constexpr int BR = 32 * RB, BC = 32 * CB;
+    static constexpr int kRowStage = BR * 128, kColStage = BC * 128, kSink = 2 * (kRowStage + kColStage), kLdsBytes = kSink + 1024;
+    static_assert((RB == 4 || RB == 8) && RB == CB && kLdsBytes <= 160 * 1024, "gradient tile: shape");
 };
 
-// A deep operand's loads: 64 rows of C elements from `base` on, `pitch` bytes apart, of which `cols` elements exist.
-template <int C, int CHUNKS>
-struct DeepLoads {
-    static constexpr int kRowsPerChunk = 1024 / (2 * C);
-    uint32_t at[CHUNKS];
-    __device__ __forceinline__ DeepLoads(int first_chunk, int lane, uint32_t pitch, int cols)
-    {
-#pragma unroll
-        for (int q = 0; q < CHUNKS; ++q) {
-            const int k = (first_chunk + q) * kRowsPerChunk + lane * 16 / (2 * C), p = lane % (C / 8);
-            const int from = ((p >> 1) ^ deep_swizzle<C>(k)) * 2 + (p & 1);
-            at[q] = from * 8 < cols ? (uint32_t)k * pitch + from * 16 : kOutOfRange;
-        }
-    }
+// A step's operands go straight to LDS while the step before it is multiplied: two stages, the loads of step s + 2 issued into the place of
+// s under the second half of s, when every wave has read all of s.  (Through registers, a step ahead of LDS: 8192 rows x 8192 x 8192, two
+// experts, dw 898 us; without any loads 772.)  Fragments come in two sets: the second half of a step is read under the MFMAs of the
+// first, the first half of the next step under those of the second.  One barrier per step, between the halves.  A step's time covers an L2
+// hit but no miss, so each workgroup also touches, a step ahead of the loads, one word per line of its share of the tiles that it shares with
+// the others on its XCD.
+// A tile of dx of at most XR rows x CW hidden elements: so little arithmetic per step that the step is as long as its loads take to arrive.
+// NST stages, the loads of NST - 1 steps in flight; 4 waves, each all rows x CW / 4 columns.  A step's fragments are read at its start.  Every wave issues
+// the same number of loads per step, also past the end (out of range: no traffic), because the wait for a stage counts the younger loads.
+template <int XR, int CW, int NST>
+struct GradShort {
+    static constexpr int kStage = (XR + CW) * 128, kLdsBytes = NST * kStage;
+    static constexpr int kLoadsR = XR / 32, kLoadsC = CW / 32, kYounger = (NST - 2) * (kLoadsR + kLoadsC);      // 1 KiB loads per wave and step
+    static constexpr int kWait = 0x0070 | (kYounger & 15) | ((kYounger >> 4) << 14);                         // vmcnt(kYounger), lgkmcnt(0)
+    static constexpr int RB = XR / 16, CB = CW / 64;
+    static_assert(XR % 32 == 0 && (CW == 64 || CW == 128) && NST >= 3 && kYounger < 64, "short gradient tile: shape");
 };
 
-// the 8 elements along the summed axis of one fragment: rows k .. k+3 and k+4 .. k+7 of a deep operand
-__device__ __forceinline__ bf16x8 read_deep(const unsigned char *p, int next4)
+template <int XR, int CW, int NST>
+__device__ __forceinline__ void grad_short_tile(const GradArgs &b, int e, int row0, int row_end, int col0, unsigned char *lds)
 {
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + next4));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
-template <bool DW, int BR, int BC, int WR, int WC, int NST>
-__device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, unsigned char *grad_lds)
-{
-    using G = GradShape<BR, BC, WR, WC, NST>;
+    using G = GradShort<XR, CW, NST>;
     const ExpertArgs &a = b.a;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-    const int wr = wave / WC, wc = wave % WC;
-    const GradTile t = find_grad_tile<DW, BR>(a, (a.H + BC - 1) / BC, lane);
-    if (t.e < 0) return;
-    const int64_t H = a.H, N = a.N;
-    const int col0 = t.ct * BC, out0 = DW ? t.rt * BR : 0;         // out0: first output feature of a tile of dw
-    const int depth = DW ? t.row_end - t.row0 : a.N;               // of the summed axis
-    const int nsteps = (depth + 63) / 64;
-
-    // columns: x (dw) or w (dx), deep in both; rows: dy, deep (dw) or flat (dx)
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));      // share nothing with the caller's other path, which has no register left to keep it in
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
     const uint32_t pitch_c = (uint32_t)a.H * 2, pitch_r = (uint32_t)a.N * 2;
-    const char *from_c = static_cast<const char *>(DW ? b.x : b.w) + (DW ? (int64_t)t.row0 * H : (int64_t)t.e * N * H) * 2 + (int64_t)col0 * 2;
-    const char *from_r = static_cast<const char *>(b.dy) + ((int64_t)t.row0 * N + out0) * 2;
-    const DeepLoads<BC, G::kCC> cols(wave * G::kCC, lane, pitch_c, a.H - col0);
-    const DeepLoads<BR, G::kCR> rows_deep(wave * G::kCR, lane, pitch_r, a.N - out0);
-    const int lr = lane >> 3;
-    auto piece = [&](int c) { return (lane & 7) ^ ((4 * c + (lr >> 1)) & 7); };
-    const auto flat = make_rsrc(from_r, DW ? 0u : (uint32_t)(t.row_end - t.row0) * pitch_r);
+    const char *const from_c = static_cast<const char *>(b.w) + ((int64_t)e * a.N * a.H + col0) * 2;
+    const auto rows = make_rsrc(static_cast<const char *>(b.dy) + (int64_t)row0 * pitch_r, (uint32_t)(row_end - row0) * pitch_r);
+    const int nsteps = (a.N + 63) / 64;
+    uint32_t at_c[G::kLoadsC], at_r[G::kLoadsR];
+    int p_r[G::kLoadsR];
+#pragma unroll
+    for (int q = 0; q < G::kLoadsC; ++q) at_c[q] = deep_at<CW>(wave * G::kLoadsC + q, lane, pitch_c, a.H - col0);
+#pragma unroll
+    for (int q = 0; q < G::kLoadsR; ++q) {
+        const int row = (wave * G::kLoadsR + q) * 8 + (lane >> 3);
+        p_r[q] = (lane & 7) ^ ((row >> 1) & 7);
+        at_r[q] = (uint32_t)row * pitch_r + p_r[q] * 16;
+    }
     auto issue = [&](int step, int slot) {
-        unsigned char *const base = grad_lds + slot * G::kStageBytes;
-        // rows of a deep operand in this step, none past the end; the descriptor begins at the step's first, `cut` bytes into its row
-        const int left = min(max(depth - step * 64, 0), 64);
-        auto records = [&](uint32_t pitch, uint32_t cut) { return left > 0 ? (uint32_t)left * pitch - cut : 0u; };
-        const auto rc = make_rsrc(from_c + (int64_t)step * 64 * pitch_c, records(pitch_c, (uint32_t)col0 * 2));
+        const int left = __builtin_amdgcn_readfirstlane(min(max(a.N - step * 64, 0), 64));
+        const auto cols = make_rsrc(from_c + (int64_t)step * 64 * pitch_c, left > 0 ? (uint32_t)left * pitch_c - (uint32_t)col0 * 2u : 0u);
+        unsigned char *const base = lds + slot * G::kStage;
 #pragma unroll
-        for (int q = 0; q < G::kCC; ++q)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void *)(base + BR * 128 + (wave * G::kCC + q) * 1024), 16, cols.at[q], 0, 0, 0);
-        if constexpr (DW) {
-            const auto rr = make_rsrc(from_r + (int64_t)step * 64 * pitch_r, records(pitch_r, (uint32_t)out0 * 2));
+        for (int q = 0; q < G::kLoadsC; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(cols, (lds_void *)(base + XR * 128 + (wave * G::kLoadsC + q) * 1024), 16, at_c[q], 0, 0, 0);
 #pragma unroll
-            for (int q = 0; q < G::kCR; ++q)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rr, (lds_void *)(base + (wave * G::kCR + q) * 1024), 16, rows_deep.at[q], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int q = 0; q < G::kCR; ++q) {
-                const int c = wave * G::kCR + q;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(flat, (lds_void *)(base + c * 1024), 16,
-                                                         piece(c) * 8 < left ? (uint32_t)(c * 8 + lr) * pitch_r + (uint32_t)step * 128u + piece(c) * 16 : kOutOfRange,
-                                                         0, 0, 0);
-            }
-        }
+        for (int q = 0; q < G::kLoadsR; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void *)(base + (wave * G::kLoadsR + q) * 1024), 16,
+                                                     p_r[q] * 8 < left ? at_r[q] + (uint32_t)step * 128u : kOutOfRange, 0, 0, 0);
     };
-
-    f32x4 acc[G::kRB][G::kCB];
+    f32x4 acc[G::RB][G::CB];
 #pragma unroll
-    for (int i = 0; i < G::kRB; ++i)
+    for (int i = 0; i < G::RB; ++i)
 #pragma unroll
-        for (int j = 0; j < G::kCB; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
-    // this lane's place in a deep operand: row 8 g + m / 4, quarter m % 4 of a segment
-    const int kl = 8 * g + (m >> 2);
-    const unsigned char *const pc = grad_lds + BR * 128 + kl * (2 * BC) + (m & 3) * 8;
-    const unsigned char *const pr = DW ? grad_lds + kl * (2 * BR) + (m & 3) * 8 : grad_lds + (wr * (BR / WR) + m) * 128;
-    const int sc = deep_swizzle<BC>(kl), sr = deep_swizzle<BR>(kl);
-
+        for (int j = 0; j < G::CB; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    const int kl = 8 * g + (m >> 2), sw = deep_swizzle<CW>(kl);
+    const unsigned char *const pc = lds + XR * 128 + kl * (2 * CW) + (m & 3) * 8, *const pr = lds + m * 128;
+    const int nb = (row_end - row0 + 15) / 16;                     // 16-row blocks with rows of the segment
 #pragma unroll
     for (int q = 0; q < NST - 1; ++q) issue(q, q);
-    int slot = 0;
-    for (int step = 0; step < nsteps; ++step) {
-        __builtin_amdgcn_s_waitcnt(G::kWait);                      // stage `step` has landed; this wave's reads of the one before are done
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        issue(step + NST - 1, slot == 0 ? NST - 1 : slot - 1);     // where stage step - 1 was
-        const int buf = slot * G::kStageBytes;
+    // with at most half of the row blocks in use only those are multiplied
+    auto run = [&](auto blocks) {
+        constexpr int BLOCKS = decltype(blocks)::value;
+        int slot = 0;
+        for (int step = 0; step < nsteps; ++step) {
+            __builtin_amdgcn_s_waitcnt(G::kWait);                  // stage `step` has landed; this wave's reads of the one before are done
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            issue(step + NST - 1, slot == 0 ? NST - 1 : slot - 1); // where stage step - 1 was
+            const int at = slot * G::kStage;
+            bf16x8 fr[2][BLOCKS], fc[2][G::CB];
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 fr[G::kRB], fc[G::kCB];
+            for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
-            for (int i = 0; i < G::kRB; ++i) {
-                if constexpr (DW) fr[i] = read_deep(pr + buf + ks * 64 * BR + ((wr * G::kRB + i) ^ sr) * 32, 8 * BR);
-                else fr[i] = *reinterpret_cast<const bf16x8 *>(pr + buf + ((4 * ks + g) ^ ((m >> 1) & 7)) * 16 + i * 2048);
+                for (int j = 0; j < G::CB; ++j) {
+                    const unsigned char *const p = pc + at + ks * 64 * CW + ((wave * G::CB + j) ^ sw) * 32;
+                    const s16x4 lo = read_deep((lds_s16x4 *)(p)), hi = read_deep((lds_s16x4 *)(p + 8 * CW));
+                    fc[ks][j] = whole_fragment(lo, hi);
+                }
+#pragma unroll
+                for (int i = 0; i < BLOCKS; ++i) fr[ks][i] = *reinterpret_cast<const bf16x8 *>(pr + at + ((4 * ks + g) ^ ((m >> 1) & 7)) * 16 + i * 2048);
             }
 #pragma unroll
-            for (int j = 0; j < G::kCB; ++j) fc[j] = read_deep(pc + buf + ks * 64 * BC + ((wc * G::kCB + j) ^ sc) * 32, 8 * BC);
+            for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int i = 0; i < G::kRB; ++i)
+                for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
-                for (int j = 0; j < G::kCB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[j], fr[i], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < G::CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[ks][j], fr[ks][i], acc[i][j], 0, 0, 0);
+            slot = slot == NST - 1 ? 0 : slot + 1;
         }
-        slot = slot == NST - 1 ? 0 : slot + 1;
-    }
-
-    // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, hidden element 16 j + 4 (lane / 16) + v of its columns
-    __bf16 *const out = static_cast<__bf16 *>(b.out) + (DW ? (int64_t)t.e * N * H : 0);
+    };
+    if (2 * nb <= G::RB) run(std::integral_constant<int, G::RB / 2>{});
+    else run(std::integral_constant<int, G::RB>{});
+    __bf16 *const out = static_cast<__bf16 *>(b.out);
 #pragma unroll
-    for (int i = 0; i < G::kRB; ++i) {
-        const int64_t r = (DW ? out0 : t.row0) + wr * (BR / WR) + i * 16 + m;
-        if (r < (DW ? a.N : t.row_end)) {
+    for (int i = 0; i < G::RB; ++i) {
+        const int64_t r = row0 + i * 16 + m;
+        if (r < row_end) {
 #pragma unroll
-            for (int j = 0; j < G::kCB; ++j) {
-                const int h = col0 + wc * (BC / WC) + j * 16 + 4 * g;
+            for (int j = 0; j < G::CB; ++j) {
+                const int h = col0 + wave * (CW / 4) + j * 16 + 4 * g;
                 if (h < a.H) {
                     bf16x4 o;
 #pragma unroll
                     for (int v = 0; v < 4; ++v) o[v] = (__bf16)acc[i][j][v];
-                    *reinterpret_cast<bf16x4 *>(out + r * H + h) = o;
+                    *reinterpret_cast<bf16x4 *>(out + r * a.H + h) = o;
                 }
             }
         }
     }
 }
 
-template <bool DW, int BR, int BC, int WR, int WC, int NST>
-__global__ __launch_bounds__(64 * WR * WC) void grad_bf16_kernel(GradArgs b)
+template <int XR, int CW, int NST>
+__global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs b)
 {
     extern __shared__ __align__(16) unsigned char grad_lds[];
-    grad_bf16_tile<DW, BR, BC, WR, WC, NST>(b, grad_lds);
+    const GradTile t = find_grad_tile<false, XR, false>(b.a, (b.a.H + CW - 1) / CW, threadIdx.x & 63, nullptr);
+    const int e = __builtin_amdgcn_readfirstlane(t.e);
+    if (e < 0) return;
+#if defined(__HIP_DEVICE_COMPILE__)
+    grad_short_tile<XR, CW, NST>(b, e, __builtin_amdgcn_readfirstlane(t.row0), __builtin_amdgcn_readfirstlane(t.row_end),
+                                 __builtin_amdgcn_readfirstlane(t.ct) * CW, grad_lds);
+#else
+    (void)grad_lds;
+#endif
+}
+
+// The rows of a ragged tile of dx are split evenly between the two row halves: the loop is compiled for RB / 2 to RB blocks of 16
+// rows each, so that only rows in use are requested, read and multiplied.
+template <bool DW, int RB, int CB, bool RAGGED_LAST>
+__device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, unsigned char *lds)
+{
+#if defined(__HIP_DEVICE_COMPILE__)         // the matrix instruction is written out: nothing for the host pass to parse
+    using G = GradShape<RB, CB>;
+    constexpr int BR = G::BR, BC = G::BC;
+    const ExpertArgs &a = b.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int wr = wave >> 1, wc = wave & 1;
+    const GradTile t = find_grad_tile<DW, BR, RAGGED_LAST>(a, (a.H + BC - 1) / BC, lane, reinterpret_cast<int *>(lds));
+    const int e = __builtin_amdgcn_readfirstlane(t.e);
+    if (e < 0) return;
+    const int row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
+    const int64_t H = a.H, N = a.N;
+    // Ragged tiles of at most 64 rows, the last ones, come in halves of 128 columns: they last as long as their weights take to arrive, and
+    // twice the workgroups have twice the loads on their way.
+    if constexpr (RAGGED_LAST) {
+        if (row_end - row0 <= kShortTileRows) {
+            const int from = __builtin_amdgcn_readfirstlane(t.ct) * 128;
+            if (from < a.H) grad_short_tile<kShortTileRows, 128, 5>(b, e, row0, row_end, from, lds);
+            return;
+        }
+    }
+    // out0: first output feature of a tile of dw
+    const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * BC, out0 = DW ? __builtin_amdgcn_readfirstlane(t.rt) * BR : 0;
+    const int depth = DW ? row_end - row0 : a.N;                   // of the summed axis
+    const int nsteps = (depth + 63) / 64;
+
+    // columns: x (dw) or w (dx), deep in both; rows: dy, deep (dw) or flat (dx).  Descriptors of deep operands begin at a step's first row.
+    const uint32_t pitch_c = (uint32_t)a.H * 2, pitch_r = (uint32_t)a.N * 2;
+    const char *from_c = static_cast<const char *>(DW ? b.x : b.w) + (DW ? (int64_t)row0 * H : (int64_t)e * N * H) * 2 + (int64_t)col0 * 2;
+    const char *from_r = static_cast<const char *>(b.dy) + ((int64_t)row0 * N + out0) * 2;
+    const auto flat = make_rsrc(from_r, DW ? 0u : (uint32_t)(row_end - row0) * pitch_r);
+    auto records = [&](int step, uint32_t pitch, int cut) {       // rows of a deep operand in the step, none past the end
+        const int left = min(max(depth - step * 64, 0), 64);       // a clamp in one vector instruction: back into a scalar register
+        return (uint32_t)__builtin_amdgcn_readfirstlane(left > 0 ? left * (int)pitch - cut * 2 : 0);
+    };
+    auto cols_of = [&](int step) { return make_rsrc(from_c + (int64_t)step * 64 * pitch_c, records(step, pitch_c, col0)); };
+    auto rows_of = [&](int step) { return DW ? make_rsrc(from_r + (int64_t)step * 64 * pitch_r, records(step, pitch_r, out0)) : flat; };
+    // the early touches: thread `tid` has line tid of a step's 64 rows of BC / 64 lines (deep) or of its rows (flat)
+    constexpr int kLinesC = BC / 64, kLinesR = BR / 64;
+    const int side = __builtin_amdgcn_readfirstlane(t.side), share = __builtin_amdgcn_readfirstlane(t.share), ct = __builtin_amdgcn_readfirstlane(t.ct);
+    const uint32_t touch_c = tid < 64 * kLinesC && tid * side / (64 * kLinesC) == share && col0 + tid % kLinesC * 64 < a.H
+                                 ? (uint32_t)(tid / kLinesC) * pitch_c + (uint32_t)(tid % kLinesC) * 128u : kOutOfRange;
+    const bool my_rows = (tid >> 6) == (ct & 3);
+    const uint32_t touch_r = !my_rows ? kOutOfRange : DW ? (tid < 64 * kLinesR && out0 + tid % kLinesR * 64 < a.N ? (uint32_t)(tid / kLinesR) * pitch_r + (uint32_t)(tid % kLinesR) * 128u : kOutOfRange)
+                                                     : (tid < BR ? (uint32_t)tid * pitch_r : kOutOfRange);
+    auto touch = [&](int step) {
+        lds_void *const sink = (lds_void *)(lds + G::kSink + wave * 256);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(cols_of(step), sink, 4, touch_c, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rows_of(step), sink, 4, DW || step * 64 >= a.N ? (DW ? touch_r : kOutOfRange) : touch_r + (touch_r == kOutOfRange ? 0u : (uint32_t)step * 128u), 0, 0, 0);
+    };
+    uint32_t at_c[CB];
+#pragma unroll
+    for (int q = 0; q < CB; ++q) at_c[q] = deep_at<BC>(wave * CB + q, lane, pitch_c, a.H - col0);
+    unsigned char *const lds_r = lds, *const lds_c = lds + 2 * G::kRowStage;
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    f32x4 acc[RB][CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    // no instruction near it reads the accumulator: the next MFMA on the same one is half a step away, and the epilogue waits first
+    bf16x8 fr[2][RB], fc[2][CB];
+    auto mma = [&](int set, int i, int j) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(fc[set][j]), "v"(fr[set][i])); };
+
+    // All steps, NB row blocks per half.
+    auto run = [&](auto nbc) {
+        constexpr int NB = decltype(nbc)::value;
+        // this lane's place in a deep operand: row 8 g + m / 4, quarter m % 4 of a segment
+        const int kl = 8 * g + (m >> 2), sw = deep_swizzle<BC>(kl);      // the same for both widths
+        const unsigned char *const fc0 = lds_c + kl * (2 * BC) + (m & 3) * 8;
+        const unsigned char *const fr0 = DW ? lds_r + kl * (2 * BR) + (m & 3) * 8 : lds_r + (wr * 16 * NB + m) * 128;
+        // Fragment r of half `ks` of the step in `stage`: those of the columns, then those of the rows.  Part 0 and part 1 of a deep one; a flat
+        // one is read whole as part 0.
+        s16x4 lo;
+        auto read = [&](int set, int stage, int ks, int r, int part) {
+            if (r < CB || DW) {
+                const int pitch = r < CB ? 2 * BC : 2 * BR, seg = r < CB ? wc * CB + r : wr * RB + r - CB;
+                const unsigned char *const p = r < CB ? fc0 + stage * G::kColStage : fr0 + stage * G::kRowStage;
+                const s16x4 v = read_deep((lds_s16x4 *)(p + ks * 32 * pitch + (seg ^ sw) * 32 + part * 4 * pitch));
+                if (part == 0) lo = v;
+                else if (r < CB) fc[set][r] = whole_fragment(lo, v);
+                else fr[set][r - CB] = whole_fragment(lo, v);
+            } else if (part == 0) {
+                fr[set][r - CB] = *reinterpret_cast<const bf16x8 *>(fr0 + stage * G::kRowStage + ((4 * ks + g) ^ ((m >> 1) & 7)) * 16 + (r - CB) * 2048);
+            }
+        };
+        uint32_t at_r[NB];
+#pragma unroll
+        for (int q = 0; q < NB; ++q) {
+            const int c = wave * NB + q, row = c * 8 + (lane >> 3), p = (lane & 7) ^ ((row >> 1) & 7);
+            at_r[q] = DW ? deep_at<BR>(c, lane, pitch_r, a.N - out0) : (uint32_t)row * pitch_r + p * 16;
+        }
+        auto issue_c = [&](__amdgpu_buffer_rsrc_t r, int stage, int q) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds_c + stage * G::kColStage + (wave * CB + q) * 1024), 16, at_c[q], 0, 0, 0);
+        };
+        auto issue_r = [&](__amdgpu_buffer_rsrc_t r, int step, int stage, int q) {
+            uint32_t at = at_r[q];
+            if (!DW) {
+                const int p = (lane & 7) ^ ((((wave * NB + q) * 8 + (lane >> 3)) >> 1) & 7);
+                at = step * 64 + p * 8 < a.N ? at + (uint32_t)step * 128u : kOutOfRange;
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds_r + stage * G::kRowStage + (wave * NB + q) * 1024), 16, at, 0, 0, 0);
+        };
+        // Half a step: NB x CB MFMAs on fragment set `set`; evenly between them the reads of the other set's fragments and, if `refill`,
+        // the loads of step `step`.  One wave has a SIMD to itself: an instruction
+        // issues in 4 clocks, an MFMA takes 16, so up to three others behind each cost nothing, and eight behind every fourth a quarter
+        // of the time (both gradients of 16384 rows x 4096 x 4096: 1076 us).
+        constexpr int kMfmas = NB * CB, kReads = NB + CB;
+        auto half_step = [&](int set, int stage, int ks, auto refill, int step) {
+            constexpr int each = decltype(refill)::value ? 3 : 2, actions = each * kReads;
+            const auto rc = cols_of(step), rr = rows_of(step);
+#pragma unroll
+            for (int n = 0; n < kMfmas; ++n) {
+#pragma unroll
+                for (int k = n * actions / kMfmas; k < (n + 1) * actions / kMfmas; ++k) {
+                    const int r = k / each, what = k % each;
+                    if (what < 2) read(set ^ 1, stage, ks, r, what);
+                    else if (r < CB) issue_c(rc, step & 1, r);
+                    else issue_r(rr, step, step & 1, r - CB);
+                }
+                mma(set, n / CB, n % CB);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            const auto rc = cols_of(step), rr = rows_of(step);
+#pragma unroll
+            for (int q = 0; q < CB; ++q) issue_c(rc, step, q);
+#pragma unroll
+            for (int q = 0; q < NB; ++q) issue_r(rr, step, step, q);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70 | (kReads & 15) | (kReads >> 4 << 14));       // stage 0: younger are the loads of stage 1
+        touch(2);
+        barrier();
+#pragma unroll
+        for (int r = 0; r < 2 * kReads; ++r) read(0, 0, 0, r / 2, r % 2);
+        for (int s = 0; s < nsteps; ++s) {
+            half_step(0, s & 1, 1, std::false_type{}, 0);
+            __builtin_amdgcn_s_waitcnt(0x0070 | 2);                // this wave has read all of stage s, its part of stage s + 1 has landed: younger are two touches
+            barrier();
+            half_step(1, (s & 1) ^ 1, 0, std::true_type{}, s + 2);
+            touch(s + 3);
+        }
+    };
+    int nb = RB;
+    if constexpr (DW) {
+        if (nsteps > 0) run(std::integral_constant<int, RB>{});
+    } else {
+        nb = max((row_end - row0 + 31) / 32, (RB + 1) / 2);
+        if (RB == 8 && nb == 7) run(std::integral_constant<int, (RB == 8 ? 7 : RB)>{});
+        else if (RB == 8 && nb == 6) run(std::integral_constant<int, (RB == 8 ? 6 : RB)>{});
+        else if (RB == 8 && nb == 5) run(std::integral_constant<int, (RB == 8 ? 5 : RB)>{});
+        else if (RB == 4 && nb == 3) run(std::integral_constant<int, (RB == 4 ? 3 : RB)>{});
+        else if (RB > 1 && nb == RB / 2) run(std::integral_constant<int, (RB > 1 ? RB / 2 : RB)>{});
+        else run(std::integral_constant<int, RB>{});
+    }
+    asm volatile("s_nop 15\n\ts_nop 15");                          // the last MFMAs' results
+    __builtin_amdgcn_sched_barrier(0);
+
+    // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, hidden element 16 j + 4 (lane / 16) + v of its columns.  Through LDS, block of
+    // 16 rows by block, so that rows leave as whole pieces of 16 bytes, 32 CB bytes of each side by side.  (8 bytes a lane straight from the registers:
+    // 268 MB of weights' gradients in 101 us.)
+    __builtin_amdgcn_s_waitcnt(0x0070);                            // nor written: the loads past the end have come back
+    barrier();                                                     // the stages are not read any more
+    constexpr int kOutPitch = 32 * CB + 16;                        // 16 bytes of padding: the 16 rows that a store of 8 bytes a lane hits begin on different banks
+    unsigned char *const own = lds + wave * (16 * kOutPitch);
+    static_assert(4 * 16 * kOutPitch <= G::kLdsBytes, "gradient tile: room for a block of rows per wave");
+    char *const out = static_cast<char *>(b.out) + ((DW ? (int64_t)e * N * H : 0) + col0 + wc * 16 * CB) * 2;
+    const int l2 = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // asked for again: kept through the loop it would be spilled
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+        if (i >= nb) break;
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            bf16x4 o;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[v] = (__bf16)acc[i][j][v];
+            *reinterpret_cast<bf16x4 *>(own + (l2 & 15) * kOutPitch + j * 32 + (l2 >> 4) * 8) = o;
+        }
+        constexpr int kLanes = 2 * CB, kRows = 64 / kLanes;        // lanes per row, rows per store
+#pragma unroll
+        for (int q = 0; q < 16 / kRows; ++q) {
+            const int row = q * kRows + l2 / kLanes, p = l2 % kLanes;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(own + row * kOutPitch + p * 16);
+            const int64_t r = (DW ? out0 : row0) + wr * 16 * nb + i * 16 + row;
+            if (r < (DW ? a.N : row_end) && col0 + wc * 16 * CB + p * 8 < a.H) *reinterpret_cast<u32x4 *>(out + r * H * 2 + p * 16) = v;
+        }
+    }
+#else
+    (void)b;
+    (void)lds;
+#endif
+}
+
+template <bool DW, int RB, int CB, bool RAGGED_LAST>
+__global__ __launch_bounds__(256, RB *CB == 64 ? 1 : 2) void grad_bf16_kernel(GradArgs b)
+{
+    extern __shared__ __align__(16) unsigned char grad_lds[];
+    grad_bf16_tile<DW, RB, CB, RAGGED_LAST>(b, grad_lds);
 }
 
 // --------------------------------------------------------------------------------------------- fp32
@@ -252,7 +505,7 @@ __global__ __launch_bounds__(256) void grad_f32_kernel(GradArgs b)
     __shared__ __align__(16) float rows[kF32Depth][kF32Pitch], cols[kF32Depth][kF32Pitch];
     const ExpertArgs &a = b.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4, wr = wave >> 1, wc = wave & 1;
-    const GradTile t = find_grad_tile<DW, kF32Tile>(a, (a.H + kF32Tile - 1) / kF32Tile, lane);
+    const GradTile t = find_grad_tile<DW, kF32Tile, false>(a, (a.H + kF32Tile - 1) / kF32Tile, lane, nullptr);
     if (t.e < 0) return;
     const int64_t H = a.H, N = a.N;
     const int col0 = t.ct * kF32Tile, out0 = DW ? t.rt * kF32Tile : 0;
@@ -331,19 +584,45 @@ int64_t grad_grid(const ExpertArgs &a, int64_t BR, int64_t BC, int64_t rows_boun
     return (n + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
 }
 
-template <bool DW, int BR, int BC, int WR, int WC, int NST>
+template <bool DW, int RB, int CB, bool RAGGED_LAST = false>
 int launch_grad_bf16(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 {
-    using G = GradShape<BR, BC, WR, WC, NST>;
+    using G = GradShape<RB, CB>;
     static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_bf16_kernel<DW, BR, BC, WR, WC, NST>), G::kLdsBytes, lds_opt_in)) return rc;
-    const int64_t grid = grad_grid<DW>(b.a, BR, BC, rows_bound);
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_bf16_kernel<DW, RB, CB, RAGGED_LAST>), G::kLdsBytes, lds_opt_in)) return rc;
+    int64_t grid = grad_grid<DW>(b.a, G::BR, G::BC, rows_bound);
+    if (RAGGED_LAST) grid += ((int64_t)b.a.E * ((b.a.H + G::BC - 1) / G::BC) + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);        // halves
     if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((grad_bf16_kernel<DW, BR, BC, WR, WC, NST>), dim3((unsigned)grid), dim3(G::kThreads), G::kLdsBytes, st, b);
+    hipLaunchKernelGGL((grad_bf16_kernel<DW, RB, CB, RAGGED_LAST>), dim3((unsigned)grid), dim3(256), G::kLdsBytes, st, b);
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
 }
 
+template <int XR, int CW, int NST>
+int launch_grad_short(const GradArgs &b, int64_t rows_bound, hipStream_t st)
+{
+    using G = GradShort<XR, CW, NST>;
+    static LdsOptIn lds_opt_in;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_short_kernel<XR, CW, NST>), G::kLdsBytes, lds_opt_in)) return rc;
+    const int64_t grid = grad_grid<false>(b.a, XR, CW, rows_bound);
+    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((grad_short_kernel<XR, CW, NST>), dim3((unsigned)grid), dim3(256), G::kLdsBytes, st, b);
+    MONTA_HIP_TRY(hipGetLastError());
+    return MONTA_OK;
+}
+
+// Which tile.  Measured on MI355X, three sets of buffers in turn, us; tokens x hidden x features, experts, top-2 (64 experts: top-8).
+// dx in tiles of 32 x 64, 32 x 128, 64 x 128, 128 x 128, 256 x 256 and those with the ragged tiles last:
+//   1 x 4096 x 4096, 8     21   29   30   31   61   34        256 x 1024 x 1024, 8      8.9  8.3  11   13   23   21
+//   64 x 4096 x 4096, 8    58   48   48   51   90   52        2048 x 512 x 512, 4       7.5  6.8  8.6  10   20   20
+//   256 x 4096 x 4096, 8   82   78   66   54   91   92        4096 x 1024 x 1024, 8     49   44   35   32   36   38
+//   1024 x 4096 x 4096, 8  202  189  130  147  108  115       256 x 2048 x 1024, 64     64   60   59   65   68   77
+//   2048 x 4096 x 4096, 8  360  308  222  208  195  155       2000 x 7168 x 2048, 64    1332 1177 833  739  627  667
+// so 256 x 256 where most CUs get one, below that what gives every CU one or two.  Deep operands want wide tiles: a row of 64 elements is
+// one line.  dw in tiles of 128 x 128 and 256 x 256:
+//   1 x 4096 x 4096, 8     50   56                            1024 x 1024 x 1024, 8     12   18
+//   256 x 4096 x 4096, 8   91   84                            4096 x 1024 x 512, 32     19   18
+//   2048 x 4096 x 4096, 8  220  181                           3000 x 1000 x 3000, 4     49   48
 template <bool DW>
 int launch_grad(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t st)
 {
@@ -356,8 +635,20 @@ int launch_grad(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t st
         return MONTA_OK;
     }
     const int64_t active = std::min<int64_t>(b.a.E, rows_bound), r = rows_bound / active;
-    if (!DW && r <= 48) return launch_grad_bf16<DW, 32, 128, 1, 4, 3>(b, rows_bound, st);
-    return launch_grad_bf16<DW, 128, 128, 2, 2, 2>(b, rows_bound, st);
+    if constexpr (DW) {
+        const int64_t tiles = b.a.E * ((b.a.N + 255) / 256) * ((b.a.H + 255) / 256);
+        return r > 8 && tiles >= 192 ? launch_grad_bf16<true, 8, 8>(b, rows_bound, st) : launch_grad_bf16<true, 4, 4>(b, rows_bound, st);
+    } else {
+        auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.H + C - 1) / C) * (2 * r + R) / (2 * R); };
+        if (tiles(32, 64) <= 256) return launch_grad_short<32, 64, 4>(b, rows_bound, st);
+        if (r <= 24 || tiles(32, 128) <= 400) return launch_grad_short<32, 128, 3>(b, rows_bound, st);
+        if (r > 56 && tiles(256, 256) >= 160) {
+            const bool ragged_last = r > 384 && b.a.E * ((b.a.H + 255) / 256) <= 256;
+            return ragged_last ? launch_grad_bf16<false, 8, 8, true>(b, rows_bound, st) : launch_grad_bf16<false, 8, 8>(b, rows_bound, st);
+        }
+        if (r <= 56 || tiles(64, 128) <= 700) return launch_grad_short<64, 128, 3>(b, rows_bound, st);
+        return launch_grad_bf16<false, 4, 4>(b, rows_bound, st);
+    }
 }
 
 }  // namespace
