@@ -138,4 +138,92 @@ __device__ __forceinline__ int walk_start(int tile, int nsteps)
     return (int)(((uint32_t)tile * 40503u & 0xffffu) * (uint32_t)nsteps >> 16);
 }
 
+// ------------------------------------------------------------------ tiles of a grouped product
+
+constexpr int kShortTileRows = 64;       // ragged tiles up to this many rows run as short tiles, where a kernel has those
+
+// What a tile of the output belongs to.
+struct RowTile {
+    int e = -1, row0 = 0, row_end = 0;   // expert (none: < 0); its rows
+    int rt = 0, ct = 0;                  // row tile and column tile inside the expert
+    int side = 1, share = 0;             // row tiles next to one another on one column tile; which of them
+};
+
+// Logical tile number of this workgroup: they go out in blocks of 256, 32 consecutive ones to each XCD (hardware deals consecutive
+// workgroups round robin to the 8 XCDs, each with its own L2).
+__device__ __forceinline__ int64_t tile_number()
+{
+    const int64_t j = blockIdx.x / kXcds;
+    return (j / 32) * (32 * kXcds) + (int64_t)(blockIdx.x % kXcds) * 32 + j % 32;
+}
+
+// Inside an expert the numbering is (panel of 8 row tiles, column tile, row tile), so that an XCD's workgroups share operand tiles.
+__device__ __forceinline__ void place_in_panels(RowTile &t, uint32_t in, int tiles, int nct)
+{
+    constexpr int P = 8;
+    const int full = tiles / P;
+    const bool whole = in < (uint32_t)(full * P) * (uint32_t)nct;
+    const uint32_t rem = whole ? in % (uint32_t)(P * nct) : in - (uint32_t)(full * P) * (uint32_t)nct;
+    t.side = whole ? P : tiles - full * P;
+    t.ct = (int)(rem / (uint32_t)t.side);
+    t.share = (int)(rem % (uint32_t)t.side);
+    t.rt = (whole ? (int)(in / (uint32_t)(P * nct)) : full) * P + t.share;
+}
+
+// Tile of BR rows of this workgroup.  RAGGED_LAST: the whole tiles of all experts come first and the segments' ragged last tiles after
+// them, the one with the most rows first, so that the last round of workgroups consists of the tiles that cost least; those of at most
+// kShortTileRows rows as halves of the column tile (ct counts halves).  For whole segments (hi_len), at least 256 threads and E <= 256; `scratch`: 257 words of LDS
+// that nothing else uses yet.
+template <int BR, bool RAGGED_LAST>
+__device__ __forceinline__ RowTile find_row_tile(const ExpertArgs &a, int nct, int lane, int *scratch)
+{
+    const int64_t L = tile_number();
+    RowTile t;
+    int lo, hi;
+    int64_t whole_tiles = 0;
+    const ExpertTileHit hit = find_expert_tile<BR, RAGGED_LAST>(a, nct, L, lane, &whole_tiles);
+    if (hit.e < a.E) {
+        t.e = hit.e;
+        lo = hit.lo;
+        hi = hit.hi;
+        place_in_panels(t, hit.L, hit.tiles, nct);
+    } else if constexpr (RAGGED_LAST) {
+        // position (L - whole tiles) / nct in the order (rows of the ragged tile, descending; expert, ascending), of the halves 2 nct
+        const int64_t Lr = L - whole_tiles;
+        const int tid = threadIdx.x;
+        int mine = 0;
+        if (tid < a.E) {
+            const int first = a.lo[tid], last = a.hi_base[tid] + a.hi_len[tid];
+            mine = last > first ? (last - first) % BR : 0;
+            scratch[tid] = mine;
+        }
+        if (tid == 0) scratch[256] = -1;
+        __syncthreads();
+        int rank = 0, long_ones = 0;
+        for (int o = 0; o < a.E; ++o) {
+            const int other = scratch[o];
+            long_ones += other > kShortTileRows ? 1 : 0;
+            rank += other > mine || (other == mine && o < tid) ? 1 : 0;
+        }
+        const int64_t halves = Lr - (int64_t)long_ones * nct;      // number among the halves
+        if (mine > 0 && rank == (halves < 0 ? Lr / nct : long_ones + halves / (2 * nct))) scratch[256] = tid;
+        __syncthreads();
+        t.e = scratch[256];
+        __syncthreads();                                           // everyone has read it before the stages are laid down
+        if (t.e < 0) return t;
+        lo = a.lo[t.e];
+        hi = a.hi_base[t.e] + a.hi_len[t.e];
+        t.ct = (int)(halves < 0 ? Lr % nct : halves % (2 * nct));
+        t.rt = (hi - lo) / BR;
+    } else {
+        return t;
+    }
+    hi = min(hi, a.max_rows);
+    lo = max(lo, 0);
+    t.row0 = lo + t.rt * BR;
+    t.row_end = min(hi, t.row0 + BR);
+    if (t.row0 >= t.row_end) t.e = -1;
+    return t;
+}
+
 }  // namespace monta

@@ -38,30 +38,14 @@ struct Tile8 {
 
 template <int XR, int WR, int WX, int WW, int NST, bool F32>
 __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, void *__restrict__ y,
-                                             const Expert8Args &b, unsigned char *lds8)
+                                             const Expert8Args &b, int e, int row0, int row_end, int col0, unsigned char *lds8)
 {
     using G = Tile8<XR, WR, WX, WW, NST>;
     const ExpertArgs &a = b.a;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));      // share nothing with the caller's other path, which has no register left to keep it in
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
     const int wx = wave / WW, ww = wave % WW;
-    const int nct = (a.N + WR - 1) / WR;
-    // logical tile numbers in blocks of 256, 32 consecutive ones per XCD; inside an expert (panel of 8 row tiles, column tile, row tile)
-    const int64_t jx = blockIdx.x / kXcds;
-    const int64_t L = (jx / 32) * (32 * kXcds) + (int64_t)(blockIdx.x % kXcds) * 32 + jx % 32;
-    const ExpertTileHit hit = find_expert_tile<XR>(a, nct, L, lane);
-    const int e = __builtin_amdgcn_readfirstlane(hit.e);
-    if (e >= a.E) return;                                          // surplus workgroup
-    constexpr int P = 8;
-    const int full = hit.tiles / P;
-    const bool whole = hit.L < (uint32_t)(full * P) * (uint32_t)nct;
-    const uint32_t rem = whole ? hit.L % (uint32_t)(P * nct) : hit.L - (uint32_t)(full * P) * (uint32_t)nct;
-    const int side = whole ? P : hit.tiles - full * P;             // row tiles of the panel
-    const int ct = __builtin_amdgcn_readfirstlane((int)(rem / (uint32_t)side));
-    const int rt = (whole ? (int)(hit.L / (uint32_t)(P * nct)) : full) * P + (int)(rem % (uint32_t)side);
-    const int row0 = __builtin_amdgcn_readfirstlane(hit.lo + rt * XR);
-    const int row_end = __builtin_amdgcn_readfirstlane(min(min(hit.hi, a.max_rows), row0 + XR));
-    if (row0 < 0 || row0 >= row_end) return;
-    const int col0 = ct * WR;
     const auto rx = make_rsrc(x + (int64_t)row0 * b.row8, (uint32_t)(row_end - row0) * (uint32_t)b.row8);
     const auto rw = make_rsrc(w + ((int64_t)e * a.N + col0) * a.H, (uint32_t)min(a.N - col0, WR) * (uint32_t)a.H);
 
@@ -105,7 +89,10 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
     const unsigned char *const ps = lds8 + (XR + WR) * 128 + (wx * (XR / WX) + m) * 4;
     const int k0 = (g ^ ((m >> 1) & 7)) * 16, k1 = ((4 + g) ^ ((m >> 1) & 7)) * 16;
     for (int step = 0; step < b.nb; ++step) {
-        if (step % 64 == 0) sw64 = ws[min(step + lane, b.nb - 1)];
+        if (step % 64 == 0) {
+            sw64 = ws[min(step + lane, b.nb - 1)];
+            asm volatile("" : "+v"(sw64));                         // waited for here: left to its use, every step would wait for its loads
+        }
         __builtin_amdgcn_s_waitcnt(G::kWait);                      // stage `step` has landed; this wave's reads of the one before are done
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -187,12 +174,225 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
     }
 }
 
+// At least two workgroups of 256 per CU: with more registers than 256 per lane the compiler would take the products through the
+// accumulator registers, a move for each.
 template <int XR, int WR, int WX, int WW, int NST, bool F32>
-__global__ __launch_bounds__(64 * WX * WW) void expert8_kernel(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w,
-                                                              void *__restrict__ y, Expert8Args b)
+__global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w,
+                                                                 void *__restrict__ y, Expert8Args b)
 {
     extern __shared__ __align__(16) unsigned char lds8[];
-    expert8_tile<XR, WR, WX, WW, NST, F32>(x, w, y, b, lds8);
+    const RowTile t = find_row_tile<XR, false>(b.a, (b.a.N + WR - 1) / WR, threadIdx.x & 63, nullptr);
+    const int e = __builtin_amdgcn_readfirstlane(t.e);
+    if (e < 0) return;
+#if defined(__HIP_DEVICE_COMPILE__)
+    expert8_tile<XR, WR, WX, WW, NST, F32>(x, w, y, b, e, __builtin_amdgcn_readfirstlane(t.row0), __builtin_amdgcn_readfirstlane(t.row_end),
+                                           __builtin_amdgcn_readfirstlane(t.ct) * WR, lds8);
+#else
+    (void)x;
+    (void)w;
+    (void)y;
+    (void)lds8;
+#endif
+}
+
+// Long segments: a 256 x 256 tile of y by 4 x 2 waves, two per SIMD, each 64 rows x 128 features, the features of one block of the weights.  The blocks'
+// sums cannot stay in the accumulators of the matrix instructions: each is a product of its own, of 32 clocks, whose four results a lane
+// scales and adds in four more instructions, 16 clocks, under the other wave's products.  A result is used four products later, so that
+// nothing waits for it.
+// Two stages of 64 KiB.  One barrier per step, before the last of the eight columns of products: then every wave has read all of
+// stage s, and stage s + 1 is there; the loads of s + 2 go to the place of s under the last column, as do the reads of the next step's
+// first fragments, each row fragment right behind its last use.
+constexpr int kBig8 = 256, kBig8Stage = 2 * kBig8 * 128 + 2048, kBig8LdsBytes = 2 * kBig8Stage;
+
+template <bool RAGGED_LAST, bool TAIL>
+__device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, __bf16 *__restrict__ y,
+                                                 const Expert8Args &b, const RowTile &t, unsigned char *lds8)
+{
+    const ExpertArgs &a = b.a;
+    const int e = __builtin_amdgcn_readfirstlane(t.e);
+    if (e < 0) return;
+    const int row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
+    if constexpr (RAGGED_LAST) {
+        if (row_end - row0 <= kShortTileRows) {
+            using Short = Tile8<kShortTileRows, 128, 2, 4, 5>;
+            static_assert(Short::kLdsBytes <= kBig8LdsBytes, "8-bit short tile: stages must fit the kernel's LDS");
+            const int from = __builtin_amdgcn_readfirstlane(t.ct) * 128;
+            if (from < a.N) expert8_tile<kShortTileRows, 128, 2, 4, 5, false>(x, w, y, b, e, row0, row_end, from, lds8);
+            return;
+        }
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int wx = wave >> 1, ww = wave & 1;
+    const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * kBig8;
+    const auto rx = make_rsrc(x + (int64_t)row0 * b.row8, (uint32_t)(row_end - row0) * (uint32_t)b.row8);
+    const auto rw = make_rsrc(w + ((int64_t)e * a.N + col0) * a.H, (uint32_t)min(a.N - col0, kBig8) * (uint32_t)a.H);
+    // a wave's loads: four neighbouring chunks of 8 rows of x and of w each; chunks 16 rows apart have the same swizzle
+    const int lr = lane >> 3;
+    uint32_t at_x[2], at_w[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int row = (wave * 4 + q) * 8 + lr;
+        const int piece = (lane & 7) ^ ((row >> 1) & 7);
+        at_x[q] = (uint32_t)row * (uint32_t)b.row8 + piece * 16;
+        at_w[q] = (uint32_t)row * (uint32_t)a.H + piece * 16;
+    }
+    const uint32_t at_s = wave < 4 ? (uint32_t)(wave * 64 + lane) * (uint32_t)b.row8 + (uint32_t)a.H : kOutOfRange;
+    // Load l of step `step`: 4 of w, 4 of x, the rows' scales (64 rows a wave; waves 4 to 7 ask for none).  Past the end the last step is fetched again, into
+    // a place that is not read any more.  TAIL: the pieces of the last step that lie past the end of a row are out of range.
+    auto issue = [&](int step, int l) {
+        unsigned char *const base = lds8 + (step & 1) * kBig8Stage;
+        const int from = min(step, b.nb - 1);
+        if (l < 8) {
+            const int q = l & 3;
+            uint32_t at = l < 4 ? at_w[q & 1] : at_x[q & 1];
+            if (q >> 1) {
+                uint32_t rows = 16u * (uint32_t)(l < 4 ? a.H : b.row8);
+                asm volatile("" : "+s"(rows));                     // added at each use: offsets kept would be spilled
+                at += rows;
+            }
+            if constexpr (TAIL) {
+                int me = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+                asm volatile("" : "+v"(me));                       // found again each time, as well
+                const int p = (me & 7) ^ (((wave * 32 + (q & 1) * 8 + (me >> 3)) >> 1) & 7);
+                at |= p >= a.H / 16 - from * 8 ? kOutOfRange : 0u;
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(l < 4 ? rw : rx, (lds_void *)(base + (l < 4 ? kBig8 * 128 : 0) + (wave * 4 + q) * 1024), 16, at,
+                                                     (uint32_t)from * 128u, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(base + 2 * kBig8 * 128 + wave * 256), 4, at_s, (uint32_t)from * 4u, 0, 0);
+        }
+    };
+
+    f32x4 acc[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    const float *const ws = b.w_scales + ((int64_t)e * ((a.N + 127) / 128) + min(col0 + ww * 128, a.N - 1) / 128) * b.nb;
+    const int k0 = (g ^ ((m >> 1) & 7)) * 16, k1 = ((4 + g) ^ ((m >> 1) & 7)) * 16;
+    const unsigned char *const pw = lds8 + kBig8 * 128 + (ww * 128 + m) * 128;
+
+    // all steps, NB blocks of 16 rows per wave: the rows of a ragged tile are split evenly over the four rows of waves
+    auto run = [&](auto nbc) {
+        constexpr int NB = decltype(nbc)::value;
+        const unsigned char *const px = lds8 + (wx * 16 * NB + m) * 128, *const ps = lds8 + 2 * kBig8 * 128 + (wx * 16 * NB + m) * 4;
+        auto fragment = [&](const unsigned char *p, int stage, int block) {
+            const u32x4 lo = *reinterpret_cast<const u32x4 *>(p + stage * kBig8Stage + block * 2048 + k0);
+            const u32x4 hi = *reinterpret_cast<const u32x4 *>(p + stage * kBig8Stage + block * 2048 + k1);
+            return __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        float sw64 = ws[min(lane, b.nb - 1)];                       // the scales of the wave's features: 64 steps at a time, one per lane
+        asm volatile("" : "+v"(sw64));
+#pragma unroll
+        for (int l = 0; l < 9; ++l) issue(0, l);
+#pragma unroll
+        for (int l = 0; l < 9; ++l) issue(1, l);
+        __builtin_amdgcn_s_waitcnt(0x0f70 | 9);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        i32x8 fx[NB], fw, fw_next;
+        float sc[NB], raw[NB];                                     // of the present step; of the next, as they are stored
+        constexpr int D = 4;                                       // a step's 8 NB products are a multiple of it: the ring begins anew with each
+        f32x4 product[D];                                          // the youngest
+#pragma unroll
+        for (int n = 0; n < D; ++n) product[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw64), 0));
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            fx[i] = fragment(px, 0, i);
+            raw[i] = *reinterpret_cast<const float *>(ps + i * 64);
+            sc[i] = 0.f;
+        }
+        fw = fragment(pw, 0, 0);
+        // scales and adds product number n of a step (row block n % NB, column block n / NB)
+        auto add = [&](const f32x4 &p, int n) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[n % NB][n / NB][v] = __builtin_fmaf(p[v], sc[n % NB], acc[n % NB][n / NB][v]);
+            asm volatile("" : "+v"(acc[n % NB][n / NB]));          // here: moved to the end of the step the products would need 128 registers
+        };
+        for (int s = 0; s < b.nb; ++s) {
+            const int stage = s & 1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j == 7) {
+                    __builtin_amdgcn_s_waitcnt(0x0070);            // this wave's part of stage s + 1 has landed, it has read all of stage s
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    if ((s + 1) % 64 == 0) {
+                        sw64 = ws[min(s + 1 + lane, b.nb - 1)];
+                        asm volatile("" : "+v"(sw64));
+                    }
+                }
+                fw_next = j < 7 ? fragment(pw, stage, j + 1) : fragment(pw, stage ^ 1, 0);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    const int n = j * NB + i;
+                    f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fx[i], (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                    asm volatile("" : "+v"(p));                    // issued here, not where its result is used
+                    if (n < D) {
+                        const int old = 8 * NB + n - D;
+                        add(product[n % D], old);
+                        if (old >= 7 * NB) sc[old % NB] = raw[old % NB] * sw;      // a row block's new scale, behind its last product of the step before
+                    } else {
+                        add(product[n % D], n - D);
+                    }
+                    product[n % D] = p;
+                    if (j == 7) {
+                        fx[i] = fragment(px, stage ^ 1, i);
+                        raw[i] = *reinterpret_cast<const float *>(ps + (stage ^ 1) * kBig8Stage + i * 64);
+#pragma unroll
+                        for (int l = i * 9 / NB; l < (i + 1) * 9 / NB; ++l) issue(s + 2, l);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                fw = fw_next;
+            }
+            sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw64), (s + 1) % 64));
+        }
+#pragma unroll
+        for (int n = 8 * NB - D; n < 8 * NB; ++n) add(product[n % D], n);
+    };
+    const int nb = max((row_end - row0 + 63) / 64, 2);
+    if (nb == 2) run(std::integral_constant<int, 2>{});
+    else if (nb == 3) run(std::integral_constant<int, 3>{});
+    else run(std::integral_constant<int, 4>{});
+
+    // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, output feature 16 j + 4 (lane / 16) + v of its columns
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = row0 + wx * 16 * nb + i * 16 + m;
+        if (i < nb && r < row_end) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int n = col0 + ww * 128 + j * 16 + 4 * g;
+                if (n < a.N) {
+                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                    bf16x4 o;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[v] = (__bf16)acc[i][j][v];
+                    *reinterpret_cast<bf16x4 *>(y + r * a.N + n) = o;
+                }
+            }
+        }
+    }
+}
+
+template <bool RAGGED_LAST, bool TAIL>
+__global__ __launch_bounds__(512, 2) void expert8_big_kernel(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, __bf16 *__restrict__ y,
+                                                             Expert8Args b)
+{
+    extern __shared__ __align__(16) unsigned char lds8[];
+    const RowTile t = find_row_tile<kBig8, RAGGED_LAST>(b.a, (b.a.N + kBig8 - 1) / kBig8, threadIdx.x & 63, reinterpret_cast<int *>(lds8));
+#if defined(__HIP_DEVICE_COMPILE__)
+    expert8_big_tile<RAGGED_LAST, TAIL>(x, w, y, b, t, lds8);
+#else
+    (void)x;
+    (void)w;
+    (void)y;
+    (void)t;
+#endif
 }
 
 template <int XR, int WR, int WX, int WW, int NST, bool F32>
@@ -210,14 +410,41 @@ int launch_expert8(const void *x, const void *w, void *y, const Expert8Args &b, 
     return MONTA_OK;
 }
 
+template <bool RAGGED_LAST, bool TAIL>
+int launch_expert8_big_k(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
+{
+    static LdsOptIn lds_opt_in;
+    constexpr int lds = kBig8LdsBytes;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<RAGGED_LAST, TAIL>), lds, lds_opt_in)) return rc;
+    const int64_t nct = (b.a.N + kBig8 - 1) / kBig8, row_tiles = rows_bound / kBig8 + std::min<int64_t>(b.a.E, rows_bound);
+    const int64_t tiles = (row_tiles + (RAGGED_LAST ? b.a.E : 0)) * nct;              // short ragged tiles come in halves
+    const int64_t grid = (tiles + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
+    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((expert8_big_kernel<RAGGED_LAST, TAIL>), dim3((unsigned)grid), dim3(512), lds, st, static_cast<const unsigned char *>(x),
+                       static_cast<const unsigned char *>(w), static_cast<__bf16 *>(y), b);
+    MONTA_HIP_TRY(hipGetLastError());
+    return MONTA_OK;
+}
+
+template <bool RAGGED_LAST>
+int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
+{
+    return b.a.H % 128 ? launch_expert8_big_k<RAGGED_LAST, true>(x, w, y, b, rows_bound, st) : launch_expert8_big_k<RAGGED_LAST, false>(x, w, y, b, rows_bound, st);
+}
+
 template <bool F32>
-int launch_expert8_tiled(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, int64_t kept_bound, hipStream_t st)
+int launch_expert8_tiled(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, int64_t kept_bound, int slice, hipStream_t st)
 {
     const int64_t active = std::min<int64_t>(b.a.E, kept_bound), r = kept_bound / active;
     auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.N + C - 1) / C) * (2 * r + R) / (2 * R); };
     if (r <= 24 || tiles(64, 128) <= 256) return launch_expert8<32, 64, 1, 4, 4, F32>(x, w, y, b, rows_bound, st);
-    if (r <= 96 || tiles(256, 256) <= 256) return launch_expert8<64, 128, 2, 2, 3, F32>(x, w, y, b, rows_bound, st);
-    return launch_expert8<256, 128, 4, 2, 3, F32>(x, w, y, b, rows_bound, st);
+    if constexpr (!F32)
+        if (r > 56 && tiles(256, 256) >= 160) {
+            // ragged tiles last: whole segments only, the search needs their lengths
+            const bool ragged_last = slice < 0 && r > 384 && (int64_t)b.a.E * ((b.a.N + kBig8 - 1) / kBig8) <= 256;
+            return ragged_last ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
+        }
+    return launch_expert8<64, 128, 2, 2, 3, F32>(x, w, y, b, rows_bound, st);
 }
 
 }  // namespace
@@ -252,6 +479,6 @@ extern "C" int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows,
     const int64_t rows_bound = slice_kept_bound(c.s, c.kept_bound, slice);
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_EXPERT_SCALED, st);
-    return c.bf16 ? launch_expert8_tiled<false>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, st)
-                  : launch_expert8_tiled<true>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, st);
+    return c.bf16 ? launch_expert8_tiled<false>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, slice, st)
+                  : launch_expert8_tiled<true>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, slice, st);
 }

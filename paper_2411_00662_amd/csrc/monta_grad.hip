@@ -21,96 +21,28 @@ struct GradArgs {
     void *out;
 };
 
-constexpr int kShortTileRows = 64;       // ragged tiles of dx up to this many rows run as short tiles
-
-// What a tile of the output belongs to.
-struct GradTile {
-    int e, row0, row_end;   // expert; rows of the tile (dx), or all rows of the expert (dw)
-    int rt, ct;             // row tile and column tile inside the expert
-    int side, share;        // row tiles next to one another on one column tile; which of them
-};
-
-// Tile of this workgroup; e < 0: none.  Logical tile numbers go out in blocks of 256, 32 consecutive ones to each XCD (hardware deals
-// consecutive workgroups round robin to the 8 XCDs, each with its own L2); inside an expert the numbering is (panel of 8 row
-// tiles, column tile, row tile), so that an XCD's workgroups share operand tiles.
-// RAGGED_LAST, of dx: the whole tiles of all experts come first and the segments' ragged last tiles after them, the one with the most
-// rows first, so that the last round of workgroups consists of the tiles that cost least.  `scratch`: 257 words of LDS that nothing else uses yet.
-template <bool DW, int BR, bool RAGGED_LAST>
-__device__ __forceinline__ GradTile find_grad_tile(const ExpertArgs &a, int nct, int lane, int *scratch)
+// Tile of dw of this workgroup, numbered like those of find_row_tile; e < 0: none.
+template <int BR>
+__device__ __forceinline__ RowTile find_weight_tile(const ExpertArgs &a, int nct)
 {
-    constexpr int P = 8;
-    static_assert(!DW || !RAGGED_LAST, "all tiles of dw are whole walks");
-    const int64_t jx = blockIdx.x / kXcds;
-    const int64_t L = (jx / 32) * (32 * kXcds) + (int64_t)(blockIdx.x % kXcds) * 32 + jx % 32;
-    GradTile t{-1, 0, 0, 0, 0, 1, 0};
-    int tiles = 0, lo = 0, hi = 0;
-    uint32_t in = 0;
-    int64_t whole_tiles = 0;
-    if constexpr (DW) {
-        tiles = (a.N + BR - 1) / BR;
-        const int64_t e = L / ((int64_t)tiles * nct);
-        if (e >= a.E) return t;
-        in = (uint32_t)(L - e * tiles * nct);
-        t.e = (int)e;
-        lo = a.lo[e];
-        hi = a.hi_base[e] + a.hi_len[e];
-    } else {
-        const ExpertTileHit hit = find_expert_tile<BR, RAGGED_LAST>(a, nct, L, lane, &whole_tiles);
-        if (hit.e < a.E) {
-            t.e = hit.e;
-            in = hit.L;
-            tiles = hit.tiles;
-            lo = hit.lo;
-            hi = hit.hi;
-        }
-    }
-    if (t.e >= 0) {
-        const int full = tiles / P;
-        const bool whole = in < (uint32_t)(full * P) * (uint32_t)nct;
-        const uint32_t rem = whole ? in % (uint32_t)(P * nct) : in - (uint32_t)(full * P) * (uint32_t)nct;
-        const int side = whole ? P : tiles - full * P;
-        t.ct = (int)(rem / (uint32_t)side);
-        t.side = side;
-        t.share = (int)(rem % (uint32_t)side);
-        t.rt = (whole ? (int)(in / (uint32_t)(P * nct)) : full) * P + t.share;
-    } else if constexpr (RAGGED_LAST) {
-        // position (L - whole tiles) / nct in the order (rows of the ragged tile, descending; expert, ascending), of the short ones, which are
-        // halves of 128 columns, 2 nct; E <= 256 threads
-        const int64_t Lr = L - whole_tiles;
-        const int tid = threadIdx.x;
-        int mine = 0;
-        if (tid < a.E) {
-            const int first = a.lo[tid], last = a.hi_base[tid] + a.hi_len[tid];
-            mine = last > first ? (last - first) % BR : 0;
-            scratch[tid] = mine;
-        }
-        if (tid == 0) scratch[256] = -1;
-        __syncthreads();
-        int rank = 0, long_ones = 0;
-        for (int o = 0; o < a.E; ++o) {
-            const int other = scratch[o];
-            long_ones += other > kShortTileRows ? 1 : 0;
-            rank += other > mine || (other == mine && o < tid) ? 1 : 0;
-        }
-        const int64_t halves = Lr - (int64_t)long_ones * nct;      // number among the halves
-        if (mine > 0 && rank == (halves < 0 ? Lr / nct : long_ones + halves / (2 * nct))) scratch[256] = tid;
-        __syncthreads();
-        t.e = scratch[256];
-        __syncthreads();                                           // everyone has read it before the stages are laid down
-        if (t.e < 0) return t;
-        lo = a.lo[t.e];
-        hi = a.hi_base[t.e] + a.hi_len[t.e];
-        t.ct = (int)(halves < 0 ? Lr % nct : halves % (2 * nct));
-        t.rt = (hi - lo) / BR;
-    } else {
-        return t;
-    }
-    hi = min(hi, a.max_rows);
-    lo = max(lo, 0);
-    t.row0 = DW ? lo : lo + t.rt * BR;
-    t.row_end = DW ? max(hi, lo) : min(hi, lo + (t.rt + 1) * BR);
-    if (!DW && t.row0 >= t.row_end) t.e = -1;
+    const int64_t L = tile_number();
+    RowTile t;
+    const int tiles = (a.N + BR - 1) / BR;
+    const int64_t e = L / ((int64_t)tiles * nct);
+    if (e >= a.E) return t;
+    t.e = (int)e;
+    place_in_panels(t, (uint32_t)(L - e * tiles * nct), tiles, nct);
+    t.row0 = max(a.lo[e], 0);
+    t.row_end = max(t.row0, min(a.hi_base[e] + a.hi_len[e], a.max_rows));
     return t;
+}
+
+template <bool DW, int BR, bool RAGGED_LAST>
+__device__ __forceinline__ RowTile find_grad_tile(const ExpertArgs &a, int nct, int lane, int *scratch)
+{
+    static_assert(!DW || !RAGGED_LAST, "all tiles of dw are whole walks");
+    if constexpr (DW) return find_weight_tile<BR>(a, nct);
+    else return find_row_tile<BR, RAGGED_LAST>(a, nct, lane, scratch);
 }
 
 // --------------------------------------------------------------------------------------------- bf16
@@ -271,7 +203,7 @@ template <int XR, int CW, int NST>
 __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs b)
 {
     extern __shared__ __align__(16) unsigned char grad_lds[];
-    const GradTile t = find_grad_tile<false, XR, false>(b.a, (b.a.H + CW - 1) / CW, threadIdx.x & 63, nullptr);
+    const RowTile t = find_grad_tile<false, XR, false>(b.a, (b.a.H + CW - 1) / CW, threadIdx.x & 63, nullptr);
     const int e = __builtin_amdgcn_readfirstlane(t.e);
     if (e < 0) return;
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -293,7 +225,7 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, unsigned char 
     const ExpertArgs &a = b.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
     const int wr = wave >> 1, wc = wave & 1;
-    const GradTile t = find_grad_tile<DW, BR, RAGGED_LAST>(a, (a.H + BC - 1) / BC, lane, reinterpret_cast<int *>(lds));
+    const RowTile t = find_grad_tile<DW, BR, RAGGED_LAST>(a, (a.H + BC - 1) / BC, lane, reinterpret_cast<int *>(lds));
     const int e = __builtin_amdgcn_readfirstlane(t.e);
     if (e < 0) return;
     const int row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
@@ -505,7 +437,7 @@ __global__ __launch_bounds__(256) void grad_f32_kernel(GradArgs b)
     __shared__ __align__(16) float rows[kF32Depth][kF32Pitch], cols[kF32Depth][kF32Pitch];
     const ExpertArgs &a = b.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4, wr = wave >> 1, wc = wave & 1;
-    const GradTile t = find_grad_tile<DW, kF32Tile, false>(a, (a.H + kF32Tile - 1) / kF32Tile, lane, nullptr);
+    const RowTile t = find_grad_tile<DW, kF32Tile, false>(a, (a.H + kF32Tile - 1) / kF32Tile, lane, nullptr);
     if (t.e < 0) return;
     const int64_t H = a.H, N = a.N;
     const int col0 = t.ct * kF32Tile, out0 = DW ? t.rt * kF32Tile : 0;

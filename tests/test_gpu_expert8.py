@@ -111,6 +111,10 @@ CASES = [  # tokens, hidden, out_features, experts, top_k, capacity factor, padd
     (1200, 384, 1160, 5, 2, 1.25, 0, 3, 2, 1.2),
     (2048, 272, 2056, 4, 2, 0.9, 1, 4, 1, 0.0),
     (900, 128, 8, 64, 8, 0.0, 0, 1, 1, 1.2),
+    (3300, 256, 2304, 6, 2, 0.0, 0, 1, 1, 0.0),        # large tiles, ragged ones of every length last
+    (3300, 400, 2056, 6, 2, 0.0, 0, 2, 1, 0.6),
+    (1100, 8320, 1032, 8, 4, 0.0, 1, 1, 1, 0.3),
+    (4000, 144, 1288, 60, 8, 0.8, 0, 1, 1, 0.9),       # large tiles, ragged ones in place
 ]
 
 

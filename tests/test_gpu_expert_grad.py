@@ -24,6 +24,9 @@ CASES = [  # tokens, hidden, out_features, experts, top_k, capacity factor, padd
     (1500, 136, 1160, 5, 2, 0.9, 1, 0.0),
     (300, 64, 200, 64, 8, 0.0, 0, 1.2),
     (2600, 776, 520, 2, 1, 0.0, 0, 0.0),
+    (3300, 2312, 136, 6, 2, 0.0, 0, 0.6),              # large tiles of dx, ragged ones of every length last
+    (3300, 2056, 2312, 6, 2, 1.1, 1, 0.0),             # large tiles of both
+    (4000, 1288, 200, 60, 8, 0.8, 0, 0.9),             # large tiles of dx, ragged ones in place
 ]
 
 
