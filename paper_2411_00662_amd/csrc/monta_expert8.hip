@@ -202,7 +202,7 @@ __global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned
 // Two stages of 64 KiB.  One barrier per step, before the last of the eight columns of products: then every wave has read all of
 // stage s, and stage s + 1 is there; the loads of s + 2 go to the place of s under the last column, as do the reads of the next step's
 // first fragments, each row fragment right behind its last use.
-constexpr int kBig8 = 256, kBig8Stage = 2 * kBig8 * 128 + 2048, kBig8LdsBytes = 2 * kBig8Stage;
+constexpr int kBig8 = 256, kBig8Stage = 2 * kBig8 * 128 + 2048, kBig8Sink = 2 * kBig8Stage, kBig8LdsBytes = kBig8Sink + 2048;
 
 template <bool RAGGED_LAST, bool TAIL>
 __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, __bf16 *__restrict__ y,
@@ -263,6 +263,18 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
         }
     };
 
+    // The early touches: a step's loads have a step's time to arrive, which covers an L2 hit but no miss, so each workgroup touches, a step
+    // ahead of them, one word per row of its share of the rows that it shares with the others on its XCD: waves 0 to 3 of x, with four column
+    // tiles, waves 4 to 7 of w, with the row tiles of the panel.
+    const int row_of_lane = (wave & 3) * 64 + lane;
+    const bool mine = wave < 4 ? wave == (__builtin_amdgcn_readfirstlane(t.ct) & 3)
+                               : row_of_lane * __builtin_amdgcn_readfirstlane(t.side) / kBig8 == __builtin_amdgcn_readfirstlane(t.share);
+    const uint32_t at_touch = mine ? (uint32_t)row_of_lane * (uint32_t)(wave < 4 ? b.row8 : a.H) : kOutOfRange;
+    const auto rt = wave < 4 ? rx : rw;
+    auto touch = [&](int step) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rt, (lds_void *)(lds8 + kBig8Sink + wave * 256), 4, at_touch, (uint32_t)min(step, b.nb - 1) * 128u, 0, 0);
+    };
+
     f32x4 acc[4][8];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -288,6 +300,7 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
 #pragma unroll
         for (int l = 0; l < 9; ++l) issue(1, l);
         __builtin_amdgcn_s_waitcnt(0x0f70 | 9);
+        touch(2);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -316,7 +329,7 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (j == 7) {
-                    __builtin_amdgcn_s_waitcnt(0x0070);            // this wave's part of stage s + 1 has landed, it has read all of stage s
+                    __builtin_amdgcn_s_waitcnt(0x0070 | 1);        // this wave's part of stage s + 1 has landed (younger: a touch), it has read all of stage s
                     asm volatile("" ::: "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
@@ -349,6 +362,7 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
                 }
                 fw = fw_next;
             }
+            touch(s + 3);
             sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw64), (s + 1) % 64));
         }
 #pragma unroll
