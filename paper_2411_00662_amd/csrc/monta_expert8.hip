@@ -294,12 +294,12 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
             return __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         };
         float sw64 = ws[min(lane, b.nb - 1)];                       // the scales of the wave's features: 64 steps at a time, one per lane
-        asm volatile("" : "+v"(sw64));
 #pragma unroll
         for (int l = 0; l < 9; ++l) issue(0, l);
 #pragma unroll
         for (int l = 0; l < 9; ++l) issue(1, l);
         __builtin_amdgcn_s_waitcnt(0x0f70 | 9);
+        asm volatile("" : "+v"(sw64));
         touch(2);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -373,22 +373,33 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
     else if (nb == 3) run(std::integral_constant<int, 3>{});
     else run(std::integral_constant<int, 4>{});
 
-    // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, output feature 16 j + 4 (lane / 16) + v of its columns
+    // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, output feature 16 j + 4 (lane / 16) + v of its columns.  Through LDS, block of 16 rows
+    // by block, so that rows leave as whole pieces of 16 bytes, 256 bytes of each side by side.
+    __builtin_amdgcn_s_waitcnt(0x0070);                            // the loads past the end have come back
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();                                  // and nobody reads the stages any more
+    asm volatile("" ::: "memory");
+    constexpr int kOutPitch = 256 + 16;
+    static_assert(8 * 16 * kOutPitch <= kBig8LdsBytes, "8-bit large tile: room for a block of rows per wave");
+    unsigned char *const own = lds8 + wave * (16 * kOutPitch);
+    __bf16 *const to = y + col0 + ww * 128;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int64_t r = row0 + wx * 16 * nb + i * 16 + m;
-        if (i < nb && r < row_end) {
+        if (i >= nb) break;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = col0 + ww * 128 + j * 16 + 4 * g;
-                if (n < a.N) {
-                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                    bf16x4 o;
+        for (int j = 0; j < 8; ++j) {
+            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            bf16x4 o;
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) o[v] = (__bf16)acc[i][j][v];
-                    *reinterpret_cast<bf16x4 *>(y + r * a.N + n) = o;
-                }
-            }
+            for (int v = 0; v < 4; ++v) o[v] = (__bf16)acc[i][j][v];
+            *reinterpret_cast<bf16x4 *>(own + m * kOutPitch + j * 32 + g * 8) = o;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int row = q * 4 + (lane >> 4), p = lane & 15;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(own + row * kOutPitch + p * 16);
+            const int64_t r = row0 + wx * 16 * nb + i * 16 + row;
+            if (r < row_end && col0 + ww * 128 + p * 8 < a.N) *reinterpret_cast<u32x4 *>(to + r * a.N + p * 8) = v;
         }
     }
 }
