@@ -199,9 +199,9 @@ __global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned
 // sums cannot stay in the accumulators of the matrix instructions: each is a product of its own, of 32 clocks, whose four results a lane
 // scales and adds in four more instructions, 16 clocks, under the other wave's products.  A result is used four products later, so that
 // nothing waits for it.
-// Two stages of 64 KiB.  One barrier per step, before the last of the eight columns of products: then every wave has read all of
-// stage s, and stage s + 1 is there; the loads of s + 2 go to the place of s under the last column, as do the reads of the next step's
-// first fragments, each row fragment right behind its last use.
+// Two stages of 64 KiB.  One barrier per step, before the last two of the eight columns of products: then every wave has read all of
+// stage s, and stage s + 1 is there; the loads of s + 2 go to the place of s under those two, as do the reads of the next step's first
+// fragments, each row fragment right behind its last use.
 constexpr int kBig8 = 256, kBig8Stage = 2 * kBig8 * 128 + 2048, kBig8Sink = 2 * kBig8Stage, kBig8LdsBytes = kBig8Sink + 2048;
 
 template <bool RAGGED_LAST, bool TAIL>
@@ -304,7 +304,7 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        i32x8 fx[NB], fw, fw_next;
+        i32x8 fx[NB], fw[4];                                       // a column's weights are read two columns ahead
         float sc[NB], raw[NB];                                     // of the present step; of the next, as they are stored
         constexpr int D = 4;                                       // a step's 8 NB products are a multiple of it: the ring begins anew with each
         f32x4 product[D];                                          // the youngest
@@ -317,7 +317,8 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
             raw[i] = *reinterpret_cast<const float *>(ps + i * 64);
             sc[i] = 0.f;
         }
-        fw = fragment(pw, 0, 0);
+        fw[0] = fragment(pw, 0, 0);
+        fw[1] = fragment(pw, 0, 1);
         // scales and adds product number n of a step (row block n % NB, column block n / NB)
         auto add = [&](const f32x4 &p, int n) {
 #pragma unroll
@@ -328,7 +329,7 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
             const int stage = s & 1;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (j == 7) {
+                if (j == 6) {
                     __builtin_amdgcn_s_waitcnt(0x0070 | 1);        // this wave's part of stage s + 1 has landed (younger: a touch), it has read all of stage s
                     asm volatile("" ::: "memory");
                     __builtin_amdgcn_s_barrier();
@@ -338,11 +339,11 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
                         asm volatile("" : "+v"(sw64));
                     }
                 }
-                fw_next = j < 7 ? fragment(pw, stage, j + 1) : fragment(pw, stage ^ 1, 0);
+                fw[(j + 2) % 4] = j < 6 ? fragment(pw, stage, j + 2) : fragment(pw, stage ^ 1, j - 6);
 #pragma unroll
                 for (int i = 0; i < NB; ++i) {
                     const int n = j * NB + i;
-                    f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fx[i], (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                    f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[j % 4], fx[i], (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
                     asm volatile("" : "+v"(p));                    // issued here, not where its result is used
                     if (n < D) {
                         const int old = 8 * NB + n - D;
@@ -355,12 +356,13 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
                     if (j == 7) {
                         fx[i] = fragment(px, stage ^ 1, i);
                         raw[i] = *reinterpret_cast<const float *>(ps + (stage ^ 1) * kBig8Stage + i * 64);
+                    }
+                    if (j >= 6) {
 #pragma unroll
-                        for (int l = i * 9 / NB; l < (i + 1) * 9 / NB; ++l) issue(s + 2, l);
+                        for (int l = ((j - 6) * NB + i) * 9 / (2 * NB); l < ((j - 6) * NB + i + 1) * 9 / (2 * NB); ++l) issue(s + 2, l);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                fw = fw_next;
             }
             touch(s + 3);
             sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw64), (s + 1) % 64));
