@@ -286,7 +286,7 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
 
     // all steps, NB blocks of 16 rows per wave: the rows of a ragged tile are split evenly over the four rows of waves
     auto run = [&](auto nbc) {
-        constexpr int NB = decltype(nbc)::value;
+        constexpr int NB = decltype(nbc)::value, kFirstLoads = 2 * NB * 9 / (4 * NB);
         const unsigned char *const px = lds8 + (wx * 16 * NB + m) * 128, *const ps = lds8 + 2 * kBig8 * 128 + (wx * 16 * NB + m) * 4;
         auto fragment = [&](const unsigned char *p, int stage, int block) {
             const u32x4 lo = *reinterpret_cast<const u32x4 *>(p + stage * kBig8Stage + block * 2048 + k0);
@@ -297,10 +297,9 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
 #pragma unroll
         for (int l = 0; l < 9; ++l) issue(0, l);
 #pragma unroll
-        for (int l = 0; l < 9; ++l) issue(1, l);
-        __builtin_amdgcn_s_waitcnt(0x0f70 | 9);
+        for (int l = 0; l < kFirstLoads; ++l) issue(1, l);          // the rest in the first step
+        __builtin_amdgcn_s_waitcnt(0x0f70 | kFirstLoads);
         asm volatile("" : "+v"(sw64));
-        touch(2);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -357,14 +356,17 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
                         fx[i] = fragment(px, stage ^ 1, i);
                         raw[i] = *reinterpret_cast<const float *>(ps + (stage ^ 1) * kBig8Stage + i * 64);
                     }
-                    if (j >= 6) {
+                    // the loads of step s + 2 begin behind the barrier and end in the second column of step s + 1: as a burst they would hold up the wave
+                    const int slot = (j + 2) % 8 * NB + i;
+                    if (slot < 4 * NB) {
 #pragma unroll
-                        for (int l = ((j - 6) * NB + i) * 9 / (2 * NB); l < ((j - 6) * NB + i + 1) * 9 / (2 * NB); ++l) issue(s + 2, l);
+                        for (int l = slot * 9 / (4 * NB); l < (slot + 1) * 9 / (4 * NB); ++l) issue(j >= 6 ? s + 2 : s + 1, l);
+                    } else if (slot == 4 * NB) {
+                        touch(s + 2);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            touch(s + 3);
             sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw64), (s + 1) % 64));
         }
 #pragma unroll
