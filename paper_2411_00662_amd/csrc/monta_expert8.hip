@@ -38,7 +38,7 @@ struct Tile8 {
 
 template <int XR, int WR, int WX, int WW, int NST, bool F32>
 __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, void *__restrict__ y,
-                                             const Expert8Args &b, int e, int row0, int row_end, int col0, unsigned char *lds8)
+                                             const Expert8Args &b, int e, int row0, int row_end, int col0, unsigned char *lds8, int start = 0)
 {
     using G = Tile8<XR, WR, WX, WW, NST>;
     const ExpertArgs &a = b.a;
@@ -54,10 +54,13 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
     auto piece = [&](int c) { return (lane & 7) ^ ((4 * c + (lr >> 1)) & 7); };
     const uint32_t rows8 = (uint32_t)b.row8, roww = (uint32_t)a.H;
     const uint32_t scale_at = (uint32_t)(wave * 64 + lane) * rows8 + roww;
+    // The walk begins at step `start` and goes round.  Past its end nothing is fetched.
+    auto place = [&](int step) { return step + start >= b.nb ? step + start - b.nb : step + start; };
     auto issue = [&](int step, int slot) {
         unsigned char *const base = lds8 + slot * G::kStageBytes;
-        const int left = step < b.nb ? a.H / 16 - step * 8 : 0;     // pieces of the row in this step; none past the end
-        const uint32_t so = step < b.nb ? (uint32_t)step * 128u : 0u;
+        const int at = step < b.nb ? place(step) : 0;
+        const int left = step < b.nb ? a.H / 16 - at * 8 : 0;       // pieces of the row in this step
+        const uint32_t so = (uint32_t)at * 128u;
 #pragma unroll
         for (int q = 0; q < G::kCW; ++q) {
             const int c = wave * G::kCW + q;
@@ -70,7 +73,7 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(base + c * 1024), 16,
                                                      piece(c) < left ? (uint32_t)(c * 8 + lr) * rows8 + piece(c) * 16 : kOutOfRange, so, 0, 0);
         }
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(base + (XR + WR) * 128 + wave * 256), 4, left > 0 ? scale_at + (uint32_t)step * 4u : kOutOfRange, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(base + (XR + WR) * 128 + wave * 256), 4, left > 0 ? scale_at + (uint32_t)at * 4u : kOutOfRange, 0, 0, 0);
     };
 
     f32x4 acc[G::kRB][G::kCB];
@@ -89,8 +92,9 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
     const unsigned char *const ps = lds8 + (XR + WR) * 128 + (wx * (XR / WX) + m) * 4;
     const int k0 = (g ^ ((m >> 1) & 7)) * 16, k1 = ((4 + g) ^ ((m >> 1) & 7)) * 16;
     for (int step = 0; step < b.nb; ++step) {
-        if (step % 64 == 0) {
-            sw64 = ws[min(step + lane, b.nb - 1)];
+        const int at = place(step);
+        if (at % 64 == 0 || step == 0) {
+            sw64 = ws[min(at / 64 * 64 + lane, b.nb - 1)];
             asm volatile("" : "+v"(sw64));                         // waited for here: left to its use, every step would wait for its loads
         }
         __builtin_amdgcn_s_waitcnt(G::kWait);                      // stage `step` has landed; this wave's reads of the one before are done
@@ -99,7 +103,7 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
         asm volatile("" ::: "memory");
         issue(step + NST - 1, slot == 0 ? NST - 1 : slot - 1);     // where stage step - 1 was
         const int buf = slot * G::kStageBytes;
-        const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw64), step % 64));
+        const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw64), at % 64));
         u32x4 fx[G::kRB][2];
         float sc[G::kRB];
 #pragma unroll
@@ -186,7 +190,8 @@ __global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned
     if (e < 0) return;
 #if defined(__HIP_DEVICE_COMPILE__)
     expert8_tile<XR, WR, WX, WW, NST, F32>(x, w, y, b, e, __builtin_amdgcn_readfirstlane(t.row0), __builtin_amdgcn_readfirstlane(t.row_end),
-                                           __builtin_amdgcn_readfirstlane(t.ct) * WR, lds8);
+                                           __builtin_amdgcn_readfirstlane(t.ct) * WR, lds8,
+                                           b.a.spread ? walk_start(e * ((b.a.N + WR - 1) / WR) + __builtin_amdgcn_readfirstlane(t.ct), b.nb) : 0);
 #else
     (void)x;
     (void)w;
@@ -461,19 +466,35 @@ int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args 
     return b.a.H % 128 ? launch_expert8_big_k<RAGGED_LAST, true>(x, w, y, b, rows_bound, st) : launch_expert8_big_k<RAGGED_LAST, false>(x, w, y, b, rows_bound, st);
 }
 
+// Which tile.  Measured on MI355X, three sets of buffers in turn, us; tokens x hidden x features, experts, top-2 (64 experts: top-8), in tiles of
+// 32 x 64, 32 x 128, 64 x 128, 128 x 128, 256 x 256 and those with the ragged tiles last:
+//   1 x 4096 x 4096, 8      13   16   20   26   37   21        256 x 1024 x 1024, 8     9.3  7.3  9.3  11   15   16
+//   64 x 4096 x 4096, 8     31   35   36   38   50   36        2048 x 512 x 512, 4      7.6  6.1  9.5  10   13   14
+//   256 x 4096 x 4096, 8    49   47   45   42   53   55        4096 x 1024 x 512, 32    24   22   20   18   22   25
+//   1024 x 4096 x 4096, 8   127  112  86   88   67   72        256 x 2048 x 1024, 64    36   35   28   29   33   41
+//   2048 x 4096 x 4096, 8   229  197  144  124  117  89        512 x 7168 x 2048, 64    296  255  223  190  201  226
+//   16 x 7168 x 2048, 64    134  143  143  149  179  162       1024 x 7168 x 2048, 64   475  399  322  289  223  241
+// Walks that start at different steps (walk_start) on weights' rows of whole 4 KiB, in 32 x 64: 64 x 4096 x 4096, 8 31.0 and 26.4 us, 8 tokens 27.5 and
+// 23.7; but 256 tokens 49.1 and 49.3, rows of 7168 133.8 and 139.3.
 template <bool F32>
-int launch_expert8_tiled(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, int64_t kept_bound, int slice, hipStream_t st)
+int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, int64_t rows_bound, int64_t kept_bound, int slice, hipStream_t st)
 {
     const int64_t active = std::min<int64_t>(b.a.E, kept_bound), r = kept_bound / active;
     auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.N + C - 1) / C) * (2 * r + R) / (2 * R); };
-    if (r <= 24 || tiles(64, 128) <= 256) return launch_expert8<32, 64, 1, 4, 4, F32>(x, w, y, b, rows_bound, st);
-    if constexpr (!F32)
-        if (r > 56 && tiles(256, 256) >= 160) {
+    if (r <= 24 || tiles(32, 64) <= 160) {
+        b.a.spread = b.a.H % 4096 == 0;
+        return launch_expert8<32, 64, 1, 4, 4, F32>(x, w, y, b, rows_bound, st);
+    }
+    if constexpr (!F32) {
+        if (tiles(32, 128) <= 300) return launch_expert8<32, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
+        if (r > 96 && tiles(256, 256) >= 140) {
             // ragged tiles last: whole segments only, the search needs their lengths
             const bool ragged_last = slice < 0 && r > 384 && (int64_t)b.a.E * ((b.a.N + kBig8 - 1) / kBig8) <= 256;
             return ragged_last ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
         }
-    return launch_expert8<64, 128, 2, 2, 3, F32>(x, w, y, b, rows_bound, st);
+        if (r > 48 && tiles(128, 128) >= 200) return launch_expert8<128, 128, 2, 2, 2, F32>(x, w, y, b, rows_bound, st);
+    }
+    return launch_expert8<64, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
 }
 
 }  // namespace
