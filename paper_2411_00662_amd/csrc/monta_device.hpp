@@ -149,12 +149,12 @@ struct RowTile {
     int side = 1, share = 0;             // row tiles next to one another on one column tile; which of them
 };
 
-// Logical tile number of this workgroup: they go out in blocks of 256, 32 consecutive ones to each XCD (hardware deals consecutive
+// Logical tile number of workgroup `block`: they go out in blocks of 256, 32 consecutive ones to each XCD (hardware deals consecutive
 // workgroups round robin to the 8 XCDs, each with its own L2).
-__device__ __forceinline__ int64_t tile_number()
+__device__ __forceinline__ int64_t tile_number(uint32_t block)
 {
-    const int64_t j = blockIdx.x / kXcds;
-    return (j / 32) * (32 * kXcds) + (int64_t)(blockIdx.x % kXcds) * 32 + j % 32;
+    const int64_t j = block / kXcds;
+    return (j / 32) * (32 * kXcds) + (int64_t)(block % kXcds) * 32 + j % 32;
 }
 
 // Inside an expert the numbering is (panel of 8 row tiles, column tile, row tile), so that an XCD's workgroups share operand tiles.
@@ -170,14 +170,14 @@ __device__ __forceinline__ void place_in_panels(RowTile &t, uint32_t in, int til
     t.rt = (whole ? (int)(in / (uint32_t)(P * nct)) : full) * P + t.share;
 }
 
-// Tile of BR rows of this workgroup.  RAGGED_LAST: the whole tiles of all experts come first and the segments' ragged last tiles after
+// Tile of BR rows of workgroup `block`.  RAGGED_LAST: the whole tiles of all experts come first and the segments' ragged last tiles after
 // them, the one with the most rows first, so that the last round of workgroups consists of the tiles that cost least; those of at most
 // kShortTileRows rows as halves of the column tile (ct counts halves).  For whole segments (hi_len), at least 256 threads and E <= 256; `scratch`: 257 words of LDS
 // that nothing else uses yet.
 template <int BR, bool RAGGED_LAST>
-__device__ __forceinline__ RowTile find_row_tile(const ExpertArgs &a, int nct, int lane, int *scratch)
+__device__ __forceinline__ RowTile find_row_tile(const ExpertArgs &a, int nct, uint32_t block, int lane, int *scratch)
 {
-    const int64_t L = tile_number();
+    const int64_t L = tile_number(block);
     RowTile t;
     int lo, hi;
     int64_t whole_tiles = 0;

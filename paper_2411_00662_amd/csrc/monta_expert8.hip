@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned
                                                                  void *__restrict__ y, Expert8Args b)
 {
     extern __shared__ __align__(16) unsigned char lds8[];
-    const RowTile t = find_row_tile<XR, false>(b.a, (b.a.N + WR - 1) / WR, threadIdx.x & 63, nullptr);
+    const RowTile t = find_row_tile<XR, false>(b.a, (b.a.N + WR - 1) / WR, blockIdx.x, threadIdx.x & 63, nullptr);
     const int e = __builtin_amdgcn_readfirstlane(t.e);
     if (e < 0) return;
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(512, 2) void expert8_big_kernel(const unsigned char
                                                              Expert8Args b)
 {
     extern __shared__ __align__(16) unsigned char lds8[];
-    const RowTile t = find_row_tile<kBig8, RAGGED_LAST>(b.a, (b.a.N + kBig8 - 1) / kBig8, threadIdx.x & 63, reinterpret_cast<int *>(lds8));
+    const RowTile t = find_row_tile<kBig8, RAGGED_LAST>(b.a, (b.a.N + kBig8 - 1) / kBig8, blockIdx.x, threadIdx.x & 63, reinterpret_cast<int *>(lds8));
 #if defined(__HIP_DEVICE_COMPILE__)
     expert8_big_tile<RAGGED_LAST, TAIL>(x, w, y, b, t, lds8);
 #else

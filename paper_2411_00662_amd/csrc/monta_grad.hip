@@ -18,14 +18,14 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 struct GradArgs {
     ExpertArgs a;           // lo, hi of the experts' rows, E, H, N, max_rows
     const void *dy, *x, *w;
-    void *out;
+    void *dx, *dw;
 };
 
-// Tile of dw of this workgroup, numbered like those of find_row_tile; e < 0: none.
+// Tile of dw of workgroup `block`, numbered like those of find_row_tile; e < 0: none.
 template <int BR>
-__device__ __forceinline__ RowTile find_weight_tile(const ExpertArgs &a, int nct)
+__device__ __forceinline__ RowTile find_weight_tile(const ExpertArgs &a, int nct, uint32_t block)
 {
-    const int64_t L = tile_number();
+    const int64_t L = tile_number(block);
     RowTile t;
     const int tiles = (a.N + BR - 1) / BR;
     const int64_t e = L / ((int64_t)tiles * nct);
@@ -38,11 +38,11 @@ __device__ __forceinline__ RowTile find_weight_tile(const ExpertArgs &a, int nct
 }
 
 template <bool DW, int BR, bool RAGGED_LAST>
-__device__ __forceinline__ RowTile find_grad_tile(const ExpertArgs &a, int nct, int lane, int *scratch)
+__device__ __forceinline__ RowTile find_grad_tile(const ExpertArgs &a, int nct, uint32_t block, int lane, int *scratch)
 {
     static_assert(!DW || !RAGGED_LAST, "all tiles of dw are whole walks");
-    if constexpr (DW) return find_weight_tile<BR>(a, nct);
-    else return find_row_tile<BR, RAGGED_LAST>(a, nct, lane, scratch);
+    if constexpr (DW) return find_weight_tile<BR>(a, nct, block);
+    else return find_row_tile<BR, RAGGED_LAST>(a, nct, block, lane, scratch);
 }
 
 // --------------------------------------------------------------------------------------------- bf16
@@ -180,7 +180,7 @@ __device__ __forceinline__ void grad_short_tile(const GradArgs &b, int e, int ro
     };
     if (2 * nb <= G::RB) run(std::integral_constant<int, G::RB / 2>{});
     else run(std::integral_constant<int, G::RB>{});
-    __bf16 *const out = static_cast<__bf16 *>(b.out);
+    __bf16 *const out = static_cast<__bf16 *>(b.dx);
 #pragma unroll
     for (int i = 0; i < G::RB; ++i) {
         const int64_t r = row0 + i * 16 + m;
@@ -199,25 +199,10 @@ __device__ __forceinline__ void grad_short_tile(const GradArgs &b, int e, int ro
     }
 }
 
-template <int XR, int CW, int NST>
-__global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs b)
-{
-    extern __shared__ __align__(16) unsigned char grad_lds[];
-    const RowTile t = find_grad_tile<false, XR, false>(b.a, (b.a.H + CW - 1) / CW, threadIdx.x & 63, nullptr);
-    const int e = __builtin_amdgcn_readfirstlane(t.e);
-    if (e < 0) return;
-#if defined(__HIP_DEVICE_COMPILE__)
-    grad_short_tile<XR, CW, NST>(b, e, __builtin_amdgcn_readfirstlane(t.row0), __builtin_amdgcn_readfirstlane(t.row_end),
-                                 __builtin_amdgcn_readfirstlane(t.ct) * CW, grad_lds);
-#else
-    (void)grad_lds;
-#endif
-}
-
 // The rows of a ragged tile of dx are split evenly between the two row halves: the loop is compiled for RB / 2 to RB blocks of 16
 // rows each, so that only rows in use are requested, read and multiplied.
 template <bool DW, int RB, int CB, bool RAGGED_LAST>
-__device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, unsigned char *lds)
+__device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block, unsigned char *lds)
 {
 #if defined(__HIP_DEVICE_COMPILE__)         // the matrix instruction is written out: nothing for the host pass to parse
     using G = GradShape<RB, CB>;
@@ -225,7 +210,7 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, unsigned char 
     const ExpertArgs &a = b.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
     const int wr = wave >> 1, wc = wave & 1;
-    const RowTile t = find_grad_tile<DW, BR, RAGGED_LAST>(a, (a.H + BC - 1) / BC, lane, reinterpret_cast<int *>(lds));
+    const RowTile t = find_grad_tile<DW, BR, RAGGED_LAST>(a, (a.H + BC - 1) / BC, block, lane, reinterpret_cast<int *>(lds));
     const int e = __builtin_amdgcn_readfirstlane(t.e);
     if (e < 0) return;
     const int row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
@@ -391,7 +376,7 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, unsigned char 
     constexpr int kOutPitch = 32 * CB + 16;                        // 16 bytes of padding: the 16 rows that a store of 8 bytes a lane hits begin on different banks
     unsigned char *const own = lds + wave * (16 * kOutPitch);
     static_assert(4 * 16 * kOutPitch <= G::kLdsBytes, "gradient tile: room for a block of rows per wave");
-    char *const out = static_cast<char *>(b.out) + ((DW ? (int64_t)e * N * H : 0) + col0 + wc * 16 * CB) * 2;
+    char *const out = static_cast<char *>(DW ? b.dw : b.dx) + ((DW ? (int64_t)e * N * H : 0) + col0 + wc * 16 * CB) * 2;
     const int l2 = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // asked for again: kept through the loop it would be spilled
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
@@ -414,88 +399,134 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, unsigned char 
     }
 #else
     (void)b;
+    (void)block;
     (void)lds;
 #endif
 }
 
-template <bool DW, int RB, int CB, bool RAGGED_LAST>
-__global__ __launch_bounds__(256, RB *CB == 64 ? 1 : 2) void grad_bf16_kernel(GradArgs b)
-{
-    extern __shared__ __align__(16) unsigned char grad_lds[];
-    grad_bf16_tile<DW, RB, CB, RAGGED_LAST>(b, grad_lds);
-}
-
 // --------------------------------------------------------------------------------------------- fp32
 //
-// 64 x 64 tiles by 2 x 2 waves, 32 elements of the summed axis at a time through registers into LDS, where both operands lie with that
-// axis outside (rows of 64 elements): a 32-bit element has nothing to be transposed with.  What bounds it is the fp32 matrix rate.
-constexpr int kF32Tile = 64, kF32Depth = 32, kF32Pitch = 68;
+// Tiles of BR x 64 by 2 x 2 waves, steps of 32 elements of the summed axis, NST stages straight to LDS, the loads of NST - 1 in flight.  A
+// 32-bit element has nothing to be transposed with: a deep operand, 32 rows of BR or 64 elements, is read element by element, MFMA v of half a
+// step taking rows 4 g + v of it (g the lane's group of 16), a flat one 16 bytes at a time, which are the same rows' elements.  Swizzles: flat as in
+// bf16; deep, the 64-byte segment s of row k at s ^ (k / 4) % 4, so that the four groups' rows are in different banks.  What bounds it is the
+// fp32 matrix rate, and with few steps the way to the first.
+template <int BR, int NST>
+struct GradShapeF32 {
+    static constexpr int BC = 64, kStage = (BR + BC) * 128, kLdsBytes = NST * kStage;
+    static constexpr int kLoadsR = BR / 32, kLoadsC = BC / 32, kYounger = (NST - 2) * (kLoadsR + kLoadsC);      // 1 KiB loads per wave and step
+    static constexpr int kWait = 0x0070 | (kYounger & 15) | ((kYounger >> 4) << 14);                         // vmcnt(kYounger), lgkmcnt(0)
+    static constexpr int RB = BR / 32;
+    static_assert((BR == 32 || BR == 64) && NST >= 3 && kYounger < 64, "fp32 gradient tile: shape");
+};
 
-template <bool DW>
-__global__ __launch_bounds__(256) void grad_f32_kernel(GradArgs b)
+// as deep_at, for 32 rows of 64 fp32 elements
+[[maybe_unused]] __device__ __forceinline__ uint32_t deep_at_f32(int c, int lane, uint32_t pitch, int exist)
 {
-    __shared__ __align__(16) float rows[kF32Depth][kF32Pitch], cols[kF32Depth][kF32Pitch];
+    const int k = (c * 64 + lane) / 16, p = lane % 16, from = ((p >> 2) ^ ((k >> 2) & 3)) * 4 + (p & 3);
+    return from * 4 < exist ? (uint32_t)k * pitch + (uint32_t)from * 16 : kOutOfRange;
+}
+
+template <bool DW, int BR, int NST>
+__device__ __forceinline__ void grad_f32_tile(const GradArgs &b, const RowTile &t, unsigned char *lds)
+{
+    using G = GradShapeF32<BR, NST>;
+    static_assert(!DW || BR == 64, "a deep operand has 64 elements");
     const ExpertArgs &a = b.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4, wr = wave >> 1, wc = wave & 1;
-    const RowTile t = find_grad_tile<DW, kF32Tile, false>(a, (a.H + kF32Tile - 1) / kF32Tile, lane, nullptr);
-    if (t.e < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4, wr = wave >> 1, wc = wave & 1;
+    const int e = __builtin_amdgcn_readfirstlane(t.e), row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
     const int64_t H = a.H, N = a.N;
-    const int col0 = t.ct * kF32Tile, out0 = DW ? t.rt * kF32Tile : 0;
-    const int depth = DW ? t.row_end - t.row0 : a.N;
-    const float *dy = static_cast<const float *>(b.dy) + (int64_t)t.row0 * N, *from_c = DW ? static_cast<const float *>(b.x) + (int64_t)t.row0 * H
-                                                                                           : static_cast<const float *>(b.w) + (int64_t)t.e * N * H;
-    constexpr f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    f32x4 pr[2], pc[2];
-    // piece q of this thread: deep operands, four elements of row k = piece / 16; flat ones, elements 4 (piece % 8) of row piece / 8
-    auto fetch = [&](int k0) {
+    const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * G::BC, out0 = DW ? __builtin_amdgcn_readfirstlane(t.rt) * BR : 0;
+    const int depth = DW ? row_end - row0 : a.N, nsteps = (depth + 31) / 32;
+    const uint32_t pitch_c = (uint32_t)a.H * 4, pitch_r = (uint32_t)a.N * 4;
+    const char *const from_c = static_cast<const char *>(DW ? b.x : b.w) + (DW ? (int64_t)row0 * H : (int64_t)e * N * H) * 4 + (int64_t)col0 * 4;
+    const char *const from_r = static_cast<const char *>(b.dy) + ((int64_t)row0 * N + out0) * 4;
+    const auto flat = make_rsrc(from_r, DW ? 0u : (uint32_t)(row_end - row0) * pitch_r);
+    uint32_t at_c[G::kLoadsC], at_r[G::kLoadsR];
+    int p_r[G::kLoadsR];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int p = tid + 256 * q, k = k0 + p / 16, c = p % 16 * 4;
-            pc[q] = k < depth && col0 + c < a.H ? *reinterpret_cast<const f32x4 *>(from_c + (int64_t)k * H + col0 + c) : zero;
-            if constexpr (DW) {
-                pr[q] = k < depth && out0 + c < a.N ? *reinterpret_cast<const f32x4 *>(dy + (int64_t)k * N + out0 + c) : zero;
-            } else {
-                const int r = p / 8, n = k0 + p % 8 * 4;
-                pr[q] = t.row0 + r < t.row_end && n < depth ? *reinterpret_cast<const f32x4 *>(dy + (int64_t)r * N + n) : zero;
+    for (int q = 0; q < G::kLoadsC; ++q) at_c[q] = deep_at_f32(wave * G::kLoadsC + q, lane, pitch_c, a.H - col0);
+#pragma unroll
+    for (int q = 0; q < G::kLoadsR; ++q) {
+        const int c = wave * G::kLoadsR + q, row = c * 8 + (lane >> 3);
+        p_r[q] = (lane & 7) ^ ((row >> 1) & 7);
+        at_r[q] = DW ? deep_at_f32(c, lane, pitch_r, a.N - out0) : (uint32_t)row * pitch_r + p_r[q] * 16;
+    }
+    auto issue = [&](int step, int slot) {
+        const int left = __builtin_amdgcn_readfirstlane(min(max(depth - step * 32, 0), 32));       // of the summed axis in this step, none past the end
+        const auto cols = make_rsrc(from_c + (int64_t)step * 32 * pitch_c, left > 0 ? (uint32_t)left * pitch_c - (uint32_t)col0 * 4u : 0u);
+        const auto deep = make_rsrc(from_r + (int64_t)step * 32 * pitch_r, DW && left > 0 ? (uint32_t)left * pitch_r - (uint32_t)out0 * 4u : 0u);
+        unsigned char *const base = lds + slot * G::kStage;
+#pragma unroll
+        for (int q = 0; q < G::kLoadsC; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(cols, (lds_void *)(base + BR * 128 + (wave * G::kLoadsC + q) * 1024), 16, at_c[q], 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < G::kLoadsR; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(DW ? deep : flat, (lds_void *)(base + (wave * G::kLoadsR + q) * 1024), 16,
+                                                     DW ? at_r[q] : p_r[q] * 4 < left ? at_r[q] + (uint32_t)step * 128u : kOutOfRange, 0, 0, 0);
+    };
+    f32x4 acc[G::RB][2];
+#pragma unroll
+    for (int i = 0; i < G::RB; ++i) acc[i][0] = acc[i][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < NST - 1; ++q) issue(q, q);
+    // One wave's blocks of 16 rows and 16 columns that exist: at the edge of the output it multiplies only those, which leaves its SIMD to other
+    // workgroups (10 experts of 516 x 516: the last of nine column tiles has four columns).
+    const int rows_left = DW ? a.N - out0 - wr * (BR / 2) : row_end - row0 - wr * (BR / 2), cols_left = a.H - col0 - wc * 32;
+    const int nr = min(max((rows_left + 15) / 16, 0), G::RB), nc = min(max((cols_left + 15) / 16, 0), 2);
+    // a loop for each count: conditions around the products inside one loop have given wrong results, a result read before it was there
+    auto walk = [&](auto rows, auto columns) {
+        constexpr int NR = decltype(rows)::value, NC = decltype(columns)::value;
+        int slot = 0;
+        for (int step = 0; step < nsteps; ++step) {
+            __builtin_amdgcn_s_waitcnt(G::kWait);                  // stage `step` has landed; this wave's reads of the one before are done
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            issue(step + NST - 1, slot == 0 ? NST - 1 : slot - 1); // where stage step - 1 was
+            const unsigned char *const base = lds + slot * G::kStage;
+            slot = slot == NST - 1 ? 0 : slot + 1;
+#pragma unroll
+            for (int ks = 0; ks < (NR * NC > 0 ? 2 : 0); ++ks) {
+                // row k = 16 ks + 4 g + v: (k / 4) % 4 = g
+                f32x4 fr[NR > 0 ? NR : 1];
+                float fc[NC > 0 ? NC : 1][4];
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    if constexpr (DW) {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) fr[i][v] = *reinterpret_cast<const float *>(base + (16 * ks + 4 * g + v) * 256 + ((wr * 2 + i) ^ g) * 64 + m * 4);
+                    } else {
+                        const int row = wr * (BR / 2) + i * 16 + m;
+                        fr[i] = *reinterpret_cast<const f32x4 *>(base + row * 128 + ((4 * ks + g) ^ ((m >> 1) & 7)) * 16);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NC; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) fc[j][v] = *reinterpret_cast<const float *>(base + BR * 128 + (16 * ks + 4 * g + v) * 256 + ((wc * 2 + j) ^ g) * 64 + m * 4);
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+#pragma unroll
+                        for (int j = 0; j < NC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fc[j][v], fr[i][v], acc[i][j], 0, 0, 0);
             }
         }
     };
-    f32x4 acc[2][2] = {{zero, zero}, {zero, zero}};
-    fetch(0);
-    for (int k0 = 0; k0 < depth; k0 += kF32Depth) {
-        __syncthreads();                                           // the previous step has been read
+    constexpr std::integral_constant<int, 0> none{};
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    if (nr == 0 || nc == 0) walk(none, none);
+    else if (G::RB == 2 && nr == 2 && nc == 2) walk(std::integral_constant<int, G::RB>{}, two);
+    else if (G::RB == 2 && nr == 2) walk(std::integral_constant<int, G::RB>{}, one);
+    else if (nc == 2) walk(one, two);
+    else walk(one, one);
+    float *const out = static_cast<float *>(DW ? b.dw : b.dx) + (DW ? (int64_t)e * N * H : 0);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int p = tid + 256 * q;
-            *reinterpret_cast<f32x4 *>(&cols[p / 16][p % 16 * 4]) = pc[q];
-            if constexpr (DW) {
-                *reinterpret_cast<f32x4 *>(&rows[p / 16][p % 16 * 4]) = pr[q];
-            } else {
-#pragma unroll
-                for (int v = 0; v < 4; ++v) rows[p % 8 * 4 + v][p / 8] = pr[q][v];
-            }
-        }
-        __syncthreads();
-        if (k0 + kF32Depth < depth) fetch(k0 + kF32Depth);
-#pragma unroll
-        for (int s = 0; s < kF32Depth / 4; ++s) {                  // group g's element: row 8 g + s, so that the groups are in two bank halves
-            float fr[2], fc[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fr[i] = rows[8 * g + s][wr * 32 + i * 16 + m];
-                fc[i] = cols[8 * g + s][wc * 32 + i * 16 + m];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fc[j], fr[i], acc[i][j], 0, 0, 0);
-        }
-    }
-    float *const out = static_cast<float *>(b.out) + (DW ? (int64_t)t.e * N * H : 0);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t r = (DW ? out0 : t.row0) + wr * 32 + i * 16 + m;
-        if (r < (DW ? a.N : t.row_end)) {
+    for (int i = 0; i < G::RB; ++i) {
+        const int64_t r = (DW ? out0 : row0) + wr * (BR / 2) + i * 16 + m;
+        if (r < (DW ? a.N : row_end)) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int h = col0 + wc * 32 + j * 16 + 4 * g;
@@ -508,37 +539,103 @@ __global__ __launch_bounds__(256) void grad_f32_kernel(GradArgs b)
 // --------------------------------------------------------------------------------------------- host
 
 // workgroups for tiles of BR x BC: of dx, as many as the rows can need (each expert may end in a ragged tile); of dw, exactly as many as there are
+int64_t whole_blocks(int64_t n) { return (n + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds); }
+
 template <bool DW>
 int64_t grad_grid(const ExpertArgs &a, int64_t BR, int64_t BC, int64_t rows_bound)
 {
     const int64_t row_tiles = DW ? a.E * ((a.N + BR - 1) / BR) : rows_bound / BR + std::min<int64_t>(a.E, rows_bound);
-    const int64_t n = row_tiles * ((a.H + BC - 1) / BC);
-    return (n + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
+    return whole_blocks(row_tiles * ((a.H + BC - 1) / BC));
 }
 
+// The forms: a tile's code for workgroup `block`, its LDS, the workgroups of a launch, the workgroups per CU that its registers allow.
 template <bool DW, int RB, int CB, bool RAGGED_LAST = false>
-int launch_grad_bf16(const GradArgs &b, int64_t rows_bound, hipStream_t st)
-{
+struct Wide {
     using G = GradShape<RB, CB>;
+    static constexpr int kLds = G::kLdsBytes, kPerCu = RB * CB == 64 ? 1 : 2;
+    static int64_t grid(const ExpertArgs &a, int64_t rows_bound)
+    {
+        // the short ragged tiles come in halves
+        return grad_grid<DW>(a, G::BR, G::BC, rows_bound) + (RAGGED_LAST ? whole_blocks((int64_t)a.E * ((a.H + G::BC - 1) / G::BC)) : 0);
+    }
+    static __device__ __forceinline__ void run(const GradArgs &b, uint32_t block, unsigned char *lds) { grad_bf16_tile<DW, RB, CB, RAGGED_LAST>(b, block, lds); }
+};
+
+template <int XR, int CW, int NST>
+struct Short {
+    static constexpr int kLds = GradShort<XR, CW, NST>::kLdsBytes, kPerCu = 2;
+    static int64_t grid(const ExpertArgs &a, int64_t rows_bound) { return grad_grid<false>(a, XR, CW, rows_bound); }
+    static __device__ __forceinline__ void run(const GradArgs &b, uint32_t block, unsigned char *lds)
+    {
+        const RowTile t = find_grad_tile<false, XR, false>(b.a, (b.a.H + CW - 1) / CW, block, threadIdx.x & 63, nullptr);
+        const int e = __builtin_amdgcn_readfirstlane(t.e);
+        if (e >= 0)
+            grad_short_tile<XR, CW, NST>(b, e, __builtin_amdgcn_readfirstlane(t.row0), __builtin_amdgcn_readfirstlane(t.row_end),
+                                         __builtin_amdgcn_readfirstlane(t.ct) * CW, lds);
+    }
+};
+
+template <bool DW, int BR, int NST>
+struct F32 {
+    static constexpr int kLds = GradShapeF32<BR, NST>::kLdsBytes, kPerCu = 2;
+    static int64_t grid(const ExpertArgs &a, int64_t rows_bound) { return grad_grid<DW>(a, BR, 64, rows_bound); }
+    static __device__ __forceinline__ void run(const GradArgs &b, uint32_t block, unsigned char *lds)
+    {
+        const RowTile t = find_grad_tile<DW, BR, false>(b.a, (b.a.H + 63) / 64, block, threadIdx.x & 63, nullptr);
+        if (__builtin_amdgcn_readfirstlane(t.e) >= 0) grad_f32_tile<DW, BR, NST>(b, t, lds);
+    }
+};
+
+template <typename Form>
+__global__ __launch_bounds__(256, Form::kPerCu) void grad_kernel(GradArgs b)
+{
+    extern __shared__ __align__(16) unsigned char grad_lds[];
+#if defined(__HIP_DEVICE_COMPILE__)
+    Form::run(b, blockIdx.x, grad_lds);
+#else
+    (void)b;
+    (void)grad_lds;
+#endif
+}
+
+// Both gradients in one launch, the first `split` workgroups those of dx.
+template <typename Dx, typename Dw>
+__global__ __launch_bounds__(256, Dx::kPerCu < Dw::kPerCu ? Dx::kPerCu : Dw::kPerCu) void grad_both_kernel(GradArgs b, uint32_t split)
+{
+    extern __shared__ __align__(16) unsigned char grad_lds[];
+#if defined(__HIP_DEVICE_COMPILE__)
+    if (blockIdx.x < split) Dx::run(b, blockIdx.x, grad_lds);
+    else Dw::run(b, blockIdx.x - split, grad_lds);
+#else
+    (void)b;
+    (void)grad_lds;
+    (void)split;
+#endif
+}
+
+template <typename Form>
+int launch_form(const GradArgs &b, int64_t rows_bound, hipStream_t st)
+{
     static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_bf16_kernel<DW, RB, CB, RAGGED_LAST>), G::kLdsBytes, lds_opt_in)) return rc;
-    int64_t grid = grad_grid<DW>(b.a, G::BR, G::BC, rows_bound);
-    if (RAGGED_LAST) grid += ((int64_t)b.a.E * ((b.a.H + G::BC - 1) / G::BC) + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);        // halves
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_kernel<Form>), Form::kLds, lds_opt_in)) return rc;
+    const int64_t grid = Form::grid(b.a, rows_bound);
     if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((grad_bf16_kernel<DW, RB, CB, RAGGED_LAST>), dim3((unsigned)grid), dim3(256), G::kLdsBytes, st, b);
+    LaunchTimer timer(MONTA_K_EXPERT_BACKWARD, st);
+    hipLaunchKernelGGL((grad_kernel<Form>), dim3((unsigned)grid), dim3(256), Form::kLds, st, b);
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
 }
 
-template <int XR, int CW, int NST>
-int launch_grad_short(const GradArgs &b, int64_t rows_bound, hipStream_t st)
+template <typename Dx, typename Dw>
+int launch_both(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 {
-    using G = GradShort<XR, CW, NST>;
+    constexpr int lds = Dx::kLds > Dw::kLds ? Dx::kLds : Dw::kLds;
     static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_short_kernel<XR, CW, NST>), G::kLdsBytes, lds_opt_in)) return rc;
-    const int64_t grid = grad_grid<false>(b.a, XR, CW, rows_bound);
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_both_kernel<Dx, Dw>), lds, lds_opt_in)) return rc;
+    const int64_t split = Dx::grid(b.a, rows_bound), grid = split + Dw::grid(b.a, rows_bound);
     if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((grad_short_kernel<XR, CW, NST>), dim3((unsigned)grid), dim3(256), G::kLdsBytes, st, b);
+    LaunchTimer timer(MONTA_K_EXPERT_BACKWARD, st);
+    hipLaunchKernelGGL((grad_both_kernel<Dx, Dw>), dim3((unsigned)grid), dim3(256), lds, st, b, (uint32_t)split);
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
 }
@@ -555,32 +652,43 @@ int launch_grad_short(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 //   1 x 4096 x 4096, 8     50   56                            1024 x 1024 x 1024, 8     12   18
 //   256 x 4096 x 4096, 8   91   84                            4096 x 1024 x 512, 32     19   18
 //   2048 x 4096 x 4096, 8  220  181                           3000 x 1000 x 3000, 4     49   48
-template <bool DW>
-int launch_grad(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t st)
+// Few tiles: both gradients go out together, as alone neither fills the chip to its end (us, one after the other and together: 1 x 1024 x 1024, 8 experts 13.7
+// and 9.1, 256 tokens 16.8 and 12.9, 4096 tokens 53.8 and 49.9; but 64 x 4096 x 4096, where dx then has as little room as dw, 122 and
+// 154, and the large tiles of 8192 x 4096 x 4096 906 and 1000).  fp32 always: 4096 x 1024 x 1024, 8 experts 351 and 310.
+int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t st)
 {
-    LaunchTimer timer(MONTA_K_EXPERT_BACKWARD, st);
-    if (!bf16) {
-        const int64_t grid = grad_grid<DW>(b.a, kF32Tile, kF32Tile, rows_bound);
-        if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((grad_f32_kernel<DW>), dim3((unsigned)grid), dim3(256), 0, st, b);
-        MONTA_HIP_TRY(hipGetLastError());
-        return MONTA_OK;
-    }
     const int64_t active = std::min<int64_t>(b.a.E, rows_bound), r = rows_bound / active;
-    if constexpr (DW) {
-        const int64_t tiles = b.a.E * ((b.a.N + 255) / 256) * ((b.a.H + 255) / 256);
-        return r > 8 && tiles >= 192 ? launch_grad_bf16<true, 8, 8>(b, rows_bound, st) : launch_grad_bf16<true, 4, 4>(b, rows_bound, st);
-    } else {
-        auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.H + C - 1) / C) * (2 * r + R) / (2 * R); };
-        if (tiles(32, 64) <= 256) return launch_grad_short<32, 64, 4>(b, rows_bound, st);
-        if (r <= 24 || tiles(32, 128) <= 400) return launch_grad_short<32, 128, 3>(b, rows_bound, st);
-        if (r > 56 && tiles(256, 256) >= 160) {
-            const bool ragged_last = r > 384 && b.a.E * ((b.a.H + 255) / 256) <= 256;
-            return ragged_last ? launch_grad_bf16<false, 8, 8, true>(b, rows_bound, st) : launch_grad_bf16<false, 8, 8>(b, rows_bound, st);
-        }
-        if (r <= 56 || tiles(64, 128) <= 700) return launch_grad_short<64, 128, 3>(b, rows_bound, st);
-        return launch_grad_bf16<false, 4, 4>(b, rows_bound, st);
+    auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.H + C - 1) / C) * (2 * r + R) / (2 * R); };
+    auto launch = [&](auto dx, auto dw, auto together) {
+        using Dx = decltype(dx);
+        using Dw = decltype(dw);
+        if constexpr (decltype(together)::value)
+            if (b.dx && b.dw) return launch_both<Dx, Dw>(b, rows_bound, st);
+        if (b.dx)
+            if (int rc = launch_form<Dx>(b, rows_bound, st)) return rc;
+        return b.dw ? launch_form<Dw>(b, rows_bound, st) : MONTA_OK;
+    };
+    constexpr std::true_type together{};
+    constexpr std::false_type apart{};
+    if (!bf16) {
+        if (tiles(64, 64) <= 1024) return launch(F32<false, 32, 3>{}, F32<true, 64, 3>{}, together);
+        return launch(F32<false, 64, 3>{}, F32<true, 64, 3>{}, together);
     }
+    const bool big_dw = r > 8 && (int64_t)b.a.E * ((b.a.N + 255) / 256) * ((b.a.H + 255) / 256) >= 192;
+    const bool few_dw = (int64_t)b.a.E * ((b.a.N + 127) / 128) * ((b.a.H + 127) / 128) <= 768;
+    auto with_dw = [&](auto dx) {
+        if (big_dw) return launch(dx, Wide<true, 8, 8>{}, apart);
+        return few_dw ? launch(dx, Wide<true, 4, 4>{}, together) : launch(dx, Wide<true, 4, 4>{}, apart);
+    };
+    if (tiles(32, 64) <= 256) return with_dw(Short<32, 64, 4>{});
+    if (r <= 24 || tiles(32, 128) <= 400) return with_dw(Short<32, 128, 3>{});
+    if (r > 56 && tiles(256, 256) >= 160) {
+        const bool ragged_last = r > 384 && b.a.E * ((b.a.H + 255) / 256) <= 256;
+        if (!big_dw) return ragged_last ? launch(Wide<false, 8, 8, true>{}, Wide<true, 4, 4>{}, apart) : launch(Wide<false, 8, 8>{}, Wide<true, 4, 4>{}, apart);
+        return ragged_last ? launch(Wide<false, 8, 8, true>{}, Wide<true, 8, 8>{}, apart) : launch(Wide<false, 8, 8>{}, Wide<true, 8, 8>{}, apart);
+    }
+    if (r <= 56 || tiles(64, 128) <= 700) return with_dw(Short<64, 128, 3>{});
+    return with_dw(Wide<false, 4, 4>{});
 }
 
 }  // namespace
@@ -616,14 +724,7 @@ extern "C" int monta_expert_linear_backward(const monta_cfg *cfg, const void *dy
     b.dy = dy;
     b.x = x_final;
     b.w = w_exp;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dx_final) {
-        b.out = dx_final;
-        if (int rc = launch_grad<false>(b, c.bf16, c.kept_bound, st)) return rc;
-    }
-    if (dw_exp) {
-        b.out = dw_exp;
-        if (int rc = launch_grad<true>(b, c.bf16, c.kept_bound, st)) return rc;
-    }
-    return MONTA_OK;
+    b.dx = dx_final;
+    b.dw = dw_exp;
+    return launch_grads(b, c.bf16, c.kept_bound, static_cast<hipStream_t>(stream));
 }
