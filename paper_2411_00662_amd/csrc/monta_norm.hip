@@ -35,6 +35,19 @@ __device__ __forceinline__ void unpack(u32x4 v, float (&f)[Elem<BF16>::kPerVec])
     }
 }
 
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load(const u32x4 *p)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool STREAM>
+__device__ __forceinline__ void store(u32x4 *p, u32x4 v)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // nearest-even; NaN stays NaN
 template <bool BF16>
 __device__ __forceinline__ u32x4 pack(const float (&f)[Elem<BF16>::kPerVec])
@@ -61,8 +74,8 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
-// The same over a whole row: across waves through `part`, which the caller alternates from row to row, so that one barrier
-// keeps a row's sums from the next row's.
+// The same over a whole row: across waves through `part`, the row's own, which the caller alternates from row to row, so that one
+// barrier keeps a row's sums from the next row's.
 template <int L, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float *part)
 {
@@ -70,7 +83,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *part)
     for (int i = 0; i < N; ++i) v[i] = lanes_sum<(L < kWave ? L : kWave)>(v[i]);
     if constexpr (L > kWave) {
         constexpr int W = L / kWave;
-        const int wave = threadIdx.x / kWave;
+        const int wave = threadIdx.x % L / kWave;
         if (threadIdx.x % kWave == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) part[i * W + wave] = v[i];
@@ -87,6 +100,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *part)
 
 template <int L>
 constexpr int threads_of() { return L <= kWave ? 256 : L; }
+// of the norm's gradient: two rows of 256 lanes, for eight waves a CU with as few partial sums as four would leave
+template <int L>
+constexpr int backward_threads_of() { return L <= kWave ? 256 : L < 512 ? 512 : L; }
 
 // --------------------------------------------------------------------------------------------- norm
 //
@@ -97,7 +113,8 @@ constexpr int threads_of() { return L <= kWave ? 256 : L; }
 // The norm is that of the stored sum, which is what the gradient reads again.  v itself goes to 8 bits, not its rounding to 16:
 // one rounding each.  e4m3 ends at 448: the largest value of a block times (448 / amax) is at most 448 (1 + 2^-23), which rounds to 448.
 // A block of zeros, or of values below 2^-40, keeps a finite factor.
-template <bool BF16, int L, int NV>
+// 8192 x 4096 bf16 with a residual, both outputs: 303 MB in 48.8 us, 6.2 TB/s; a copy of that size reaches 6.2 to 6.5.
+template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_kernel(const u32x4 *x, const u32x4 *residual, const u32x4 *w, u32x4 *sum,
                                                                   u32x4 *out, unsigned char *rows8, int T, int vpr, int row8_bytes, float eps)
 {
@@ -118,8 +135,8 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_kernel(const u32x4 *x
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             const int i = l + q * L;
-            s[q] = i < vpr ? x[row * vpr + i] : (u32x4){0u, 0u, 0u, 0u};
-            if (residual) add[q] = i < vpr ? residual[row * vpr + i] : (u32x4){0u, 0u, 0u, 0u};
+            s[q] = i < vpr ? load<STREAM>(x + row * vpr + i) : (u32x4){0u, 0u, 0u, 0u};
+            if (residual) add[q] = i < vpr ? load<STREAM>(residual + row * vpr + i) : (u32x4){0u, 0u, 0u, 0u};
         }
         float ss[1] = {0.f};
 #pragma unroll
@@ -148,8 +165,8 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_kernel(const u32x4 *x
 #pragma unroll
             for (int e = 0; e < EV; ++e) v[e] = v[e] * r * g[e];
             const bool mine = live && i < vpr;
-            if (mine && residual) sum[row * vpr + i] = s[q];
-            if (mine && out) out[row * vpr + i] = pack<BF16>(v);
+            if (mine && residual) store<STREAM>(sum + row * vpr + i, s[q]);
+            if (mine && out) store<STREAM>(out + row * vpr + i, pack<BF16>(v));
             if (rows8) {
                 float amax = 0.f;
 #pragma unroll
@@ -183,13 +200,15 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_kernel(const u32x4 *x
 // A workgroup walks over rows and keeps the weight's and its gradient's share in registers; the next row is requested before the
 // present one's sums are known.  The gradient's partial sums, one row of H per workgroup, are added by rmsnorm_dweight_kernel: a fixed
 // order, no atomics.
-template <bool BF16, int L, int NV>
-__global__ __launch_bounds__(threads_of<L>()) void rmsnorm_backward_kernel(const u32x4 *s_in, const u32x4 *w, const u32x4 *dout, const u32x4 *dsum,
+// 8192 x 4096 bf16 with dsum: 268 MB in 52 us with the sum of the partials, 5.2 TB/s; one row of 256 lanes a workgroup instead of two
+// takes 50.3, but 1155 x 2048 fp32 9.7 us for 8.8 and 517 x 1155 8.3 for 7.4.
+template <bool BF16, int L, int NV, bool STREAM>
+__global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_kernel(const u32x4 *s_in, const u32x4 *w, const u32x4 *dout, const u32x4 *dsum,
                                                                            u32x4 *dx, float *partial, int T, int vpr, float eps)
 {
-    constexpr int EV = Elem<BF16>::kPerVec, kRows = threads_of<L>() / L;
+    constexpr int EV = Elem<BF16>::kPerVec, kRows = backward_threads_of<L>() / L;
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
-    __shared__ float part[2][2 * (L > kWave ? L / kWave : 1)];
+    __shared__ float part[2][kRows][2 * (L > kWave ? L / kWave : 1)];
     const int l = threadIdx.x % L, group = threadIdx.x / L;
     const int H = vpr * EV;
     u32x4 wv[NV];
@@ -207,9 +226,9 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_backward_kernel(const
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             const int i = l + q * L;
-            s[q] = i < vpr ? s_in[row * vpr + i] : zero;
-            d[q] = i < vpr ? dout[row * vpr + i] : zero;
-            t[q] = dsum && i < vpr ? dsum[row * vpr + i] : zero;
+            s[q] = i < vpr ? load<STREAM>(s_in + row * vpr + i) : zero;
+            d[q] = i < vpr ? load<STREAM>(dout + row * vpr + i) : zero;
+            t[q] = dsum && i < vpr ? load<STREAM>(dsum + row * vpr + i) : zero;
         }
     };
     int parity = 0;
@@ -236,7 +255,7 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_backward_kernel(const
             }
         }
         if (kAhead && base + (int)gridDim.x * kRows < T) fetch(base + gridDim.x * kRows);
-        row_sums<L>(sums, part[parity]);
+        row_sums<L>(sums, part[parity][group]);
         const float r = 1.f / __builtin_sqrtf(sums[0] / (float)H + eps);
         const float c = r * r * (sums[1] / (float)H);               // dx = r (g - s c) + dsum
 #pragma unroll
@@ -269,7 +288,7 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_backward_kernel(const
 #pragma unroll
             for (int e = 0; e < EV; ++e) cols[group][(l + q * L) * EV + e] = dw[q][e];
         __syncthreads();
-        for (int h = threadIdx.x; h < H; h += threads_of<L>()) {
+        for (int h = threadIdx.x; h < H; h += backward_threads_of<L>()) {
             float v = 0.f;
 #pragma unroll
             for (int g = 0; g < kRows; ++g) v += cols[g][h];
@@ -278,14 +297,21 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_backward_kernel(const
     }
 }
 
-// Adds `n` rows of H partial sums: a workgroup takes 32 columns, its 32 half waves every 32nd row each.
+// Adds `n` rows of H partial sums: a workgroup takes 32 columns, its 32 half waves every 32nd row each, eight loads at a time (one at a
+// time costs 1.5 us of the 9 that 517 x 1155 takes, all of it latency).
 __global__ __launch_bounds__(1024) void rmsnorm_dweight_kernel(const float *partial, float *dweight, int n, int H)
 {
     __shared__ float part[32][33];
     const int c = threadIdx.x % 32, r = threadIdx.x / 32, h = blockIdx.x * 32 + c;
     float v = 0.f;
     if (h < H)
-        for (int i = r; i < n; i += 32) v += partial[(int64_t)i * H + h];
+        for (int i = r; i < n; i += 8 * 32) {                      // eight loads at a time
+            float p[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) p[q] = i + q * 32 < n ? partial[(int64_t)(i + q * 32) * H + h] : 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v += p[q];
+        }
     part[r][c] = v;
     __syncthreads();
     if (r == 0 && h < H) {
@@ -299,38 +325,43 @@ __global__ __launch_bounds__(1024) void rmsnorm_dweight_kernel(const float *part
 // --------------------------------------------------------------------------------------------- gradient of the combine
 //
 // out[t] = sum_j g[t][j] y[row(t, j)]:   dy[row(t, j)] = g[t][j] dout[t],   dg[t][j] = <dout[t], y[row(t, j)]>.
-// A token's lanes keep its row of dout in registers and go over its choices, the next choice's row of y on its way while the
-// present one is multiplied.  A dropped choice has no row: its gate's gradient is 0.
-template <bool BF16, int L, int NV>
+// A token's lanes keep its row of dout in registers and go over its kept choices, the next one's row of y on its way while the present
+// one is multiplied.  A wave knows all choices from one load, lane j's is choice j (k <= 32); a dropped one has no row: its gate's gradient is 0.
+// 8192 x 4096 bf16 over 8 experts, top-2: 336 MB in 52.9 us, 6.3 TB/s.
+template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(threads_of<L>()) void combine_backward_kernel(const u32x4 *dout, const u32x4 *y, const float *gates, u32x4 *dy,
                                                                            float *dgates, const int32_t *pos_final, int T, int k, int vpr, int max_rows)
 {
-    constexpr int EV = Elem<BF16>::kPerVec, kRows = threads_of<L>() / L, W = L > kWave ? L / kWave : 1;
+    static_assert(L >= kWave, "a wave has one token");
+    constexpr int EV = Elem<BF16>::kPerVec, kRows = threads_of<L>() / L, W = L / kWave;
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
     __shared__ float part[32][W];
-    const int l = threadIdx.x % L, group = threadIdx.x / L;
-    const int t = blockIdx.x * kRows + group;
-    const bool live = t < T;
-    const int64_t tk = (int64_t)(live ? t : T - 1) * k;
+    const int l = threadIdx.x % L, lane = threadIdx.x % kWave, wave = l / kWave;
+    const int t = blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / L);
+    if (t >= T) return;                                            // a whole wave, and with L > 64 never
+    const int64_t tk = (int64_t)t * k;
+    const int pos = lane < k ? pos_final[tk + lane] : -1;
+    const float gate = lane < k ? gates[tk + lane] : 0.f;
     u32x4 d[NV], cur[NV];
 #pragma unroll
-    for (int q = 0; q < NV; ++q) d[q] = l + q * L < vpr ? dout[(int64_t)(live ? t : T - 1) * vpr + l + q * L] : zero;
-    auto row_of = [&](int j) {
-        const int p = pos_final[tk + j];
-        return p >= 0 && p < max_rows ? p : -1;
-    };
-    auto fetch = [&](int row, u32x4(&to)[NV]) {
+    for (int q = 0; q < NV; ++q) d[q] = l + q * L < vpr ? dout[(int64_t)t * vpr + l + q * L] : zero;
+    const bool kept = pos >= 0 && pos < max_rows;
+    unsigned long long left = __ballot(kept);
+    auto row_of = [&](int j) { return (int64_t)__builtin_amdgcn_readlane(pos, j); };
+    auto fetch = [&](int64_t row, u32x4(&to)[NV]) {
 #pragma unroll
-        for (int q = 0; q < NV; ++q) to[q] = row >= 0 && l + q * L < vpr ? y[(int64_t)row * vpr + l + q * L] : zero;
+        for (int q = 0; q < NV; ++q) to[q] = l + q * L < vpr ? load<STREAM>(y + row * vpr + l + q * L) : zero;
     };
-    int row = row_of(0);
-    fetch(row, cur);
-    for (int j = 0; j < k; ++j) {
+    float mine = 0.f;                                              // lane j: the wave's share of choice j's gradient
+    if (left) fetch(row_of(__builtin_ctzll(left)), cur);
+    while (left) {
+        const int j = __builtin_ctzll(left);
+        left &= left - 1;
         u32x4 next[NV];
-        const int row_next = j + 1 < k ? row_of(j + 1) : -1;
-        fetch(row_next, next);
-        const float g = gates[tk + j];
-        float dot[1] = {0.f};
+        if (left) fetch(row_of(__builtin_ctzll(left)), next);
+        const int64_t row = row_of(j);
+        const float g = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(gate), j));
+        float dot = 0.f;
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             const int i = l + q * L;
@@ -339,28 +370,26 @@ __global__ __launch_bounds__(threads_of<L>()) void combine_backward_kernel(const
             unpack<BF16>(cur[q], b);
 #pragma unroll
             for (int e = 0; e < EV; ++e) {
-                dot[0] = __builtin_fmaf(a[e], b[e], dot[0]);
+                dot = __builtin_fmaf(a[e], b[e], dot);
                 a[e] *= g;
             }
-            if (live && row >= 0 && i < vpr) dy[(int64_t)row * vpr + i] = pack<BF16>(a);
+            if (i < vpr) store<STREAM>(dy + row * vpr + i, pack<BF16>(a));
         }
-        dot[0] = lanes_sum<(L < kWave ? L : kWave)>(dot[0]);
-        if constexpr (L <= kWave) {
-            if (live && l == 0) dgates[tk + j] = row >= 0 ? dot[0] : 0.f;
-        } else {
-            if (threadIdx.x % kWave == 0) part[j][threadIdx.x / kWave] = row >= 0 ? dot[0] : 0.f;
-        }
-        row = row_next;
+        dot = lanes_sum<kWave>(dot);
+        if (lane == j) mine = dot;
 #pragma unroll
         for (int q = 0; q < NV; ++q) cur[q] = next[q];
     }
-    if constexpr (L > kWave) {
+    if constexpr (W == 1) {
+        if (lane < k) dgates[tk + lane] = mine;
+    } else {
+        if (lane < k) part[lane][wave] = mine;
         __syncthreads();
-        if ((int)threadIdx.x < k) {
+        if (l < k) {
             float v = 0.f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) v += part[threadIdx.x][w];
-            dgates[tk + threadIdx.x] = v;
+            for (int w = 0; w < W; ++w) v += part[l][w];
+            dgates[tk + l] = v;
         }
     }
 }
@@ -380,18 +409,31 @@ int with_row_shape(int vpr, F f)
     return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 
+// f(bf16, streamed, lanes of a row, vectors of a lane), all of them as types
 template <typename F>
-int with_dtype(bool bf16, F f)
+int with_form(bool bf16, bool streamed, int vpr, F f)
 {
-    return bf16 ? f(std::true_type{}) : f(std::false_type{});
+    return with_row_shape(vpr, [&](auto lanes, auto vecs) {
+        if (bf16) return streamed ? f(std::true_type{}, std::true_type{}, lanes, vecs) : f(std::true_type{}, std::false_type{}, lanes, vecs);
+        return streamed ? f(std::false_type{}, std::true_type{}, lanes, vecs) : f(std::false_type{}, std::false_type{}, lanes, vecs);
+    });
 }
 
 int rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : 1; }
+int backward_rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : vpr <= 512 ? 2 : 1; }
 
-constexpr int kNormGrid = 2048;             // workgroups that are resident together: 256 CUs x 8
-constexpr int kNormBackwardGrid = 512;      // rows of partial sums at most
+constexpr int kNormGrid = 1 << 16;
+// More than the memory-side cache holds (256 MiB) is streamed past it.  Plain and streamed, three sets of buffers in turn, us: norm of
+// 8192 x 4096 bf16, 303 MB, 52.8 and 48.0, its gradient, whose loads alone are streamed, 55.4 and 49.7, the combine's on 8 experts,
+// top-2, 336 MB, 64.7 and 52.9; but of 2048 x 4096 13.1 and 15.2, 18.6 and 20.5, 14.3 and 16.6.
+constexpr int64_t kStreamFrom = 256ll << 20;
 
-int backward_grid(const Call &c) { return (int)std::min<int64_t>((c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr), kNormBackwardGrid); }
+// rows of partial sums: each is written and read again, and costs more than a row of the norm itself
+int backward_grid(const Call &c)
+{
+    const int rows = backward_rows_per_wg(c.s.vpr);
+    return (int)std::min<int64_t>((c.s.T + rows - 1) / rows, c.s.vpr <= 64 ? 512 : 256);
+}
 
 // the same memory, or none of it shared
 bool same_or_apart(const void *a, const void *b, int64_t n) { return a == b || !overlap(a, n, b, n); }
@@ -448,14 +490,12 @@ int monta_rmsnorm(const monta_cfg *cfg, const void *x, const void *residual, con
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_NORM, st);
     const int wgs = (int)std::min<int64_t>((c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr), kNormGrid);
-    with_dtype(c.bf16, [&](auto bf) {
-        return with_row_shape(c.s.vpr, [&](auto lc, auto nv) {
-            constexpr int L = decltype(lc)::value, NV = decltype(nv)::value;
-            hipLaunchKernelGGL((rmsnorm_kernel<decltype(bf)::value, L, NV>), dim3(wgs), dim3(threads_of<L>()), 0, st, static_cast<const u32x4 *>(x),
-                               static_cast<const u32x4 *>(residual), static_cast<const u32x4 *>(weight), static_cast<u32x4 *>(sum),
-                               static_cast<u32x4 *>(out), static_cast<unsigned char *>(out_fp8), c.s.T, c.s.vpr, (int)row8, eps);
-            return MONTA_OK;
-        });
+    with_form(c.bf16, n * (residual ? 4 : 2) + (out_fp8 ? n8 : 0) > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
+        hipLaunchKernelGGL((rmsnorm_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(wgs), dim3(threads_of<L>()), 0, st,
+                           static_cast<const u32x4 *>(x), static_cast<const u32x4 *>(residual), static_cast<const u32x4 *>(weight),
+                           static_cast<u32x4 *>(sum), static_cast<u32x4 *>(out), static_cast<unsigned char *>(out_fp8), c.s.T, c.s.vpr, (int)row8, eps);
+        return MONTA_OK;
     });
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
@@ -499,14 +539,12 @@ int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *we
     float *partial = static_cast<float *>(scratch);
     {
         LaunchTimer timer(MONTA_K_NORM_BACKWARD, st);
-        with_dtype(c.bf16, [&](auto bf) {
-            return with_row_shape(c.s.vpr, [&](auto lc, auto nv) {
-                constexpr int L = decltype(lc)::value, NV = decltype(nv)::value;
-                hipLaunchKernelGGL((rmsnorm_backward_kernel<decltype(bf)::value, L, NV>), dim3(grid), dim3(threads_of<L>()), 0, st,
-                                   static_cast<const u32x4 *>(sum), static_cast<const u32x4 *>(weight), static_cast<const u32x4 *>(dout),
-                                   static_cast<const u32x4 *>(dsum), static_cast<u32x4 *>(dx), partial, c.s.T, c.s.vpr, eps);
-                return MONTA_OK;
-            });
+        with_form(c.bf16, n * (dsum ? 4 : 3) > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+            constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
+            hipLaunchKernelGGL((rmsnorm_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(grid), dim3(backward_threads_of<L>()), 0, st,
+                               static_cast<const u32x4 *>(sum), static_cast<const u32x4 *>(weight), static_cast<const u32x4 *>(dout),
+                               static_cast<const u32x4 *>(dsum), static_cast<u32x4 *>(dx), partial, c.s.T, c.s.vpr, eps);
+            return MONTA_OK;
         });
         MONTA_HIP_TRY(hipGetLastError());
     }
@@ -535,15 +573,12 @@ int monta_combine_backward(const monta_cfg *cfg, const void *dout, const void *y
     if (overlap(dy, nr, dgates, ng)) return MONTA_ERR_INVALID;
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_COMBINE_BACKWARD, st);
-    const int wgs = (c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr);
-    with_dtype(c.bf16, [&](auto bf) {
-        return with_row_shape(c.s.vpr, [&](auto lc, auto nv) {
-            constexpr int L = decltype(lc)::value, NV = decltype(nv)::value;
-            hipLaunchKernelGGL((combine_backward_kernel<decltype(bf)::value, L, NV>), dim3(wgs), dim3(threads_of<L>()), 0, st,
-                               static_cast<const u32x4 *>(dout), static_cast<const u32x4 *>(y), gates, static_cast<u32x4 *>(dy), dgates,
-                               c.p.pos_final, c.s.T, c.s.k, c.s.vpr, c.s.max_rows);
-            return MONTA_OK;
-        });
+    with_form(c.bf16, n + 2 * c.kept_bound * c.row_bytes > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+        constexpr int L = decltype(lanes)::value < kWave ? kWave : decltype(lanes)::value, NV = decltype(vecs)::value, kRows = threads_of<L>() / L;
+        hipLaunchKernelGGL((combine_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3((unsigned)((c.s.T + kRows - 1) / kRows)),
+                           dim3(threads_of<L>()), 0, st, static_cast<const u32x4 *>(dout), static_cast<const u32x4 *>(y), gates, static_cast<u32x4 *>(dy),
+                           dgates, c.p.pos_final, c.s.T, c.s.k, c.s.vpr, c.s.max_rows);
+        return MONTA_OK;
     });
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
