@@ -204,12 +204,16 @@ __global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned
 // sums cannot stay in the accumulators of the matrix instructions: each is a product of its own, of 32 clocks, whose four results a lane
 // scales and adds in four more instructions, 16 clocks, under the other wave's products.  A result is used four products later, so that
 // nothing waits for it.
+// A tile of at most 128 rows computes for half as long and waits for its weights: 128 x 256 or 64 x 256, three stages.  4096 x 7168 x 2048 with
+// 64 experts, top-8, a load of which 21 experts have most and 43 at most 100 rows, takes 360 us with both, 370 with the higher one alone, 396
+// without; 512 rows for every expert 556 to 560 us with and without.
 // Two stages of 64 KiB.  One barrier per step, before the last two of the eight columns of products: then every wave has read all of
 // stage s, and stage s + 1 is there; the loads of s + 2 go to the place of s under those two, as do the reads of the next step's first
 // fragments, each row fragment right behind its last use.
-constexpr int kBig8 = 256, kBig8Stage = 2 * kBig8 * 128 + 2048, kBig8Sink = 2 * kBig8Stage, kBig8LdsBytes = kBig8Sink + 2048;
+constexpr int kBig8 = 256, kBig8Stage = 2 * kBig8 * 128 + 2048, kBig8Sink = 2 * kBig8Stage;
+constexpr int kBig8LdsBytes = Tile8<128, kBig8, 2, 4, 3>::kLdsBytes;
 
-template <bool RAGGED_LAST, bool TAIL>
+template <bool TAIL>
 __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, __bf16 *__restrict__ y,
                                                  const Expert8Args &b, const RowTile &t, unsigned char *lds8)
 {
@@ -217,18 +221,17 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
     const int e = __builtin_amdgcn_readfirstlane(t.e);
     if (e < 0) return;
     const int row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
-    if constexpr (RAGGED_LAST) {
-        if (row_end - row0 <= kShortTileRows) {
-            using Short = Tile8<kShortTileRows, 128, 2, 4, 5>;
-            static_assert(Short::kLdsBytes <= kBig8LdsBytes, "8-bit short tile: stages must fit the kernel's LDS");
-            const int from = __builtin_amdgcn_readfirstlane(t.ct) * 128;
-            if (from < a.N) expert8_tile<kShortTileRows, 128, 2, 4, 5, false>(x, w, y, b, e, row0, row_end, from, lds8);
-            return;
-        }
+    const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * kBig8;
+    if (row_end - row0 <= 128) {
+        using Half = Tile8<128, kBig8, 2, 4, 3>;
+        using Quarter = Tile8<64, kBig8, 2, 4, 3>;
+        static_assert(Half::kLdsBytes <= kBig8LdsBytes && Quarter::kLdsBytes <= kBig8LdsBytes, "8-bit lower tiles: stages must fit the kernel's LDS");
+        if (row_end - row0 <= 64) expert8_tile<64, kBig8, 2, 4, 3, false>(x, w, y, b, e, row0, row_end, col0, lds8);
+        else expert8_tile<128, kBig8, 2, 4, 3, false>(x, w, y, b, e, row0, row_end, col0, lds8);
+        return;
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
     const int wx = wave >> 1, ww = wave & 1;
-    const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * kBig8;
     const auto rx = make_rsrc(x + (int64_t)row0 * b.row8, (uint32_t)(row_end - row0) * (uint32_t)b.row8);
     const auto rw = make_rsrc(w + ((int64_t)e * a.N + col0) * a.H, (uint32_t)min(a.N - col0, kBig8) * (uint32_t)a.H);
     // a wave's loads: four neighbouring chunks of 8 rows of x and of w each; chunks 16 rows apart have the same swizzle
@@ -389,7 +392,7 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
     __builtin_amdgcn_s_barrier();                                  // and nobody reads the stages any more
     asm volatile("" ::: "memory");
     constexpr int kOutPitch = 256 + 16;
-    static_assert(8 * 16 * kOutPitch <= kBig8LdsBytes, "8-bit large tile: room for a block of rows per wave");
+    static_assert(kBig8Sink + 2048 <= kBig8LdsBytes && 8 * 16 * kOutPitch <= kBig8LdsBytes, "8-bit large tile: room for a block of rows per wave");
     unsigned char *const own = lds8 + wave * (16 * kOutPitch);
     __bf16 *const to = y + col0 + ww * 128;
 #pragma unroll
@@ -413,14 +416,14 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
     }
 }
 
-template <bool RAGGED_LAST, bool TAIL>
+template <bool TAIL>
 __global__ __launch_bounds__(512, 2) void expert8_big_kernel(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, __bf16 *__restrict__ y,
                                                              Expert8Args b)
 {
     extern __shared__ __align__(16) unsigned char lds8[];
-    const RowTile t = find_row_tile<kBig8, RAGGED_LAST>(b.a, (b.a.N + kBig8 - 1) / kBig8, blockIdx.x, threadIdx.x & 63, reinterpret_cast<int *>(lds8));
+    const RowTile t = find_row_tile<kBig8, false>(b.a, (b.a.N + kBig8 - 1) / kBig8, blockIdx.x, threadIdx.x & 63, nullptr);
 #if defined(__HIP_DEVICE_COMPILE__)
-    expert8_big_tile<RAGGED_LAST, TAIL>(x, w, y, b, t, lds8);
+    expert8_big_tile<TAIL>(x, w, y, b, t, lds8);
 #else
     (void)x;
     (void)w;
@@ -444,40 +447,34 @@ int launch_expert8(const void *x, const void *w, void *y, const Expert8Args &b, 
     return MONTA_OK;
 }
 
-template <bool RAGGED_LAST, bool TAIL>
-int launch_expert8_big_k(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
+template <bool TAIL>
+int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
 {
     static LdsOptIn lds_opt_in;
     constexpr int lds = kBig8LdsBytes;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<RAGGED_LAST, TAIL>), lds, lds_opt_in)) return rc;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<TAIL>), lds, lds_opt_in)) return rc;
     const int64_t nct = (b.a.N + kBig8 - 1) / kBig8, row_tiles = rows_bound / kBig8 + std::min<int64_t>(b.a.E, rows_bound);
-    const int64_t tiles = (row_tiles + (RAGGED_LAST ? b.a.E : 0)) * nct;              // short ragged tiles come in halves
-    const int64_t grid = (tiles + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
+    const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
     if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((expert8_big_kernel<RAGGED_LAST, TAIL>), dim3((unsigned)grid), dim3(512), lds, st, static_cast<const unsigned char *>(x),
+    hipLaunchKernelGGL((expert8_big_kernel<TAIL>), dim3((unsigned)grid), dim3(512), lds, st, static_cast<const unsigned char *>(x),
                        static_cast<const unsigned char *>(w), static_cast<__bf16 *>(y), b);
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
 }
 
-template <bool RAGGED_LAST>
-int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
-{
-    return b.a.H % 128 ? launch_expert8_big_k<RAGGED_LAST, true>(x, w, y, b, rows_bound, st) : launch_expert8_big_k<RAGGED_LAST, false>(x, w, y, b, rows_bound, st);
-}
-
 // Which tile.  Measured on MI355X, three sets of buffers in turn, us; tokens x hidden x features, experts, top-2 (64 experts: top-8), in tiles of
-// 32 x 64, 32 x 128, 64 x 128, 128 x 128, 256 x 256 and those with the ragged tiles last:
-//   1 x 4096 x 4096, 8      13   16   20   26   37   21        256 x 1024 x 1024, 8     9.3  7.3  9.3  11   15   16
-//   64 x 4096 x 4096, 8     31   35   36   38   50   36        2048 x 512 x 512, 4      7.6  6.1  9.5  10   13   14
-//   256 x 4096 x 4096, 8    49   47   45   42   53   55        4096 x 1024 x 512, 32    24   22   20   18   22   25
-//   1024 x 4096 x 4096, 8   127  112  86   88   67   72        256 x 2048 x 1024, 64    36   35   28   29   33   41
-//   2048 x 4096 x 4096, 8   229  197  144  124  117  89        512 x 7168 x 2048, 64    296  255  223  190  201  226
-//   16 x 7168 x 2048, 64    134  143  143  149  179  162       1024 x 7168 x 2048, 64   475  399  322  289  223  241
+// 32 x 64, 32 x 128, 64 x 128, 128 x 128 and 256 x 256:
+//   1 x 4096 x 4096, 8      13   16   20   26   30         256 x 1024 x 1024, 8     9.3  7.3  9.3  11   16
+//   64 x 4096 x 4096, 8     31   35   36   38   41         2048 x 512 x 512, 4      7.6  6.1  9.5  10   14
+//   256 x 4096 x 4096, 8    49   47   45   44   50         4096 x 1024 x 512, 32    24   22   20   18   22
+//   512 x 4096 x 4096, 8    75   70   62   60   59         512 x 2048 x 1024, 64    51   45   41   35   35
+//   1024 x 4096 x 4096, 8   127  112  86   88   68         256 x 2048 x 1024, 64    36   35   28   29   30
+//   2048 x 4096 x 4096, 8   229  197  144  124  120        512 x 7168 x 2048, 64    296  255  223  196  186
+//   16 x 7168 x 2048, 64    134  143  143  149  143        1024 x 7168 x 2048, 64   475  399  322  289  228
 // Walks that start at different steps (walk_start) on weights' rows of whole 4 KiB, in 32 x 64: 64 x 4096 x 4096, 8 31.0 and 26.4 us, 8 tokens 27.5 and
 // 23.7; but 256 tokens 49.1 and 49.3, rows of 7168 133.8 and 139.3.
 template <bool F32>
-int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, int64_t rows_bound, int64_t kept_bound, int slice, hipStream_t st)
+int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, int64_t rows_bound, int64_t kept_bound, hipStream_t st)
 {
     const int64_t active = std::min<int64_t>(b.a.E, kept_bound), r = kept_bound / active;
     auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.N + C - 1) / C) * (2 * r + R) / (2 * R); };
@@ -487,11 +484,8 @@ int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, i
     }
     if constexpr (!F32) {
         if (tiles(32, 128) <= 300) return launch_expert8<32, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
-        if (r > 96 && tiles(256, 256) >= 140) {
-            // ragged tiles last: whole segments only, the search needs their lengths
-            const bool ragged_last = slice < 0 && r > 384 && (int64_t)b.a.E * ((b.a.N + kBig8 - 1) / kBig8) <= 256;
-            return ragged_last ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
-        }
+        if (r > 48 && tiles(256, 256) >= 120)
+            return b.a.H % 128 ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
         if (r > 48 && tiles(128, 128) >= 200) return launch_expert8<128, 128, 2, 2, 2, F32>(x, w, y, b, rows_bound, st);
     }
     return launch_expert8<64, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
@@ -529,6 +523,6 @@ extern "C" int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows,
     const int64_t rows_bound = slice_kept_bound(c.s, c.kept_bound, slice);
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_EXPERT_SCALED, st);
-    return c.bf16 ? launch_expert8_tiled<false>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, slice, st)
-                  : launch_expert8_tiled<true>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, slice, st);
+    return c.bf16 ? launch_expert8_tiled<false>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, st)
+                  : launch_expert8_tiled<true>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, st);
 }
