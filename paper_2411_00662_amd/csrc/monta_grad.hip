@@ -404,6 +404,114 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
 #endif
 }
 
+// A tile of dw of 64 x 64 for outputs of few tiles: the four waves share the rows of the expert instead of the tile, steps of 32 rows in
+// turn, each with NST stages of its own and no barrier, and their sums are added at the end, in the order of the waves.  Twice the operand
+// bytes per product of a 128 x 128 tile, but four times the workgroups and half the walk.
+template <int NST>
+struct GradSlim {
+    static constexpr int kStage = 2 * 64 * 64, kLdsBytes = 4 * NST * kStage, kPitch = 64 * 4 + 16;
+    static constexpr int kLoads = 8, kYounger = (NST - 2) * kLoads;
+    static constexpr int kWait = 0x0070 | (kYounger & 15) | ((kYounger >> 4) << 14);                         // vmcnt(kYounger), lgkmcnt(0)
+    static_assert(NST >= 2 && kYounger < 64 && 4 * 64 * kPitch <= 160 * 1024, "slim gradient tile: shape");
+    static constexpr int kLds = kLdsBytes > 4 * 64 * kPitch ? kLdsBytes : 4 * 64 * kPitch;
+};
+
+template <int NST>
+__device__ __forceinline__ void grad_slim_tile(const GradArgs &b, const RowTile &t, unsigned char *lds)
+{
+    using G = GradSlim<NST>;
+    const ExpertArgs &a = b.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int e = __builtin_amdgcn_readfirstlane(t.e), row0 = __builtin_amdgcn_readfirstlane(t.row0), depth = __builtin_amdgcn_readfirstlane(t.row_end) - row0;
+    const int64_t H = a.H, N = a.N;
+    const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * 64, out0 = __builtin_amdgcn_readfirstlane(t.rt) * 64;
+    const uint32_t pitch_c = (uint32_t)a.H * 2, pitch_r = (uint32_t)a.N * 2;
+    const char *const from_c = static_cast<const char *>(b.x) + ((int64_t)row0 * H + col0) * 2;
+    const char *const from_r = static_cast<const char *>(b.dy) + ((int64_t)row0 * N + out0) * 2;
+    uint32_t at_c[4], at_r[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) at_c[q] = deep_at<64>(q, lane, pitch_c, a.H - col0), at_r[q] = deep_at<64>(q, lane, pitch_r, a.N - out0);
+    unsigned char *const own = lds + wave * (NST * G::kStage);
+    auto issue = [&](int step, int slot) {
+        const int first = (step * 4 + wave) * 32, left = __builtin_amdgcn_readfirstlane(min(max(depth - first, 0), 32));
+        const auto cols = make_rsrc(from_c + (int64_t)first * pitch_c, left > 0 ? (uint32_t)left * pitch_c - (uint32_t)col0 * 2u : 0u);
+        const auto rows = make_rsrc(from_r + (int64_t)first * pitch_r, left > 0 ? (uint32_t)left * pitch_r - (uint32_t)out0 * 2u : 0u);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(cols, (lds_void *)(own + slot * G::kStage + q * 1024), 16, at_c[q], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void *)(own + slot * G::kStage + 4096 + q * 1024), 16, at_r[q], 0, 0, 0);
+        }
+    };
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    const int kl = 8 * g + (m >> 2), sw = deep_swizzle<64>(kl);
+    const unsigned char *const from = own + kl * 128 + (m & 3) * 8;
+    bf16x8 fc[2][4], fr[2][4];
+    // reads the fragments of stage `slot` into set `set`
+    auto read = [&](int set, int slot) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const unsigned char *const p = from + slot * G::kStage + (j ^ sw) * 32;
+            const s16x4 cl = read_deep((lds_s16x4 *)(p)), ch = read_deep((lds_s16x4 *)(p + 512));
+            const s16x4 rl = read_deep((lds_s16x4 *)(p + 4096)), rh = read_deep((lds_s16x4 *)(p + 4096 + 512));
+            fc[set][j] = whole_fragment(cl, ch);
+            fr[set][j] = whole_fragment(rl, rh);
+        }
+    };
+    auto multiply = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[set][j], fr[set][i], acc[i][j], 0, 0, 0);
+    };
+#pragma unroll
+    for (int q = 0; q < NST; ++q) issue(q, q);
+    __builtin_amdgcn_s_waitcnt(0x0f70 | ((NST - 1) * 8 & 15) | (((NST - 1) * 8) >> 4 << 14));        // stage 0
+    asm volatile("" ::: "memory");
+    read(0, 0);
+    // past the end there are zeros, which a walk of an odd number of steps multiplies too
+    const int nsteps = (depth + 127) / 128;
+    int slot = 0;
+    for (int step = 0; step < nsteps; step += 2) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            __builtin_amdgcn_s_waitcnt(G::kWait);                  // the next stage has landed; this one has been read
+            asm volatile("" ::: "memory");
+            issue(step + half + NST, slot);
+            slot = slot == NST - 1 ? 0 : slot + 1;
+            read(half ^ 1, slot);
+            multiply(half);
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);                            // the loads past the end have come back
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(lds);
+    constexpr int kRow = G::kPitch / 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(sums + (wave * 64 + i * 16 + m) * kRow + j * 16 + 4 * g) = acc[i][j];
+    __syncthreads();
+    __bf16 *const out = static_cast<__bf16 *>(b.dw) + (int64_t)e * N * H;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int row = q * 32 + tid / 8, c = tid % 8 * 8;
+        f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            lo += *reinterpret_cast<const f32x4 *>(sums + (w * 64 + row) * kRow + c);
+            hi += *reinterpret_cast<const f32x4 *>(sums + (w * 64 + row) * kRow + c + 4);
+        }
+        bf16x8 o;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[v] = (__bf16)lo[v], o[4 + v] = (__bf16)hi[v];
+        if (out0 + row < a.N && col0 + c < a.H) *reinterpret_cast<bf16x8 *>(out + (int64_t)(out0 + row) * H + col0 + c) = o;
+    }
+}
+
 // --------------------------------------------------------------------------------------------- fp32
 //
 // Tiles of BR x 64 by 2 x 2 waves, steps of 32 elements of the summed axis, NST stages straight to LDS, the loads of NST - 1 in flight.  A
@@ -575,6 +683,17 @@ struct Short {
     }
 };
 
+template <int NST>
+struct Slim {
+    static constexpr int kLds = GradSlim<NST>::kLds, kPerCu = 2;
+    static int64_t grid(const ExpertArgs &a, int64_t rows_bound) { return grad_grid<true>(a, 64, 64, rows_bound); }
+    static __device__ __forceinline__ void run(const GradArgs &b, uint32_t block, unsigned char *lds)
+    {
+        const RowTile t = find_grad_tile<true, 64, false>(b.a, (b.a.H + 63) / 64, block, threadIdx.x & 63, nullptr);
+        if (__builtin_amdgcn_readfirstlane(t.e) >= 0) grad_slim_tile<NST>(b, t, lds);
+    }
+};
+
 template <bool DW, int BR, int NST>
 struct F32 {
     static constexpr int kLds = GradShapeF32<BR, NST>::kLdsBytes, kPerCu = 2;
@@ -598,18 +717,21 @@ __global__ __launch_bounds__(256, Form::kPerCu) void grad_kernel(GradArgs b)
 #endif
 }
 
-// Both gradients in one launch, the first `split` workgroups those of dx.
+// Both gradients in one launch, the first `split` workgroups those of dx or, if dw_first, of dw: a walk along the longer axis begins first.
 template <typename Dx, typename Dw>
-__global__ __launch_bounds__(256, Dx::kPerCu < Dw::kPerCu ? Dx::kPerCu : Dw::kPerCu) void grad_both_kernel(GradArgs b, uint32_t split)
+__global__ __launch_bounds__(256, Dx::kPerCu < Dw::kPerCu ? Dx::kPerCu : Dw::kPerCu) void grad_both_kernel(GradArgs b, uint32_t split, bool dw_first)
 {
     extern __shared__ __align__(16) unsigned char grad_lds[];
 #if defined(__HIP_DEVICE_COMPILE__)
-    if (blockIdx.x < split) Dx::run(b, blockIdx.x, grad_lds);
-    else Dw::run(b, blockIdx.x - split, grad_lds);
+    const bool first = blockIdx.x < split;
+    const uint32_t block = first ? blockIdx.x : blockIdx.x - split;
+    if (first != dw_first) Dx::run(b, block, grad_lds);
+    else Dw::run(b, block, grad_lds);
 #else
     (void)b;
     (void)grad_lds;
     (void)split;
+    (void)dw_first;
 #endif
 }
 
@@ -632,10 +754,11 @@ int launch_both(const GradArgs &b, int64_t rows_bound, hipStream_t st)
     constexpr int lds = Dx::kLds > Dw::kLds ? Dx::kLds : Dw::kLds;
     static LdsOptIn lds_opt_in;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_both_kernel<Dx, Dw>), lds, lds_opt_in)) return rc;
-    const int64_t split = Dx::grid(b.a, rows_bound), grid = split + Dw::grid(b.a, rows_bound);
+    const int64_t of_dx = Dx::grid(b.a, rows_bound), of_dw = Dw::grid(b.a, rows_bound), grid = of_dx + of_dw;
+    const bool dw_first = rows_bound / std::min<int64_t>(b.a.E, rows_bound) > b.a.N;
     if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
     LaunchTimer timer(MONTA_K_EXPERT_BACKWARD, st);
-    hipLaunchKernelGGL((grad_both_kernel<Dx, Dw>), dim3((unsigned)grid), dim3(256), lds, st, b, (uint32_t)split);
+    hipLaunchKernelGGL((grad_both_kernel<Dx, Dw>), dim3((unsigned)grid), dim3(256), lds, st, b, (uint32_t)(dw_first ? of_dw : of_dx), dw_first);
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
 }
@@ -652,9 +775,15 @@ int launch_both(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 //   1 x 4096 x 4096, 8     50   56                            1024 x 1024 x 1024, 8     12   18
 //   256 x 4096 x 4096, 8   91   84                            4096 x 1024 x 512, 32     19   18
 //   2048 x 4096 x 4096, 8  220  181                           3000 x 1000 x 3000, 4     49   48
+// and where a few CUs have all of it, in tiles of 128 x 128 and in slim ones of 64 x 64 (both gradients in brackets):
+//   8192 x 512 x 512, 2    70   37   (75   42)             1024 x 512 x 512, 4      7.5  5.4 (9.5  7.4)
+//   8192 x 512 x 512, 4    43   23   (50   37)             4096 x 64 x 64, 2        36   19  (36   19)
+//   8192 x 512 x 768, 4    25   18   (37   35)             64 x 512 x 512, 4        5.4  4.7 (6.6  5.8)
+//   8192 x 1024 x 512, 4   40   41   (73   73)             1024 x 512 x 512, 8      6.4  6.3 (8.4  11)
 // Few tiles: both gradients go out together, as alone neither fills the chip to its end (us, one after the other and together: 1 x 1024 x 1024, 8 experts 13.7
 // and 9.1, 256 tokens 16.8 and 12.9, 4096 tokens 53.8 and 49.9; but 64 x 4096 x 4096, where dx then has as little room as dw, 122 and
 // 154, and the large tiles of 8192 x 4096 x 4096 906 and 1000).  fp32 always: 4096 x 1024 x 1024, 8 experts 351 and 310.
+// The longer walk first: 8192 x 512 x 512, 4 experts, dx first and dw first, 71 and 48, fp32 214 and 150; 1 x 1024 x 1024, fp32, 17 and 23.
 int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t st)
 {
     const int64_t active = std::min<int64_t>(b.a.E, rows_bound), r = rows_bound / active;
@@ -675,10 +804,11 @@ int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t s
         return launch(F32<false, 64, 3>{}, F32<true, 64, 3>{}, together);
     }
     const bool big_dw = r > 8 && (int64_t)b.a.E * ((b.a.N + 255) / 256) * ((b.a.H + 255) / 256) >= 192;
-    const bool few_dw = (int64_t)b.a.E * ((b.a.N + 127) / 128) * ((b.a.H + 127) / 128) <= 768;
+    const int64_t dw_tiles = (int64_t)b.a.E * ((b.a.N + 127) / 128) * ((b.a.H + 127) / 128);
     auto with_dw = [&](auto dx) {
+        if (dw_tiles <= 96) return launch(dx, Slim<2>{}, together);
         if (big_dw) return launch(dx, Wide<true, 8, 8>{}, apart);
-        return few_dw ? launch(dx, Wide<true, 4, 4>{}, together) : launch(dx, Wide<true, 4, 4>{}, apart);
+        return dw_tiles <= 768 ? launch(dx, Wide<true, 4, 4>{}, together) : launch(dx, Wide<true, 4, 4>{}, apart);
     };
     if (tiles(32, 64) <= 256) return with_dw(Short<32, 64, 4>{});
     if (r <= 24 || tiles(32, 128) <= 400) return with_dw(Short<32, 128, 3>{});

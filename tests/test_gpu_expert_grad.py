@@ -83,6 +83,21 @@ def test_gradients(m, case, dtype, exact):  # noqa: F811
                 assert bool(((got.double() - want).abs() <= terms * U * mag + half * want.abs()).all()), (e, terms)
 
 
+LONG = [  # experts with so many rows and so few weights that the walk over the rows is what takes time
+    (5000, 72, 64, 2, 2, 0.0, 0, 0.4),                 # a single tile of dw for each
+    (130, 136, 72, 7, 3, 0.0, 0, 2.0),                 # from a few rows to all of them
+    (7000, 504, 392, 4, 2, 0.0, 0, 0.4),
+    (4100, 776, 264, 8, 2, 0.9, 1, 0.0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", LONG, ids=lambda c: "-".join(map(str, c)))
+def test_long_walks(m, case, dtype):  # noqa: F811
+    test_gradients(m, case, dtype, 1)
+    test_gradients(m, case, dtype, 0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_either_alone(m, dtype):  # noqa: F811
     import torch
