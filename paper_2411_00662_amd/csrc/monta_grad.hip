@@ -312,9 +312,8 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds_r + stage * G::kRowStage + (wave * NB + q) * 1024), 16, at, 0, 0, 0);
         };
         // Half a step: NB x CB MFMAs on fragment set `set`; evenly between them the reads of the other set's fragments and, if `refill`,
-        // the loads of step `step`.  One wave has a SIMD to itself: an instruction
-        // issues in 4 clocks, an MFMA takes 16, so up to three others behind each cost nothing, and eight behind every fourth a quarter
-        // of the time (both gradients of 16384 rows x 4096 x 4096: 1076 us).
+        // the loads of step `step`.  One wave has a SIMD to itself: an instruction issues in 4 clocks, an MFMA takes 16, so up to three others
+        // behind each cost nothing (in bursts behind every fourth 1 % more time).
         constexpr int kMfmas = NB * CB, kReads = NB + CB;
         auto half_step = [&](int set, int stage, int ks, auto refill, int step) {
             constexpr int each = decltype(refill)::value ? 3 : 2, actions = each * kReads;
@@ -370,7 +369,8 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
 
     // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, hidden element 16 j + 4 (lane / 16) + v of its columns.  Through LDS, block of
     // 16 rows by block, so that rows leave as whole pieces of 16 bytes, 32 CB bytes of each side by side.  (8 bytes a lane straight from the registers:
-    // 268 MB of weights' gradients in 101 us.)
+    // 268 MB of weights' gradients in 101 us.)  dw is read by nobody soon and is streamed past the cache, where it would drive out the weights: both
+    // gradients of 128 rows x 4096 x 4096, 8 experts, 153 and 125 us, of 1024 rows 203 and 190; dx gains 1 %, but is read next.
     __builtin_amdgcn_s_waitcnt(0x0070);                            // nor written: the loads past the end have come back
     barrier();                                                     // the stages are not read any more
     constexpr int kOutPitch = 32 * CB + 16;                        // 16 bytes of padding: the 16 rows that a store of 8 bytes a lane hits begin on different banks
@@ -394,7 +394,11 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
             const int row = q * kRows + l2 / kLanes, p = l2 % kLanes;
             const u32x4 v = *reinterpret_cast<const u32x4 *>(own + row * kOutPitch + p * 16);
             const int64_t r = (DW ? out0 : row0) + wr * 16 * nb + i * 16 + row;
-            if (r < (DW ? a.N : row_end) && col0 + wc * 16 * CB + p * 8 < a.H) *reinterpret_cast<u32x4 *>(out + r * H * 2 + p * 16) = v;
+            if (r < (DW ? a.N : row_end) && col0 + wc * 16 * CB + p * 8 < a.H) {
+                u32x4 *const to = reinterpret_cast<u32x4 *>(out + r * H * 2 + p * 16);
+                if constexpr (DW) __builtin_nontemporal_store(v, to);
+                else *to = v;
+            }
         }
     }
 #else
