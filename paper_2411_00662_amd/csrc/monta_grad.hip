@@ -776,9 +776,10 @@ int launch_both(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 //   2048 x 4096 x 4096, 8  360  308  222  208  195  155       2000 x 7168 x 2048, 64    1332 1177 833  739  627  667
 // so 256 x 256 where most CUs get one, below that what gives every CU one or two.  Deep operands want wide tiles: a row of 64 elements is
 // one line.  dw in tiles of 128 x 128 and 256 x 256:
-//   1 x 4096 x 4096, 8     50   56                            1024 x 1024 x 1024, 8     12   18
-//   256 x 4096 x 4096, 8   91   84                            4096 x 1024 x 512, 32     19   18
-//   2048 x 4096 x 4096, 8  220  181                           3000 x 1000 x 3000, 4     49   48
+//   1 x 4096 x 4096, 8     47   56                            1024 x 1024 x 1024, 8     11   16
+//   256 x 4096 x 4096, 8   78   80                            4096 x 1024 x 512, 32     19   18
+//   2048 x 4096 x 4096, 8  176  164                           3000 x 1000 x 3000, 4     51   47
+//   8192 x 2048 x 2048, 4  154  111                           512 x 2048 x 1024, 64     74   75 (both gradients 169 154)
 // and where a few CUs have all of it, in tiles of 128 x 128 and in slim ones of 64 x 64 (both gradients in brackets):
 //   8192 x 512 x 512, 2    70   37   (75   42)             1024 x 512 x 512, 4      7.5  5.4 (9.5  7.4)
 //   8192 x 512 x 512, 4    43   23   (50   37)             4096 x 64 x 64, 2        36   19  (36   19)
