@@ -120,17 +120,19 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_kernel(const u32x4 *x
 {
     constexpr int EV = Elem<BF16>::kPerVec, kRows = threads_of<L>() / L;
     __shared__ float part[2][L > kWave ? L / kWave : 1];
-    const int l = threadIdx.x % L, group = threadIdx.x / L;
+    const int l = threadIdx.x % L;
+    const uint32_t group = threadIdx.x / L;
     const int H = vpr * EV, nb = (H + kBlock - 1) / kBlock;
     u32x4 wv[NV];
 #pragma unroll
     for (int q = 0; q < NV; ++q) wv[q] = l + q * L < vpr ? w[l + q * L] : (u32x4){0u, 0u, 0u, 0u};
 
     int parity = 0;
-    // every lane goes round as often as the others: the moves between lanes and the barrier take all of them
-    for (int base = blockIdx.x * kRows; base < T; base += gridDim.x * kRows, parity ^= 1) {
-        const bool live = base + group < T;
-        const int64_t row = live ? base + group : T - 1;
+    // every lane goes round as often as the others: the moves between lanes and the barrier take all of them.  Unsigned: base passes T by up to
+    // a round, and T may be 2^31 - 1
+    for (uint32_t base = blockIdx.x * kRows; base < (uint32_t)T; base += gridDim.x * kRows, parity ^= 1) {
+        const bool live = base + group < (uint32_t)T;
+        const int64_t row = live ? base + group : (uint32_t)T - 1;
         u32x4 s[NV], add[NV];
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
@@ -209,7 +211,8 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_ker
     constexpr int EV = Elem<BF16>::kPerVec, kRows = backward_threads_of<L>() / L;
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
     __shared__ float part[2][kRows][2 * (L > kWave ? L / kWave : 1)];
-    const int l = threadIdx.x % L, group = threadIdx.x / L;
+    const int l = threadIdx.x % L;
+    const uint32_t group = threadIdx.x / L;
     const int H = vpr * EV;
     u32x4 wv[NV];
     float dw[NV][EV];
@@ -221,8 +224,8 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_ker
     }
     constexpr bool kAhead = L < 1024;                               // 1024 lanes have no registers for a second row
     u32x4 s[NV], d[NV], t[NV];
-    auto fetch = [&](int base) {
-        const int64_t row = min(base + group, T - 1);
+    auto fetch = [&](uint32_t base) {
+        const int64_t row = min(base + group, (uint32_t)T - 1);
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             const int i = l + q * L;
@@ -233,9 +236,9 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_ker
     };
     int parity = 0;
     if (kAhead) fetch(blockIdx.x * kRows);
-    for (int base = blockIdx.x * kRows; base < T; base += gridDim.x * kRows, parity ^= 1) {
-        const bool live = base + group < T;
-        const int64_t row = live ? base + group : T - 1;
+    for (uint32_t base = blockIdx.x * kRows; base < (uint32_t)T; base += gridDim.x * kRows, parity ^= 1) {
+        const bool live = base + group < (uint32_t)T;
+        const int64_t row = live ? base + group : (uint32_t)T - 1;
         if (!kAhead) fetch(base);
         u32x4 s0[NV], d0[NV], t0[NV];
         float sums[2] = {0.f, 0.f};
@@ -254,7 +257,7 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_ker
                 sums[1] = __builtin_fmaf(a[e], b[e] * g[e], sums[1]);
             }
         }
-        if (kAhead && base + (int)gridDim.x * kRows < T) fetch(base + gridDim.x * kRows);
+        if (kAhead && base + gridDim.x * kRows < (uint32_t)T) fetch(base + gridDim.x * kRows);
         row_sums<L>(sums, part[parity][group]);
         const float r = 1.f / __builtin_sqrtf(sums[0] / (float)H + eps);
         const float c = r * r * (sums[1] / (float)H);               // dx = r (g - s c) + dsum
@@ -337,8 +340,8 @@ __global__ __launch_bounds__(threads_of<L>()) void combine_backward_kernel(const
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
     __shared__ float part[32][W];
     const int l = threadIdx.x % L, lane = threadIdx.x % kWave, wave = l / kWave;
-    const int t = blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / L);
-    if (t >= T) return;                                            // a whole wave, and with L > 64 never
+    const uint32_t t = blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / L);
+    if (t >= (uint32_t)T) return;                                            // a whole wave, and with L > 64 never
     const int64_t tk = (int64_t)t * k;
     const int pos = lane < k ? pos_final[tk + lane] : -1;
     const float gate = lane < k ? gates[tk + lane] : 0.f;
@@ -432,7 +435,7 @@ constexpr int64_t kStreamFrom = 256ll << 20;
 int backward_grid(const Call &c)
 {
     const int rows = backward_rows_per_wg(c.s.vpr);
-    return (int)std::min<int64_t>((c.s.T + rows - 1) / rows, c.s.vpr <= 64 ? 512 : 256);
+    return (int)std::min<int64_t>(((int64_t)c.s.T + rows - 1) / rows, c.s.vpr <= 64 ? 512 : 256);
 }
 
 // the same memory, or none of it shared
@@ -489,7 +492,7 @@ int monta_rmsnorm(const monta_cfg *cfg, const void *x, const void *residual, con
         return MONTA_ERR_INVALID;
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_NORM, st);
-    const int wgs = (int)std::min<int64_t>((c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr), kNormGrid);
+    const int wgs = (int)std::min<int64_t>(((int64_t)c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr), kNormGrid);
     with_form(c.bf16, n * (residual ? 4 : 2) + (out_fp8 ? n8 : 0) > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
         hipLaunchKernelGGL((rmsnorm_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(wgs), dim3(threads_of<L>()), 0, st,
@@ -575,7 +578,7 @@ int monta_combine_backward(const monta_cfg *cfg, const void *dout, const void *y
     LaunchTimer timer(MONTA_K_COMBINE_BACKWARD, st);
     with_form(c.bf16, n + 2 * c.kept_bound * c.row_bytes > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value < kWave ? kWave : decltype(lanes)::value, NV = decltype(vecs)::value, kRows = threads_of<L>() / L;
-        hipLaunchKernelGGL((combine_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3((unsigned)((c.s.T + kRows - 1) / kRows)),
+        hipLaunchKernelGGL((combine_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3((unsigned)(((int64_t)c.s.T + kRows - 1) / kRows)),
                            dim3(threads_of<L>()), 0, st, static_cast<const u32x4 *>(dout), static_cast<const u32x4 *>(y), gates, static_cast<u32x4 *>(dy),
                            dgates, c.p.pos_final, c.s.T, c.s.k, c.s.vpr, c.s.max_rows);
         return MONTA_OK;

@@ -290,3 +290,25 @@ def test_graph_streams_and_large_offsets(m):
     m.monta_rmsnorm(cfg, x, None, w, 1e-5, None, x)
     torch.cuda.synchronize()
     assert torch.equal(x[0], x[T - 1]) and torch.equal(x[T // 2], x[T - 1]) and bool((x == x[0]).all())
+
+
+def test_most_tokens(m):
+    """2^31 - 1 tokens: the walk's counter passes 2^31."""
+    import torch
+    T, H = 2 ** 31 - 1, 8
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB")
+    cfg = make(m, T, H, "bf16")
+    x = torch.ones((T, H), dtype=torch.bfloat16, device="cuda")
+    x[-1], x[5] = 3.0, float("nan")
+    w = torch.full((H,), 2.0, dtype=torch.bfloat16, device="cuda")
+    m.monta_rmsnorm(cfg, x, None, w, 0.0, None, x)
+    torch.cuda.synchronize()
+    for part in x.split(1 << 28):
+        bad = (part != 2.0).any(1)                     # of a row of equal numbers every norm is one
+        if part.data_ptr() == x.data_ptr():
+            assert bool(bad[5]) and int(bad.sum()) == 1 and bool(torch.isnan(x[5]).all())
+        else:
+            assert not bool(bad.any())
+    del x, part, bad
+    torch.cuda.empty_cache()
