@@ -328,7 +328,7 @@ int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *we
  *   y[r][n] = sum_b xs[r][b] * ws[e][n / 128][b] * sum_{h in block b} xc[r][h] * wc[e][n][h]   for every kept row r of expert e,
  * x_rows [max_rows] rows as above in FINAL order, w_codes [E][out_features][H] e4m3, w_scales [E][ceil(out_features / 128)]
  * [ceil(H / 128)] fp32, one for each 128 x 128 block of an expert's weights; y [max_rows][out_features] in cfg->dtype.  Device
- * pointers, 16-byte aligned (w_scales 4-byte); H a multiple of 16, at most 65536; out_features a multiple of 8 (bf16) or 4 (fp32), slice, rows that are not written
+ * pointers, 16-byte aligned (w_scales 4-byte); H a multiple of 16, at most 65536; out_features a multiple of 8 (bf16) or 4 (fp32), at most 2^20; slice, rows that are not written
  * and the workspace as in monta_expert_linear.  y, rounded once to cfg->dtype, may share no memory with what is read.  With cfg->dtype
  * MONTA_BF16 the codes are multiplied by the matrix cores' 8-bit instructions, which drop what lies more than 13 bits below the
  * largest of a few neighbouring products (1.5e-5 of a block's sum on normal data, a hundredth of the rounding of y); the blocks'

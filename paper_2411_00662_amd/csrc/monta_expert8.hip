@@ -380,9 +380,8 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
 #pragma unroll
         for (int n = 8 * NB - D; n < 8 * NB; ++n) add(product[n % D], n);
     };
-    const int nb = max((row_end - row0 + 63) / 64, 2);
-    if (nb == 2) run(std::integral_constant<int, 2>{});
-    else if (nb == 3) run(std::integral_constant<int, 3>{});
+    const int nb = (row_end - row0 + 63) / 64;                     // more than 128 rows
+    if (nb == 3) run(std::integral_constant<int, 3>{});
     else run(std::integral_constant<int, 4>{});
 
     // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, output feature 16 j + 4 (lane / 16) + v of its columns.  Through LDS, block of 16 rows
@@ -506,7 +505,7 @@ extern "C" int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows,
     const int bpe = c.bf16 ? 2 : 4;
     if (out_features < 1 || (int64_t)out_features * bpe % 16 != 0 || c.H % 16 != 0) return MONTA_ERR_INVALID;
     if (slice < -1 || slice >= c.s.S) return MONTA_ERR_INVALID;
-    if (c.H > kMaxHidden8) return MONTA_ERR_UNSUPPORTED;
+    if (c.H > kMaxHidden8 || out_features > kBigMaxHidden) return MONTA_ERR_UNSUPPORTED;
     Expert8Args b{};
     b.row8 = (int32_t)fp8_row_bytes(c.H);
     b.nb = (c.H + 127) / 128;

@@ -114,7 +114,11 @@ CASES = [  # tokens, hidden, out_features, experts, top_k, capacity factor, padd
     (3300, 256, 2304, 6, 2, 0.0, 0, 1, 1, 0.0),        # large tiles, ragged ones of every length last
     (3300, 400, 2056, 6, 2, 0.0, 0, 2, 1, 0.6),
     (1100, 8320, 1032, 8, 4, 0.0, 1, 1, 1, 0.3),
-    (4000, 144, 1288, 60, 8, 0.8, 0, 1, 1, 0.9),       # large tiles, ragged ones in place
+    (4000, 144, 1288, 60, 8, 0.8, 0, 1, 1, 0.9),       # large tiles and lower ones, fewer steps than stages
+    (1500, 8336, 1032, 40, 4, 0.0, 0, 1, 1, 1.2),      # the same, 66 blocks
+    (5, 12288, 136, 3, 2, 0.0, 0, 1, 1, 0.0),          # walks that begin at different blocks and go round: 96 of them,
+    (40, 8192, 520, 8, 2, 0.0, 0, 2, 1, 0.0),          # 64
+    (3, 65536, 72, 2, 1, 0.0, 0, 1, 1, 0.0),           # and 512, the longest rows
 ]
 
 

@@ -116,6 +116,7 @@ def test_expert_linear_fp8_refuses(kw, code):
 def test_expert_linear_fp8_sizes():
     assert expert8(cfg(hidden=520)) == -1
     assert expert8(cfg(hidden=65536 + 16)) == -2
+    assert expert8(cfg(), n=(1 << 20) + 8) == -2
 
 
 def grads(c, dy=A[0], x=A[1], w=A[2], n=256, dx=A[3], dw=A[4], ws=A[5]):
