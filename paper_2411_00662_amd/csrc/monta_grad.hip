@@ -215,12 +215,18 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
     if (e < 0) return;
     const int row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
     const int64_t H = a.H, N = a.N;
-    // Ragged tiles of at most 64 rows, the last ones, come in halves of 128 columns: they last as long as their weights take to arrive, and
-    // twice the workgroups have twice the loads on their way.
-    if constexpr (RAGGED_LAST) {
+    // Tiles of dx of at most 64 rows last as long as their weights take to arrive: four stages of them on their way.  Those of RAGGED_LAST come in
+    // halves of 128 columns, twice the workgroups with twice the loads; in place both halves follow one another (dx of 4096 x 7168 x 2048 over 64
+    // experts, top-8, most of which have few rows: 600 us, as 256 x 256 620).
+    if constexpr (!DW && RB == 8) {
         if (row_end - row0 <= kShortTileRows) {
-            const int from = __builtin_amdgcn_readfirstlane(t.ct) * 128;
-            if (from < a.H) grad_short_tile<kShortTileRows, 128, 5>(b, e, row0, row_end, from, lds);
+            constexpr int kCols = RAGGED_LAST ? 128 : BC;
+            const int from = __builtin_amdgcn_readfirstlane(t.ct) * kCols;
+            for (int c = from; c < min(from + kCols, a.H); c += 128) {
+                grad_short_tile<kShortTileRows, 128, 5>(b, e, row0, row_end, c, lds);
+                __builtin_amdgcn_s_waitcnt(0x0070);                // the loads past the end have come back
+                __syncthreads();
+            }
             return;
         }
     }
