@@ -528,14 +528,16 @@ __device__ __forceinline__ void grad_slim_tile(const GradArgs &b, const RowTile 
 // 32-bit element has nothing to be transposed with: a deep operand, 32 rows of BR or 64 elements, is read element by element, MFMA v of half a
 // step taking rows 4 g + v of it (g the lane's group of 16), a flat one 16 bytes at a time, which are the same rows' elements.  Swizzles: flat as in
 // bf16; deep, the 64-byte segment s of row k at s ^ (k / 4) % 4, so that the four groups' rows are in different banks.  What bounds it is the
-// fp32 matrix rate, and with few steps the way to the first.
+// fp32 matrix rate, and with few steps the way to the first.  Two stages, five workgroups a CU, do better than three and three (both gradients,
+// us: 1024 rows x 1024 x 1024, 8 experts 56 and 62, 600 x 2048 x 2048, 4 experts 109 and 116, 8192 x 1024 x 1024 310 and 312), but for 32 rows,
+// whose walks are short of work (2 rows x 1024 x 1024 17 and 19).
 template <int BR, int NST>
 struct GradShapeF32 {
     static constexpr int BC = 64, kStage = (BR + BC) * 128, kLdsBytes = NST * kStage;
     static constexpr int kLoadsR = BR / 32, kLoadsC = BC / 32, kYounger = (NST - 2) * (kLoadsR + kLoadsC);      // 1 KiB loads per wave and step
     static constexpr int kWait = 0x0070 | (kYounger & 15) | ((kYounger >> 4) << 14);                         // vmcnt(kYounger), lgkmcnt(0)
     static constexpr int RB = BR / 32;
-    static_assert((BR == 32 || BR == 64) && NST >= 3 && kYounger < 64, "fp32 gradient tile: shape");
+    static_assert((BR == 32 || BR == 64) && NST >= 2 && kYounger < 64, "fp32 gradient tile: shape");
 };
 
 // as deep_at, for 32 rows of 64 fp32 elements
@@ -811,8 +813,8 @@ int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t s
     constexpr std::true_type together{};
     constexpr std::false_type apart{};
     if (!bf16) {
-        if (tiles(64, 64) <= 1024) return launch(F32<false, 32, 3>{}, F32<true, 64, 3>{}, together);
-        return launch(F32<false, 64, 3>{}, F32<true, 64, 3>{}, together);
+        if (tiles(64, 64) <= 1024) return launch(F32<false, 32, 3>{}, F32<true, 64, 2>{}, together);
+        return launch(F32<false, 64, 2>{}, F32<true, 64, 2>{}, together);
     }
     const bool big_dw = r > 8 && (int64_t)b.a.E * ((b.a.N + 255) / 256) * ((b.a.H + 255) / 256) >= 192;
     const int64_t dw_tiles = (int64_t)b.a.E * ((b.a.N + 127) / 128) * ((b.a.H + 127) / 128);
