@@ -21,6 +21,33 @@ struct Expert8Args {
     int32_t nb;             // blocks of 128 along the hidden axis: steps of the walk
 };
 
+// The product of 16 output features (a lane's 32 codes of one: pieces g and 4 + g of the block, g = lane / 16) and 16 rows over a block.
+template <bool F32>
+__device__ __forceinline__ f32x4 block_product(const u32x4 (&w)[2], const u32x4 (&x)[2])
+{
+    f32x4 part = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (!F32) {
+        const i32x8 f = __builtin_bit_cast(i32x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        const i32x8 r = __builtin_bit_cast(i32x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f, r, part, 0, 0, 0, 0, 0, 0);
+    } else {
+        // every e4m3 number is a bf16 number, and a product of two is an fp32 number
+        auto wide = [](u32x4 c, int h) {
+            bf16x8 o;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[2 * h + q], 1.f, false);
+                const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[2 * h + q], 1.f, true);
+                o[4 * q] = lo[0], o[4 * q + 1] = lo[1], o[4 * q + 2] = hi[0], o[4 * q + 3] = hi[1];
+            }
+            return o;
+        };
+#pragma unroll
+        for (int q = 0; q < 4; ++q) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide(w[q / 2], q % 2), wide(x[q / 2], q % 2), part, 0, 0, 0);
+    }
+    return part;
+}
+
 // A tile of XR rows x WR output features by WX x WW waves, each (XR / WX) x (WR / WW); NST stages of 128 bytes of every row, which is
 // one block of the hidden axis, go straight to LDS, the loads of NST - 1 of them in flight.
 template <int XR, int WR, int WX, int WW, int NST>
@@ -117,38 +144,11 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
             u32x4 fw[2];
             fw[0] = *reinterpret_cast<const u32x4 *>(pw + buf + k0 + j * 2048);
             fw[1] = *reinterpret_cast<const u32x4 *>(pw + buf + k1 + j * 2048);
-            if constexpr (!F32) {
-                const i32x8 f = __builtin_bit_cast(i32x8, __builtin_shufflevector(fw[0], fw[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int i = 0; i < G::kRB; ++i) {
-                    const i32x8 r = __builtin_bit_cast(i32x8, __builtin_shufflevector(fx[i][0], fx[i][1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f, r, (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+            for (int i = 0; i < G::kRB; ++i) {
+                const f32x4 part = block_product<F32>(fw, fx[i]);
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(part[v], sc[i], acc[i][j][v]);
-                }
-            } else {
-                // every e4m3 number is a bf16 number, and a product of two is an fp32 number
-                auto wide = [](u32x4 c, int h) {
-                    bf16x8 o;
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[2 * h + q], 1.f, false);
-                        const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[2 * h + q], 1.f, true);
-                        o[4 * q] = lo[0], o[4 * q + 1] = lo[1], o[4 * q + 2] = hi[0], o[4 * q + 3] = hi[1];
-                    }
-                    return o;
-                };
-                bf16x8 f[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) f[q] = wide(fw[q / 2], q % 2);
-#pragma unroll
-                for (int i = 0; i < G::kRB; ++i) {
-                    f32x4 part = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[q], wide(fx[i][q / 2], q % 2), part, 0, 0, 0);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(part[v], sc[i], acc[i][j][v]);
-                }
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(part[v], sc[i], acc[i][j][v]);
             }
         }
         slot = slot == NST - 1 ? 0 : slot + 1;
@@ -174,6 +174,79 @@ __device__ __forceinline__ void expert8_tile(const unsigned char *__restrict__ x
                     }
                 }
             }
+        }
+    }
+}
+
+// Few tiles: a walk along the hidden axis would be all latency.  The W waves of a workgroup share the blocks of a tile of 16 rows x 16 CB
+// output features, wave after wave, D of them at a time straight to registers: 16 bytes a lane, the lanes of a row side by side.  The
+// waves' sums meet in LDS and are added in the order of the waves.
+template <int CB, int W, int D, bool F32>
+__global__ __launch_bounds__(64 * W) void expert8_split_kernel(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, void *__restrict__ y,
+                                                               Expert8Args b)
+{
+    constexpr int WR = 16 * CB, kPitch = WR + 4;
+    static_assert(128 % WR == 0 && W * 16 * kPitch * 4 <= 64 * 1024, "8-bit split tile: shape");
+    __shared__ __align__(16) float sums[W * 16 * kPitch];
+    const ExpertArgs &a = b.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const RowTile t = find_row_tile<16, false>(a, (a.N + WR - 1) / WR, blockIdx.x, lane, nullptr);
+    const int e = __builtin_amdgcn_readfirstlane(t.e);
+    if (e < 0) return;
+    const int row0 = __builtin_amdgcn_readfirstlane(t.row0), row_end = __builtin_amdgcn_readfirstlane(t.row_end);
+    const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * WR;
+    const auto rx = make_rsrc(x + (int64_t)row0 * b.row8, (uint32_t)(row_end - row0) * (uint32_t)b.row8);
+    const auto rw = make_rsrc(w + ((int64_t)e * a.N + col0) * a.H, (uint32_t)min(a.N - col0, WR) * (uint32_t)a.H);
+    const float *const ws = b.w_scales + ((int64_t)e * ((a.N + 127) / 128) + col0 / 128) * b.nb;
+    f32x4 acc[CB];
+#pragma unroll
+    for (int j = 0; j < CB; ++j) acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int first = wave; first < b.nb; first += W * D) {
+        u32x4 fx[D][2], fw[D][CB][2];
+        float sx[D], sw[D];
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int step = first + d * W;                        // past the end everything is out of range: zeros
+            sw[d] = ws[min(step, b.nb - 1)];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = step * 128 + h * 64 + g * 16;
+#pragma unroll
+                for (int j = 0; j < CB; ++j)
+                    fw[d][j][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, at < a.H ? (j * 16 + m) * a.H + at : (int)kOutOfRange, 0, 0));
+                fx[d][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, at < a.H ? m * b.row8 + at : (int)kOutOfRange, 0, 0));
+            }
+            sx[d] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rx, step < b.nb ? m * b.row8 + a.H + step * 4 : (int)kOutOfRange, 0, 0));
+        }
+        __builtin_amdgcn_sched_barrier(0);                         // all loads first
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                const f32x4 part = block_product<F32>(fw[d][j], fx[d]);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[j][v] = __builtin_fmaf(part[v], sx[d] * sw[d], acc[j][v]);
+            }
+    }
+    // acc[j][v]: row lane % 16, output feature 16 j + 4 (lane / 16) + v
+#pragma unroll
+    for (int j = 0; j < CB; ++j) *reinterpret_cast<f32x4 *>(sums + (wave * 16 + m) * kPitch + j * 16 + 4 * g) = acc[j];
+    __syncthreads();
+    static_assert(16 * WR / 4 <= 64 * W, "8-bit split tile: four features a lane");
+    const int row = tid / (WR / 4), c = tid % (WR / 4) * 4;
+    if (row0 + row < row_end && row < 16 && col0 + c < a.N) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < W; ++p) v += *reinterpret_cast<const f32x4 *>(sums + (p * 16 + row) * kPitch + c);
+        const int64_t at = (int64_t)(row0 + row) * a.N + col0 + c;
+        if constexpr (F32) {
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(y) + at) = v;
+        } else {
+            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            bf16x4 o;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = (__bf16)v[k];
+            *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(y) + at) = o;
         }
     }
 }
@@ -446,6 +519,18 @@ int launch_expert8(const void *x, const void *w, void *y, const Expert8Args &b, 
     return MONTA_OK;
 }
 
+template <int CB, int W, int D, bool F32>
+int launch_expert8_split(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
+{
+    const int64_t row_tiles = rows_bound / 16 + std::min<int64_t>(b.a.E, rows_bound), nct = (b.a.N + 16 * CB - 1) / (16 * CB);
+    const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
+    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((expert8_split_kernel<CB, W, D, F32>), dim3((unsigned)grid), dim3(64 * W), 0, st, static_cast<const unsigned char *>(x),
+                       static_cast<const unsigned char *>(w), y, b);
+    MONTA_HIP_TRY(hipGetLastError());
+    return MONTA_OK;
+}
+
 template <bool TAIL>
 int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
 {
@@ -470,6 +555,15 @@ int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args 
 //   1024 x 4096 x 4096, 8   127  112  86   88   68         256 x 2048 x 1024, 64    36   35   28   29   30
 //   2048 x 4096 x 4096, 8   229  197  144  124  120        512 x 7168 x 2048, 64    296  255  223  196  186
 //   16 x 7168 x 2048, 64    134  143  143  149  143        1024 x 7168 x 2048, 64   475  399  322  289  228
+// Few tiles: those of 32 x 64, and split ones of 16 x 16 by 8 waves and 16 x 32 by 4 (calls of one graph, one after the other):
+//   1 x 4096 x 4096, 8     13.7 9.0  9.0                      1 x 1024 x 1024, 8      5.9  3.9  4.3
+//   1 x 4096 x 1024, 8     12.9 5.9  7.9                      1 x 512 x 4096, 8       4.3  4.0  4.0
+//   3 x 8192 x 552, top-1  21.9 8.2  12                       40 x 2048 x 512, 4      8.6  5.3  6.0
+//   8 x 8192 x 2048, top-1 22.5 17.1 18.9                     100 x 4096 x 512, 4     13.6 12.5 9.8
+//   8 x 4096 x 4096, 8     24   28   30                       196 x 2048 x 88, 8      8.4  7.5  6.1
+//   1 x 7168 x 2048, 64    24.6 26.1 26.3                     64 x 2048 x 2048, 8     8.9  22   16
+//   60 x 4096 x 2048, top-1, 4  13.9 16.7                     60 x 4096 x 1024, 2     13.6 -    9.4
+//   4 x 512 x 512, 64      4.4  5.0                           256 x 2048 x 256, 8     8.6  -    9.2
 // Walks that start at different steps (walk_start) on weights' rows of whole 4 KiB, in 32 x 64: 64 x 4096 x 4096, 8 31.0 and 26.4 us, 8 tokens 27.5 and
 // 23.7; but 256 tokens 49.1 and 49.3, rows of 7168 133.8 and 139.3.
 template <bool F32>
@@ -477,6 +571,9 @@ int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, i
 {
     const int64_t active = std::min<int64_t>(b.a.E, kept_bound), r = kept_bound / active;
     auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.N + C - 1) / C) * (2 * r + R) / (2 * R); };
+    auto split_tiles = [&](int64_t C) { return active * ((b.a.N + C - 1) / C) * std::max<int64_t>(2 * r + 16, 32) / 32; };
+    if (r <= 24 && split_tiles(16) <= (r <= 8 && b.nb >= 8 ? 1024 : 512)) return launch_expert8_split<1, 8, 2, F32>(x, w, y, b, rows_bound, st);
+    if (split_tiles(32) <= (b.nb >= 32 ? 512 : 256)) return launch_expert8_split<2, 4, 4, F32>(x, w, y, b, rows_bound, st);
     if (r <= 24 || tiles(32, 64) <= 160) {
         b.a.spread = b.a.H % 4096 == 0;
         return launch_expert8<32, 64, 1, 4, 4, F32>(x, w, y, b, rows_bound, st);

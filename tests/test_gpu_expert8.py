@@ -119,6 +119,9 @@ CASES = [  # tokens, hidden, out_features, experts, top_k, capacity factor, padd
     (5, 12288, 136, 3, 2, 0.0, 0, 1, 1, 0.0),          # walks that begin at different blocks and go round: 96 of them,
     (40, 8192, 520, 8, 2, 0.0, 0, 2, 1, 0.0),          # 64
     (3, 65536, 72, 2, 1, 0.0, 0, 1, 1, 0.0),           # and 512, the longest rows
+    (2, 8208, 24, 8, 2, 0.0, 0, 1, 1, 0.0),            # few tiles, whose waves share the blocks: 65 of them
+    (90, 4112, 40, 3, 2, 0.0, 1, 2, 1, 0.7),           # the same, several row tiles
+    (12, 4096, 4096, 8, 2, 0.0, 0, 1, 1, 0.0),
 ]
 
 
