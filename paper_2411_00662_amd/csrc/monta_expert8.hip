@@ -582,8 +582,8 @@ int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, i
         if (tiles(32, 128) <= 300) return launch_expert8<32, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
         if (r > 48 && tiles(256, 256) >= 120)
             return b.a.H % 128 ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
-        if (r > 48 && tiles(128, 128) >= 200) return launch_expert8<128, 128, 2, 2, 2, F32>(x, w, y, b, rows_bound, st);
     }
+    if (r > 48 && tiles(128, 128) >= 200) return launch_expert8<128, 128, 2, 2, 2, F32>(x, w, y, b, rows_bound, st);
     return launch_expert8<64, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
 }
 

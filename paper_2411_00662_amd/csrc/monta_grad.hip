@@ -19,6 +19,7 @@ struct GradArgs {
     ExpertArgs a;           // lo, hi of the experts' rows, E, H, N, max_rows
     const void *dy, *x, *w;
     void *dx, *dw;
+    bool stream_dw;         // dw goes past the cache
 };
 
 // Tile of dw of workgroup `block`, numbered like those of find_row_tile; e < 0: none.
@@ -376,7 +377,8 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
     // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, hidden element 16 j + 4 (lane / 16) + v of its columns.  Through LDS, block of
     // 16 rows by block, so that rows leave as whole pieces of 16 bytes, 32 CB bytes of each side by side.  (8 bytes a lane straight from the registers:
     // 268 MB of weights' gradients in 101 us.)  dw is read by nobody soon and is streamed past the cache, where it would drive out the weights: both
-    // gradients of 128 rows x 4096 x 4096, 8 experts, 153 and 125 us, of 1024 rows 203 and 190; dx gains 1 %, but is read next.
+    // gradients of 128 rows x 4096 x 4096, 8 experts, 153 and 125 us, of 1024 rows 203 and 190.  Not where more than the memory-side cache holds
+    // (256 MiB) leaves in parts of lines: 64 x 4424 x 1768, few rows, 470 us streamed and 290 through it, with 1792 elements a row 186.  dx gains 1 %, but is read next.
     __builtin_amdgcn_s_waitcnt(0x0070);                            // nor written: the loads past the end have come back
     barrier();                                                     // the stages are not read any more
     constexpr int kOutPitch = 32 * CB + 16;                        // 16 bytes of padding: the 16 rows that a store of 8 bytes a lane hits begin on different banks
@@ -384,29 +386,33 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
     static_assert(4 * 16 * kOutPitch <= G::kLdsBytes, "gradient tile: room for a block of rows per wave");
     char *const out = static_cast<char *>(DW ? b.dw : b.dx) + ((DW ? (int64_t)e * N * H : 0) + col0 + wc * 16 * CB) * 2;
     const int l2 = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // asked for again: kept through the loop it would be spilled
+    auto leave = [&](auto past_cache) {                            // a question at each store would cost dw of few rows a third
 #pragma unroll
-    for (int i = 0; i < RB; ++i) {
-        if (i >= nb) break;
+        for (int i = 0; i < RB; ++i) {
+            if (i >= nb) break;
 #pragma unroll
-        for (int j = 0; j < CB; ++j) {
-            bf16x4 o;
+            for (int j = 0; j < CB; ++j) {
+                bf16x4 o;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) o[v] = (__bf16)acc[i][j][v];
-            *reinterpret_cast<bf16x4 *>(own + (l2 & 15) * kOutPitch + j * 32 + (l2 >> 4) * 8) = o;
-        }
-        constexpr int kLanes = 2 * CB, kRows = 64 / kLanes;        // lanes per row, rows per store
+                for (int v = 0; v < 4; ++v) o[v] = (__bf16)acc[i][j][v];
+                *reinterpret_cast<bf16x4 *>(own + (l2 & 15) * kOutPitch + j * 32 + (l2 >> 4) * 8) = o;
+            }
+            constexpr int kLanes = 2 * CB, kRows = 64 / kLanes;        // lanes per row, rows per store
 #pragma unroll
-        for (int q = 0; q < 16 / kRows; ++q) {
-            const int row = q * kRows + l2 / kLanes, p = l2 % kLanes;
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(own + row * kOutPitch + p * 16);
-            const int64_t r = (DW ? out0 : row0) + wr * 16 * nb + i * 16 + row;
-            if (r < (DW ? a.N : row_end) && col0 + wc * 16 * CB + p * 8 < a.H) {
-                u32x4 *const to = reinterpret_cast<u32x4 *>(out + r * H * 2 + p * 16);
-                if constexpr (DW) __builtin_nontemporal_store(v, to);
-                else *to = v;
+            for (int q = 0; q < 16 / kRows; ++q) {
+                const int row = q * kRows + l2 / kLanes, p = l2 % kLanes;
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(own + row * kOutPitch + p * 16);
+                const int64_t r = (DW ? out0 : row0) + wr * 16 * nb + i * 16 + row;
+                if (r < (DW ? a.N : row_end) && col0 + wc * 16 * CB + p * 8 < a.H) {
+                    u32x4 *const to = reinterpret_cast<u32x4 *>(out + r * H * 2 + p * 16);
+                    if constexpr (DW && decltype(past_cache)::value) __builtin_nontemporal_store(v, to);
+                    else *to = v;
+                }
             }
         }
-    }
+    };
+    if (DW && b.stream_dw) leave(std::true_type{});
+    else leave(std::false_type{});
 #else
     (void)b;
     (void)block;
@@ -783,11 +789,14 @@ int launch_both(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 //   1024 x 4096 x 4096, 8  202  189  130  147  108  115       256 x 2048 x 1024, 64     64   60   59   65   68   77
 //   2048 x 4096 x 4096, 8  360  308  222  208  195  155       2000 x 7168 x 2048, 64    1332 1177 833  739  627  667
 // so 256 x 256 where most CUs get one, below that what gives every CU one or two.  Deep operands want wide tiles: a row of 64 elements is
-// one line.  dw in tiles of 128 x 128 and 256 x 256:
+// one line.  A walk of less than 512 features is over before a workgroup alone on its CU has begun the next: in 256 x 256 and in 128 x 128 with both
+// gradients in one launch 2735 x 2264 x 168, 4, top-4, 50 and 36, 5107 x 2480 x 112, 8, top-2, 43 and 34, 4096 x 2048 x 256, 8 36 and 31, x 512 56 and 55.  dw in tiles of 128 x 128 and 256 x 256:
 //   1 x 4096 x 4096, 8     47   56                            1024 x 1024 x 1024, 8     11   16
 //   256 x 4096 x 4096, 8   78   80                            4096 x 1024 x 512, 32     19   18
 //   2048 x 4096 x 4096, 8  176  164                           3000 x 1000 x 3000, 4     51   47
 //   8192 x 2048 x 2048, 4  154  111                           512 x 2048 x 1024, 64     74   75 (both gradients 169 154)
+//   148 x 8192 x 288, 21   32   44                            823 x 4096 x 120, 32      15   23
+//   64 x 4096 x 4096, 8    67   70                            400 x 1032 x 4096, 16     54   53
 // and where a few CUs have all of it, in tiles of 128 x 128 and in slim ones of 64 x 64 (both gradients in brackets):
 //   8192 x 512 x 512, 2    70   37   (75   42)             1024 x 512 x 512, 4      7.5  5.4 (9.5  7.4)
 //   8192 x 512 x 512, 4    43   23   (50   37)             4096 x 64 x 64, 2        36   19  (36   19)
@@ -816,7 +825,7 @@ int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t s
         if (tiles(64, 64) <= 1024) return launch(F32<false, 32, 3>{}, F32<true, 64, 2>{}, together);
         return launch(F32<false, 64, 2>{}, F32<true, 64, 2>{}, together);
     }
-    const bool big_dw = r > 8 && (int64_t)b.a.E * ((b.a.N + 255) / 256) * ((b.a.H + 255) / 256) >= 192;
+    const bool big_dw = r > 48 && b.a.N > 128 && b.a.H > 128 && (int64_t)b.a.E * ((b.a.N + 255) / 256) * ((b.a.H + 255) / 256) >= 192;
     const int64_t dw_tiles = (int64_t)b.a.E * ((b.a.N + 127) / 128) * ((b.a.H + 127) / 128);
     auto with_dw = [&](auto dx) {
         if (dw_tiles <= 96) return launch(dx, Slim<2>{}, together);
@@ -825,7 +834,7 @@ int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t s
     };
     if (tiles(32, 64) <= 256) return with_dw(Short<32, 64, 4>{});
     if (r <= 24 || tiles(32, 128) <= 400) return with_dw(Short<32, 128, 3>{});
-    if (r > 56 && tiles(256, 256) >= 160) {
+    if (r > 56 && b.a.N >= 512 && tiles(256, 256) >= 160) {
         const bool ragged_last = r > 384 && b.a.E * ((b.a.H + 255) / 256) <= 256;
         if (!big_dw) return ragged_last ? launch(Wide<false, 8, 8, true>{}, Wide<true, 4, 4>{}, apart) : launch(Wide<false, 8, 8>{}, Wide<true, 4, 4>{}, apart);
         return ragged_last ? launch(Wide<false, 8, 8, true>{}, Wide<true, 8, 8>{}, apart) : launch(Wide<false, 8, 8>{}, Wide<true, 8, 8>{}, apart);
@@ -869,5 +878,6 @@ extern "C" int monta_expert_linear_backward(const monta_cfg *cfg, const void *dy
     b.w = w_exp;
     b.dx = dx_final;
     b.dw = dw_exp;
+    b.stream_dw = nw <= (256ll << 20) || c.row_bytes % 128 == 0;
     return launch_grads(b, c.bf16, c.kept_bound, static_cast<hipStream_t>(stream));
 }
