@@ -202,8 +202,8 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_kernel(const u32x4 *x
 // A workgroup walks over rows and keeps the weight's and its gradient's share in registers; the next row is requested before the
 // present one's sums are known.  The gradient's partial sums, one row of H per workgroup, are added by rmsnorm_dweight_kernel: a fixed
 // order, no atomics.
-// 8192 x 4096 bf16 with dsum: 268 MB in 52 us with the sum of the partials, 5.2 TB/s; one row of 256 lanes a workgroup instead of two
-// takes 50.3, but 1155 x 2048 fp32 9.7 us for 8.8 and 517 x 1155 8.3 for 7.4.
+// 8192 x 4096 bf16 with dsum: 268 MB in 48 us with the sum of the partials, 5.6 TB/s; one row of 256 lanes a workgroup instead of two
+// does as well there, but takes for 1155 x 2048 bf16 9.7 us for 8.8 and 517 x 1155 8.3 for 7.4.
 template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_kernel(const u32x4 *s_in, const u32x4 *w, const u32x4 *dout, const u32x4 *dsum,
                                                                            u32x4 *dx, float *partial, int T, int vpr, float eps)
@@ -426,8 +426,8 @@ int rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : 1; }
 int backward_rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : vpr <= 512 ? 2 : 1; }
 
 constexpr int kNormGrid = 1 << 16;
-// More than the memory-side cache holds (256 MiB) is streamed past it.  Plain and streamed, three sets of buffers in turn, us: norm of
-// 8192 x 4096 bf16, 303 MB, 52.8 and 48.0, its gradient, whose loads alone are streamed, 55.4 and 49.7, the combine's on 8 experts,
+// As much as the memory-side cache holds (256 MiB) and more is streamed past it.  Plain and streamed, three sets of buffers in turn, us: norm of
+// 8192 x 4096 bf16, 303 MB, 52.8 and 48.0, its gradient, whose loads alone are streamed, 52.5 and 48, the combine's on 8 experts,
 // top-2, 336 MB, 64.7 and 52.9; but of 2048 x 4096 13.1 and 15.2, 18.6 and 20.5, 14.3 and 16.6.
 constexpr int64_t kStreamFrom = 256ll << 20;
 
@@ -493,7 +493,7 @@ int monta_rmsnorm(const monta_cfg *cfg, const void *x, const void *residual, con
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_NORM, st);
     const int wgs = (int)std::min<int64_t>(((int64_t)c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr), kNormGrid);
-    with_form(c.bf16, n * (residual ? 4 : 2) + (out_fp8 ? n8 : 0) > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+    with_form(c.bf16, n * (residual ? 4 : 2) + (out_fp8 ? n8 : 0) >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
         hipLaunchKernelGGL((rmsnorm_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(wgs), dim3(threads_of<L>()), 0, st,
                            static_cast<const u32x4 *>(x), static_cast<const u32x4 *>(residual), static_cast<const u32x4 *>(weight),
@@ -542,7 +542,7 @@ int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *we
     float *partial = static_cast<float *>(scratch);
     {
         LaunchTimer timer(MONTA_K_NORM_BACKWARD, st);
-        with_form(c.bf16, n * (dsum ? 4 : 3) > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+        with_form(c.bf16, n * (dsum ? 4 : 3) >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
             constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
             hipLaunchKernelGGL((rmsnorm_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(grid), dim3(backward_threads_of<L>()), 0, st,
                                static_cast<const u32x4 *>(sum), static_cast<const u32x4 *>(weight), static_cast<const u32x4 *>(dout),
@@ -576,7 +576,7 @@ int monta_combine_backward(const monta_cfg *cfg, const void *dout, const void *y
     if (overlap(dy, nr, dgates, ng)) return MONTA_ERR_INVALID;
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_COMBINE_BACKWARD, st);
-    with_form(c.bf16, n + 2 * c.kept_bound * c.row_bytes > kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+    with_form(c.bf16, n + 2 * c.kept_bound * c.row_bytes >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value < kWave ? kWave : decltype(lanes)::value, NV = decltype(vecs)::value, kRows = threads_of<L>() / L;
         hipLaunchKernelGGL((combine_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3((unsigned)(((int64_t)c.s.T + kRows - 1) / kRows)),
                            dim3(threads_of<L>()), 0, st, static_cast<const u32x4 *>(dout), static_cast<const u32x4 *>(y), gates, static_cast<u32x4 *>(dy),
