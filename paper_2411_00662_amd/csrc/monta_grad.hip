@@ -26,13 +26,13 @@ struct GradArgs {
 template <int BR>
 __device__ __forceinline__ RowTile find_weight_tile(const ExpertArgs &a, int nct, uint32_t block)
 {
-    const int64_t L = tile_number(block);
+    const uint32_t L = (uint32_t)tile_number(block);
     RowTile t;
     const int tiles = (a.N + BR - 1) / BR;
-    const int64_t e = L / ((int64_t)tiles * nct);
-    if (e >= a.E) return t;
+    const uint32_t per = (uint32_t)tiles * (uint32_t)nct, e = L / per;         // per: at most 2^14 squared
+    if (e >= (uint32_t)a.E) return t;
     t.e = (int)e;
-    place_in_panels(t, (uint32_t)(L - e * tiles * nct), tiles, nct);
+    place_in_panels(t, L - e * per, tiles, nct);
     t.row0 = max(a.lo[e], 0);
     t.row_end = max(t.row0, min(a.hi_base[e] + a.hi_len[e], a.max_rows));
     return t;
