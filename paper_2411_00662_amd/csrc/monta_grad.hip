@@ -499,6 +499,7 @@ __device__ __forceinline__ void grad_slim_tile(const GradArgs &b, const RowTile 
             issue(step + half + NST, slot);
             slot = slot == NST - 1 ? 0 : slot + 1;
             read(half ^ 1, slot);
+            __builtin_amdgcn_sched_barrier(0);                     // left alone the reads come behind the products: 15 % more time
             multiply(half);
         }
     }
@@ -798,10 +799,10 @@ int launch_both(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 //   148 x 8192 x 288, 21   32   44                            823 x 4096 x 120, 32      15   23
 //   64 x 4096 x 4096, 8    67   70                            400 x 1032 x 4096, 16     54   53
 // and where a few CUs have all of it, in tiles of 128 x 128 and in slim ones of 64 x 64 (both gradients in brackets):
-//   8192 x 512 x 512, 2    70   37   (75   42)             1024 x 512 x 512, 4      7.5  5.4 (9.5  7.4)
-//   8192 x 512 x 512, 4    43   23   (50   37)             4096 x 64 x 64, 2        36   19  (36   19)
-//   8192 x 512 x 768, 4    25   18   (37   35)             64 x 512 x 512, 4        5.4  4.7 (6.6  5.8)
-//   8192 x 1024 x 512, 4   40   41   (73   73)             1024 x 512 x 512, 8      6.4  6.3 (8.4  11)
+//   8192 x 512 x 512, 2    64   31   (70   38)             1024 x 512 x 512, 4      6.6  5.0 (9.0  7.1)
+//   8192 x 512 x 512, 4    37   19   (45   34)             4096 x 64 x 64, 2        35   15  (35   16)
+//   8192 x 512 x 768, 4    24   18   (35   33)             64 x 512 x 512, 4        4.9  4.5 (6.0  6.1)
+//   8192 x 1024 x 512, 4   39   38   (71   70)             1024 x 512 x 512, 8      5.7  6.2 (7.8  11)
 // Few tiles: both gradients go out together, as alone neither fills the chip to its end (us, one after the other and together: 1 x 1024 x 1024, 8 experts 13.7
 // and 9.1, 256 tokens 16.8 and 12.9, 4096 tokens 53.8 and 49.9; but 64 x 4096 x 4096, where dx then has as little room as dw, 122 and
 // 154, and the large tiles of 8192 x 4096 x 4096 906 and 1000).  fp32 always: 4096 x 1024 x 1024, 8 experts 351 and 310.
