@@ -137,3 +137,44 @@ def test_training_step(m, T, H, E, k, tp, S, cf, padded, dtype):  # noqa: F811
             ("dweight", dw, w64.grad, (dnm * sm * r).sum(0), 4), ("dx", dx, s64.grad + dsum.double(), dxm, 5)):
         off = (got.double() - ref).abs()
         assert bool((off <= (adds + roundings * h * 1.05) * mag).all()), (name, (off / mag.clamp_min(1e-300)).max().item())
+
+
+def test_two_streams(m):  # noqa: F811
+    """Two layers at once, each on a stream of its own, one handed over by the argument and one the current one; the results are those of the calls one after
+    the other."""
+    import torch
+    from test_gpu_expert8 import problem, routed
+    made = []
+    for T, H, N, E, seed in ((700, 512, 520, 4, 1), (90, 1040, 264, 8, 2)):
+        cfg, ws, _, rows = routed(m, T, H, "bf16", E, 2, seed=seed)
+        packed, wc, wsc, _, _ = problem(m, cfg, rows, N, False, seed)
+        a = torch.bfloat16
+        t = dict(x=normal((T, H), a, seed), w=normal((H,), a, seed + 10), dy=normal((rows, N), a, seed + 20), fin=normal((rows, H), a, seed + 30),
+                 we=normal((E, N, H), a, seed + 40), gates=normal((T, 2), torch.float32, seed + 50))
+        new = lambda *s, d=a: torch.zeros(s, dtype=d, device="cuda")  # noqa: E731
+        out = dict(n=new(T, H), r8=new(T, m.monta_fp8_rows(cfg)[1], d=torch.uint8), y=new(rows, N), dx=new(rows, H), dw=new(E, N, H),
+                   dfin=new(rows, H), dg=new(T, 2, d=torch.float32), dn=new(T, H), dnw=new(H, d=torch.float32))
+        scratch = new(m.monta_rmsnorm_scratch_bytes(cfg), d=torch.uint8)
+
+        def calls(stream, cfg=cfg, ws=ws, packed=packed, wc=wc, wsc=wsc, t=t, out=out, N=N, scratch=scratch):
+            m.monta_rmsnorm(cfg, t["x"], None, t["w"], EPS, None, out["n"], out["r8"], stream=stream)
+            m.monta_expert_linear_fp8(cfg, packed, wc, wsc, N, out["y"], ws, stream=stream)
+            m.monta_combine_backward(cfg, t["x"], t["fin"], t["gates"], out["dfin"], out["dg"], ws, stream=stream)
+            m.monta_expert_linear_backward(cfg, t["dy"], t["fin"], t["we"], N, out["dx"], out["dw"], ws, stream=stream)
+            m.monta_rmsnorm_backward(cfg, t["x"], t["w"], EPS, out["n"], None, out["dn"], out["dnw"], scratch, stream=stream)
+
+        calls(None)
+        torch.cuda.synchronize()
+        made.append((calls, out, {k: v.clone() for k, v in out.items()}))
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        for _, out, _ in made:
+            for v in out.values():
+                v.zero_()
+        torch.cuda.synchronize()
+        made[0][0](side.cuda_stream)
+        with torch.cuda.stream(other):
+            made[1][0](None)
+        torch.cuda.synchronize()
+        for _, out, want in made:
+            assert all(torch.equal(out[k], want[k]) for k in want), [k for k in want if not torch.equal(out[k], want[k])]
