@@ -492,12 +492,12 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
     }
 }
 
-template <bool TAIL>
+template <bool RAGGED_LAST, bool TAIL>
 __global__ __launch_bounds__(512, 2) void expert8_big_kernel(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, __bf16 *__restrict__ y,
                                                              Expert8Args b)
 {
     extern __shared__ __align__(16) unsigned char lds8[];
-    const RowTile t = find_row_tile<kBig8, false>(b.a, (b.a.N + kBig8 - 1) / kBig8, blockIdx.x, threadIdx.x & 63, nullptr);
+    const RowTile t = find_row_tile<kBig8, RAGGED_LAST, 0>(b.a, (b.a.N + kBig8 - 1) / kBig8, blockIdx.x, threadIdx.x & 63, reinterpret_cast<int *>(lds8));
 #if defined(__HIP_DEVICE_COMPILE__)
     expert8_big_tile<TAIL>(x, w, y, b, t, lds8);
 #else
@@ -535,19 +535,25 @@ int launch_expert8_split(const void *x, const void *w, void *y, const Expert8Arg
     return MONTA_OK;
 }
 
-template <bool TAIL>
-int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
+template <bool RAGGED_LAST, bool TAIL>
+int launch_expert8_big_k(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
 {
     static LdsOptIn lds_opt_in;
     constexpr int lds = kBig8LdsBytes;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<TAIL>), lds, lds_opt_in)) return rc;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<RAGGED_LAST, TAIL>), lds, lds_opt_in)) return rc;
     const int64_t nct = (b.a.N + kBig8 - 1) / kBig8, row_tiles = rows_bound / kBig8 + std::min<int64_t>(b.a.E, rows_bound);
     const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
     if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((expert8_big_kernel<TAIL>), dim3((unsigned)grid), dim3(512), lds, st, static_cast<const unsigned char *>(x),
+    hipLaunchKernelGGL((expert8_big_kernel<RAGGED_LAST, TAIL>), dim3((unsigned)grid), dim3(512), lds, st, static_cast<const unsigned char *>(x),
                        static_cast<const unsigned char *>(w), static_cast<__bf16 *>(y), b);
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
+}
+
+template <bool RAGGED_LAST>
+int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
+{
+    return b.a.H % 128 ? launch_expert8_big_k<RAGGED_LAST, true>(x, w, y, b, rows_bound, st) : launch_expert8_big_k<RAGGED_LAST, false>(x, w, y, b, rows_bound, st);
 }
 
 // Which tile.  Measured on MI355X, three sets of buffers in turn, us; tokens x hidden x features, experts, top-2 (64 experts: top-8), in tiles of
@@ -559,6 +565,11 @@ int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args 
 //   1024 x 4096 x 4096, 8   127  112  86   88   68         256 x 2048 x 1024, 64    36   35   28   29   30
 //   2048 x 4096 x 4096, 8   229  197  144  124  120        512 x 7168 x 2048, 64    296  255  223  196  186
 //   16 x 7168 x 2048, 64    134  143  143  149  143        1024 x 7168 x 2048, 64   475  399  322  289  228
+// 256 x 256 with the ragged tiles in place and last: an even load leaves each expert whole tiles and a few rows, which then share the last round,
+// but read the weights again:
+//   2048 x 4096 x 4096, 8  120  99   (load skewed 70   73)     8192 x 4096 x 4096, 16  310  316
+//   4096 x 7168 x 2048, 8  187  152                           4096 x 2048 x 2048, 16  71   56   (35   40)
+//   8192 x 4096 x 4096, 8  313  301                           4096 x 7168 x 2048, 64  566  611  (352  388)
 // Few tiles: those of 32 x 64, and split ones of 16 x 16 by 8 waves and 16 x 32 by 4 (calls of one graph, one after the other):
 //   1 x 4096 x 4096, 8     13.7 9.0  9.0                      1 x 1024 x 1024, 8      5.9  3.9  4.3
 //   1 x 4096 x 1024, 8     12.9 5.9  7.9                      1 x 512 x 4096, 8       4.3  4.0  4.0
@@ -571,7 +582,7 @@ int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args 
 // Walks that start at different steps (walk_start) on weights' rows of whole 4 KiB, in 32 x 64: 64 x 4096 x 4096, 8 31.0 and 26.4 us, 8 tokens 27.5 and
 // 23.7; but 256 tokens 49.1 and 49.3, rows of 7168 133.8 and 139.3.
 template <bool F32>
-int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, int64_t rows_bound, int64_t kept_bound, hipStream_t st)
+int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, int64_t rows_bound, int64_t kept_bound, int slice, hipStream_t st)
 {
     const int64_t active = std::min<int64_t>(b.a.E, kept_bound), r = kept_bound / active;
     auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.N + C - 1) / C) * (2 * r + R) / (2 * R); };
@@ -584,8 +595,11 @@ int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, i
     }
     if constexpr (!F32) {
         if (tiles(32, 128) <= 300) return launch_expert8<32, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
-        if (r > 48 && tiles(256, 256) >= 120)
-            return b.a.H % 128 ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
+        if (r > 48 && tiles(256, 256) >= 120) {
+            // ragged tiles last: whole segments only, the search needs their lengths
+            const bool ragged_last = slice < 0 && r > 384 && (int64_t)b.a.E * ((b.a.N + kBig8 - 1) / kBig8) <= 256;
+            return ragged_last ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
+        }
     }
     if (r > 48 && tiles(128, 128) >= 200) return launch_expert8<128, 128, 2, 2, 2, F32>(x, w, y, b, rows_bound, st);
     return launch_expert8<64, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
@@ -623,6 +637,6 @@ extern "C" int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows,
     const int64_t rows_bound = slice_kept_bound(c.s, c.kept_bound, slice);
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_EXPERT_SCALED, st);
-    return c.bf16 ? launch_expert8_tiled<false>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, st)
-                  : launch_expert8_tiled<true>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, st);
+    return c.bf16 ? launch_expert8_tiled<false>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, slice, st)
+                  : launch_expert8_tiled<true>(x_rows, w_codes, y, b, rows_bound, c.kept_bound, slice, st);
 }
