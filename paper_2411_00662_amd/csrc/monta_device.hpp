@@ -172,9 +172,9 @@ __device__ __forceinline__ void place_in_panels(RowTile &t, uint32_t in, int til
 
 // Tile of BR rows of workgroup `block`.  RAGGED_LAST: the whole tiles of all experts come first and the segments' ragged last tiles after
 // them, the one with the most rows first, so that the last round of workgroups consists of the tiles that cost least; those of at most
-// HALF_ROWS rows as halves of the column tile (ct counts halves).  For whole segments (hi_len), at least 256 threads and E <= 256; `scratch`: 257
+// kShortTileRows rows as halves of the column tile (ct counts halves).  For whole segments (hi_len), at least 256 threads and E <= 256; `scratch`: 257
 // words of LDS that nothing else uses yet.
-template <int BR, bool RAGGED_LAST, int HALF_ROWS = kShortTileRows>
+template <int BR, bool RAGGED_LAST>
 __device__ __forceinline__ RowTile find_row_tile(const ExpertArgs &a, int nct, uint32_t block, int lane, int *scratch)
 {
     const int64_t L = tile_number(block);
@@ -202,7 +202,7 @@ __device__ __forceinline__ RowTile find_row_tile(const ExpertArgs &a, int nct, u
         int rank = 0, long_ones = 0;
         for (int o = 0; o < a.E; ++o) {
             const int other = scratch[o];
-            long_ones += other > HALF_ROWS ? 1 : 0;
+            long_ones += other > kShortTileRows ? 1 : 0;
             rank += other > mine || (other == mine && o < tid) ? 1 : 0;
         }
         const int64_t halves = Lr - (int64_t)long_ones * nct;      // number among the halves

@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned
 constexpr int kBig8 = 256, kBig8Stage = 2 * kBig8 * 128 + 2048, kBig8Sink = 2 * kBig8Stage;
 constexpr int kBig8LdsBytes = Tile8<128, kBig8, 2, 4, 3>::kLdsBytes;
 
-template <bool TAIL>
+template <bool RAGGED_LAST, bool TAIL>
 __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict__ x, const unsigned char *__restrict__ w, __bf16 *__restrict__ y,
                                                  const Expert8Args &b, const RowTile &t, unsigned char *lds8)
 {
@@ -301,10 +301,17 @@ __device__ __forceinline__ void expert8_big_tile(const unsigned char *__restrict
     const int col0 = __builtin_amdgcn_readfirstlane(t.ct) * kBig8;
     if (row_end - row0 <= 128) {
         using Half = Tile8<128, kBig8, 2, 4, 3>;
-        using Quarter = Tile8<64, kBig8, 2, 4, 3>;
-        static_assert(Half::kLdsBytes <= kBig8LdsBytes && Quarter::kLdsBytes <= kBig8LdsBytes, "8-bit lower tiles: stages must fit the kernel's LDS");
-        if (row_end - row0 <= 64) expert8_tile<64, kBig8, 2, 4, 3, false>(x, w, y, b, e, row0, row_end, col0, lds8);
-        else expert8_tile<128, kBig8, 2, 4, 3, false>(x, w, y, b, e, row0, row_end, col0, lds8);
+        using Quarter = Tile8<kShortTileRows, kBig8, 2, 4, 3>;
+        using Last = Tile8<kShortTileRows, 128, 2, 4, 5>;
+        static_assert(std::max({Half::kLdsBytes, Quarter::kLdsBytes, Last::kLdsBytes}) <= kBig8LdsBytes, "8-bit lower tiles: stages must fit the kernel's LDS");
+        if (row_end - row0 > kShortTileRows) {
+            expert8_tile<128, kBig8, 2, 4, 3, false>(x, w, y, b, e, row0, row_end, col0, lds8);
+        } else if constexpr (RAGGED_LAST) {                        // by halves of the column tile, twice the workgroups
+            const int from = __builtin_amdgcn_readfirstlane(t.ct) * 128;
+            if (from < a.N) expert8_tile<kShortTileRows, 128, 2, 4, 5, false>(x, w, y, b, e, row0, row_end, from, lds8);
+        } else {
+            expert8_tile<kShortTileRows, kBig8, 2, 4, 3, false>(x, w, y, b, e, row0, row_end, col0, lds8);
+        }
         return;
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
@@ -497,9 +504,9 @@ __global__ __launch_bounds__(512, 2) void expert8_big_kernel(const unsigned char
                                                              Expert8Args b)
 {
     extern __shared__ __align__(16) unsigned char lds8[];
-    const RowTile t = find_row_tile<kBig8, RAGGED_LAST, 0>(b.a, (b.a.N + kBig8 - 1) / kBig8, blockIdx.x, threadIdx.x & 63, reinterpret_cast<int *>(lds8));
+    const RowTile t = find_row_tile<kBig8, RAGGED_LAST>(b.a, (b.a.N + kBig8 - 1) / kBig8, blockIdx.x, threadIdx.x & 63, reinterpret_cast<int *>(lds8));
 #if defined(__HIP_DEVICE_COMPILE__)
-    expert8_big_tile<TAIL>(x, w, y, b, t, lds8);
+    expert8_big_tile<RAGGED_LAST, TAIL>(x, w, y, b, t, lds8);
 #else
     (void)x;
     (void)w;
@@ -542,7 +549,8 @@ int launch_expert8_big_k(const void *x, const void *w, void *y, const Expert8Arg
     constexpr int lds = kBig8LdsBytes;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<RAGGED_LAST, TAIL>), lds, lds_opt_in)) return rc;
     const int64_t nct = (b.a.N + kBig8 - 1) / kBig8, row_tiles = rows_bound / kBig8 + std::min<int64_t>(b.a.E, rows_bound);
-    const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
+    const int64_t tiles = (row_tiles + (RAGGED_LAST ? b.a.E : 0)) * nct;              // short ragged tiles come in halves
+    const int64_t grid = (tiles + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
     if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((expert8_big_kernel<RAGGED_LAST, TAIL>), dim3((unsigned)grid), dim3(512), lds, st, static_cast<const unsigned char *>(x),
                        static_cast<const unsigned char *>(w), static_cast<__bf16 *>(y), b);
@@ -565,11 +573,12 @@ int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args 
 //   1024 x 4096 x 4096, 8   127  112  86   88   68         256 x 2048 x 1024, 64    36   35   28   29   30
 //   2048 x 4096 x 4096, 8   229  197  144  124  120        512 x 7168 x 2048, 64    296  255  223  196  186
 //   16 x 7168 x 2048, 64    134  143  143  149  143        1024 x 7168 x 2048, 64   475  399  322  289  228
-// 256 x 256 with the ragged tiles in place and last: an even load leaves each expert whole tiles and a few rows, which then share the last round,
-// but read the weights again:
-//   2048 x 4096 x 4096, 8  120  99   (load skewed 70   73)     8192 x 4096 x 4096, 16  310  316
-//   4096 x 7168 x 2048, 8  187  152                           4096 x 2048 x 2048, 16  71   56   (35   40)
-//   8192 x 4096 x 4096, 8  313  301                           4096 x 7168 x 2048, 64  566  611  (352  388)
+// 256 x 256 with the ragged tiles in place and last, those of at most 64 rows by halves: an even load leaves each expert whole tiles and a few
+// rows, which then share the last round, but read the weights again:
+//   2048 x 4096 x 4096, 8  120  92   (load skewed 70   71)     8192 x 4096 x 4096, 16  310  305
+//   4096 x 7168 x 2048, 8  187  137                           4096 x 2048 x 2048, 16  71   52   (35   41)
+//   8192 x 4096 x 4096, 8  313  303                           4096 x 4096 x 2048, 32           (118  134)
+//   8192 x 8192 x 8192, 2  519  507                           4096 x 7168 x 2048, 64  566  613  (352  388)
 // Few tiles: those of 32 x 64, and split ones of 16 x 16 by 8 waves and 16 x 32 by 4 (calls of one graph, one after the other):
 //   1 x 4096 x 4096, 8     13.7 9.0  9.0                      1 x 1024 x 1024, 8      5.9  3.9  4.3
 //   1 x 4096 x 1024, 8     12.9 5.9  7.9                      1 x 512 x 4096, 8       4.3  4.0  4.0
@@ -597,7 +606,7 @@ int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, i
         if (tiles(32, 128) <= 300) return launch_expert8<32, 128, 1, 4, 3, F32>(x, w, y, b, rows_bound, st);
         if (r > 48 && tiles(256, 256) >= 120) {
             // ragged tiles last: whole segments only, the search needs their lengths
-            const bool ragged_last = slice < 0 && r > 384 && (int64_t)b.a.E * ((b.a.N + kBig8 - 1) / kBig8) <= 256;
+            const bool ragged_last = slice < 0 && r > 384 && (int64_t)b.a.E * ((b.a.N + kBig8 - 1) / kBig8) < 256;
             return ragged_last ? launch_expert8_big<true>(x, w, y, b, rows_bound, st) : launch_expert8_big<false>(x, w, y, b, rows_bound, st);
         }
     }
