@@ -278,8 +278,9 @@ __global__ __launch_bounds__(64 * WX * WW, 2) void expert8_kernel(const unsigned
 // sums cannot stay in the accumulators of the matrix instructions: each is a product of its own, of 32 clocks, whose four results a lane
 // scales and adds in four more instructions, 16 clocks, under the other wave's products.  A result is used four products later, so that
 // nothing waits for it.
-// 8192 x 4096 x 4096, 8 experts, top-2: 273 to 310 us by the box, 1.8 to 2.0 PFLOP/s; without its loads 235, so what bounds it is the matrix pipe
-// and the scaling beside it at the clock the card holds (a library product of one scale reaches 2.5), and behind them the way to LDS.
+// 8192 x 4096 x 4096, 8 experts, top-2: 270 to 305 us by the box, 1.8 to 2.0 PFLOP/s; without its loads 235, so what bounds it is the matrix pipe
+// and the scaling beside it at the clock the card holds (a library product of one scale reaches 2.5), and LDS beside them: stages written and fragments
+// read are 256 KiB a step, as many clocks as its products.
 // 8192 x 8192 x 8192, 2 experts, 500 to 545 us, 2.0 to 2.2.
 // A tile of at most 128 rows computes for half as long and waits for its weights: 128 x 256 or 64 x 256, three stages.  4096 x 7168 x 2048 with
 // 64 experts, top-8, a load of which 21 experts have most and 43 at most 100 rows, takes 360 us with both, 370 with the higher one alone, 396
