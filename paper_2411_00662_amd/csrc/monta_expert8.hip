@@ -594,6 +594,7 @@ int launch_expert8_big(const void *x, const void *w, void *y, const Expert8Args 
 template <bool F32>
 int launch_expert8_tiled(const void *x, const void *w, void *y, Expert8Args b, int64_t rows_bound, int64_t kept_bound, int slice, hipStream_t st)
 {
+    // of the whole problem, also for a slice: it then runs as the whole would, and its rows are the same bit for bit
     const int64_t active = std::min<int64_t>(b.a.E, kept_bound), r = kept_bound / active;
     auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.N + C - 1) / C) * (2 * r + R) / (2 * R); };
     auto split_tiles = [&](int64_t C) { return active * ((b.a.N + C - 1) / C) * std::max<int64_t>(2 * r + 16, 32) / 32; };

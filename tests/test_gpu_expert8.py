@@ -143,6 +143,24 @@ def test_random(m, case, dtype):
     check(m, cfg, ws, tabs, rows, N, dtype, False)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [(3300, 400, 2056, 6, 2, 2, 0.6), (40, 8192, 520, 8, 2, 2, 0.0), (90, 4112, 40, 3, 2, 2, 0.7), (2048, 272, 2056, 4, 2, 4, 0.0),
+                                  (4096, 256, 520, 16, 2, 4, 1.2)], ids=str)
+def test_slices_are_the_whole(m, case, dtype):
+    """Slice after slice or all at once, on codes whose sums are rounded: the same bits; and again: the same bits."""
+    import torch
+    T, H, N, E, k, S, zipf = case
+    cfg, ws, _, rows = routed(m, T, H, dtype, E, k, slices=S, zipf=zipf)
+    packed, wc, wsc, _, _ = problem(m, cfg, rows, N, False)
+    y = [torch.zeros((rows, N), dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda") for _ in range(3)]
+    m.monta_expert_linear_fp8(cfg, packed, wc, wsc, N, y[0], ws)
+    for j in range(S):
+        m.monta_expert_linear_fp8(cfg, packed, wc, wsc, N, y[1], ws, j)
+    m.monta_expert_linear_fp8(cfg, packed, wc, wsc, N, y[2], ws)
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2])
+
+
 def test_special_codes(m):
     """A NaN code or an infinite scale stays in its row; largest and smallest codes multiply as the numbers they are."""
     import torch
