@@ -837,8 +837,11 @@ int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t s
     if (r <= 24 || tiles(32, 128) <= 400) return with_dw(Short<32, 128, 3>{});
     if (r > 56 && b.a.N >= 512 && tiles(256, 256) >= 160) {
         const bool ragged_last = r > 384 && b.a.E * ((b.a.H + 255) / 256) <= 256;
-        if (!big_dw) return ragged_last ? launch(Wide<false, 8, 8, true>{}, Wide<true, 4, 4>{}, apart) : launch(Wide<false, 8, 8>{}, Wide<true, 4, 4>{}, apart);
-        return ragged_last ? launch(Wide<false, 8, 8, true>{}, Wide<true, 8, 8>{}, apart) : launch(Wide<false, 8, 8>{}, Wide<true, 8, 8>{}, apart);
+        auto large = [&](auto dx) {
+            if (big_dw) return launch(dx, Wide<true, 8, 8>{}, apart);
+            return dw_tiles <= 96 ? launch(dx, Slim<2>{}, apart) : launch(dx, Wide<true, 4, 4>{}, apart);
+        };
+        return ragged_last ? large(Wide<false, 8, 8, true>{}) : large(Wide<false, 8, 8>{});
     }
     if (r <= 56 || tiles(64, 128) <= 700) return with_dw(Short<64, 128, 3>{});
     return with_dw(Wide<false, 4, 4>{});

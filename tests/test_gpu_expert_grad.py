@@ -88,6 +88,7 @@ LONG = [  # experts with so many rows and so few weights that the walk over the 
     (130, 136, 72, 7, 3, 0.0, 0, 2.0),                 # from a few rows to all of them
     (7000, 504, 392, 4, 2, 0.0, 0, 0.4),
     (4100, 776, 264, 8, 2, 0.9, 1, 0.0),
+    (10500, 504, 512, 4, 4, 0.0, 0, 0.0),              # and so many rows that dx goes in its largest tiles
 ]
 
 
