@@ -328,7 +328,7 @@ int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *we
  *   y[r][n] = sum_b xs[r][b] * ws[e][n / 128][b] * sum_{h in block b} xc[r][h] * wc[e][n][h]   for every kept row r of expert e,
  * x_rows [max_rows] rows as above in FINAL order, w_codes [E][out_features][H] e4m3, w_scales [E][ceil(out_features / 128)]
  * [ceil(H / 128)] fp32, one for each 128 x 128 block of an expert's weights; y [max_rows][out_features] in cfg->dtype.  Device
- * pointers, 16-byte aligned (w_scales 4-byte); H a multiple of 16, at most 65536; out_features a multiple of 8 (bf16) or 4 (fp32), at most 2^20; slice, rows that are not written
+ * pointers, 16-byte aligned (w_scales 4-byte); H a multiple of 16, at most 65536; out_features a multiple of 8 (bf16) or 4 (fp32), at most 2^20; max_rows at most 2^31 - 4097; slice, rows that are not written
  * and the workspace as in monta_expert_linear.  y, rounded once to cfg->dtype, may share no memory with what is read.  With cfg->dtype
  * MONTA_BF16 the codes are multiplied by the matrix cores' 8-bit instructions, which drop what lies more than 13 bits below the
  * largest of a few neighbouring products (1.5e-5 of a block's sum on normal data, a hundredth of the rounding of y); the blocks'
@@ -344,7 +344,7 @@ int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows, const void
  * Layouts, types and alignment as in monta_expert_linear, dy like y, dx_final like x_final, dw_exp like w_exp.  Either of dx_final and
  * dw_exp may be NULL (then w_exp, or x_final, may be, too).  fp32 accumulation, one rounding; the order of the additions is fixed for a
  * shape and a load.  Rows of no expert are neither read nor written.  No output may share memory with an input or the other output.
- * hidden and out_features at most 2^20. */
+ * hidden and out_features at most 2^20, max_rows at most 2^31 - 4097. */
 int monta_expert_linear_backward(const monta_cfg *cfg, const void *dy, const void *x_final, const void *w_exp, int32_t out_features,
                                  void *dx_final, void *dw_exp, const void *ws, void *stream);
 

@@ -128,6 +128,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 constexpr uint32_t kOutOfRange = 0x80000000u;                      // a lane offset past every descriptor: no access
 
 constexpr int kBigMaxHidden = 1 << 20;                             // a tile's 256 rows end far below it
+constexpr int64_t kMostRows = 0x7fffffff - 4096;                   // row numbers some steps past the last one are still numbers of 32 bits
 
 // Where tile number `tile` starts its walk along the hidden axis.  Rows that are a multiple of 4096 bytes apart begin on the same memory
 // channels, so that workgroups which walk in step all wait for a few of them: 256 MiB of weights in rows of 8192 bytes, 64 rows a workgroup,

@@ -631,7 +631,7 @@ extern "C" int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows,
     const int bpe = c.bf16 ? 2 : 4;
     if (out_features < 1 || (int64_t)out_features * bpe % 16 != 0 || c.H % 16 != 0) return MONTA_ERR_INVALID;
     if (slice < -1 || slice >= c.s.S) return MONTA_ERR_INVALID;
-    if (c.H > kMaxHidden8 || out_features > kBigMaxHidden) return MONTA_ERR_UNSUPPORTED;
+    if (c.H > kMaxHidden8 || out_features > kBigMaxHidden || c.max_rows > kMostRows) return MONTA_ERR_UNSUPPORTED;
     Expert8Args b{};
     b.row8 = (int32_t)fp8_row_bytes(c.H);
     b.nb = (c.H + 127) / 128;

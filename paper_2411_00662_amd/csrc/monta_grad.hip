@@ -862,7 +862,7 @@ extern "C" int monta_expert_linear_backward(const monta_cfg *cfg, const void *dy
         return MONTA_ERR_ALIGN;
     const int bpe = c.bf16 ? 2 : 4;
     if (out_features < 1 || (int64_t)out_features * bpe % 16 != 0) return MONTA_ERR_INVALID;
-    if (out_features > kBigMaxHidden || c.H > kBigMaxHidden) return MONTA_ERR_UNSUPPORTED;
+    if (out_features > kBigMaxHidden || c.H > kBigMaxHidden || c.max_rows > kMostRows) return MONTA_ERR_UNSUPPORTED;
     const int64_t nx = c.max_rows * c.row_bytes, ny = c.max_rows * out_features * bpe, nw = (int64_t)c.s.E * out_features * c.row_bytes;
     const struct {
         const void *p;

@@ -117,6 +117,7 @@ def test_expert_linear_fp8_sizes():
     assert expert8(cfg(hidden=520)) == -1
     assert expert8(cfg(hidden=65536 + 16)) == -2
     assert expert8(cfg(), n=(1 << 20) + 8) == -2
+    assert expert8(cfg(tokens=2 ** 31 - 4096, hidden=16, top_k=1, slices=1), n=8) == -2
 
 
 def grads(c, dy=A[0], x=A[1], w=A[2], n=256, dx=A[3], dw=A[4], ws=A[5]):
@@ -135,6 +136,7 @@ def test_expert_linear_backward_refuses(kw, code):
 def test_expert_linear_backward_sizes():
     assert grads(cfg(), n=(1 << 20) + 8) == -2
     assert grads(cfg(hidden=(1 << 20) + 8)) == -2
+    assert grads(cfg(tokens=2 ** 31 - 4096, hidden=16, top_k=1, slices=1), n=8) == -2
 
 
 CALLS = {
