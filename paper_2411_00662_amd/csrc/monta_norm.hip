@@ -338,61 +338,64 @@ __global__ __launch_bounds__(threads_of<L>()) void combine_backward_kernel(const
     static_assert(L >= kWave, "a wave has one token");
     constexpr int EV = Elem<BF16>::kPerVec, kRows = threads_of<L>() / L, W = L / kWave;
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
-    __shared__ float part[32][W];
+    __shared__ float part[2][32][W];                                // alternated, so that one barrier keeps a token's sums from the next one's
     const int l = threadIdx.x % L, lane = threadIdx.x % kWave, wave = l / kWave;
-    const uint32_t t = blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / L);
-    if (t >= (uint32_t)T) return;                                            // a whole wave, and with L > 64 never
-    const int64_t tk = (int64_t)t * k;
-    const int pos = lane < k ? pos_final[tk + lane] : -1;
-    const float gate = lane < k ? gates[tk + lane] : 0.f;
-    u32x4 d[NV], cur[NV];
+    int parity = 0;
+    // a whole wave goes round, and with L > 64 the whole workgroup
+    for (uint32_t t = blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / L); t < (uint32_t)T; t += gridDim.x * kRows, parity ^= 1) {
+        const int64_t tk = (int64_t)t * k;
+        const int pos = lane < k ? pos_final[tk + lane] : -1;
+        const float gate = lane < k ? gates[tk + lane] : 0.f;
+        u32x4 d[NV], cur[NV];
 #pragma unroll
-    for (int q = 0; q < NV; ++q) d[q] = l + q * L < vpr ? dout[(int64_t)t * vpr + l + q * L] : zero;
-    const bool kept = pos >= 0 && pos < max_rows;
-    unsigned long long left = __ballot(kept);
-    auto row_of = [&](int j) { return (int64_t)__builtin_amdgcn_readlane(pos, j); };
-    auto fetch = [&](int64_t row, u32x4(&to)[NV]) {
+        for (int q = 0; q < NV; ++q) d[q] = l + q * L < vpr ? dout[(int64_t)t * vpr + l + q * L] : zero;
+        const bool kept = pos >= 0 && pos < max_rows;
+        unsigned long long left = __ballot(kept);
+        auto row_of = [&](int j) { return (int64_t)__builtin_amdgcn_readlane(pos, j); };
+        auto fetch = [&](int64_t row, u32x4(&to)[NV]) {
 #pragma unroll
-        for (int q = 0; q < NV; ++q) to[q] = l + q * L < vpr ? load<STREAM>(y + row * vpr + l + q * L) : zero;
-    };
-    float mine = 0.f;                                              // lane j: the wave's share of choice j's gradient
-    if (left) fetch(row_of(__builtin_ctzll(left)), cur);
-    while (left) {
-        const int j = __builtin_ctzll(left);
-        left &= left - 1;
-        u32x4 next[NV];
-        if (left) fetch(row_of(__builtin_ctzll(left)), next);
-        const int64_t row = row_of(j);
-        const float g = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(gate), j));
-        float dot = 0.f;
+            for (int q = 0; q < NV; ++q) to[q] = l + q * L < vpr ? load<STREAM>(y + row * vpr + l + q * L) : zero;
+        };
+        float mine = 0.f;                                          // lane j: the wave's share of choice j's gradient
+        if (left) fetch(row_of(__builtin_ctzll(left)), cur);
+        while (left) {
+            const int j = __builtin_ctzll(left);
+            left &= left - 1;
+            u32x4 next[NV];
+            if (left) fetch(row_of(__builtin_ctzll(left)), next);
+            const int64_t row = row_of(j);
+            const float g = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(gate), j));
+            float dot = 0.f;
 #pragma unroll
-        for (int q = 0; q < NV; ++q) {
-            const int i = l + q * L;
-            float a[EV], b[EV];
-            unpack<BF16>(d[q], a);
-            unpack<BF16>(cur[q], b);
+            for (int q = 0; q < NV; ++q) {
+                const int i = l + q * L;
+                float a[EV], b[EV];
+                unpack<BF16>(d[q], a);
+                unpack<BF16>(cur[q], b);
 #pragma unroll
-            for (int e = 0; e < EV; ++e) {
-                dot = __builtin_fmaf(a[e], b[e], dot);
-                a[e] *= g;
+                for (int e = 0; e < EV; ++e) {
+                    dot = __builtin_fmaf(a[e], b[e], dot);
+                    a[e] *= g;
+                }
+                if (i < vpr) store<STREAM>(dy + row * vpr + i, pack<BF16>(a));
             }
-            if (i < vpr) store<STREAM>(dy + row * vpr + i, pack<BF16>(a));
+            dot = lanes_sum<kWave>(dot);
+            if (lane == j) mine = dot;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) cur[q] = next[q];
         }
-        dot = lanes_sum<kWave>(dot);
-        if (lane == j) mine = dot;
+        if constexpr (W == 1) {
+            if (lane < k) dgates[tk + lane] = mine;
+        } else {
+            float(*const sums)[W] = part[parity];
+            if (lane < k) sums[lane][wave] = mine;
+            __syncthreads();
+            if (l < k) {
+                float v = 0.f;
 #pragma unroll
-        for (int q = 0; q < NV; ++q) cur[q] = next[q];
-    }
-    if constexpr (W == 1) {
-        if (lane < k) dgates[tk + lane] = mine;
-    } else {
-        if (lane < k) part[lane][wave] = mine;
-        __syncthreads();
-        if (l < k) {
-            float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) v += part[l][w];
-            dgates[tk + l] = v;
+                for (int w = 0; w < W; ++w) v += sums[l][w];
+                dgates[tk + l] = v;
+            }
         }
     }
 }
@@ -426,6 +429,8 @@ int rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : 1; }
 int backward_rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : vpr <= 512 ? 2 : 1; }
 
 constexpr int kNormGrid = 1 << 16;
+// HIP launches fewer than 2^32 threads; with up to 1024 a workgroup these are half of that.  Fewer tokens have a workgroup, or a wave, each.
+constexpr int64_t kCombineGrid = 1 << 21;
 // As much as the memory-side cache holds (256 MiB) and more is streamed past it.  Plain and streamed, three sets of buffers in turn, us: norm of
 // 8192 x 4096 bf16, 303 MB, 52.8 and 48.0, its gradient, whose loads alone are streamed, 52.5 and 48, the combine's on 8 experts,
 // top-2, 336 MB, 64.7 and 52.9; but of 2048 x 4096 13.1 and 15.2, 18.6 and 20.5, 14.3 and 16.6.
@@ -578,8 +583,9 @@ int monta_combine_backward(const monta_cfg *cfg, const void *dout, const void *y
     LaunchTimer timer(MONTA_K_COMBINE_BACKWARD, st);
     with_form(c.bf16, n + 2 * c.kept_bound * c.row_bytes >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value < kWave ? kWave : decltype(lanes)::value, NV = decltype(vecs)::value, kRows = threads_of<L>() / L;
-        hipLaunchKernelGGL((combine_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3((unsigned)(((int64_t)c.s.T + kRows - 1) / kRows)),
-                           dim3(threads_of<L>()), 0, st, static_cast<const u32x4 *>(dout), static_cast<const u32x4 *>(y), gates, static_cast<u32x4 *>(dy),
+        const unsigned wgs = (unsigned)std::min<int64_t>(((int64_t)c.s.T + kRows - 1) / kRows, kCombineGrid);
+        hipLaunchKernelGGL((combine_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(wgs), dim3(threads_of<L>()), 0, st,
+                           static_cast<const u32x4 *>(dout), static_cast<const u32x4 *>(y), gates, static_cast<u32x4 *>(dy),
                            dgates, c.p.pos_final, c.s.T, c.s.k, c.s.vpr, c.s.max_rows);
         return MONTA_OK;
     });
