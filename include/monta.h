@@ -332,7 +332,8 @@ int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *we
  * and the workspace as in monta_expert_linear.  y, rounded once to cfg->dtype, may share no memory with what is read.  With cfg->dtype
  * MONTA_BF16 the codes are multiplied by the matrix cores' 8-bit instructions, which drop what lies more than 13 bits below the
  * largest of a few neighbouring products (1.5e-5 of a block's sum on normal data, a hundredth of the rounding of y); the blocks'
- * sums are scaled and added in fp32.  With MONTA_FP32 products are exact and all sums fp32, at a lower rate. */
+ * sums are scaled and added in fp32.  With MONTA_FP32 products are exact and all sums fp32, at a lower rate.  MONTA_ERR_UNSUPPORTED
+ * where y has more tiles than one launch has workgroups for (2^32 threads: 2^23 tiles of 256 x 256 or more). */
 int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows, const void *w_codes, const float *w_scales, int32_t out_features,
                             void *y, const void *ws, int slice, void *stream);
 
@@ -344,7 +345,8 @@ int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows, const void
  * Layouts, types and alignment as in monta_expert_linear, dy like y, dx_final like x_final, dw_exp like w_exp.  Either of dx_final and
  * dw_exp may be NULL (then w_exp, or x_final, may be, too).  fp32 accumulation, one rounding; the order of the additions is fixed for a
  * shape and a load.  Rows of no expert are neither read nor written.  No output may share memory with an input or the other output.
- * hidden and out_features at most 2^20, max_rows at most 2^31 - 4097. */
+ * hidden and out_features at most 2^20, max_rows at most 2^31 - 4097; MONTA_ERR_UNSUPPORTED, before anything is launched, where the
+ * outputs have more tiles than one launch has workgroups for (2^32 threads: 2^24 tiles, of 256 x 256 in bf16 and of 64 x 64 in fp32). */
 int monta_expert_linear_backward(const monta_cfg *cfg, const void *dy, const void *x_final, const void *w_exp, int32_t out_features,
                                  void *dx_final, void *dw_exp, const void *ws, void *stream);
 

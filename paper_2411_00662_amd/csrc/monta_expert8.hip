@@ -520,11 +520,11 @@ template <int XR, int WR, int WX, int WW, int NST, bool F32>
 int launch_expert8(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
 {
     using G = Tile8<XR, WR, WX, WW, NST>;
-    static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_kernel<XR, WR, WX, WW, NST, F32>), G::kLdsBytes, lds_opt_in)) return rc;
     const int64_t row_tiles = rows_bound / XR + std::min<int64_t>(b.a.E, rows_bound), nct = (b.a.N + WR - 1) / WR;
     const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid, G::kThreads)) return MONTA_ERR_UNSUPPORTED;
+    static LdsOptIn lds_opt_in;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_kernel<XR, WR, WX, WW, NST, F32>), G::kLdsBytes, lds_opt_in)) return rc;
     hipLaunchKernelGGL((expert8_kernel<XR, WR, WX, WW, NST, F32>), dim3((unsigned)grid), dim3(G::kThreads), G::kLdsBytes, st,
                        static_cast<const unsigned char *>(x), static_cast<const unsigned char *>(w), y, b);
     MONTA_HIP_TRY(hipGetLastError());
@@ -536,7 +536,7 @@ int launch_expert8_split(const void *x, const void *w, void *y, const Expert8Arg
 {
     const int64_t row_tiles = rows_bound / 16 + std::min<int64_t>(b.a.E, rows_bound), nct = (b.a.N + 16 * CB - 1) / (16 * CB);
     const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid, 64 * W)) return MONTA_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((expert8_split_kernel<CB, W, D, F32>), dim3((unsigned)grid), dim3(64 * W), 0, st, static_cast<const unsigned char *>(x),
                        static_cast<const unsigned char *>(w), y, b);
     MONTA_HIP_TRY(hipGetLastError());
@@ -546,13 +546,13 @@ int launch_expert8_split(const void *x, const void *w, void *y, const Expert8Arg
 template <bool RAGGED_LAST, bool TAIL>
 int launch_expert8_big_k(const void *x, const void *w, void *y, const Expert8Args &b, int64_t rows_bound, hipStream_t st)
 {
-    static LdsOptIn lds_opt_in;
     constexpr int lds = kBig8LdsBytes;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<RAGGED_LAST, TAIL>), lds, lds_opt_in)) return rc;
     const int64_t nct = (b.a.N + kBig8 - 1) / kBig8, row_tiles = rows_bound / kBig8 + std::min<int64_t>(b.a.E, rows_bound);
     const int64_t tiles = (row_tiles + (RAGGED_LAST ? b.a.E : 0)) * nct;              // short ragged tiles come in halves
     const int64_t grid = (tiles + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid, 512)) return MONTA_ERR_UNSUPPORTED;
+    static LdsOptIn lds_opt_in;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert8_big_kernel<RAGGED_LAST, TAIL>), lds, lds_opt_in)) return rc;
     hipLaunchKernelGGL((expert8_big_kernel<RAGGED_LAST, TAIL>), dim3((unsigned)grid), dim3(512), lds, st, static_cast<const unsigned char *>(x),
                        static_cast<const unsigned char *>(w), static_cast<__bf16 *>(y), b);
     MONTA_HIP_TRY(hipGetLastError());

@@ -757,10 +757,10 @@ __global__ __launch_bounds__(256, Dx::kPerCu < Dw::kPerCu ? Dx::kPerCu : Dw::kPe
 template <typename Form>
 int launch_form(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 {
+    const int64_t grid = Form::grid(b.a, rows_bound);
+    if (!launchable(grid, 256)) return MONTA_ERR_UNSUPPORTED;
     static LdsOptIn lds_opt_in;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_kernel<Form>), Form::kLds, lds_opt_in)) return rc;
-    const int64_t grid = Form::grid(b.a, rows_bound);
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
     LaunchTimer timer(MONTA_K_EXPERT_BACKWARD, st);
     hipLaunchKernelGGL((grad_kernel<Form>), dim3((unsigned)grid), dim3(256), Form::kLds, st, b);
     MONTA_HIP_TRY(hipGetLastError());
@@ -771,11 +771,11 @@ template <typename Dx, typename Dw>
 int launch_both(const GradArgs &b, int64_t rows_bound, hipStream_t st)
 {
     constexpr int lds = Dx::kLds > Dw::kLds ? Dx::kLds : Dw::kLds;
-    static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_both_kernel<Dx, Dw>), lds, lds_opt_in)) return rc;
     const int64_t of_dx = Dx::grid(b.a, rows_bound), of_dw = Dw::grid(b.a, rows_bound), grid = of_dx + of_dw;
     const bool dw_first = rows_bound / std::min<int64_t>(b.a.E, rows_bound) > b.a.N;
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid, 256)) return MONTA_ERR_UNSUPPORTED;
+    static LdsOptIn lds_opt_in;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(grad_both_kernel<Dx, Dw>), lds, lds_opt_in)) return rc;
     LaunchTimer timer(MONTA_K_EXPERT_BACKWARD, st);
     hipLaunchKernelGGL((grad_both_kernel<Dx, Dw>), dim3((unsigned)grid), dim3(256), lds, st, b, (uint32_t)(dw_first ? of_dw : of_dx), dw_first);
     MONTA_HIP_TRY(hipGetLastError());
@@ -811,11 +811,12 @@ int launch_grads(const GradArgs &b, bool bf16, int64_t rows_bound, hipStream_t s
 {
     const int64_t active = std::min<int64_t>(b.a.E, rows_bound), r = rows_bound / active;
     auto tiles = [&](int64_t R, int64_t C) { return active * ((b.a.H + C - 1) / C) * (2 * r + R) / (2 * R); };
-    auto launch = [&](auto dx, auto dw, auto together) {
+    auto launch = [&](auto dx, auto dw, auto together) -> int {
         using Dx = decltype(dx);
         using Dw = decltype(dw);
         if constexpr (decltype(together)::value)
             if (b.dx && b.dw) return launch_both<Dx, Dw>(b, rows_bound, st);
+        if (b.dx && b.dw && !launchable(Dw::grid(b.a, rows_bound), 256)) return MONTA_ERR_UNSUPPORTED;        // before dx goes out
         if (b.dx)
             if (int rc = launch_form<Dx>(b, rows_bound, st)) return rc;
         return b.dw ? launch_form<Dw>(b, rows_bound, st) : MONTA_OK;
