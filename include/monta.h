@@ -42,6 +42,10 @@
  *     hidden * sizeof(element) % 16 == 0; activation base pointers 16-byte
  *     aligned, all others 4-byte aligned.  Logits must be finite (NaN is
  *     treated as -inf; the result is then unspecified but in bounds).
+ *     A call that would need 2^32 threads or more in one launch is refused
+ *     (MONTA_ERR_UNSUPPORTED): routing from 2^24 route workgroups on, the gate
+ *     from 2^26 (fp32, at most 4 experts) to 2^30 tokens on, the expert layer by
+ *     its tiles.
  *
  * Units.  U = slices * tp units of Tu = tokens / U consecutive tokens; unit u is
  * slice u / tp, virtual TP rank u % tp.  Expert e lives on virtual EP rank

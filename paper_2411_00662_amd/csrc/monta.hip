@@ -495,12 +495,13 @@ template <int MT, int NT, int KS, bool DEEP, bool SPLIT = false, bool STREAM = f
 int launch_gate(const u32x4 *x, const u32x4 *w, float *logits, int64_t T, int H, int E, hipStream_t st)
 {
     using G = GateTile<MT, NT, KS>;
+    const int64_t grid = (T + G::kTokens - 1) / G::kTokens;
+    if (!launchable(grid, kGateThreads)) return MONTA_ERR_UNSUPPORTED;
     static LdsOptIn lds_opt_in;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(gate_bf16_kernel<MT, NT, KS, DEEP, SPLIT, STREAM>),
                             (int)G::lds_bytes(32 * NT, !SPLIT), lds_opt_in))
         return rc;
-    const unsigned grid = (unsigned)((T + G::kTokens - 1) / G::kTokens);
-    hipLaunchKernelGGL((gate_bf16_kernel<MT, NT, KS, DEEP, SPLIT, STREAM>), dim3(grid), dim3(kGateThreads), G::lds_bytes(E, !SPLIT), st, x, w, logits,
+    hipLaunchKernelGGL((gate_bf16_kernel<MT, NT, KS, DEEP, SPLIT, STREAM>), dim3((unsigned)grid), dim3(kGateThreads), G::lds_bytes(E, !SPLIT), st, x, w, logits,
                        T, H, E);
     return MONTA_OK;
 }
@@ -532,10 +533,10 @@ template <int XR, int WR, int NST, bool F32, bool SPREAD>
 int launch_gate_short_t(const u32x4 *x, const u32x4 *w, float *logits, int64_t T, int H, int E, hipStream_t st)
 {
     using G = ShortTile<XR, WR, NST>;
+    const int64_t grid = (T + XR - 1) / XR * ((E + WR - 1) / WR);
+    if (!launchable(grid, 256)) return MONTA_ERR_UNSUPPORTED;
     static LdsOptIn lds_opt_in;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(gate_short_kernel<XR, WR, NST, F32, SPREAD>), G::kLdsBytes, lds_opt_in)) return rc;
-    const int64_t grid = (T + XR - 1) / XR * ((E + WR - 1) / WR);
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((gate_short_kernel<XR, WR, NST, F32, SPREAD>), dim3((unsigned)grid), dim3(256), G::kLdsBytes, st, x, w, logits, T, H, E);
     return MONTA_OK;
 }
@@ -576,7 +577,7 @@ template <bool BF16>
 int launch_gate_split(const u32x4 *x, const u32x4 *w, float *logits, int64_t T, int64_t cpr, int E, int nb, hipStream_t st)
 {
     const int64_t grid = (T + 15) / 16 * ((E + 16 * nb - 1) / (16 * nb));
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid, 512)) return MONTA_ERR_UNSUPPORTED;
     constexpr int kMany = BF16 ? 2 : 4;
     if (nb == kMany) hipLaunchKernelGGL((gate_split_kernel<BF16, kMany>), dim3((unsigned)grid), dim3(512), 0, st, x, w, logits, T, cpr, E);
     else if (nb == 1) hipLaunchKernelGGL((gate_split_kernel<BF16, 1>), dim3((unsigned)grid), dim3(512), 0, st, x, w, logits, T, cpr, E);
@@ -588,10 +589,10 @@ template <int XB, int CB, int W, int NST>
 int launch_gate_ring(const u32x4 *x, const u32x4 *w, float *logits, int64_t T, int H, int E, hipStream_t st)
 {
     using G = SplitTile<XB, CB, W, NST>;
+    const int64_t grid = (T + 16 * XB - 1) / (16 * XB) * ((E + 16 * CB - 1) / (16 * CB));
+    if (!launchable(grid, G::kThreads)) return MONTA_ERR_UNSUPPORTED;
     static LdsOptIn lds_opt_in;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(gate_ring_kernel<XB, CB, W, NST>), G::kLdsBytes, lds_opt_in)) return rc;
-    const int64_t grid = (T + 16 * XB - 1) / (16 * XB) * ((E + 16 * CB - 1) / (16 * CB));
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((gate_ring_kernel<XB, CB, W, NST>), dim3((unsigned)grid), dim3(G::kThreads), G::kLdsBytes, st, x, w, logits, T, H / 8, E);
     return MONTA_OK;
 }
@@ -618,6 +619,7 @@ int launch_gate_few(const u32x4 *x, const u32x4 *w, float *logits, int64_t T, in
 
 int launch_gate_f32_few(const float4 *x, const float4 *w, float *logits, int64_t T, int H, int E, hipStream_t st)
 {
+    if (!launchable((T + 3) / 4, 256)) return MONTA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)((T + 3) / 4)), block(256);
     const int vpr = H / 4;
     if (E == 1) hipLaunchKernelGGL(gate_f32_few_kernel<1>, grid, block, 0, st, x, w, logits, T, vpr);
@@ -659,7 +661,7 @@ int launch_expert_big(const void *x_final, const void *w_exp, void *y, ExpertArg
     // whole blocks of 256 workgroups: the kernel hands out tile numbers in such blocks, 32 per XCD
     auto rounded = [](int64_t n) { return (n + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds); };
     const int64_t grid = rounded(row_tiles * nct), grid_last = rounded((row_tiles + a.E) * nct);     // ragged tiles may come in halves
-    if (grid_last > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid_last, kBigThreads)) return MONTA_ERR_UNSUPPORTED;
     // The segments' ragged last tiles go to the end of the numbering only when there are few of them, at most one round
     // of 256 workgroups: measured on MI355X, eight segments of about 2048 rows 464 us against 480 with the ragged tiles in
     // place; 64 segments of 191 rows, where every tile is ragged, 448 against 440.
@@ -700,12 +702,12 @@ int launch_expert_short_t(const void *x_final, const void *w_exp, void *y, Exper
     // 4504, 20 rows 20.4 and 14.8; 32 of 1064 x 1616, one row 9.4, 10.8 and 10.0, 10.4; but 512 tiles, 8 of 4096 x 4096, 16 rows 40.0, 41.5 and, in fours, 41.8, 43.8; and with several row
     // tiles, 4 of 4096 x 2048, 100 rows, 20.0 and 20.7, one by one 38).
     a.deal = rows_per_expert <= XR && std::min<int64_t>(a.E, rows_bound) * ((a.N + WR - 1) / WR) < 512 ? 3 : 5;
-    static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert_short_kernel<XR, WR, NST, F32, FINE>), G::kLdsBytes, lds_opt_in)) return rc;
     const int64_t row_tiles = rows_bound / XR + std::min<int64_t>(a.E, rows_bound);
     const int64_t nct = (a.N + WR - 1) / WR;
     const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid, 256)) return MONTA_ERR_UNSUPPORTED;
+    static LdsOptIn lds_opt_in;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert_short_kernel<XR, WR, NST, F32, FINE>), G::kLdsBytes, lds_opt_in)) return rc;
     hipLaunchKernelGGL((expert_short_kernel<XR, WR, NST, F32, FINE>), dim3((unsigned)grid), dim3(256), G::kLdsBytes, st,
                        static_cast<const u32x4 *>(x_final), static_cast<const u32x4 *>(w_exp), y, a);
     return MONTA_OK;
@@ -715,11 +717,11 @@ template <int XB, int CB, int W, int NST, bool F32>
 int launch_expert_split(const void *x_final, const void *w_exp, void *y, const ExpertArgs &a, int64_t rows_bound, hipStream_t st)
 {
     using G = SplitTile<XB, CB, W, NST>;
-    static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert_split_kernel<XB, CB, W, NST, F32>), G::kLdsBytes, lds_opt_in)) return rc;
     const int64_t row_tiles = rows_bound / (16 * XB) + std::min<int64_t>(a.E, rows_bound), nct = (a.N + 16 * CB - 1) / (16 * CB);
     const int64_t grid = (row_tiles * nct + 8 * kXcds - 1) / (8 * kXcds) * (8 * kXcds);
-    if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid, G::kThreads)) return MONTA_ERR_UNSUPPORTED;
+    static LdsOptIn lds_opt_in;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert_split_kernel<XB, CB, W, NST, F32>), G::kLdsBytes, lds_opt_in)) return rc;
     hipLaunchKernelGGL((expert_split_kernel<XB, CB, W, NST, F32>), dim3((unsigned)grid), dim3(G::kThreads), G::kLdsBytes, st,
                        static_cast<const u32x4 *>(x_final), static_cast<const u32x4 *>(w_exp), y, a);
     return MONTA_OK;
@@ -773,14 +775,13 @@ template <int BM, int BN, int WM, int WN>
 int launch_expert(const void *x_final, const void *w_exp, void *y, ExpertArgs a, int64_t rows_bound, hipStream_t st)
 {
     using G = ExpertTile<BM, BN, WM, WN>;
-    static LdsOptIn lds_opt_in;
-    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert_bf16_kernel<BM, BN, WM, WN>), G::kLdsBytes, lds_opt_in))
-        return rc;
     const int64_t row_tiles = (rows_bound + BM - 1) / BM + a.E;      // each expert may end in a ragged tile
     const int64_t nct = (a.N + BN - 1) / BN;
     constexpr int64_t block = 32 * G::kWgsPerCu * kXcds;            // the kernel numbers its tiles in such blocks
     const int64_t grid8 = (row_tiles * nct + block - 1) / block * block;
-    if (grid8 > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+    if (!launchable(grid8, G::kThreads)) return MONTA_ERR_UNSUPPORTED;
+    static LdsOptIn lds_opt_in;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(expert_bf16_kernel<BM, BN, WM, WN>), G::kLdsBytes, lds_opt_in)) return rc;
     hipLaunchKernelGGL((expert_bf16_kernel<BM, BN, WM, WN>), dim3((unsigned)grid8), dim3(G::kThreads), G::kLdsBytes, st,
                        static_cast<const u32x4 *>(x_final), static_cast<const u32x4 *>(w_exp),
                        static_cast<unsigned short *>(y), a);
@@ -845,7 +846,7 @@ int launch_expert_f32(const void *x_final, const void *w_exp, void *y, const Exp
     if (a.H > kBigMaxHidden) {
         const int64_t row_tiles = rows_bound / kF32Tile + a.E, nct = (a.N + kF32Tile - 1) / kF32Tile;
         const int64_t grid = (row_tiles * nct + 32 * kXcds - 1) / (32 * kXcds) * (32 * kXcds);
-        if (grid > 0x7fffffff) return MONTA_ERR_UNSUPPORTED;
+        if (!launchable(grid, 256)) return MONTA_ERR_UNSUPPORTED;
         hipLaunchKernelGGL(expert_f32_kernel, dim3((unsigned)grid), dim3(256), 0, st, static_cast<const u32x4 *>(x_final),
                            static_cast<const u32x4 *>(w_exp), static_cast<float *>(y), a);
         return MONTA_OK;
@@ -860,6 +861,8 @@ int launch_expert_f32(const void *x_final, const void *w_exp, void *y, const Exp
 int launch_route(const Geometry &g, const PlanPtrs &p, const float *logits, int32_t *topk_idx, float *gates,
                  hipStream_t st)
 {
+    // the calls that finish the plan have as many workgroups, of kPlanThreads
+    if (!launchable(g.s.num_blocks, std::max(g.route_threads, kPlanThreads))) return MONTA_ERR_UNSUPPORTED;
     const int per_lane = (g.s.E + g.s.rl - 1) / g.s.rl;
     auto launch = [&](auto lc, auto ne) -> int {
         constexpr int L = decltype(lc)::value, NE = decltype(ne)::value;
