@@ -431,10 +431,21 @@ int backward_rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : vpr 
 constexpr int kNormGrid = 1 << 16;
 // HIP launches fewer than 2^32 threads; with up to 1024 a workgroup these are half of that.  Fewer tokens have a workgroup, or a wave, each.
 constexpr int64_t kCombineGrid = 1 << 21;
-// As much as the memory-side cache holds (256 MiB) and more is streamed past it.  Plain and streamed, three sets of buffers in turn, us: norm of
-// 8192 x 4096 bf16, 303 MB, 52.8 and 48.0, its gradient, whose loads alone are streamed, 52.5 and 48, the combine's on 8 experts,
-// top-2, 336 MB, 64.7 and 52.9; but of 2048 x 4096 13.1 and 15.2, 18.6 and 20.5, 14.3 and 16.6.
-constexpr int64_t kStreamFrom = 256ll << 20;
+// From three quarters of the memory-side cache (256 MiB) on what a call touches is streamed past it.  Rows of 4096 bf16, plain and streamed, us:
+//                                      110 MB       140 MB       170 MB       200 MB       230 MB       260 MB       300 MB       400 MB
+//   three sets in turn   norm          24.1  21.9   29.8  26.4   34.3  30.6   39.2  35.1   44.6  39.6   49.2  44.0   56.5  50.1   73.2  65.1
+//                        its gradient  25.3  25.5   32.3  30.0   37.4  34.4   42.5  37.9   48.0  42.5   53.1  47.0   59.9  52.4   77.3  72.8
+//                        the combine's 23.1  21.7   30.2  26.2   36.3  30.3   41.0  34.5   46.5  38.5   51.5  42.7   59.0  48.2   76.8  62.4
+//   one set, all of it   norm          19.0  21.2   23.1  25.8   27.8  30.1   31.7  34.9   35.8  39.3   40.9  43.8   50.2  49.8   72.7  64.8
+//   in the cache         its gradient  23.0  25.3   27.1  29.9   31.4  34.2   34.7  37.8   39.4  42.3   43.8  46.9   50.5  52.5   76.6  68.1
+//                        the combine's 19.0  19.9   22.6  24.9   27.5  30.2   31.9  34.8   35.8  38.3   40.3  42.5   48.0  48.3   75.7  62.1
+//   three sets, with the norm          28.7  30.9   34.7  36.3   41.7  42.4   47.3  47.0   55.2  51.4   61.9  57.8   68.8  67.7
+//   gate beside it that  its gradient  31.8  34.2   38.2  40.9   44.5  45.0   49.2  48.5   54.8  54.2   60.4  62.3   69.8  73.5
+//   reads out, dout, dy  the combine's 31.0  33.6   39.4  38.8   49.4  49.2   55.5  56.4   63.0  64.5   69.9  71.3   79.6  81.1
+// The line is where the last of these break even: below it a call may find its inputs in the cache, and the next one its result.  (Of
+// the gradient of the norm only the loads are streamed.)  It does not depend on whole lines: 330 MB in rows of 72, 520, 1032, 4104 and 7168 elements, on
+// 128 bytes or 16 past them, are streamed in 0.85 to 1.03 of the plain time.
+constexpr int64_t kStreamFrom = 192ll << 20;
 
 // rows of partial sums: each is written and read again, and costs more than a row of the norm itself
 int backward_grid(const Call &c)
@@ -498,7 +509,8 @@ int monta_rmsnorm(const monta_cfg *cfg, const void *x, const void *residual, con
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_NORM, st);
     const int wgs = (int)std::min<int64_t>(((int64_t)c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr), kNormGrid);
-    with_form(c.bf16, n * (residual ? 4 : 2) + (out_fp8 ? n8 : 0) >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+    const int64_t touched = n * (residual ? 3 : 1) + (out ? n : 0) + (out_fp8 ? n8 : 0);
+    with_form(c.bf16, touched >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
         hipLaunchKernelGGL((rmsnorm_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(wgs), dim3(threads_of<L>()), 0, st,
                            static_cast<const u32x4 *>(x), static_cast<const u32x4 *>(residual), static_cast<const u32x4 *>(weight),
