@@ -377,8 +377,8 @@ __device__ __forceinline__ void grad_bf16_tile(const GradArgs &b, uint32_t block
     // acc[i][j][v]: row 16 i + lane % 16 of the wave's rows, hidden element 16 j + 4 (lane / 16) + v of its columns.  Through LDS, block of
     // 16 rows by block, so that rows leave as whole pieces of 16 bytes, 32 CB bytes of each side by side.  (8 bytes a lane straight from the registers:
     // 268 MB of weights' gradients in 101 us.)  dw is read by nobody soon and is streamed past the cache, where it would drive out the weights: both
-    // gradients of 128 rows x 4096 x 4096, 8 experts, 153 and 125 us, of 1024 rows 203 and 190.  Not where more than the memory-side cache holds
-    // (256 MiB) leaves in parts of lines: 64 x 4424 x 1768, few rows, 470 us streamed and 290 through it, with 1792 elements a row 186.  dx gains 1 %, but is read next.
+    // gradients of 128 rows x 4096 x 4096, 8 experts, 153 and 125 us, of 1024 rows 203 and 190.  Where it leaves in
+    // parts of half lines only with rows enough (at its flag).  dx gains 1 %, but is read next.
     __builtin_amdgcn_s_waitcnt(0x0070);                            // nor written: the loads past the end have come back
     barrier();                                                     // the stages are not read any more
     constexpr int kOutPitch = 32 * CB + 16;                        // 16 bytes of padding: the 16 rows that a store of 8 bytes a lane hits begin on different banks
@@ -885,6 +885,12 @@ extern "C" int monta_expert_linear_backward(const monta_cfg *cfg, const void *dy
     b.w = w_exp;
     b.dx = dx_final;
     b.dw = dw_exp;
-    b.stream_dw = nw <= (256ll << 20) || c.row_bytes % 128 == 0;
+    // Parts of half lines, of rows that are not whole 64 bytes or of a base between two, are streamed only where a tile's walk gives them time.  dw alone, through
+    // the cache and streamed, us: 64 experts of 2048 x 1768, 1 row 141 and 179, 4 rows 158 and 176, 16 rows 167 and 173, 32 rows 171 and 167;
+    // 400 x 1768, 1 row 29 and 32, 8 rows 34 and 33; 8 of 4096 x 4104, 1 row 84 and 95, 16 rows 99 and 90, 64 rows 104 and 96; 4424 x 1792, 16
+    // bytes behind a line, 1 row 301 and 445, 64 rows 384 and 363; 64 bytes behind it 217 and 218, 326 and 294; on it 210 and 188, 318 and 277;
+    // 64 experts of 2048 x 1824, rows of 57 half lines, 1 row 117 and 106, 8 rows 147 and 119.
+    const bool whole = c.row_bytes % 64 == 0 && !misaligned(dw_exp, 64);
+    b.stream_dw = whole || c.kept_bound >= 16 * std::min<int64_t>(c.s.E, c.kept_bound);
     return launch_grads(b, c.bf16, c.kept_bound, static_cast<hipStream_t>(stream));
 }

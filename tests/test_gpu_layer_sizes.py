@@ -92,15 +92,18 @@ def test_combine_backward_beyond_the_cache(m, H, dtype):  # noqa: F811
 @pytest.mark.parametrize("T,N,E,k", [(120, 2056, 16, 8), (24, 2056, 16, 4)])
 @pytest.mark.parametrize("H", [4104, 4224])
 def test_weights_beyond_the_cache(m, T, N, E, k, H):  # noqa: F811
-    """dw of more than 256 MiB, on rows that are whole 128-byte lines (streamed) and on others; off the lines as a whole: the same bits."""
+    """dw of more than 256 MiB for many and for few rows, on rows that are whole 64-byte half lines and on others; off them as a whole:
+    the same bits."""
     import torch
     grads.test_gradients(m, (T, H, N, E, k, 0.0, 0, 0.0), "bf16", 1)
     cfg, ws, tabs, rows = experts8.routed(m, T, H, "bf16", E, k)
     dy, x, w, _, dw = grads.run(m, cfg, ws, tabs, rows, N, "bf16", 0)
-    off = torch.full((E * N * H + 16,), 3.0, dtype=torch.bfloat16, device="cuda")
-    m.monta_expert_linear_backward(cfg, dy, x, None, N, None, off[8:8 + E * N * H].view(E, N, H), ws)
-    torch.cuda.synchronize()
-    assert torch.equal(off[8:8 + E * N * H].view(E, N, H), dw) and bool((off[:8] == 3.0).all()) and bool((off[8 + E * N * H:] == 3.0).all())
+    n = E * N * H
+    for by in (8, 32):                                 # 16 bytes, which leaves parts of half lines, and 64
+        off = torch.full((n + 64,), 3.0, dtype=torch.bfloat16, device="cuda")
+        m.monta_expert_linear_backward(cfg, dy, x, None, N, None, off[by:by + n].view(E, N, H), ws)
+        torch.cuda.synchronize()
+        assert torch.equal(off[by:by + n].view(E, N, H), dw) and bool((off[:by] == 3.0).all()) and bool((off[by + n:] == 3.0).all())
 
 
 def spread(n, count=64):
