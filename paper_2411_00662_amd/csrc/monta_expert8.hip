@@ -221,13 +221,15 @@ __global__ __launch_bounds__(64 * W) void expert8_split_kernel(const unsigned ch
         }
         __builtin_amdgcn_sched_barrier(0);                         // all loads first
 #pragma unroll
-        for (int d = 0; d < D; ++d)
+        for (int d = 0; d < D; ++d) {
+            const float scale = sx[d] * (first + d * W < b.nb ? sw[d] : 0.f);      // the last block's may be infinite: not past the end
 #pragma unroll
             for (int j = 0; j < CB; ++j) {
                 const f32x4 part = block_product<F32>(fw[d][j], fx[d]);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[j][v] = __builtin_fmaf(part[v], sx[d] * sw[d], acc[j][v]);
+                for (int v = 0; v < 4; ++v) acc[j][v] = __builtin_fmaf(part[v], scale, acc[j][v]);
             }
+        }
     }
     // acc[j][v]: row lane % 16, output feature 16 j + 4 (lane / 16) + v
 #pragma unroll
