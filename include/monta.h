@@ -308,8 +308,8 @@ int monta_fp8_rows(const monta_cfg *cfg, monta_cfg *rows, int64_t *row_bytes);
  * x, residual, sum, out [T][H] and weight [H] in cfg->dtype, out_fp8 [T] rows as above, all device pointers, 16-byte aligned.  sum takes s; it
  * is given if and only if residual is.  out or out_fp8 may be NULL, not both.  sum and out may be x or residual themselves (not
  * both the same buffer); otherwise nothing may share memory.  Sums are held in fp32: the squares of a row have to add up to a
- * finite fp32 number; a row with an infinity or a NaN gives NaN in its own outputs and changes no other row.  eps >= 0 (with eps =
- * 0 a row of zeros gives NaN).  Rows of at most 32 KiB (MONTA_ERR_UNSUPPORTED beyond).  Uses only tokens, hidden and dtype of cfg (all of it is
+ * finite fp32 number, and squares below 2^-149 count as zero.  A row with a NaN gives NaN throughout, one with an infinity NaN there and
+ * zeros elsewhere; no other row changes.  eps >= 0 (with eps = 0 a row whose squares are all zero gives NaN where it is zero, infinities elsewhere).  Rows of at most 32 KiB (MONTA_ERR_UNSUPPORTED beyond).  Uses only tokens, hidden and dtype of cfg (all of it is
  * validated); needs no workspace. */
 int monta_rmsnorm(const monta_cfg *cfg, const void *x, const void *residual, const void *weight, float eps, void *sum, void *out,
                   void *out_fp8, void *stream);
@@ -341,7 +341,10 @@ int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *we
 int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows, const void *w_codes, const float *w_scales, int32_t out_features,
                             void *y, const void *ws, int slice, void *stream);
 
-/* ---- gradients ---- */
+/* ---- gradients ----
+ * From the combine's output back to the rows that were dispatched, the experts' weights, the gates and the norm's input.  They end at the gates:
+ * the softmax or renormalisation behind the logits and the projection of monta_gate have no gradient here, so the caller adds the part of
+ * the norm's dout that comes through the logits. */
 
 /* Gradient of monta_expert_linear over all kept rows:
  *   dx_final[r][h] = sum_n dy[r][n] * w_exp[e][n][h]  for every kept row r of expert e,
