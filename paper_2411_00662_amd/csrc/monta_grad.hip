@@ -535,9 +535,9 @@ __device__ __forceinline__ void grad_slim_tile(const GradArgs &b, const RowTile 
 // 32-bit element has nothing to be transposed with: a deep operand, 32 rows of BR or 64 elements, is read element by element, MFMA v of half a
 // step taking rows 4 g + v of it (g the lane's group of 16), a flat one 16 bytes at a time, which are the same rows' elements.  Swizzles: flat as in
 // bf16; deep, the 64-byte segment s of row k at s ^ (k / 4) % 4, so that the four groups' rows are in different banks.  What bounds it is the
-// fp32 matrix rate, and with few steps the way to the first.  Two stages, five workgroups a CU, do better than three and three (both gradients,
-// us: 1024 rows x 1024 x 1024, 8 experts 56 and 62, 600 x 2048 x 2048, 4 experts 109 and 116, 8192 x 1024 x 1024 310 and 312), but for 32 rows,
-// whose walks are short of work (2 rows x 1024 x 1024 17 and 19).
+// fp32 matrix rate, and with few steps the way to the first.  Two stages of 64 rows, 32 KiB or five workgroups a CU, do better than three,
+// three a CU (both gradients, us: 1024 rows x 1024 x 1024, 8 experts 56 and 62, 600 x 2048 x 2048, 4 experts 109 and 116, 8192 x 1024 x 1024 310 and 312), but for 32 rows,
+// whose walks are short of work (2 rows x 1024 x 1024 17 and 19): three, 36 KiB, which leave four workgroups a CU where dw goes out with them.
 template <int BR, int NST>
 struct GradShapeF32 {
     static constexpr int BC = 64, kStage = (BR + BC) * 128, kLdsBytes = NST * kStage;

@@ -203,7 +203,7 @@ __global__ __launch_bounds__(threads_of<L>()) void rmsnorm_kernel(const u32x4 *x
 // present one's sums are known.  The gradient's partial sums, one row of H per workgroup, are added by rmsnorm_dweight_kernel: a fixed
 // order, no atomics.
 // 8192 x 4096 bf16 with dsum: 268 MB in 48 us with the sum of the partials, 5.6 TB/s; one row of 256 lanes a workgroup instead of two
-// does as well there, but takes for 1155 x 2048 bf16 9.7 us for 8.8 and 517 x 1155 8.3 for 7.4.
+// takes 51, 1155 x 2048 bf16 11.1 for 9.9, 1155 x 516 fp32 9.2 for 8.2 (1155 x 2048 fp32 12.0 either way).
 template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_kernel(const u32x4 *s_in, const u32x4 *w, const u32x4 *dout, const u32x4 *dsum,
                                                                            u32x4 *dx, float *partial, int T, int vpr, float eps)
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_ker
 }
 
 // Adds `n` rows of H partial sums: a workgroup takes 32 columns, its 32 half waves every 32nd row each, eight loads at a time (one at a
-// time costs 1.5 us of the 9 that 517 x 1155 takes, all of it latency).
+// time costs 1.5 us of the 9.7 that 1155 x 516 fp32 then takes, all of it latency).
 __global__ __launch_bounds__(1024) void rmsnorm_dweight_kernel(const float *partial, float *dweight, int n, int H)
 {
     __shared__ float part[32][33];
