@@ -341,10 +341,75 @@ int monta_rmsnorm_backward(const monta_cfg *cfg, const void *sum, const void *we
 int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows, const void *w_codes, const float *w_scales, int32_t out_features,
                             void *y, const void *ws, int slice, void *stream);
 
+/* Layer norm of token rows, with the addition of a residual before it and 8-bit rows behind it:
+ *   s = x + residual, rounded to cfg->dtype (s = x where residual is NULL);  m = mean_h(s);  r = 1 / sqrt(mean_h((s - m)^2) + eps)
+ *   v[h] = (s[h] - m) * r * weight[h] + bias[h];  out and out_fp8 from v as in monta_rmsnorm.
+ * bias [H] in cfg->dtype, 16-byte aligned, or NULL; every other argument, what may share memory and the limits as in monta_rmsnorm.  Sums are held in
+ * fp32, those of squares around a mean that is known by then, so that a row's mean may be far larger than its spread; the squares of a row's differences
+ * from its mean have to add up to a finite fp32 number, and those below 2^-149 count as zero.  A row with a NaN or an infinity gives NaN throughout; no
+ * other row changes.  eps >= 0 (with eps = 0 a row of equal numbers gives NaN). */
+int monta_layernorm(const monta_cfg *cfg, const void *x, const void *residual, const void *weight, const void *bias, float eps, void *sum,
+                    void *out, void *out_fp8, void *stream);
+
+/* Host only: bytes of the scratch buffer of monta_layernorm_backward. */
+int monta_layernorm_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
+
+/* Gradient of the layer norm.  With n = (s - m) r and g = dout weight:
+ *   dx = r (g - mean_h(g) - n mean_h(g n)) + dsum, rounded once: the gradient of x and of the residual alike;
+ *   dweight[h] = sum_t dout[t][h] n[t][h];  dbias[h] = sum_t dout[t][h], fp32; dbias may be NULL.
+ * Every other argument as in monta_rmsnorm_backward, what may share memory and the limits, too. */
+int monta_layernorm_backward(const monta_cfg *cfg, const void *sum, const void *weight, float eps, const void *dout, const void *dsum,
+                             void *dx, float *dweight, float *dbias, void *scratch, void *stream);
+
+/* ---- the router's losses ---- */
+
+/* Host only: bytes of the scratch buffer of monta_route_loss. */
+int monta_route_loss_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
+
+/* What keeps the load of the experts even and the logits small.  Over the n tokens t with token_mask[t] != 0 (all T if token_mask is NULL), with
+ * p[t] the softmax of logits[t] over all experts and lse[t] the logarithm of the sum of its exponentials:
+ *   counts[e] = pairs (t, j) with topk_idx[t][j] == e (before any capacity);  counts[E] = n;  means[e] = sum_t p[t][e] / n
+ *   losses[0] = sum_e f[e] * means[e],  f[e] = E * counts[e] / (k * n): 1 where the load is even;
+ *   losses[1] = sum_t lse[t]^2 / n.
+ * n = 0 gives zeros.  logits [T][E] fp32, topk_idx [T][k] int32 as monta_route wrote it, token_mask [T] bytes: a token with 0 is padding and none of
+ * its values counts, whatever they are.  losses [2], means [E] fp32, counts [E + 1] int32.  A logit may be -infinity (p is 0 there), not all of a
+ * token's; a NaN counts as -infinity.  An index outside 0 .. E - 1 counts for no expert.  scratch 16-byte aligned, its contents are of no use
+ * afterwards and calls that overlap in time need one each.  Sums are held in fp32, their order is fixed for a shape.  Nothing that is written may share
+ * memory with anything else.  Uses tokens, experts and top_k of cfg (all of it is validated); needs no workspace. */
+int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask, float *losses, int32_t *counts,
+                     float *means, void *scratch, void *stream);
+
 /* ---- gradients ----
- * From the combine's output back to the rows that were dispatched, the experts' weights, the gates and the norm's input.  They end at the gates:
- * the softmax or renormalisation behind the logits and the projection of monta_gate have no gradient here, so the caller adds the part of
- * the norm's dout that comes through the logits. */
+ * From the combine's output back to the rows that were dispatched, the experts' weights and the gates; from the gates and the router's losses to the
+ * logits, and from those to the gate's weights and the token rows; and from these to the norm's input.  The choice of the experts and the counts
+ * are taken as constants. */
+
+/* Gradient of monta_route's gates and of monta_route_loss by the logits.  With g = gates[t], d = dgates[t], D = sum_j g[j] d[j], p, lse, f and n as in
+ * monta_route_loss, n and f from `counts`:
+ *   dlogits[t][e] = sum over j with topk_idx[t][j] == e of g[j] * (d[j] - D)           (cfg->renorm = 1)
+ *                 = sum over these j of g[j] * d[j],  - p[e] * D                       (cfg->renorm = 0)
+ *                 + p[e] * (dlosses[0] / n * (f[e] - sum_i p[i] f[i]) + 2 * dlosses[1] / n * lse).
+ * logits, topk_idx, gates, token_mask and counts as those calls took and wrote them; dgates [T][k] fp32, as monta_combine_backward writes it (0
+ * for a dropped choice), or NULL (then topk_idx and gates may be, too): no gradient by the gates; dlosses [2] fp32, the gradients by the two losses, or
+ * NULL (then counts may be, too): none by them.  Not both.  The counts may have been added up over several calls, and the gradient is then that of the loss
+ * of all their tokens (n of 0 counts as 1).  dlogits [T][E] fp32, written in full: zeros for a token whose mask is 0, of which no value
+ * counts.  An index outside 0 .. E - 1 is no choice.  dlogits may share no memory with what is read. */
+int monta_route_backward(const monta_cfg *cfg, const float *logits, const int32_t *topk_idx, const float *gates, const float *dgates,
+                         const uint8_t *token_mask, const float *dlosses, const int32_t *counts, float *dlogits, void *stream);
+
+/* Host only: bytes of the scratch buffer of monta_gate_backward. */
+int monta_gate_backward_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
+
+/* Gradient of monta_gate:
+ *   dx[t][h] = sum_e dlogits[t][e] * w_gate[e][h] + dadd[t][h], rounded once to cfg->dtype;
+ *   dw_gate[e][h] = sum_t dlogits[t][e] * x[t][h], fp32.
+ * dadd: the gradient that reaches x by another way (through the dispatch), or NULL.  dlogits [T][E] fp32; x, dadd, dx [T][H] and w_gate [E][H] in
+ * cfg->dtype, dw_gate [E][H] fp32, all but dlogits 16-byte aligned.  Either of dx and dw_gate may be NULL (then w_gate and dadd, or x and scratch, may be, too).
+ * scratch 16-byte aligned, its contents are of no use afterwards and calls that overlap in time need one each.  dx may be dadd itself; otherwise nothing
+ * that is written may share memory with anything else.  All sums are fp32, and their order is fixed for a shape.  hidden at most 2^20.
+ * Uses tokens, hidden, dtype and experts of cfg (all of it is validated); needs no workspace. */
+int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *x, const void *w_gate, const void *dadd, void *dx, float *dw_gate,
+                        void *scratch, void *stream);
 
 /* Gradient of monta_expert_linear over all kept rows:
  *   dx_final[r][h] = sum_n dy[r][n] * w_exp[e][n][h]  for every kept row r of expert e,
@@ -455,7 +520,14 @@ enum monta_kernel_id {
     MONTA_K_EXPERT_SCALED = 22, /* expert layer on 8-bit rows and weights     */
     MONTA_K_EXPERT_BACKWARD = 23, /* gradients of the expert layer            */
     MONTA_K_COMBINE_BACKWARD = 24, /* gradients of the combine                */
-    MONTA_K_COUNT = 25
+    MONTA_K_LAYERNORM = 25,     /* layer norm                                 */
+    MONTA_K_LAYERNORM_BACKWARD = 26, /* its gradient by the input             */
+    MONTA_K_LAYERNORM_DPARAMS = 27, /* the weight's and the bias's partial sums added */
+    MONTA_K_ROUTE_LOSS = 28,    /* the router's losses                        */
+    MONTA_K_ROUTE_BACKWARD = 29, /* gradient by the router's logits           */
+    MONTA_K_GATE_BACKWARD = 30, /* gradients of the gate projection           */
+    MONTA_K_GATE_DWEIGHT = 31,  /* its weight's partial sums added            */
+    MONTA_K_COUNT = 32
 };
 int monta_profile_enable(int on);
 int monta_profile_reset(void);

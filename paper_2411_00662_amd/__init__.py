@@ -11,7 +11,9 @@ from .binding import (BF16, FP32, MontaError, make_cfg, monta_cfg, monta_ws_layo
                       monta_copy, monta_profile_enable, monta_profile_reset, monta_profile_read, monta_strerror,
                       monta_last_hip_error, monta_shutdown, monta_route_dispatch_combine_static, make_plan_in, monta_plan_chunk_times, monta_plan_strategy, monta_plan_in,
                       monta_plan_out, monta_curve, monta_fp8_rows, monta_rmsnorm, monta_rmsnorm_scratch_bytes, monta_rmsnorm_backward, monta_combine_backward,
-                      monta_expert_linear_fp8, monta_expert_linear_backward, KERNEL_NAMES, EXPORTS, LIB_PATH)
+                      monta_expert_linear_fp8, monta_expert_linear_backward, monta_layernorm, monta_layernorm_scratch_bytes, monta_layernorm_backward,
+                      monta_route_loss_scratch_bytes, monta_route_loss, monta_route_backward, monta_gate_backward_scratch_bytes, monta_gate_backward,
+                      KERNEL_NAMES, EXPORTS, LIB_PATH)
 from .buffers import Buffers, alloc_buffers, read_tables
 
 __all__ = [n for n in dir() if not n.startswith("_")]

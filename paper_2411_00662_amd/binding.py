@@ -25,7 +25,8 @@ FP32, BF16 = 0, 1
  K_UNREGATHER_COMBINE, K_ALLGATHER, K_GATE, K_EXPERT) = range(13)
 KERNEL_NAMES = ["route_plan", "positions", "pack", "regather", "pack_regather", "combine", "copy", "plan_pack",
                 "unregather", "unregather_combine", "allgather", "gate", "expert", "allgather_regather", "place", "plan_place", "return",
-                "block_scan", "small_step", "norm", "norm_backward", "norm_dweight", "expert_scaled", "expert_backward", "combine_backward"]
+                "block_scan", "small_step", "norm", "norm_backward", "norm_dweight", "expert_scaled", "expert_backward", "combine_backward",
+                "layernorm", "layernorm_backward", "layernorm_dparams", "route_loss", "route_backward", "gate_backward", "gate_dweight"]
 
 
 class MontaError(RuntimeError):
@@ -81,7 +82,9 @@ EXPORTS = ["monta_workspace_bytes", "monta_ws_layout_query", "monta_ws_init", "m
            "monta_profile_read", "monta_plan_chunk_times", "monta_plan_strategy", "monta_strerror",
            "monta_last_hip_error", "monta_shutdown", "monta_route_dispatch_combine_static", "monta_pipeline_query", "monta_allgather_regather",
            "monta_fp8_rows", "monta_rmsnorm", "monta_rmsnorm_scratch_bytes", "monta_rmsnorm_backward", "monta_combine_backward",
-           "monta_expert_linear_fp8", "monta_expert_linear_backward"]
+           "monta_expert_linear_fp8", "monta_expert_linear_backward",
+           "monta_layernorm", "monta_layernorm_scratch_bytes", "monta_layernorm_backward", "monta_route_loss_scratch_bytes", "monta_route_loss",
+           "monta_route_backward", "monta_gate_backward_scratch_bytes", "monta_gate_backward"]
 
 _lib = None
 
@@ -137,6 +140,14 @@ def lib() -> ctypes.CDLL:
         L.monta_combine_backward.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp]
         L.monta_expert_linear_fp8.argtypes = [cfgp, vp, vp, vp, i32, vp, vp, i32, vp]
         L.monta_expert_linear_backward.argtypes = [cfgp, vp, vp, vp, i32, vp, vp, vp, vp]
+        L.monta_layernorm.argtypes = [cfgp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp]
+        L.monta_layernorm_scratch_bytes.argtypes = [cfgp, ctypes.POINTER(ctypes.c_size_t)]
+        L.monta_layernorm_backward.argtypes = [cfgp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp]
+        L.monta_route_loss_scratch_bytes.argtypes = [cfgp, ctypes.POINTER(ctypes.c_size_t)]
+        L.monta_route_loss.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.monta_route_backward.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.monta_gate_backward_scratch_bytes.argtypes = [cfgp, ctypes.POINTER(ctypes.c_size_t)]
+        L.monta_gate_backward.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp]
         for name in EXPORTS:
             if name != "monta_strerror":
                 getattr(L, name).restype = ctypes.c_int
@@ -147,7 +158,8 @@ def lib() -> ctypes.CDLL:
 _HOST_ENTRIES = ["monta_ws_layout_query", "monta_route", "monta_route_dispatch_regather", "monta_route_dispatch_combine_static",
                  "monta_combine", "monta_unregather_combine", "monta_gate", "monta_expert_linear", "monta_route_dispatch_expert",
                  "monta_rmsnorm", "monta_rmsnorm_scratch_bytes", "monta_rmsnorm_backward", "monta_combine_backward", "monta_expert_linear_fp8",
-                 "monta_expert_linear_backward"]
+                 "monta_expert_linear_backward", "monta_layernorm", "monta_layernorm_scratch_bytes", "monta_layernorm_backward",
+                 "monta_route_loss_scratch_bytes", "monta_route_loss", "monta_route_backward", "monta_gate_backward_scratch_bytes", "monta_gate_backward"]
 _native = None
 
 
@@ -419,6 +431,44 @@ def monta_expert_linear_fp8(cfg, x_rows, w_codes, w_scales, out_features: int, y
 
 def monta_expert_linear_backward(cfg, dy, x_final, w_exp, out_features: int, dx_final, dw_exp, ws, stream=None):
     (_native or _host()).expert_linear_backward(cfg, dy, x_final, w_exp, int(out_features), dx_final, dw_exp, ws, stream)
+
+
+def monta_layernorm(cfg, x, residual, weight, bias, eps: float, sum, out, out_fp8=None, stream=None):
+    (_native or _host()).layernorm(cfg, x, residual, weight, bias, eps, sum, out, out_fp8, stream)
+
+
+def _scratch_bytes(name, cfg) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(lib(), name)(ctypes.byref(cfg), ctypes.byref(n)), name)
+    return int(n.value)
+
+
+def monta_layernorm_scratch_bytes(cfg) -> int:
+    return _scratch_bytes("monta_layernorm_scratch_bytes", cfg)
+
+
+def monta_layernorm_backward(cfg, sum, weight, eps: float, dout, dsum, dx, dweight, dbias, scratch, stream=None):
+    (_native or _host()).layernorm_backward(cfg, sum, weight, eps, dout, dsum, dx, dweight, dbias, scratch, stream)
+
+
+def monta_route_loss_scratch_bytes(cfg) -> int:
+    return _scratch_bytes("monta_route_loss_scratch_bytes", cfg)
+
+
+def monta_route_loss(cfg, logits, topk_idx, token_mask, losses, counts, means, scratch, stream=None):
+    (_native or _host()).route_loss(cfg, logits, topk_idx, token_mask, losses, counts, means, scratch, stream)
+
+
+def monta_route_backward(cfg, logits, topk_idx, gates, dgates, token_mask, dlosses, counts, dlogits, stream=None):
+    (_native or _host()).route_backward(cfg, logits, topk_idx, gates, dgates, token_mask, dlosses, counts, dlogits, stream)
+
+
+def monta_gate_backward_scratch_bytes(cfg) -> int:
+    return _scratch_bytes("monta_gate_backward_scratch_bytes", cfg)
+
+
+def monta_gate_backward(cfg, dlogits, x, w_gate, dadd, dx, dw_gate, scratch, stream=None):
+    (_native or _host()).gate_backward(cfg, dlogits, x, w_gate, dadd, dx, dw_gate, scratch, stream)
 
 
 def monta_copy(dst, src, nbytes: int, stream=None):

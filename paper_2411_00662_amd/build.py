@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 _SHARED = ["monta_internal.hpp", "monta_device.hpp"]
 # translation units and the headers of their own
-SOURCES = {"monta.hip": ["monta_kernels.hpp", "monta_planner.hpp"], "monta_norm.hip": [], "monta_expert8.hip": [], "monta_grad.hip": []}
+SOURCES = {"monta.hip": ["monta_kernels.hpp", "monta_planner.hpp"], "monta_norm.hip": ["monta_rows.hpp"], "monta_expert8.hip": [],
+           "monta_grad.hip": [], "monta_layernorm.hip": ["monta_rows.hpp", "monta_lanes.hpp"], "monta_router.hip": ["monta_lanes.hpp"], "monta_gate_grad.hip": []}
 OBJECTS = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmonta.so")
 HOST_SRC = os.path.join(PKG, "csrc", "host.cpp")

@@ -29,6 +29,14 @@ decltype(&monta_rmsnorm_backward) g_rmsnorm_backward;
 decltype(&monta_combine_backward) g_combine_backward;
 decltype(&monta_expert_linear_fp8) g_expert_linear_fp8;
 decltype(&monta_expert_linear_backward) g_expert_linear_backward;
+decltype(&monta_layernorm) g_layernorm;
+decltype(&monta_layernorm_scratch_bytes) g_layernorm_scratch_bytes;
+decltype(&monta_layernorm_backward) g_layernorm_backward;
+decltype(&monta_route_loss_scratch_bytes) g_route_loss_scratch_bytes;
+decltype(&monta_route_loss) g_route_loss;
+decltype(&monta_route_backward) g_route_backward;
+decltype(&monta_gate_backward_scratch_bytes) g_gate_backward_scratch_bytes;
+decltype(&monta_gate_backward) g_gate_backward;
 
 // One call: sizes from its cfg, then its arguments in order.  The first failure leaves a Python error and ends the rest.
 struct Call {
@@ -328,11 +336,87 @@ PyObject *expert_linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     return c.finish([&] { return g_expert_linear_backward(&c.cfg, dy, x, w, out_features, dx, dw, ws, st); });
 }
 
+PyObject *layernorm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_layernorm", a, n, 10, false);
+    if (!c.ok) return nullptr;
+    const Call::Size rows = c.T * c.row, H = c.cfg.hidden;
+    const void *x = c.on_device(a[1], rows, "x"), *residual = c.on_device(a[2], rows, "residual"), *w = c.on_device(a[3], c.row, "weight"),
+               *b = c.on_device(a[4], c.row, "bias");
+    const double eps = c.real(a[5]);
+    void *sum = c.on_device(a[6], rows, "sum"), *out = c.on_device(a[7], rows, "out");
+    void *out8 = c.on_device(a[8], c.T * ((H + 4 * ((H + 127) / 128) + 127) / 128 * 128), "out_fp8"), *st = c.stream(a[9]);
+    return c.finish([&] { return g_layernorm(&c.cfg, x, residual, w, b, (float)eps, sum, out, out8, st); });
+}
+
+PyObject *layernorm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_layernorm_backward", a, n, 11, false);
+    if (!c.ok) return nullptr;
+    const Call::Size rows = c.T * c.row, params = (Call::Size)c.cfg.hidden * 4;
+    size_t scratch_bytes = 0;
+    if (const int rc = g_layernorm_scratch_bytes(&c.cfg, &scratch_bytes)) return Call::check(rc, c.what);
+    const void *sum = c.on_device(a[1], rows, "sum"), *w = c.on_device(a[2], c.row, "weight");
+    const double eps = c.real(a[3]);
+    const void *dout = c.on_device(a[4], rows, "dout"), *dsum = c.on_device(a[5], rows, "dsum");
+    void *dx = c.on_device(a[6], rows, "dx");
+    float *dw = c.on_device<float>(a[7], params, "dweight"), *db = c.on_device<float>(a[8], params, "dbias");
+    void *scratch = c.on_device(a[9], scratch_bytes, "scratch"), *st = c.stream(a[10]);
+    return c.finish([&] { return g_layernorm_backward(&c.cfg, sum, w, (float)eps, dout, dsum, dx, dw, db, scratch, st); });
+}
+
+PyObject *route_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_route_loss", a, n, 9, false);
+    if (!c.ok) return nullptr;
+    size_t scratch_bytes = 0;
+    if (const int rc = g_route_loss_scratch_bytes(&c.cfg, &scratch_bytes)) return Call::check(rc, c.what);
+    const float *logits = c.on_device<float>(a[1], c.T * c.E * 4, "logits");
+    const int32_t *idx = c.on_device<int32_t>(a[2], c.T * c.k * 4, "topk_idx");
+    const uint8_t *mask = c.on_device<uint8_t>(a[3], c.T, "token_mask");
+    float *losses = c.on_device<float>(a[4], 8, "losses");
+    int32_t *counts = c.on_device<int32_t>(a[5], (c.E + 1) * 4, "counts");
+    float *means = c.on_device<float>(a[6], c.E * 4, "means");
+    void *scratch = c.on_device(a[7], scratch_bytes, "scratch"), *st = c.stream(a[8]);
+    return c.finish([&] { return g_route_loss(&c.cfg, logits, idx, mask, losses, counts, means, scratch, st); });
+}
+
+PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_route_backward", a, n, 10, false);
+    if (!c.ok) return nullptr;
+    const Call::Size pairs = c.T * c.k * 4;
+    const float *logits = c.on_device<float>(a[1], c.T * c.E * 4, "logits");
+    const int32_t *idx = c.on_device<int32_t>(a[2], pairs, "topk_idx");
+    const float *gates = c.on_device<float>(a[3], pairs, "gates"), *dgates = c.on_device<float>(a[4], pairs, "dgates");
+    const uint8_t *mask = c.on_device<uint8_t>(a[5], c.T, "token_mask");
+    const float *dlosses = c.on_device<float>(a[6], 8, "dlosses");
+    const int32_t *counts = c.on_device<int32_t>(a[7], (c.E + 1) * 4, "counts");
+    float *dlogits = c.on_device<float>(a[8], c.T * c.E * 4, "dlogits");
+    void *st = c.stream(a[9]);
+    return c.finish([&] { return g_route_backward(&c.cfg, logits, idx, gates, dgates, mask, dlosses, counts, dlogits, st); });
+}
+
+PyObject *gate_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Call c("monta_gate_backward", a, n, 9, false);
+    if (!c.ok) return nullptr;
+    const Call::Size rows = c.T * c.row;
+    size_t scratch_bytes = 0;
+    if (const int rc = g_gate_backward_scratch_bytes(&c.cfg, &scratch_bytes)) return Call::check(rc, c.what);
+    const float *dlogits = c.on_device<float>(a[1], c.T * c.E * 4, "dlogits");
+    const void *x = c.on_device(a[2], rows, "x"), *w = c.on_device(a[3], c.E * c.row, "w_gate"), *dadd = c.on_device(a[4], rows, "dadd");
+    void *dx = c.on_device(a[5], rows, "dx");
+    float *dw = c.on_device<float>(a[6], c.E * (Call::Size)c.cfg.hidden * 4, "dw_gate");
+    void *scratch = c.on_device(a[7], scratch_bytes, "scratch"), *st = c.stream(a[8]);
+    return c.finish([&] { return g_gate_backward(&c.cfg, dlogits, x, w, dadd, dx, dw, scratch, st); });
+}
+
 // setup(cfg class, _ptr, _stream, _current_raw_stream, _check, _current_device, address of each entry point in the order below)
 PyObject *setup(PyObject *, PyObject *args)
 {
     PyObject *cfg, *ptr, *stream, *current, *check, *device, *entries;
-    constexpr int kEntries = 15;
+    constexpr int kEntries = 23;
     unsigned long long f[kEntries];
     if (!PyArg_ParseTuple(args, "OOOOOOO!", &cfg, &ptr, &stream, &current, &check, &device, &PyTuple_Type, &entries)) return nullptr;
     if (PyTuple_GET_SIZE(entries) != kEntries) {
@@ -365,6 +449,14 @@ PyObject *setup(PyObject *, PyObject *args)
     set(g_combine_backward, f[12]);
     set(g_expert_linear_fp8, f[13]);
     set(g_expert_linear_backward, f[14]);
+    set(g_layernorm, f[15]);
+    set(g_layernorm_scratch_bytes, f[16]);
+    set(g_layernorm_backward, f[17]);
+    set(g_route_loss_scratch_bytes, f[18]);
+    set(g_route_loss, f[19]);
+    set(g_route_backward, f[20]);
+    set(g_gate_backward_scratch_bytes, f[21]);
+    set(g_gate_backward, f[22]);
     Py_RETURN_NONE;
 }
 
@@ -373,6 +465,7 @@ PyMethodDef g_methods[] = {
     {"setup", setup, METH_VARARGS, nullptr}, MONTA_FAST(route), MONTA_FAST(route_dispatch_regather), MONTA_FAST(route_dispatch_combine_static),
     MONTA_FAST(combine), MONTA_FAST(unregather_combine), MONTA_FAST(gate), MONTA_FAST(expert_linear), MONTA_FAST(route_dispatch_expert),
     MONTA_FAST(rmsnorm), MONTA_FAST(rmsnorm_backward), MONTA_FAST(combine_backward), MONTA_FAST(expert_linear_fp8), MONTA_FAST(expert_linear_backward),
+    MONTA_FAST(layernorm), MONTA_FAST(layernorm_backward), MONTA_FAST(route_loss), MONTA_FAST(route_backward), MONTA_FAST(gate_backward),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -61,6 +61,9 @@ inline bool overlap(const void *a, int64_t na, const void *b, int64_t nb)
     return pa < pb + (uintptr_t)nb && pb < pa + (uintptr_t)na;
 }
 
+// The same memory, or none of it shared.
+inline bool same_or_apart(const void *a, const void *b, int64_t n) { return a == b || !overlap(a, n, b, n); }
+
 // Does HIP launch that many workgroups?  A dimension has fewer than 2^32 threads; of a greater number it launches the low 32 bits' worth
 // and reports no error.
 inline bool launchable(int64_t workgroups, int threads) { return workgroups < (1ll << 32) / threads; }

@@ -1,0 +1,427 @@
+// The router's losses, and the gradient from the gates and those losses to the logits.
+//
+// A token's E logits belong to L lanes of a wave, the least power of two with 4 L >= E; lane l has experts 4 l to 4 l + 3.  Sums over a token's
+// experts are moves between its lanes.
+#include "monta_internal.hpp"
+#include "monta_lanes.hpp"
+
+#include <algorithm>
+
+namespace monta {
+namespace {
+
+constexpr float kNone = -__builtin_inff();
+
+// Four numbers at p, of which the first `exist` are there; the others are `rest`.
+__device__ __forceinline__ f32x4 load_some(const float *p, int exist, float rest)
+{
+    if (exist >= 4) return *reinterpret_cast<const f32x4_any *>(p);
+    f32x4 v = {rest, rest, rest, rest};
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (i < exist) v[i] = p[i];
+    return v;
+}
+
+__device__ __forceinline__ void store_some(float *p, int exist, f32x4 v)
+{
+    if (exist >= 4) {
+        *reinterpret_cast<f32x4_any *>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (i < exist) p[i] = v[i];
+}
+
+// e^x for x <= 0 (NaN counts as -infinity): x log2(e) in two parts, of which the first has all but 2^-24 of it, 2^(h + l) = 2^h (1 + l ln 2).  One
+// multiplication alone loses |x| / 2 steps of the result.  Below -128 the result is less than the smallest fp32 number.
+__device__ __forceinline__ float exp_neg(float x)
+{
+    constexpr double kLog2e = 1.4426950408889634074;
+    constexpr float kHigh = (float)kLog2e, kLow = (float)(kLog2e - (double)kHigh);
+    x = fmaxf(x, -128.f);
+    const float h = x * kHigh, l = __builtin_fmaf(x, kLow, __builtin_fmaf(x, kHigh, -h)), p = __builtin_amdgcn_exp2f(h);
+    return __builtin_fmaf(p, l * 0.69314718056f, p);
+}
+
+struct Softmax {
+    f32x4 p;       // of the lane's experts; 0 past the last one
+    float lse;     // log of the sum of all exponentials
+};
+
+// of the L lanes' logits; kNone past the last expert
+template <int L>
+__device__ __forceinline__ Softmax softmax(f32x4 v)
+{
+    const float top = group_max<L>(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+    Softmax s;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s.p[i] = exp_neg(v[i] - top);
+        sum += s.p[i];
+    }
+    sum = group_sum<L>(sum);
+    s.lse = top + logf(sum);
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s.p[i] *= inv;
+    return s;
+}
+
+// --------------------------------------------------------------------------------------------- losses
+//
+// Over the n tokens that are no padding:  c[e] = pairs that chose e, f[e] = E c[e] / (k n), P[e] = mean of p[t][e];
+//   balance = sum_e f[e] P[e],   z = mean of lse[t]^2.
+// A workgroup sums a run of tokens; its E + 1 sums and E + 1 counts are a column each of `partial`, one word a workgroup, which
+// route_loss_join_kernel adds, a wave a column.  One workgroup alone finishes by itself.
+
+constexpr int kLossThreads = 512, kLossWaves = kLossThreads / kWave, kLossGrid = 512, kMaxExperts = 256;
+
+struct LossOut {
+    float *losses;
+    int32_t *counts;
+    float *means;
+};
+
+// Sums and counts of all tokens, in LDS (index E: the squares of lse, the tokens), to the results; the first 256 threads of the workgroup, after
+// a barrier.  `part`: four words of LDS.
+__device__ __forceinline__ void finish_losses(const float *sums, const int32_t *cnt, float *part, const LossOut &o, int E, int k)
+{
+    const int e = threadIdx.x;
+    const int n = cnt[E];
+    float f = 0.f;
+    if (e < E) {
+        const float mean = n > 0 ? sums[e] / (float)n : 0.f;
+        f = n > 0 ? (float)cnt[e] * ((float)E / (float)k) / (float)n * mean : 0.f;
+        o.means[e] = mean;
+        o.counts[e] = cnt[e];
+    }
+    f = group_sum<kWave>(f);
+    if (e % kWave == 0 && e < kMaxExperts) part[e / kWave] = f;
+    __syncthreads();
+    if (e == 0) {
+        o.losses[0] = (part[0] + part[1]) + (part[2] + part[3]);
+        o.losses[1] = n > 0 ? sums[E] / (float)n : 0.f;
+        o.counts[E] = n;
+    }
+}
+
+template <int L>
+__global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *logits, const int32_t *idx, const uint8_t *mask, float *partial, LossOut o,
+                                                                  int T, int E, int k, int per)
+{
+    constexpr int kTokens = kLossThreads / L, kAtOnce = 4;          // tokens of a round; rounds whose logits are requested together
+    __shared__ float sums[kLossWaves][kMaxExperts + 1], all[kMaxExperts + 1], part[4];
+    __shared__ int32_t cnt[kMaxExperts + 1];
+    const int tid = threadIdx.x, l = tid % L, exist = E - 4 * l, wave = tid / kWave;
+    for (int i = tid; i <= E; i += kLossThreads) cnt[i] = 0;
+    __syncthreads();
+    const int64_t t0 = (int64_t)blockIdx.x * per, t1 = min(t0 + per, (int64_t)T);
+    {
+        const int64_t p0 = t0 * k, pairs = (t1 - t0) * k;
+        for (int64_t p = tid; p < pairs; p += kLossThreads) {
+            const int e = idx[p0 + p];
+            if ((uint32_t)e < (uint32_t)E && (!mask || mask[t0 + (uint32_t)p / (uint32_t)k])) atomicAdd(&cnt[e], 1);
+        }
+    }
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float z = 0.f;
+    int n = 0;
+    for (int64_t base = t0; base < t1; base += kTokens * kAtOnce) {
+        f32x4 v[kAtOnce];
+        bool live[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int64_t t = base + q * kTokens + tid / L;
+            live[q] = t < t1 && (!mask || mask[t]);
+            v[q] = (f32x4){kNone, kNone, kNone, kNone};
+            if (t < t1 && exist > 0) v[q] = load_some(logits + t * E + 4 * l, exist, kNone);
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            if (base + q * kTokens >= t1) break;                    // all lanes together
+            const Softmax s = softmax<L>(v[q]);
+            if (live[q]) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] += s.p[i];
+                if (l == 0) {
+                    z = __builtin_fmaf(s.lse, s.lse, z);
+                    ++n;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int d = L; d < kWave; d <<= 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], d, kWave);
+        z += __shfl_xor(z, d, kWave);
+        n += __shfl_xor(n, d, kWave);
+    }
+    if (tid % kWave < L)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < exist) sums[wave][4 * l + i] = acc[i];
+    if (tid % kWave == 0) {
+        sums[wave][E] = z;
+        atomicAdd(&cnt[E], n);
+    }
+    __syncthreads();
+    const bool alone = gridDim.x == 1;
+    for (int i = tid; i <= E; i += kLossThreads) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kLossWaves; ++w) v += sums[w][i];
+        if (alone) {
+            all[i] = v;
+        } else {
+            partial[(int64_t)i * gridDim.x + blockIdx.x] = v;
+            reinterpret_cast<int32_t *>(partial)[(int64_t)(E + 1 + i) * gridDim.x + blockIdx.x] = cnt[i];
+        }
+    }
+    if (alone) {
+        __syncthreads();
+        finish_losses(all, cnt, part, o, E, k);
+    }
+}
+
+__global__ __launch_bounds__(1024) void route_loss_join_kernel(const float *partial, LossOut o, int G, int E, int k)
+{
+    __shared__ float all[kMaxExperts + 1], part[4];
+    __shared__ int32_t cnt[kMaxExperts + 1];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    for (int c = wave; c < 2 * (E + 1); c += 1024 / kWave) {
+        float v = 0.f;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kLossGrid / kWave; ++i) {
+            const int at = i * kWave + lane;
+            const float p = at < G ? partial[(int64_t)c * G + at] : 0.f;
+            if (c <= E) v += p;
+            else n += __float_as_int(p);
+        }
+        if (c <= E) {
+            v = group_sum<kWave>(v);
+            if (lane == 0) all[c] = v;
+        } else {
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) n += __shfl_xor(n, d, kWave);
+            if (lane == 0) cnt[c - E - 1] = n;
+        }
+    }
+    __syncthreads();
+    finish_losses(all, cnt, part, o, E, k);
+}
+
+// --------------------------------------------------------------------------------------------- gradient by the logits
+//
+// Gates g_j of the chosen i_j, their gradients d_j, D = sum_j g_j d_j; p the softmax over all experts:
+//   renormalised over the choices:  dl[i_j] += g_j (d_j - D);     otherwise:  dl[i_j] += g_j d_j,  dl[e] -= p[e] D.
+// The losses' part, with their gradients b and c, f and n as above:
+//   dl[e] += p[e] ( b / n (f[e] - sum_i p[i] f[i]) + 2 c / n lse ).
+// A workgroup takes 256 / L tokens.  A thread has a pair: it goes over its token's pairs in LDS for D, and puts what its expert gets (once, by the
+// first of its pairs if an expert is named twice) into the token's row in LDS, which the token's lanes then add to what p asks for.
+
+constexpr int kGradThreads = 256, kRouteGrid = 1 << 20;
+
+struct RouteGradArgs {
+    const float *logits, *gates, *dgates, *dlosses;
+    const int32_t *idx, *counts;
+    const uint8_t *mask;
+    float *dlogits;
+    int32_t T, E, k, renorm;
+    FastDiv by_k;
+};
+
+template <int L, bool SOFTMAX>
+__global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradArgs a)
+{
+    constexpr int kTokens = kGradThreads / L, kPairs = 4 * kGradThreads;        // k <= E <= 4 L
+    __shared__ float row[kTokens][4 * L], dots[kTokens], prod[kPairs], gate[kPairs];
+    __shared__ int32_t expert[kPairs];
+    const int tid = threadIdx.x, l = tid % L, mine = tid / L, exist = a.E - 4 * l, k = a.k;
+    f32x4 f = {0.f, 0.f, 0.f, 0.f};
+    float b = 0.f, c = 0.f;
+    if (SOFTMAX && a.dlosses) {
+        const float n = (float)max(a.counts[a.E], 1);
+        b = a.dlosses[0] / n;
+        c = 2.f * (a.dlosses[1] / n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < exist) f[i] = (float)a.counts[4 * l + i] * ((float)a.E / (float)k) / n;
+    }
+    const int64_t chunks = ((int64_t)a.T + kTokens - 1) / kTokens;
+    for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+        const int64_t t0 = chunk * kTokens, t = t0 + mine;
+        const int tokens = (int)min((int64_t)kTokens, a.T - t0);
+        const bool there = mine < tokens, live = there && (!a.mask || a.mask[t]);
+        f32x4 v = {kNone, kNone, kNone, kNone};
+        if (SOFTMAX && there && exist > 0) v = load_some(a.logits + t * a.E + 4 * l, exist, kNone);
+        *reinterpret_cast<f32x4 *>(&row[mine][4 * l]) = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (l == 0) dots[mine] = 0.f;
+        if (a.dgates) {
+            const int pairs = tokens * k;
+            for (int p = tid; p < pairs; p += kGradThreads) {
+                const int64_t at = t0 * k + p;
+                const int e = a.idx[at];
+                const float g = a.gates[at], d = a.dgates[at];
+                const bool counts = (uint32_t)e < (uint32_t)a.E && (!a.mask || a.mask[t0 + p / a.by_k]);
+                expert[p] = counts ? e : -1;
+                gate[p] = counts ? g : 0.f;
+                prod[p] = counts ? g * d : 0.f;
+            }
+            __syncthreads();
+            for (int p = tid; p < pairs; p += kGradThreads) {
+                const int tok = p / a.by_k, first = tok * k, e = expert[p];
+                float dot = 0.f, sp = 0.f, sg = 0.f;
+                bool owner = e >= 0;
+                for (int i = 0; i < k; ++i) {
+                    const float q = prod[first + i];
+                    dot += q;
+                    if (expert[first + i] == e) {
+                        sp += q;
+                        sg += gate[first + i];
+                        owner = owner && first + i >= p;
+                    }
+                }
+                if (owner) row[tok][e] = a.renorm ? __builtin_fmaf(-sg, dot, sp) : sp;
+                if (p == first) dots[tok] = dot;
+            }
+        }
+        __syncthreads();
+        f32x4 d = *reinterpret_cast<const f32x4 *>(&row[mine][4 * l]);
+        if constexpr (SOFTMAX) {
+            const Softmax s = softmax<L>(v);
+            const float dot = a.renorm ? 0.f : dots[mine];
+            float pf = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pf = __builtin_fmaf(s.p[i], f[i], pf);
+            pf = group_sum<L>(pf);
+            const float every = __builtin_fmaf(c, s.lse, -dot);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = __builtin_fmaf(s.p[i], __builtin_fmaf(b, f[i] - pf, every), d[i]);
+        }
+        if (!live) d = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (there && exist > 0) store_some(a.dlogits + t * a.E + 4 * l, exist, d);
+        __syncthreads();                                           // the next tokens' pairs take the place of these
+    }
+}
+
+// f(lanes of a token)
+template <typename F>
+int with_lanes(int E, F f)
+{
+    using std::integral_constant;
+    if (E <= 4) return f(integral_constant<int, 1>{});
+    if (E <= 8) return f(integral_constant<int, 2>{});
+    if (E <= 16) return f(integral_constant<int, 4>{});
+    if (E <= 32) return f(integral_constant<int, 8>{});
+    if (E <= 64) return f(integral_constant<int, 16>{});
+    if (E <= 128) return f(integral_constant<int, 32>{});
+    return f(integral_constant<int, 64>{});
+}
+
+int lanes_of(int E)
+{
+    return with_lanes(E, [](auto lanes) { return (int)decltype(lanes)::value; });
+}
+
+// workgroups of the losses: whole rounds of tokens each
+int loss_grid(const Shape &s, int *per)
+{
+    const int64_t round = kLossThreads / lanes_of(s.E), rounds = (s.T + round - 1) / round;
+    const int64_t each = (rounds + kLossGrid - 1) / kLossGrid;
+    *per = (int)std::min<int64_t>(each * round, 0x7fffffff);
+    return (int)((rounds + each - 1) / each);
+}
+
+}  // namespace
+}  // namespace monta
+
+using namespace monta;
+
+extern "C" {
+
+int monta_route_loss_scratch_bytes(const monta_cfg *cfg, size_t *bytes)
+{
+    if (!bytes) return MONTA_ERR_NULL;
+    Call c;
+    if (int rc = open_call(cfg, nullptr, &c)) return rc;
+    int per;
+    *bytes = (size_t)loss_grid(c.s, &per) * 2 * (c.s.E + 1) * 4;
+    return MONTA_OK;
+}
+
+int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask, float *losses, int32_t *counts,
+                     float *means, void *scratch, void *stream)
+{
+    Call c;
+    if (int rc = open_call(cfg, nullptr, &c)) return rc;
+    if (!logits || !topk_idx || !losses || !counts || !means || !scratch) return MONTA_ERR_NULL;
+    if (misaligned(logits, 4) || misaligned(topk_idx, 4) || misaligned(losses, 4) || misaligned(counts, 4) || misaligned(means, 4) || misaligned(scratch, 16))
+        return MONTA_ERR_ALIGN;
+    int per;
+    const int grid = loss_grid(c.s, &per);
+    const int64_t T = c.s.T, E = c.s.E;
+    const struct {
+        const void *p;
+        int64_t n;
+    } read[] = {{logits, T * E * 4}, {topk_idx, T * c.s.k * 4}, {token_mask, T}},
+      written[] = {{losses, 8}, {counts, (E + 1) * 4}, {means, E * 4}, {scratch, (int64_t)grid * 2 * (E + 1) * 4}};
+    for (const auto &w : written) {
+        for (const auto &r : read)
+            if (r.p && overlap(w.p, w.n, r.p, r.n)) return MONTA_ERR_INVALID;
+        for (const auto &o : written)
+            if (&o != &w && overlap(w.p, w.n, o.p, o.n)) return MONTA_ERR_INVALID;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    float *partial = static_cast<float *>(scratch);
+    const LossOut o = {losses, counts, means};
+    LaunchTimer timer(MONTA_K_ROUTE_LOSS, st);
+    with_lanes(c.s.E, [&](auto lanes) {
+        hipLaunchKernelGGL((route_loss_kernel<decltype(lanes)::value>), dim3(grid), dim3(kLossThreads), 0, st, logits, topk_idx, token_mask, partial, o, c.s.T,
+                           c.s.E, c.s.k, per);
+        return MONTA_OK;
+    });
+    MONTA_HIP_TRY(hipGetLastError());
+    if (grid > 1) {
+        hipLaunchKernelGGL(route_loss_join_kernel, dim3(1), dim3(1024), 0, st, partial, o, grid, c.s.E, c.s.k);
+        MONTA_HIP_TRY(hipGetLastError());
+    }
+    return MONTA_OK;
+}
+
+int monta_route_backward(const monta_cfg *cfg, const float *logits, const int32_t *topk_idx, const float *gates, const float *dgates,
+                         const uint8_t *token_mask, const float *dlosses, const int32_t *counts, float *dlogits, void *stream)
+{
+    Call c;
+    if (int rc = open_call(cfg, nullptr, &c)) return rc;
+    if (!logits || !dlogits || (!dgates && !dlosses) || (dgates && (!topk_idx || !gates)) || (dlosses && !counts)) return MONTA_ERR_NULL;
+    if (misaligned(logits, 4) || misaligned(topk_idx, 4) || misaligned(gates, 4) || misaligned(dgates, 4) || misaligned(dlosses, 4) || misaligned(counts, 4) ||
+        misaligned(dlogits, 4))
+        return MONTA_ERR_ALIGN;
+    const int64_t T = c.s.T, E = c.s.E, pairs = T * c.s.k * 4;
+    const struct {
+        const void *p;
+        int64_t n;
+    } read[] = {{logits, T * E * 4}, {topk_idx, pairs}, {gates, pairs}, {dgates, pairs}, {token_mask, T}, {dlosses, 8}, {counts, (E + 1) * 4}};
+    for (const auto &r : read)
+        if (r.p && overlap(dlogits, T * E * 4, r.p, r.n)) return MONTA_ERR_INVALID;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const RouteGradArgs a = {logits, gates, dgates, dlosses, topk_idx, counts, token_mask, dlogits, c.s.T, c.s.E, c.s.k, c.s.renorm, c.s.by_k};
+    const bool softmax = dlosses || (dgates && !c.s.renorm);
+    LaunchTimer timer(MONTA_K_ROUTE_BACKWARD, st);
+    with_lanes(c.s.E, [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value, kTokens = kGradThreads / L;
+        const int grid = (int)std::min<int64_t>((T + kTokens - 1) / kTokens, kRouteGrid);
+        if (softmax) hipLaunchKernelGGL((route_backward_kernel<L, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
+        else hipLaunchKernelGGL((route_backward_kernel<L, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
+        return MONTA_OK;
+    });
+    MONTA_HIP_TRY(hipGetLastError());
+    return MONTA_OK;
+}
+
+}  // extern "C"

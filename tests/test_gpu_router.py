@@ -1,0 +1,315 @@
+"""GPU parity of the router's losses and of the gradient by its logits, against 64 bits.
+
+Bars, with u = 2^-24 and X the largest difference between a token's logits and their maximum:
+  - an exponential is off by X u (the rounding of the difference) and 4 u; a token's sum has at most 4 + 6 additions of such; p by X + 24 u;
+    lse by (X + 24) u and the rounding of its own sum, |lse| u;
+  - a sum over tokens has chains of at most tokens / 4096 (512 workgroups, at least 8 tokens a round) + 4, joined over 6 moves, 8 waves and 14 more;
+  - sums over a token's k choices or E experts: k + 12 additions.
+"""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def m():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2411_00662_amd as mod
+    mod.binding.lib()
+    return mod
+
+
+def make(m, T, E, k, renorm=1):
+    return m.make_cfg(T, 64, m.BF16, E, k, 1, 1, 1, 0.0, renorm)
+
+
+def inputs(T, E, k, seed, renorm=1, padding=0.0, scale=1.5):
+    """logits, the library's kind of choices and gates, gradients, mask."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    logits = torch.randn((T, E), generator=g, device="cuda") * scale
+    idx = torch.sort(logits, dim=1, descending=True, stable=True).indices[:, :k].to(torch.int32).contiguous()
+    won = torch.gather(logits.double(), 1, idx.long())
+    gates = (torch.softmax(won, 1) if renorm else torch.exp(won - torch.logsumexp(logits.double(), 1, keepdim=True))).float()
+    dgates = torch.randn((T, k), generator=g, device="cuda") * (torch.rand((T, k), generator=g, device="cuda") < 0.8)
+    mask = None
+    if padding:
+        mask = (torch.rand(T, generator=g, device="cuda") >= padding).to(torch.uint8) * 3
+    return logits, idx, gates, dgates, mask
+
+
+def scratch(n):
+    import torch
+    return torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")
+
+
+def run_loss(m, cfg, logits, idx, mask):
+    import torch
+    E = cfg.experts
+    losses, counts, means = torch.full((3,), 7.0, device="cuda"), torch.full((E + 2,), 7, dtype=torch.int32, device="cuda"), torch.full((E + 1,), 7.0, device="cuda")
+    m.monta_route_loss(cfg, logits, idx, mask, losses[:2], counts[:E + 1], means[:E], scratch(m.monta_route_loss_scratch_bytes(cfg)))
+    torch.cuda.synchronize()
+    assert losses[2].item() == 7 and counts[E + 1].item() == 7 and means[E].item() == 7
+    return losses[:2], counts[:E + 1], means[:E]
+
+
+def check_loss(cfg, got, logits, idx, mask):
+    import torch
+    T, E, k = cfg.tokens, cfg.experts, cfg.top_k
+    keep = torch.ones(T, dtype=torch.bool, device="cuda") if mask is None else mask != 0
+    losses, counts, means = got
+    live, n = logits[keep].double(), int(keep.sum())
+    want = torch.bincount(idx[keep].reshape(-1).long(), minlength=E)
+    assert torch.equal(counts[:E].long(), want) and counts[E].item() == n
+    if n == 0:
+        assert bool((losses == 0).all()) and bool((means == 0).all())
+        return
+    p, lse = torch.softmax(live, 1), torch.logsumexp(live, 1)
+    fin = torch.where(torch.isinf(live), live.amax(1, keepdim=True), live)
+    X = (fin.amax(1) - fin.amin(1)).max().item()
+    chain = T / 4096 + 40
+    P = p.sum(0) / n
+    assert bool(((means.double() - P).abs() <= P * (chain + X + 24) * U).all())
+    balance = (want.double() * E / (n * k) * P).sum().item()
+    assert abs(losses[0].item() - balance) <= balance * (chain + X + 24 + 20) * U
+    z = (lse ** 2).mean().item()
+    assert abs(losses[1].item() - z) <= U * ((2 * lse.abs() * (X + 24 + 2 * lse.abs()) + (X + 24) ** 2 * U).mean().item() + z * (chain + 4))
+
+
+# every number of lanes of a token, odd numbers of experts, one workgroup and several, up to two rounds of each
+SIZES = [(1, 1, 1), (1, 2, 1), (7, 3, 3), (256, 4, 2), (513, 4, 4), (1000, 5, 2), (333, 8, 8), (4097, 8, 2), (700, 10, 3), (129, 16, 4), (1025, 17, 6),
+         (64, 32, 32), (2050, 33, 8), (1, 64, 8), (8192, 64, 8), (100, 65, 7), (1500, 128, 8), (3, 129, 1), (1111, 255, 32), (2048, 256, 8), (20000, 6, 2),
+         (300001, 2, 2), (40000, 100, 4)]
+
+
+@pytest.mark.parametrize("padding", [0.0, 0.3])
+@pytest.mark.parametrize("T,E,k", SIZES)
+def test_loss(m, T, E, k, padding):
+    import torch
+    logits, idx, _, _, mask = inputs(T, E, k, T + E, padding=padding)
+    if mask is not None:
+        logits[mask == 0] = float("nan")               # padding holds anything
+        idx[mask == 0] = 1 << 30
+    cfg = make(m, T, E, k)
+    got = run_loss(m, cfg, logits, idx, mask)
+    check_loss(cfg, got, logits, idx, mask)
+    again = run_loss(m, cfg, logits, idx, mask)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    if mask is None:                                   # bytes that are not 0 are all alike
+        same = run_loss(m, cfg, logits, idx, torch.arange(T, device="cuda").remainder(255).to(torch.uint8) + 1)
+        assert all(torch.equal(a, b) for a, b in zip(got, same))
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 4, 2), (300, 8, 2), (5000, 64, 8)])
+def test_loss_edges(m, T, E, k):
+    """Nothing but padding; one token that counts; experts that no logit allows; large logits; indexes out of range; addresses of 4 bytes."""
+    import torch
+    logits, idx, _, _, _ = inputs(T, E, k, 5)
+    cfg = make(m, T, E, k)
+    none = torch.zeros(T, dtype=torch.uint8, device="cuda")
+    check_loss(cfg, run_loss(m, cfg, logits, idx, none), logits, idx, none)
+    one = none.clone()
+    one[T - 1] = 1
+    check_loss(cfg, run_loss(m, cfg, logits, idx, one), logits, idx, one)
+    closed = logits.clone()
+    closed[:, 1::2] = float("-inf")
+    check_loss(cfg, run_loss(m, cfg, closed, idx, None), closed, idx, None)
+    nan = torch.where(torch.isinf(closed), float("nan"), closed)
+    assert all(torch.equal(a, b) for a, b in zip(run_loss(m, cfg, nan, idx, None), run_loss(m, cfg, closed, idx, None)))
+    big = logits * 1e4
+    check_loss(cfg, run_loss(m, cfg, big, idx, None), big, idx, None)
+    wrong = idx.clone()
+    wrong[0, 0], wrong[T - 1, k - 1] = E, -1
+    got, ok = run_loss(m, cfg, logits, wrong, None), run_loss(m, cfg, logits, idx, None)
+    ok[1][idx[0, 0].item()] -= 1
+    ok[1][idx[T - 1, k - 1].item()] -= 1
+    assert torch.equal(got[1], ok[1]) and torch.equal(got[2], ok[2])
+    store = torch.empty(T * E + 1, device="cuda")
+    store[1:] = logits.view(-1)
+    assert all(torch.equal(a, b) for a, b in zip(run_loss(m, cfg, store[1:].view(T, E), idx, None), run_loss(m, cfg, logits, idx, None)))
+
+
+def check_grad(cfg, got, logits, idx, gates, dgates, mask, dlosses, counts):
+    import torch
+    T, E, k = cfg.tokens, cfg.experts, cfg.top_k
+    keep = torch.ones(T, dtype=torch.bool, device="cuda") if mask is None else mask != 0
+    assert bool((got[~keep] == 0).all())
+    x, got = logits[keep].double(), got[keep].double()
+    p, lse = torch.softmax(x, 1), torch.logsumexp(x, 1)[:, None]
+    want, mag = torch.zeros_like(p), torch.zeros_like(p)
+    if dgates is not None:
+        g, d, i = gates[keep].double(), dgates[keep].double(), idx[keep].long()
+        D, absD = (g * d).sum(1, keepdim=True), (g * d).abs().sum(1, keepdim=True)
+        if cfg.renorm:
+            want.scatter_add_(1, i, g * (d - D))
+            mag.scatter_add_(1, i, g * (d.abs() + absD))
+        else:
+            want.scatter_add_(1, i, g * d)
+            mag.scatter_add_(1, i, (g * d).abs())
+            want, mag = want - p * D, mag + p * absD
+    if dlosses is not None:
+        n, (b, c) = max(1, counts[E].item()), dlosses.double().tolist()
+        f = counts[:E].double() * E / (n * k)
+        pf = (p * f).sum(1, keepdim=True)
+        want += p * (b / n * (f - pf) + 2 * c / n * lse)
+        mag += p * (abs(b) / n * (f + pf) + 2 * abs(c) / n * lse.abs().clamp_min(1))
+    fin = torch.where(torch.isinf(x), x.amax(1, keepdim=True), x)
+    X = (fin.amax(1, keepdim=True) - fin.amin(1, keepdim=True))
+    # a probability below the smallest normal number may be 0
+    assert bool(((got - want).abs() <= mag * (X + 48 + 2 * k) * U + 2.0 ** -120).all())
+
+
+def run_grad(m, cfg, logits, idx, gates, dgates, mask, dlosses, counts):
+    import torch
+    T, E = cfg.tokens, cfg.experts
+    out = torch.full((T * E + 3,), 7.0, device="cuda")
+    m.monta_route_backward(cfg, logits, idx, gates, dgates, mask, dlosses, counts, out[:T * E].view(T, E))
+    torch.cuda.synchronize()
+    assert bool((out[T * E:] == 7).all())
+    return out[:T * E].view(T, E)
+
+
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("padding", [0.0, 0.3])
+@pytest.mark.parametrize("T,E,k", SIZES)
+def test_grad(m, T, E, k, padding, renorm):
+    import torch
+    logits, idx, gates, dgates, mask = inputs(T, E, k, 2 * T + E, renorm, padding)
+    cfg = make(m, T, E, k, renorm)
+    counts = run_loss(m, cfg, logits, idx, mask)[1]
+    if mask is not None:
+        for t in (logits, gates, dgates):
+            t[mask == 0] = float("nan")
+        idx[mask == 0] = -5
+    dlosses = torch.tensor([0.7, -0.3], device="cuda") * T
+    for d, dl in ((dgates, dlosses), (dgates, None), (None, dlosses)):
+        got = run_grad(m, cfg, logits, idx if d is not None else None, gates if d is not None else None, d, mask, dl, counts if dl is not None else None)
+        check_grad(cfg, got, logits, idx, gates, d, mask, dl, counts)
+
+
+@pytest.mark.parametrize("renorm", [0, 1])
+def test_grad_edges(m, renorm):
+    """An expert named twice, indexes out of range, experts that no logit allows, counts of nothing, counts of several calls."""
+    import torch
+    T, E, k = 777, 12, 5
+    logits, idx, gates, dgates, _ = inputs(T, E, k, 9, renorm)
+    cfg = make(m, T, E, k, renorm)
+    counts = run_loss(m, cfg, logits, idx, None)[1]
+    dl = torch.tensor([3.0, 2.0], device="cuda")
+    twice = idx.clone()
+    twice[::2, 1], twice[::3, 4], twice[::3, 2] = idx[::2, 0], idx[::3, 0], idx[::3, 0]
+    check_grad(cfg, run_grad(m, cfg, logits, twice, gates, dgates, None, dl, counts), logits, twice, gates, dgates, None, dl, counts)
+    wrong, g0 = idx.clone(), gates.clone()
+    wrong[5, 2], wrong[6, 0], g0[5, 2], g0[6, 0] = E, -2147483648, 0, 0
+    check_grad(cfg, run_grad(m, cfg, logits, wrong, gates, dgates, None, dl, counts), logits, idx, g0, dgates, None, dl, counts)
+    closed = logits.clone()
+    closed[:, 3] = float("-inf")
+    closed[:, 7] = float("nan")
+    none = closed.clone()
+    none[:, 7] = float("-inf")
+    got = run_grad(m, cfg, closed, idx, gates, None, None, dl, counts)
+    check_grad(cfg, got, none, idx, gates, None, None, dl, counts)
+    assert bool((got[:, [3, 7]] == 0).all())
+    empty = torch.zeros_like(counts)
+    check_grad(cfg, run_grad(m, cfg, logits, idx, gates, dgates, None, dl, empty), logits, idx, gates, dgates, None, dl, empty)
+    # counts of two batches: the gradient of the loss over both
+    more, midx, mgates, _, _ = inputs(300, E, k, 10, renorm)
+    both = counts + run_loss(m, make(m, 300, E, k, renorm), more, midx, None)[1]
+    whole = make(m, T + 300, E, k, renorm)
+    cat = [torch.cat(p) for p in ((logits, more), (idx, midx), (gates, mgates))]
+    assert torch.equal(run_loss(m, whole, cat[0], cat[1], None)[1], both)
+    one = run_grad(m, whole, cat[0], None, None, None, None, dl, both)
+    parts = [run_grad(m, make(m, p.shape[0], E, k, renorm), p, None, None, None, None, dl, both) for p in (logits, more)]
+    assert torch.equal(one, torch.cat(parts))
+
+
+def test_grad_of_what_routing_wrote(m):
+    """Choices and gates of monta_route itself: the losses and their gradient against those differentiated in 64 bits, and against differences."""
+    import torch
+    for renorm in (0, 1):
+        T, E, k = 40, 9, 3
+        cfg = make(m, T, E, k, renorm)
+        b = m.alloc_buffers(cfg, np.random.default_rng(3).normal(size=(T, E)).astype(np.float32))
+        m.monta_route(cfg, b.logits, b.topk_idx, b.gates, b.ws)
+        dgates = torch.randn((T, k), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+        losses, counts, means = run_loss(m, cfg, b.logits, b.topk_idx, None)
+        dl = torch.tensor([2.0, 0.5], device="cuda")
+        got = run_grad(m, cfg, b.logits, b.topk_idx, b.gates, dgates, None, dl, counts)
+
+        def whole(x):
+            p = torch.softmax(x, 1)
+            won = torch.gather(x if renorm else torch.log(p), 1, b.topk_idx.long())
+            g = torch.softmax(won, 1) if renorm else torch.exp(won)
+            f = counts[:E].double() * E / (T * k)
+            return (g * dgates.double()).sum() + 2.0 * (f * p.mean(0)).sum() + 0.5 * (torch.logsumexp(x, 1) ** 2).mean()
+
+        x = b.logits.double().requires_grad_()
+        want, = torch.autograd.grad(whole(x), x)
+        # gates are rounded once (u), then as in check_grad: terms of at most 2 (gates up to 1, gradients up to 4) each
+        assert bool(((got.double() - want).abs() <= 8 * 100 * U).all())
+        for t, e in ((0, 0), (11, 5), (39, 8)):
+            step = torch.zeros_like(x)
+            step[t, e] = 1e-4
+            with torch.no_grad():
+                diff = (whole(x + step) - whole(x - step)) / 2e-4
+            assert abs(diff.item() - got[t, e].item()) <= 1e-4                # third derivatives below 100, times step^2 / 6; rounding of the sum
+
+def test_graph_and_streams(m):
+    """Captured and replayed with eager work between the replays; two calls at once on streams of their own; rows beyond 2^31 bytes."""
+    import torch
+    T, E, k = 6000, 24, 4
+    cfg = make(m, T, E, k)
+    logits, idx, gates, dgates, mask = inputs(T, E, k, 21, padding=0.2)
+    dl = torch.tensor([1.0, 0.1], device="cuda")
+    bufs = [(torch.empty(2, device="cuda"), torch.empty(E + 1, dtype=torch.int32, device="cuda"), torch.empty(E, device="cuda"), torch.empty((T, E), device="cuda"),
+             scratch(m.monta_route_loss_scratch_bytes(cfg))) for _ in range(3)]
+
+    def step(to):
+        m.monta_route_loss(cfg, logits, idx, mask, *to[:3], to[4])
+        m.monta_route_backward(cfg, logits, idx, gates, dgates, mask, dl, to[1], to[3])
+
+    step(bufs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(bufs[1])
+    for seed in (22, 23, 24):
+        for old, new in zip((logits, idx, gates, dgates, mask), inputs(T, E, k, seed, padding=0.2)):
+            old.copy_(new)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        step(bufs[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(bufs[0][:4], bufs[1][:4]))
+        for t in bufs[0][:4] + bufs[1][:4]:
+            t.zero_()
+    del graph
+    step(bufs[0])
+    side = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, to in zip(side, bufs[1:]):
+            with torch.cuda.stream(s):
+                step(to)
+    torch.cuda.synchronize()
+    for to in bufs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(bufs[0][:4], to[:4]))
+    T, E, k = (1 << 21) + 77, 256, 2                   # 2.1 GB of logits, their last row beyond 2^31
+    cfg = make(m, T, E, k)
+    logits = torch.randn((1, E), generator=torch.Generator("cuda").manual_seed(4), device="cuda").expand(T, E).contiguous()
+    logits[0] = 0
+    idx = torch.sort(logits[1], descending=True).indices[:k].to(torch.int32).expand(T, k).contiguous()
+    idx[0] = torch.tensor([0, 1])
+    losses, counts, means = run_loss(m, cfg, logits, idx, None)
+    p = torch.softmax(logits[:2].double(), 1)
+    want = (p[0] + (T - 1) * p[1]) / T
+    assert bool(((means.double() - want).abs() <= want * (T / 4096 + 80) * U).all()) and counts[E].item() == T and counts[:E].sum().item() == k * T
+    got = run_grad(m, cfg, logits, None, None, None, None, torch.tensor([0.0, float(T)], device="cuda"), counts)
+    assert bool((got[1:] == got[1]).all())
+    lse = torch.logsumexp(logits[:2].double(), 1, keepdim=True)
+    assert bool(((got[:2].double() - 2 * lse * p).abs() <= 2 * lse.abs() * p * 80 * U).all())
