@@ -185,6 +185,237 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a, int 
             }
 }
 
+// --------------------------------------------------------------------------------------------- bf16
+//
+// bf16 activations on the bf16 matrix instruction (16 x 16 x 32).  A gradient of a logit is split into bf16 numbers, each the rest of the one before
+// it: with two the products of dx, which is rounded to bf16 (2^-8), are off by 2^-17, with three those of dw, which is fp32, by 2^-26.  A step is 32 tokens; a
+// wave has 16 CT columns of it, a workgroup 64 CT.
+//   dx: rows h, columns t, summed over e.  The wave keeps the weights of its columns in registers.  Row r of tile i is column 32 (i / 2) + 8 (r / 4)
+//       + 4 (i % 2) + r % 4, so that a lane gets 8 neighbours of one token and four lanes 64 bytes.
+//   dw: rows h, columns e, summed over t.  Both operands lie across the summed axis: they are kept in LDS as they come, rows of 32 bytes' segments, and
+//       read by the transposing LDS read, as in the experts' gradients.  A wave's x is its own; the split gradients are the workgroup's, in two
+//       buffers, so that a step has one barrier.
+// Loads and stores go through descriptors that end at the run's last token and lanes past the last column hand in an address past every descriptor: no
+// branch, so that the next step's loads stay outstanding while this step's results are stored.
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int kSplitTokens = 32;
+
+// Segment s of row k sits at s ^ row_swizzle<C>(k) in rows of C elements: the 8 rows (8 g + j, g = 0, 1, j = 0..3) of which half a wave reads a
+// segment each are then in different banks.
+template <int C>
+__device__ __forceinline__ constexpr int row_swizzle(int k)
+{
+    if constexpr (C == 16) return 0;
+    else if constexpr (C == 32) return (k >> 3) & 1;
+    else if constexpr (C == 64) return ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
+    else return (k & 3) | ((k >> 3) & 1) << 2;
+}
+
+[[maybe_unused]] __device__ __forceinline__ bf16x8 read_across(lds_s16x4 *__restrict__ p, int four_rows)
+{
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(reinterpret_cast<__attribute__((address_space(3))) char *>(p) + four_rows));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+template <int EB, int CT>
+struct GateShape {
+    static constexpr int CW = 16 * CT, BC = 4 * CW;                 // columns of a wave, of a workgroup
+    static constexpr int EP = EB == 1 ? 32 : 16 * EB;               // experts, in whole steps of the sum of dx
+    static constexpr int KS = EP / 32;
+    static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece;
+    static constexpr int kRowX = 2 * CW, kX = kSplitTokens * kRowX;
+    static constexpr int kLdsBytes = 2 * kDl + 4 * kX;
+    static constexpr int kItems = kSplitTokens * EP / 8, kItemsEach = (kItems + 255) / 256;      // 8 neighbours of dl
+    static constexpr int kLoadsX = kX / 1024, kPerRowX = CW / 8;
+    static constexpr int kOut = CT >= 2 ? CT / 2 : 1, kOutBytes = CT >= 2 ? 16 : 8;              // pieces of a token's columns in a lane
+};
+
+template <int EB, int CT>
+__global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kernel([[maybe_unused]] GateGradArgs a, [[maybe_unused]] int runs)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    using G = GateShape<EB, CT>;
+    __shared__ __attribute__((aligned(16))) unsigned char lds_dl[2 * G::kDl], lds_x[4 * G::kX];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const GatePart part = gate_part(a, blockIdx.x, runs, G::BC);
+    if (part.run < 0) return;
+    const int col = part.col + wave * G::CW, H = a.H, E = a.E;
+    const uint32_t pitch = (uint32_t)H * 2;
+    const bool whole4 = (E & 3) == 0;
+    auto bytes_of = [&](int rows) { return col < H ? (uint32_t)rows * pitch - (uint32_t)col * 2u : 0u; };      // from the first one's column `col` on
+
+    bf16x8 w[G::KS][CT];
+#pragma unroll
+    for (int ks = 0; ks < G::KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < CT; ++i) {
+            const int h = col + (CT == 1 ? m : 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int e = 32 * ks + 8 * g + j;
+                w[ks][i][j] = a.dx && e < E && h < H ? static_cast<const __bf16 *>(a.w)[(int64_t)e * H + h] : (__bf16)0.f;
+            }
+        }
+    f32x4 sum[EB][CT];
+#pragma unroll
+    for (int j = 0; j < EB; ++j)
+#pragma unroll
+        for (int i = 0; i < CT; ++i) sum[j][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+    // this lane's places in a step: of x, of dadd and dx, of dl
+    uint32_t at_x[G::kLoadsX], at_o[2][G::kOut];
+    int to_x[G::kLoadsX];
+#pragma unroll
+    for (int q = 0; q < G::kLoadsX; ++q) {
+        const int row = (q * 64 + lane) / G::kPerRowX, p = lane % G::kPerRowX;
+        at_x[q] = col + p * 8 < H ? (uint32_t)row * pitch + (uint32_t)p * 16u : kOutOfRange;
+        to_x[q] = row * G::kRowX + ((p >> 1) ^ row_swizzle<G::CW>(row)) * 32 + (p & 1) * 16;
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int q = 0; q < G::kOut; ++q) {
+            const int h = CT == 1 ? 4 * g : 32 * q + 8 * g;
+            at_o[half][q] = col + h < H ? (uint32_t)(16 * half + m) * pitch + (uint32_t)h * 2u : kOutOfRange;
+        }
+
+    u32x4 x[G::kLoadsX], add[2][G::kOut];
+    f32x4 dl[G::kItemsEach][2];
+    auto fetch = [&](int64_t t0) {
+        const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)kSplitTokens, part.t1 - t0));
+        const int64_t first = t0 * H + col;
+        const uint32_t bytes = bytes_of(rows);
+        const auto from_dl = make_rsrc(a.dl + t0 * E, (uint32_t)rows * (uint32_t)E * 4u);
+#pragma unroll
+        for (int n = 0; n < G::kItemsEach; ++n) {
+            const int item = tid + 256 * n, row = item / (G::EP / 8), e0 = item % (G::EP / 8) * 8;
+            const uint32_t at = ((uint32_t)row * (uint32_t)E + (uint32_t)e0) * 4u;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                if (whole4) {
+                    dl[n][v] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from_dl, row < kSplitTokens && e0 + 4 * v < E ? at + 16u * v : kOutOfRange, 0, 0));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        dl[n][v][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+                            from_dl, row < kSplitTokens && e0 + 4 * v + i < E ? at + 16u * v + 4u * i : kOutOfRange, 0, 0));
+                }
+            }
+        }
+        const auto from_x = make_rsrc(static_cast<const __bf16 *>(a.x) + first, a.dw ? bytes : 0u);
+#pragma unroll
+        for (int q = 0; q < G::kLoadsX; ++q) x[q] = __builtin_amdgcn_raw_buffer_load_b128(from_x, at_x[q], 0, 0);
+        const auto from_add = make_rsrc(static_cast<const __bf16 *>(a.dadd) + first, a.dadd ? bytes : 0u);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int q = 0; q < G::kOut; ++q) {
+                if constexpr (CT >= 2) {
+                    add[half][q] = __builtin_amdgcn_raw_buffer_load_b128(from_add, at_o[half][q], 0, 0);
+                } else {
+                    const auto two = __builtin_amdgcn_raw_buffer_load_b64(from_add, at_o[half][q], 0, 0);
+                    add[half][q][0] = two[0];
+                    add[half][q][1] = two[1];
+                }
+            }
+    };
+
+    // this lane's places in LDS: row 8 g + m / 4, quarter m % 4 of a segment, for what is read across; row m, half g % 2 of a segment along
+    unsigned char *const my_x = lds_x + wave * G::kX;
+    const int ka = 8 * g + (m >> 2), across_x = ka * G::kRowX + (m & 3) * 8, across_dl = ka * G::kRow + (m & 3) * 8, along_dl = m * G::kRow + (g & 1) * 16;
+    const int sx = row_swizzle<G::CW>(ka) * 32, sd = row_swizzle<G::EP>(ka) * 32, sl = row_swizzle<G::EP>(m) * 32;
+
+    fetch(part.t0);
+    int buf = 0;
+    for (int64_t t0 = part.t0; t0 < part.t1; t0 += kSplitTokens, buf ^= G::kDl) {
+#pragma unroll
+        for (int n = 0; n < G::kItemsEach; ++n) {
+            const int item = tid + 256 * n, row = item / (G::EP / 8), p = item % (G::EP / 8);
+            if (G::kItems % 256 == 0 || item < G::kItems) {
+                unsigned char *const to = lds_dl + buf + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = dl[n][i / 4][i % 4];
+#pragma unroll
+                for (int piece = 0; piece < 3; ++piece) {
+                    bf16x8 b;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        b[i] = (__bf16)v[i];
+                        v[i] -= (float)b[i];
+                    }
+                    *reinterpret_cast<bf16x8 *>(to + piece * G::kPiece) = b;
+                }
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < G::kLoadsX; ++q) *reinterpret_cast<u32x4 *>(my_x + to_x[q]) = x[q];
+        f32x4 out[2][CT];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int i = 0; i < CT; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const uint32_t word = add[half][i / 2][(CT >= 2 ? i % 2 * 2 : 0) + v / 2];
+                    out[half][i][v] = __uint_as_float(v % 2 ? word & 0xffff0000u : word << 16);
+                }
+        __syncthreads();                                           // of two buffers the other one has been read by all before this
+        if (t0 + kSplitTokens < part.t1) fetch(t0 + kSplitTokens);
+
+        const unsigned char *const dls = lds_dl + buf;
+#pragma unroll
+        for (int ks = 0; ks < G::KS; ++ks)
+#pragma unroll
+            for (int piece = 0; piece < 2; ++piece)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const bf16x8 b = *reinterpret_cast<const bf16x8 *>(dls + piece * G::kPiece + half * 16 * G::kRow + along_dl + (((2 * ks + (g >> 1)) * 32) ^ sl));
+#pragma unroll
+                    for (int i = 0; i < CT; ++i) out[half][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[ks][i], b, out[half][i], 0, 0, 0);
+                }
+        {
+            const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)kSplitTokens, part.t1 - t0));
+            const auto to = make_rsrc(static_cast<__bf16 *>(a.dx) + (t0 * H + col), a.dx ? bytes_of(rows) : 0u);
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int q = 0; q < G::kOut; ++q) {
+                    bf16x8 o;
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) o[v] = (__bf16)(CT >= 2 || v < 4 ? out[half][(CT >= 2 ? 2 * q + v / 4 : 0)][v % 4] : 0.f);
+                    const u32x4 words = __builtin_bit_cast(u32x4, o);
+                    if constexpr (CT >= 2) __builtin_amdgcn_raw_buffer_store_b128(words, to, at_o[half][q], 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b64(__builtin_shufflevector(words, words, 0, 1), to, at_o[half][q], 0, 0);
+                }
+        }
+        bf16x8 fx[CT];
+#pragma unroll
+        for (int i = 0; i < CT; ++i) fx[i] = read_across((lds_s16x4 *)(my_x + across_x + ((i * 32) ^ sx)), 4 * G::kRowX);
+#pragma unroll
+        for (int j = 0; j < EB; ++j)
+#pragma unroll
+            for (int piece = 0; piece < 3; ++piece) {
+                const bf16x8 b = read_across((lds_s16x4 *)(dls + piece * G::kPiece + across_dl + ((j * 32) ^ sd)), 4 * G::kRow);
+#pragma unroll
+                for (int i = 0; i < CT; ++i) sum[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], b, sum[j][i], 0, 0, 0);
+            }
+    }
+    if (a.dw)
+#pragma unroll
+        for (int j = 0; j < EB; ++j)
+#pragma unroll
+            for (int i = 0; i < CT; ++i) {
+                const int e = 16 * j + m, h = col + 16 * i + 4 * g;
+                if (e < E && h < H) *reinterpret_cast<f32x4 *>(a.dw + ((int64_t)part.run * E + e) * H + h) = sum[j][i];
+            }
+#endif
+}
+
 // Adds the runs' sums, eight loads at a time.
 __global__ __launch_bounds__(256) void gate_dweight_kernel(const f32x4 *partial, f32x4 *dw, int runs, int64_t n)
 {
@@ -215,6 +446,9 @@ int with_expert_blocks(int E, F f)
     return f(integral_constant<int, 16>{});
 }
 
+template <int EB>
+constexpr int split_tiles_of() { return EB <= 4 ? 4 : 2; }
+
 struct GatePlan {
     int width, blocks, per, runs;
 };
@@ -222,11 +456,11 @@ struct GatePlan {
 GatePlan plan_gate_grad(const Call &c)
 {
     GatePlan p;
-    p.width = with_expert_blocks(c.s.E, [](auto eb) { return 4 * 16 * tiles_of<decltype(eb)::value>(); });
+    p.width = with_expert_blocks(c.s.E, [&](auto eb) { return 4 * 16 * (c.bf16 ? split_tiles_of<decltype(eb)::value>() : tiles_of<decltype(eb)::value>()); });
     p.blocks = (c.H + p.width - 1) / p.width;
     const int64_t T = c.s.T, most = std::max<int64_t>(1, 512 / p.blocks), wanted = std::min<int64_t>(most, (T + 63) / 64);
-    const int64_t per = ((T + wanted - 1) / wanted + kStepTokens - 1) / kStepTokens * kStepTokens;
-    p.per = (int)std::min<int64_t>(per, 0x7ffffff0);
+    const int64_t per = ((T + wanted - 1) / wanted + kSplitTokens - 1) / kSplitTokens * kSplitTokens;
+    p.per = (int)std::min<int64_t>(per, 0x7fffffe0);
     p.runs = (int)((T + p.per - 1) / p.per);
     return p;
 }
@@ -285,7 +519,7 @@ int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *
         LaunchTimer timer(MONTA_K_GATE_BACKWARD, st);
         with_expert_blocks(c.s.E, [&](auto eb) {
             constexpr int EB = decltype(eb)::value;
-            if (c.bf16) hipLaunchKernelGGL((gate_backward_kernel<true, EB>), dim3(each * kXcds), dim3(256), 0, st, a, p.runs);
+            if (c.bf16) hipLaunchKernelGGL((gate_backward_bf16_kernel<EB, split_tiles_of<EB>()>), dim3(each * kXcds), dim3(256), 0, st, a, p.runs);
             else hipLaunchKernelGGL((gate_backward_kernel<false, EB>), dim3(each * kXcds), dim3(256), 0, st, a, p.runs);
             return MONTA_OK;
         });
