@@ -193,10 +193,10 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a, int 
 //   dx: rows h, columns t, summed over e.  The wave keeps the weights of its columns in registers.  Row r of tile i is column 32 (i / 2) + 8 (r / 4)
 //       + 4 (i % 2) + r % 4, so that a lane gets 8 neighbours of one token and four lanes 64 bytes.
 //   dw: rows h, columns e, summed over t.  Both operands lie across the summed axis: they are kept in LDS as they come, rows of 32 bytes' segments, and
-//       read by the transposing LDS read, as in the experts' gradients.  A wave's x is its own; the split gradients are the workgroup's, in two
-//       buffers, so that a step has one barrier.
-// Loads and stores go through descriptors that end at the run's last token and lanes past the last column hand in an address past every descriptor: no
-// branch, so that the next step's loads stay outstanding while this step's results are stored.
+//       read by the transposing LDS read, as in the experts' gradients.  A wave's x is its own, straight from memory to LDS in a ring of stages; the
+//       split gradients are the workgroup's, in two buffers, so that a step has one barrier.
+// Loads and stores go through descriptors that end at the run's last token, and lanes past the last column hand in an address past every descriptor: no
+// branch, every step issues the same number of them, also past the end, and the wait for a stage of x counts the younger ones.
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -214,6 +214,7 @@ __device__ __forceinline__ constexpr int row_swizzle(int k)
     else return (k & 3) | ((k >> 3) & 1) << 2;
 }
 
+// __restrict__ here and below: without alias information on an access to LDS the compiler waits for every outstanding load to LDS before it.
 [[maybe_unused]] __device__ __forceinline__ bf16x8 read_across(lds_s16x4 *__restrict__ p, int four_rows)
 {
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
@@ -221,45 +222,42 @@ __device__ __forceinline__ constexpr int row_swizzle(int k)
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-template <int EB, int CT>
+typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+[[maybe_unused]] __device__ __forceinline__ bf16x8 read_along(lds_bf16x8 *__restrict__ p) { return *p; }
+[[maybe_unused]] __device__ __forceinline__ void put(lds_bf16x8 *__restrict__ p, bf16x8 v) { *p = v; }
+
+template <int EB, int CT, int NST>
 struct GateShape {
     static constexpr int CW = 16 * CT, BC = 4 * CW;                 // columns of a wave, of a workgroup
     static constexpr int EP = EB == 1 ? 32 : 16 * EB;               // experts, in whole steps of the sum of dx
     static constexpr int KS = EP / 32;
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece;
     static constexpr int kRowX = 2 * CW, kX = kSplitTokens * kRowX;
-    static constexpr int kLdsBytes = 2 * kDl + 4 * kX;
+    static constexpr int kLdsX = 4 * NST * kX, kLdsBytes = kLdsX + 2 * kDl;
     static constexpr int kItems = kSplitTokens * EP / 8, kItemsEach = (kItems + 255) / 256;      // 8 neighbours of dl
     static constexpr int kLoadsX = kX / 1024, kPerRowX = CW / 8;
-    static constexpr int kOut = CT >= 2 ? CT / 2 : 1, kOutBytes = CT >= 2 ? 16 : 8;              // pieces of a token's columns in a lane
+    static constexpr int kOut = CT >= 2 ? CT / 2 : 1;                                            // pieces of a token's columns in a lane
+    static constexpr int kYounger = (NST - 2) * kLoadsX + 2 * kOut;     // at the least: the stages behind a step's, and its dadd (before the first step) or stores
+    static constexpr int kWait = 0x0070 | (kYounger & 15) | ((kYounger >> 4) << 14);             // vmcnt(kYounger), lgkmcnt(0)
+    static_assert(NST >= 3 && kYounger < 64, "gate gradient: stages");
 };
 
-template <int EB, int CT>
+template <int EB, int CT, int NST>
 __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kernel([[maybe_unused]] GateGradArgs a, [[maybe_unused]] int runs)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using G = GateShape<EB, CT>;
-    __shared__ __attribute__((aligned(16))) unsigned char lds_dl[2 * G::kDl], lds_x[4 * G::kX];
+    using G = GateShape<EB, CT, NST>;
+    extern __shared__ __align__(16) unsigned char gate_lds[];
+    unsigned char *const lds_x = gate_lds, *const lds_dl = gate_lds + G::kLdsX;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
     const GatePart part = gate_part(a, blockIdx.x, runs, G::BC);
     if (part.run < 0) return;
     const int col = part.col + wave * G::CW, H = a.H, E = a.E;
     const uint32_t pitch = (uint32_t)H * 2;
     const bool whole4 = (E & 3) == 0;
-    auto bytes_of = [&](int rows) { return col < H ? (uint32_t)rows * pitch - (uint32_t)col * 2u : 0u; };      // from the first one's column `col` on
+    // what a descriptor may reach of `rows` rows, from the first one's column `col` on: nothing of no rows, and nothing past the last column
+    auto bytes_of = [&](int rows) { return rows > 0 && col < H ? (uint32_t)rows * pitch - (uint32_t)col * 2u : 0u; };
 
-    bf16x8 w[G::KS][CT];
-#pragma unroll
-    for (int ks = 0; ks < G::KS; ++ks)
-#pragma unroll
-        for (int i = 0; i < CT; ++i) {
-            const int h = col + (CT == 1 ? m : 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3));
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int e = 32 * ks + 8 * g + j;
-                w[ks][i][j] = a.dx && e < E && h < H ? static_cast<const __bf16 *>(a.w)[(int64_t)e * H + h] : (__bf16)0.f;
-            }
-        }
     f32x4 sum[EB][CT];
 #pragma unroll
     for (int j = 0; j < EB; ++j)
@@ -268,12 +266,10 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
 
     // this lane's places in a step: of x, of dadd and dx, of dl
     uint32_t at_x[G::kLoadsX], at_o[2][G::kOut];
-    int to_x[G::kLoadsX];
 #pragma unroll
-    for (int q = 0; q < G::kLoadsX; ++q) {
-        const int row = (q * 64 + lane) / G::kPerRowX, p = lane % G::kPerRowX;
+    for (int q = 0; q < G::kLoadsX; ++q) {                         // the place in LDS is fixed by the instruction, so the swizzle is applied here
+        const int row = (q * 64 + lane) / G::kPerRowX, at = lane % G::kPerRowX, p = ((at >> 1) ^ row_swizzle<G::CW>(row)) * 2 + (at & 1);
         at_x[q] = col + p * 8 < H ? (uint32_t)row * pitch + (uint32_t)p * 16u : kOutOfRange;
-        to_x[q] = row * G::kRowX + ((p >> 1) ^ row_swizzle<G::CW>(row)) * 32 + (p & 1) * 16;
     }
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -283,12 +279,18 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
             at_o[half][q] = col + h < H ? (uint32_t)(16 * half + m) * pitch + (uint32_t)h * 2u : kOutOfRange;
         }
 
-    u32x4 x[G::kLoadsX], add[2][G::kOut];
+    unsigned char *const my_x = lds_x + wave * (NST * G::kX);
+    auto rows_at = [&](int64_t t0) { return __builtin_amdgcn_readfirstlane((int)max((int64_t)0, min((int64_t)kSplitTokens, part.t1 - t0))); };
+    auto issue = [&](int64_t t0, int stage) {
+        const int rows = rows_at(t0);
+        const auto from = make_rsrc(static_cast<const __bf16 *>(a.x) + (t0 * H + col), a.dw ? bytes_of(rows) : 0u);
+#pragma unroll
+        for (int q = 0; q < G::kLoadsX; ++q) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(my_x + stage + q * 1024), 16, at_x[q], 0, 0, 0);
+    };
+    u32x4 add[2][G::kOut];
     f32x4 dl[G::kItemsEach][2];
     auto fetch = [&](int64_t t0) {
-        const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)kSplitTokens, part.t1 - t0));
-        const int64_t first = t0 * H + col;
-        const uint32_t bytes = bytes_of(rows);
+        const int rows = rows_at(t0);
         const auto from_dl = make_rsrc(a.dl + t0 * E, (uint32_t)rows * (uint32_t)E * 4u);
 #pragma unroll
         for (int n = 0; n < G::kItemsEach; ++n) {
@@ -306,10 +308,7 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
                 }
             }
         }
-        const auto from_x = make_rsrc(static_cast<const __bf16 *>(a.x) + first, a.dw ? bytes : 0u);
-#pragma unroll
-        for (int q = 0; q < G::kLoadsX; ++q) x[q] = __builtin_amdgcn_raw_buffer_load_b128(from_x, at_x[q], 0, 0);
-        const auto from_add = make_rsrc(static_cast<const __bf16 *>(a.dadd) + first, a.dadd ? bytes : 0u);
+        const auto from_add = make_rsrc(static_cast<const __bf16 *>(a.dadd) + (t0 * H + col), a.dadd ? bytes_of(rows) : 0u);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -325,13 +324,28 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
     };
 
     // this lane's places in LDS: row 8 g + m / 4, quarter m % 4 of a segment, for what is read across; row m, half g % 2 of a segment along
-    unsigned char *const my_x = lds_x + wave * G::kX;
     const int ka = 8 * g + (m >> 2), across_x = ka * G::kRowX + (m & 3) * 8, across_dl = ka * G::kRow + (m & 3) * 8, along_dl = m * G::kRow + (g & 1) * 16;
     const int sx = row_swizzle<G::CW>(ka) * 32, sd = row_swizzle<G::EP>(ka) * 32, sl = row_swizzle<G::EP>(m) * 32;
 
-    fetch(part.t0);
-    int buf = 0;
-    for (int64_t t0 = part.t0; t0 < part.t1; t0 += kSplitTokens, buf ^= G::kDl) {
+#pragma unroll
+    for (int q = 0; q < NST - 1; ++q) {
+        if (q == NST - 2) fetch(part.t0);
+        issue(part.t0 + q * kSplitTokens, q * G::kX);
+    }
+    bf16x8 w[G::KS][CT];
+#pragma unroll
+    for (int ks = 0; ks < G::KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < CT; ++i) {
+            const int h = col + (CT == 1 ? m : 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int e = 32 * ks + 8 * g + j;
+                w[ks][i][j] = a.dx && e < E && h < H ? static_cast<const __bf16 *>(a.w)[(int64_t)e * H + h] : (__bf16)0.f;
+            }
+        }
+    int buf = 0, stage = 0;
+    for (int64_t t0 = part.t0; t0 < part.t1; t0 += kSplitTokens) {
 #pragma unroll
         for (int n = 0; n < G::kItemsEach; ++n) {
             const int item = tid + 256 * n, row = item / (G::EP / 8), p = item % (G::EP / 8);
@@ -348,12 +362,10 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
                         b[i] = (__bf16)v[i];
                         v[i] -= (float)b[i];
                     }
-                    *reinterpret_cast<bf16x8 *>(to + piece * G::kPiece) = b;
+                    put((lds_bf16x8 *)(to + piece * G::kPiece), b);
                 }
             }
         }
-#pragma unroll
-        for (int q = 0; q < G::kLoadsX; ++q) *reinterpret_cast<u32x4 *>(my_x + to_x[q]) = x[q];
         f32x4 out[2][CT];
 #pragma unroll
         for (int half = 0; half < 2; ++half)
@@ -364,23 +376,26 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
                     const uint32_t word = add[half][i / 2][(CT >= 2 ? i % 2 * 2 : 0) + v / 2];
                     out[half][i][v] = __uint_as_float(v % 2 ? word & 0xffff0000u : word << 16);
                 }
-        __syncthreads();                                           // of two buffers the other one has been read by all before this
-        if (t0 + kSplitTokens < part.t1) fetch(t0 + kSplitTokens);
+        __builtin_amdgcn_s_waitcnt(G::kWait);                      // this step's x has landed, this wave's part of dl is written
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();                              // of two buffers of dl the other one has been read by all before this
+        asm volatile("" ::: "memory");
+        fetch(t0 + kSplitTokens);
+        issue(t0 + (NST - 1) * kSplitTokens, stage == 0 ? (NST - 1) * G::kX : stage - G::kX);       // where the step before was
 
-        const unsigned char *const dls = lds_dl + buf;
+        const unsigned char *const dls = lds_dl + buf, *const xs = my_x + stage;
 #pragma unroll
         for (int ks = 0; ks < G::KS; ++ks)
 #pragma unroll
             for (int piece = 0; piece < 2; ++piece)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const bf16x8 b = *reinterpret_cast<const bf16x8 *>(dls + piece * G::kPiece + half * 16 * G::kRow + along_dl + (((2 * ks + (g >> 1)) * 32) ^ sl));
+                    const bf16x8 b = read_along((lds_bf16x8 *)(dls + piece * G::kPiece + half * 16 * G::kRow + along_dl + (((2 * ks + (g >> 1)) * 32) ^ sl)));
 #pragma unroll
                     for (int i = 0; i < CT; ++i) out[half][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[ks][i], b, out[half][i], 0, 0, 0);
                 }
         {
-            const int rows = __builtin_amdgcn_readfirstlane((int)min((int64_t)kSplitTokens, part.t1 - t0));
-            const auto to = make_rsrc(static_cast<__bf16 *>(a.dx) + (t0 * H + col), a.dx ? bytes_of(rows) : 0u);
+            const auto to = make_rsrc(static_cast<__bf16 *>(a.dx) + (t0 * H + col), a.dx ? bytes_of(rows_at(t0)) : 0u);
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -395,7 +410,7 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
         }
         bf16x8 fx[CT];
 #pragma unroll
-        for (int i = 0; i < CT; ++i) fx[i] = read_across((lds_s16x4 *)(my_x + across_x + ((i * 32) ^ sx)), 4 * G::kRowX);
+        for (int i = 0; i < CT; ++i) fx[i] = read_across((lds_s16x4 *)(xs + across_x + ((i * 32) ^ sx)), 4 * G::kRowX);
 #pragma unroll
         for (int j = 0; j < EB; ++j)
 #pragma unroll
@@ -404,7 +419,10 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
 #pragma unroll
                 for (int i = 0; i < CT; ++i) sum[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], b, sum[j][i], 0, 0, 0);
             }
+        buf ^= G::kDl;
+        stage = stage == (NST - 1) * G::kX ? 0 : stage + G::kX;
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);                            // the loads past the end have come back: the LDS is another workgroup's after this
     if (a.dw)
 #pragma unroll
         for (int j = 0; j < EB; ++j)
@@ -416,23 +434,42 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
 #endif
 }
 
-// Adds the runs' sums, eight loads at a time.
+// Adds the runs' sums: a workgroup takes 32 vectors of them, its eight groups of 32 lanes every eighth run each, four loads at a time.
 __global__ __launch_bounds__(256) void gate_dweight_kernel(const f32x4 *partial, f32x4 *dw, int runs, int64_t n)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int r = 0; r < runs; r += 8) {
-            f32x4 p[8];
+    __shared__ f32x4 part[8][32];
+    const int c = threadIdx.x % 32, r = threadIdx.x / 32;
+    const int64_t i = (int64_t)blockIdx.x * 32 + c;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (i < n)
+        for (int q = r; q < runs; q += 4 * 8) {
+            f32x4 p[4];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) p[q] = r + q < runs ? partial[(r + q) * n + i] : (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < 4; ++u) p[u] = q + u * 8 < runs ? partial[(int64_t)(q + u * 8) * n + i] : (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v += p[q];
+            for (int u = 0; u < 4; ++u) v += p[u];
         }
+    part[r][c] = v;
+    __syncthreads();
+    if (r == 0 && i < n) {
+#pragma unroll
+        for (int u = 1; u < 8; ++u) v += part[u][c];
         dw[i] = v;
     }
 }
 
 // --------------------------------------------------------------------------------------------- host
+
+template <int EB, int CT, int NST>
+int launch_split(const GateGradArgs &a, int runs, hipStream_t st)
+{
+    using G = GateShape<EB, CT, NST>;
+    const auto kernel = gate_backward_bf16_kernel<EB, CT, NST>;
+    static LdsOptIn opted;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(kernel), G::kLdsBytes, opted)) return rc;
+    hipLaunchKernelGGL(kernel, dim3(a.each * kXcds), dim3(256), G::kLdsBytes, st, a, runs);
+    return MONTA_OK;
+}
 
 // f(blocks of 16 experts), a power of two
 template <typename F>
@@ -517,18 +554,19 @@ int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *
     const GateGradArgs a = {dlogits, x, w_gate, dadd, dx, dw_gate && p.runs > 1 ? static_cast<float *>(scratch) : dw_gate, T, c.s.E, c.H, p.per, p.blocks, each};
     {
         LaunchTimer timer(MONTA_K_GATE_BACKWARD, st);
-        with_expert_blocks(c.s.E, [&](auto eb) {
+        const int rc = with_expert_blocks(c.s.E, [&](auto eb) {
             constexpr int EB = decltype(eb)::value;
-            if (c.bf16) hipLaunchKernelGGL((gate_backward_bf16_kernel<EB, split_tiles_of<EB>()>), dim3(each * kXcds), dim3(256), 0, st, a, p.runs);
-            else hipLaunchKernelGGL((gate_backward_kernel<false, EB>), dim3(each * kXcds), dim3(256), 0, st, a, p.runs);
-            return MONTA_OK;
+            if (c.bf16) return launch_split<EB, split_tiles_of<EB>(), 3>(a, p.runs, st);
+            hipLaunchKernelGGL((gate_backward_kernel<false, EB>), dim3(each * kXcds), dim3(256), 0, st, a, p.runs);
+            return (int)MONTA_OK;
         });
+        if (rc) return rc;
         MONTA_HIP_TRY(hipGetLastError());
     }
     if (dw_gate && p.runs > 1) {
         LaunchTimer timer(MONTA_K_GATE_DWEIGHT, st);
         const int64_t n4 = E * c.H / 4;
-        hipLaunchKernelGGL(gate_dweight_kernel, dim3((unsigned)std::min<int64_t>((n4 + 255) / 256, 4096)), dim3(256), 0, st, static_cast<const f32x4 *>(scratch),
+        hipLaunchKernelGGL(gate_dweight_kernel, dim3((unsigned)((n4 + 31) / 32)), dim3(256), 0, st, static_cast<const f32x4 *>(scratch),
                            reinterpret_cast<f32x4 *>(dw_gate), p.runs, n4);
         MONTA_HIP_TRY(hipGetLastError());
     }

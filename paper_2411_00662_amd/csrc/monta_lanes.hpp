@@ -10,7 +10,7 @@ namespace monta {
 // 16 and halves.  Each step joins the same two groups as a move across the step's distance would.  No LDS: a step through it waits for about 60
 // clocks, one here for a few.
 template <int L, typename Op>
-__device__ __forceinline__ float group_join(float v, Op op)
+__device__ __forceinline__ float group_join(float v, [[maybe_unused]] Op op)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     auto moved = [](float u, auto ctrl) {
