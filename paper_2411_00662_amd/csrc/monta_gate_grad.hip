@@ -8,33 +8,31 @@
 namespace monta {
 namespace {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 struct GateGradArgs {
     const float *dl;
     const void *x, *w, *dadd;
     void *dx;
-    float *dw;              // sums of each run of tokens, [runs][E][H]; with one run the result
+    float *dw;              // the sums of each share of the tokens, [shares][E][H]; with one share the result
     int64_t T;
-    int32_t E, H, per;      // tokens of a run, a multiple of the step
-    int32_t blocks, each;   // column blocks; workgroups of an XCD
+    int32_t E, H;
+    int32_t blocks, shares;             // column blocks; shares of the tokens
 };
 
-// What workgroup `block` does: the workgroups of an XCD go through the column blocks of a run one after the other, so that its dl is read from
-// memory once and then found in the XCD's L2.
+// What workgroup `block` does: column block `col`, and of the steps of tokens every `shares`-th from the one numbered `share` on (none: share < 0).  All
+// workgroups so move through the rows together, in one window of them for each buffer: with a run of neighbouring steps for each share, 18 windows 50 MB apart,
+// 65536 x 7168 over 8 experts took 373 us, in windows of nine 340, in one RRR.  The workgroups of an XCD go through the column blocks of a share one after the
+// other, so that its dl is read from memory once and then found in the XCD's L2.
 struct GatePart {
-    int64_t t0, t1;
-    int run, col;
+    int share, col;
 };
-__device__ __forceinline__ GatePart gate_part(const GateGradArgs &a, uint32_t block, int runs, int width)
+__device__ __forceinline__ GatePart gate_part(const GateGradArgs &a, uint32_t block, int width)
 {
     GatePart p;
-    const uint32_t n = block % kXcds * (uint32_t)a.each + block / kXcds;
-    p.run = (int)(n / (uint32_t)a.blocks);
-    p.col = (int)(n % (uint32_t)a.blocks) * width;
-    if (p.run >= runs) p.run = -1;
-    p.t0 = (int64_t)p.run * a.per;
-    p.t1 = min(p.t0 + a.per, a.T);
+    p.share = (int)(block / (uint32_t)a.blocks);
+    p.col = (int)(block % (uint32_t)a.blocks) * width;
     return p;
 }
 
@@ -70,13 +68,12 @@ struct Piece {                  // N neighbouring elements of a row
 constexpr int kStepTokens = 16;
 
 template <bool BF16, int EB>
-__global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a, int runs)
+__global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
 {
     constexpr int CT = tiles_of<EB>(), CW = 16 * CT, kPitch = 16 * EB + 4;
     __shared__ float dlt[2][kStepTokens][kPitch];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
-    const GatePart part = gate_part(a, blockIdx.x, runs, 4 * CW);
-    if (part.run < 0) return;
+    const GatePart part = gate_part(a, blockIdx.x, 4 * CW);
     const int64_t H = a.H;
     const int col = part.col + wave * CW;                          // first column of the wave
     const bool want_dx = a.dx != nullptr, want_dw = a.dw != nullptr;
@@ -107,26 +104,27 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a, int 
 #pragma unroll
         for (int q = 0; q < EB; ++q) {
             const int e = (tid & 15) + 16 * q;
-            dl[q] = t < part.t1 && e < a.E ? a.dl[t * a.E + e] : 0.f;
+            dl[q] = t < a.T && e < a.E ? a.dl[t * a.E + e] : 0.f;
         }
         if (want_dw)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int64_t at = t0 + 4 * s + g;
                 x[s].clear();
-                if (at < part.t1 && col + m * CT < a.H) x[s].get(a.x, at * H + col + m * CT);
+                if (at < a.T && col + m * CT < a.H) x[s].get(a.x, at * H + col + m * CT);
             }
         if (want_dx)
 #pragma unroll
             for (int i = 0; i < CT; ++i) {
                 const int h = col + 4 * CT * g + 4 * i;
                 add[i].clear();
-                if (a.dadd && t0 + m < part.t1 && h < a.H) add[i].get(a.dadd, (t0 + m) * H + h);
+                if (a.dadd && t0 + m < a.T && h < a.H) add[i].get(a.dadd, (t0 + m) * H + h);
             }
     };
-    fetch(part.t0);
+    const int64_t first = (int64_t)part.share * kStepTokens, stride = (int64_t)a.shares * kStepTokens;
+    fetch(first);
     int buf = 0;
-    for (int64_t t0 = part.t0; t0 < part.t1; t0 += kStepTokens, buf ^= 1) {
+    for (int64_t t0 = first; t0 < a.T; t0 += stride, buf ^= 1) {
 #pragma unroll
         for (int q = 0; q < EB; ++q) dlt[buf][tid >> 4][(tid & 15) + 16 * q] = dl[q];
         Piece<BF16, CT> x0[4];
@@ -138,7 +136,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a, int 
 #pragma unroll
             for (int v = 0; v < 4; ++v) out[i][v] = add[i][v];
         __syncthreads();                                           // of two buffers the other one has been read by all before this
-        if (t0 + kStepTokens < part.t1) fetch(t0 + kStepTokens);
+        if (t0 + stride < a.T) fetch(t0 + stride);
         if (want_dx) {
 #pragma unroll
             for (int kk = 0; kk < 4 * EB; ++kk) {
@@ -146,7 +144,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a, int 
 #pragma unroll
                 for (int i = 0; i < CT; ++i) out[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i][kk], b, out[i], 0, 0, 0);
             }
-            if (t0 + m < part.t1)
+            if (t0 + m < a.T)
 #pragma unroll
                 for (int i = 0; i < CT; ++i) {
                     const int h = col + 4 * CT * g + 4 * i;
@@ -179,7 +177,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a, int 
             for (int v = 0; v < 4; ++v) {
                 const int e = 16 * j + m, h = col + (4 * g + v) * CT;
                 if (e >= a.E || h >= a.H) continue;
-                float *const to = a.dw + ((int64_t)part.run * a.E + e) * H + h;
+                float *const to = a.dw + ((int64_t)part.share * a.E + e) * H + h;
 #pragma unroll
                 for (int i = 0; i < CT; ++i) to[i] = sum[j][i][v];
             }
@@ -202,14 +200,14 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int kSplitTokens = 32;
+[[maybe_unused]] constexpr int kNt = 2;         // past the cache
 
 // Segment s of row k sits at s ^ row_swizzle<C>(k) in rows of C elements: the 8 rows (8 g + j, g = 0, 1, j = 0..3) of which half a wave reads a
 // segment each are then in different banks.
 template <int C>
 __device__ __forceinline__ constexpr int row_swizzle(int k)
 {
-    if constexpr (C == 16) return 0;
-    else if constexpr (C == 32) return (k >> 3) & 1;
+    if constexpr (C == 32) return (k >> 3) & 1;
     else if constexpr (C == 64) return ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
     else return (k & 3) | ((k >> 3) & 1) << 2;
 }
@@ -223,35 +221,40 @@ __device__ __forceinline__ constexpr int row_swizzle(int k)
 }
 
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 [[maybe_unused]] __device__ __forceinline__ bf16x8 read_along(lds_bf16x8 *__restrict__ p) { return *p; }
-[[maybe_unused]] __device__ __forceinline__ void put(lds_bf16x8 *__restrict__ p, bf16x8 v) { *p = v; }
+[[maybe_unused]] __device__ __forceinline__ void put(lds_u32x4 *__restrict__ p, u32x4 v) { *p = v; }
 
-template <int EB, int CT, int NST>
+template <int EB, int CT, int NW, int NST>
 struct GateShape {
-    static constexpr int CW = 16 * CT, BC = 4 * CW;                 // columns of a wave, of a workgroup
+    static constexpr int kThreads = 64 * NW, CW = 16 * CT, BC = NW * CW;        // columns of a wave, of a workgroup of NW
     static constexpr int EP = EB == 1 ? 32 : 16 * EB;               // experts, in whole steps of the sum of dx
     static constexpr int KS = EP / 32;
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece;
     static constexpr int kRowX = 2 * CW, kX = kSplitTokens * kRowX;
-    static constexpr int kLdsX = 4 * NST * kX, kLdsBytes = kLdsX + 2 * kDl;
-    static constexpr int kItems = kSplitTokens * EP / 8, kItemsEach = (kItems + 255) / 256;      // 8 neighbours of dl
+    static constexpr int kLdsX = NW * NST * kX, kLdsBytes = kLdsX + 2 * kDl;
+    static constexpr int kItems = kSplitTokens * EP / 8, kItemsEach = (kItems + kThreads - 1) / kThreads;      // 8 neighbours of dl
     static constexpr int kLoadsX = kX / 1024, kPerRowX = CW / 8;
-    static constexpr int kOut = CT >= 2 ? CT / 2 : 1;                                            // pieces of a token's columns in a lane
-    static constexpr int kYounger = (NST - 2) * kLoadsX + 2 * kOut;     // at the least: the stages behind a step's, and its dadd (before the first step) or stores
-    static constexpr int kWait = 0x0070 | (kYounger & 15) | ((kYounger >> 4) << 14);             // vmcnt(kYounger), lgkmcnt(0)
+    static constexpr int kOut = CT / 2;                             // pieces of a token's columns in a lane
+    static_assert(CT == 2 || CT == 4, "gate gradient: columns");
+    // accesses that every step issues after a stage's: the stages behind it and, for two steps, dadd and stores.  (dl is waited for by its use, and a wave
+    // without a part in it may skip its loads.)  Before the first step: the stages and dadd.
+    static constexpr int kSurely = (NST - 2) * kLoadsX + 3 * 2 * kOut, kFirst = (NST - 2) * kLoadsX + 2 * kOut;
+    static constexpr int kLate = kFirst + 2 * kItemsEach;           // those that need not have come back: the stages, the stores, dl
+    static constexpr int kYounger = kLate < kSurely ? kLate : kSurely;
+    static constexpr int wait_for(int vmcnt) { return 0x0070 | (vmcnt & 15) | ((vmcnt >> 4) << 14); }      // and lgkmcnt(0)
     static_assert(NST >= 3 && kYounger < 64, "gate gradient: stages");
 };
 
-template <int EB, int CT, int NST>
-__global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kernel([[maybe_unused]] GateGradArgs a, [[maybe_unused]] int runs)
+template <int EB, int CT, int NW, int NST>
+__global__ __launch_bounds__(64 * NW, EB <= 8 ? 2 : 1) void gate_backward_bf16_kernel([[maybe_unused]] GateGradArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using G = GateShape<EB, CT, NST>;
+    using G = GateShape<EB, CT, NW, NST>;
     extern __shared__ __align__(16) unsigned char gate_lds[];
     unsigned char *const lds_x = gate_lds, *const lds_dl = gate_lds + G::kLdsX;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
-    const GatePart part = gate_part(a, blockIdx.x, runs, G::BC);
-    if (part.run < 0) return;
+    const GatePart part = gate_part(a, blockIdx.x, G::BC);
     const int col = part.col + wave * G::CW, H = a.H, E = a.E;
     const uint32_t pitch = (uint32_t)H * 2;
     const bool whole4 = (E & 3) == 0;
@@ -264,7 +267,7 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
 #pragma unroll
         for (int i = 0; i < CT; ++i) sum[j][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
-    // this lane's places in a step: of x, of dadd and dx, of dl
+    // this lane's places in a step: of x and dx, of dadd
     uint32_t at_x[G::kLoadsX], at_o[2][G::kOut];
 #pragma unroll
     for (int q = 0; q < G::kLoadsX; ++q) {                         // the place in LDS is fixed by the instruction, so the swizzle is applied here
@@ -275,26 +278,27 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
     for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int q = 0; q < G::kOut; ++q) {
-            const int h = CT == 1 ? 4 * g : 32 * q + 8 * g;
+            const int h = 32 * q + 8 * g;
             at_o[half][q] = col + h < H ? (uint32_t)(16 * half + m) * pitch + (uint32_t)h * 2u : kOutOfRange;
         }
 
     unsigned char *const my_x = lds_x + wave * (NST * G::kX);
-    auto rows_at = [&](int64_t t0) { return __builtin_amdgcn_readfirstlane((int)max((int64_t)0, min((int64_t)kSplitTokens, part.t1 - t0))); };
+    const int64_t first = (int64_t)part.share * kSplitTokens, stride = (int64_t)a.shares * kSplitTokens;
+    auto rows_at = [&](int64_t t0) { return __builtin_amdgcn_readfirstlane((int)max((int64_t)0, min((int64_t)kSplitTokens, a.T - t0))); };
     auto issue = [&](int64_t t0, int stage) {
         const int rows = rows_at(t0);
         const auto from = make_rsrc(static_cast<const __bf16 *>(a.x) + (t0 * H + col), a.dw ? bytes_of(rows) : 0u);
 #pragma unroll
-        for (int q = 0; q < G::kLoadsX; ++q) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(my_x + stage + q * 1024), 16, at_x[q], 0, 0, 0);
+        for (int q = 0; q < G::kLoadsX; ++q) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(my_x + stage + q * 1024), 16, at_x[q], 0, 0, kNt);
     };
     u32x4 add[2][G::kOut];
     f32x4 dl[G::kItemsEach][2];
-    auto fetch = [&](int64_t t0) {
+    auto fetch_dl = [&](int64_t t0) {
         const int rows = rows_at(t0);
         const auto from_dl = make_rsrc(a.dl + t0 * E, (uint32_t)rows * (uint32_t)E * 4u);
 #pragma unroll
         for (int n = 0; n < G::kItemsEach; ++n) {
-            const int item = tid + 256 * n, row = item / (G::EP / 8), e0 = item % (G::EP / 8) * 8;
+            const int item = tid + G::kThreads * n, row = item / (G::EP / 8), e0 = item % (G::EP / 8) * 8;
             const uint32_t at = ((uint32_t)row * (uint32_t)E + (uint32_t)e0) * 4u;
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
@@ -308,36 +312,60 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
                 }
             }
         }
+    };
+    auto fetch_add = [&](int64_t t0) {
+        const int rows = rows_at(t0);
         const auto from_add = make_rsrc(static_cast<const __bf16 *>(a.dadd) + (t0 * H + col), a.dadd ? bytes_of(rows) : 0u);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int q = 0; q < G::kOut; ++q) {
-                if constexpr (CT >= 2) {
-                    add[half][q] = __builtin_amdgcn_raw_buffer_load_b128(from_add, at_o[half][q], 0, 0);
-                } else {
-                    const auto two = __builtin_amdgcn_raw_buffer_load_b64(from_add, at_o[half][q], 0, 0);
-                    add[half][q][0] = two[0];
-                    add[half][q][1] = two[1];
-                }
-            }
+            for (int q = 0; q < G::kOut; ++q) add[half][q] = __builtin_amdgcn_raw_buffer_load_b128(from_add, at_o[half][q], 0, kNt);
     };
 
     // this lane's places in LDS: row 8 g + m / 4, quarter m % 4 of a segment, for what is read across; row m, half g % 2 of a segment along
     const int ka = 8 * g + (m >> 2), across_x = ka * G::kRowX + (m & 3) * 8, across_dl = ka * G::kRow + (m & 3) * 8, along_dl = m * G::kRow + (g & 1) * 16;
-    const int sx = row_swizzle<G::CW>(ka) * 32, sd = row_swizzle<G::EP>(ka) * 32, sl = row_swizzle<G::EP>(m) * 32;
+    const int sx = row_swizzle<G::CW>(ka) * 32, sd = row_swizzle<G::EP>(ka) * 32, sl = row_swizzle<G::EP>(m) * 32, so = row_swizzle<G::CW>(m) * 32;
 
+    auto split = [&](unsigned char *to_dl) {
+#pragma unroll
+        for (int n = 0; n < G::kItemsEach; ++n) {
+            const int item = tid + G::kThreads * n, row = item / (G::EP / 8), p = item % (G::EP / 8);
+            if (G::kItems % G::kThreads == 0 || item < G::kItems) {
+                unsigned char *const to = to_dl + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = dl[n][i / 4][i % 4];
+#pragma unroll
+                for (int piece = 0; piece < 3; ++piece) {
+                    u32x4 b;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        bf16x2 two;
+                        two[0] = (__bf16)v[2 * i];
+                        two[1] = (__bf16)v[2 * i + 1];
+                        b[i] = __builtin_bit_cast(uint32_t, two);
+                        v[2 * i] -= __uint_as_float(b[i] << 16);
+                        v[2 * i + 1] -= __uint_as_float(b[i] & 0xffff0000u);
+                    }
+                    put((lds_u32x4 *)(to + piece * G::kPiece), b);
+                }
+            }
+        }
+    };
 #pragma unroll
     for (int q = 0; q < NST - 1; ++q) {
-        if (q == NST - 2) fetch(part.t0);
-        issue(part.t0 + q * kSplitTokens, q * G::kX);
+        if (q == NST - 2) {
+            fetch_dl(first);
+            fetch_add(first);
+        }
+        issue(first + q * stride, q * G::kX);
     }
     bf16x8 w[G::KS][CT];
 #pragma unroll
     for (int ks = 0; ks < G::KS; ++ks)
 #pragma unroll
         for (int i = 0; i < CT; ++i) {
-            const int h = col + (CT == 1 ? m : 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3));
+            const int h = col + 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int e = 32 * ks + 8 * g + j;
@@ -345,27 +373,10 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
             }
         }
     int buf = 0, stage = 0;
-    for (int64_t t0 = part.t0; t0 < part.t1; t0 += kSplitTokens) {
-#pragma unroll
-        for (int n = 0; n < G::kItemsEach; ++n) {
-            const int item = tid + 256 * n, row = item / (G::EP / 8), p = item % (G::EP / 8);
-            if (G::kItems % 256 == 0 || item < G::kItems) {
-                unsigned char *const to = lds_dl + buf + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16;
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = dl[n][i / 4][i % 4];
-#pragma unroll
-                for (int piece = 0; piece < 3; ++piece) {
-                    bf16x8 b;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        b[i] = (__bf16)v[i];
-                        v[i] -= (float)b[i];
-                    }
-                    put((lds_bf16x8 *)(to + piece * G::kPiece), b);
-                }
-            }
-        }
+    __builtin_amdgcn_s_waitcnt(G::wait_for(G::kFirst));
+    split(lds_dl);
+    fetch_dl(first + stride);
+    for (int64_t t0 = first; t0 < a.T; t0 += stride) {
         f32x4 out[2][CT];
 #pragma unroll
         for (int half = 0; half < 2; ++half)
@@ -373,17 +384,21 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
             for (int i = 0; i < CT; ++i)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const uint32_t word = add[half][i / 2][(CT >= 2 ? i % 2 * 2 : 0) + v / 2];
+                    const uint32_t word = add[half][i / 2][i % 2 * 2 + v / 2];
                     out[half][i][v] = __uint_as_float(v % 2 ? word & 0xffff0000u : word << 16);
                 }
-        __builtin_amdgcn_s_waitcnt(G::kWait);                      // this step's x has landed, this wave's part of dl is written
+        __builtin_amdgcn_s_waitcnt(G::wait_for(G::kYounger));                      // this step's x has landed, this wave's part of dl is written
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();                              // of two buffers of dl the other one has been read by all before this
         asm volatile("" ::: "memory");
-        fetch(t0 + kSplitTokens);
-        issue(t0 + (NST - 1) * kSplitTokens, stage == 0 ? (NST - 1) * G::kX : stage - G::kX);       // where the step before was
+        fetch_add(t0 + stride);
+        issue(t0 + (NST - 1) * stride, stage == 0 ? (NST - 1) * G::kX : stage - G::kX);       // where the step before was
 
-        const unsigned char *const dls = lds_dl + buf, *const xs = my_x + stage;
+        const unsigned char *const dls = lds_dl + buf;
+        unsigned char *const xs = my_x + stage;
+        bf16x8 fx[CT];
+#pragma unroll
+        for (int i = 0; i < CT; ++i) fx[i] = read_across((lds_s16x4 *)(xs + across_x + ((i * 32) ^ sx)), 4 * G::kRowX);
 #pragma unroll
         for (int ks = 0; ks < G::KS; ++ks)
 #pragma unroll
@@ -394,23 +409,23 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
 #pragma unroll
                     for (int i = 0; i < CT; ++i) out[half][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[ks][i], b, out[half][i], 0, 0, 0);
                 }
+        // dx takes the place of x, in the same layout, and leaves it in whole lines
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int q = 0; q < G::kOut; ++q) {
+                bf16x8 o;
+#pragma unroll
+                for (int v = 0; v < 8; ++v) o[v] = (__bf16)out[half][2 * q + v / 4][v % 4];
+                const int c = 4 * q + g;                           // its piece of the row
+                put((lds_u32x4 *)(xs + (16 * half + m) * G::kRowX + ((c >> 1) * 32 ^ so) + (c & 1) * 16), __builtin_bit_cast(u32x4, o));
+            }
         {
             const auto to = make_rsrc(static_cast<__bf16 *>(a.dx) + (t0 * H + col), a.dx ? bytes_of(rows_at(t0)) : 0u);
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int q = 0; q < G::kOut; ++q) {
-                    bf16x8 o;
-#pragma unroll
-                    for (int v = 0; v < 8; ++v) o[v] = (__bf16)(CT >= 2 || v < 4 ? out[half][(CT >= 2 ? 2 * q + v / 4 : 0)][v % 4] : 0.f);
-                    const u32x4 words = __builtin_bit_cast(u32x4, o);
-                    if constexpr (CT >= 2) __builtin_amdgcn_raw_buffer_store_b128(words, to, at_o[half][q], 0, 0);
-                    else __builtin_amdgcn_raw_buffer_store_b64(__builtin_shufflevector(words, words, 0, 1), to, at_o[half][q], 0, 0);
-                }
+            for (int q = 0; q < G::kLoadsX; ++q)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, read_along((lds_bf16x8 *)(xs + q * 1024 + lane * 16))), to, at_x[q], 0, kNt);
         }
-        bf16x8 fx[CT];
-#pragma unroll
-        for (int i = 0; i < CT; ++i) fx[i] = read_across((lds_s16x4 *)(xs + across_x + ((i * 32) ^ sx)), 4 * G::kRowX);
 #pragma unroll
         for (int j = 0; j < EB; ++j)
 #pragma unroll
@@ -420,6 +435,8 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
                 for (int i = 0; i < CT; ++i) sum[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], b, sum[j][i], 0, 0, 0);
             }
         buf ^= G::kDl;
+        split(lds_dl + buf);                                       // for the next step, among this one's products
+        fetch_dl(t0 + 2 * stride);
         stage = stage == (NST - 1) * G::kX ? 0 : stage + G::kX;
     }
     __builtin_amdgcn_s_waitcnt(0x0070);                            // the loads past the end have come back: the LDS is another workgroup's after this
@@ -429,23 +446,23 @@ __global__ __launch_bounds__(256, EB <= 8 ? 2 : 1) void gate_backward_bf16_kerne
 #pragma unroll
             for (int i = 0; i < CT; ++i) {
                 const int e = 16 * j + m, h = col + 16 * i + 4 * g;
-                if (e < E && h < H) *reinterpret_cast<f32x4 *>(a.dw + ((int64_t)part.run * E + e) * H + h) = sum[j][i];
+                if (e < E && h < H) *reinterpret_cast<f32x4 *>(a.dw + ((int64_t)part.share * E + e) * H + h) = sum[j][i];
             }
 #endif
 }
 
-// Adds the runs' sums: a workgroup takes 32 vectors of them, its eight groups of 32 lanes every eighth run each, four loads at a time.
-__global__ __launch_bounds__(256) void gate_dweight_kernel(const f32x4 *partial, f32x4 *dw, int runs, int64_t n)
+// Adds the shares' sums: a workgroup takes 32 vectors of them, its eight groups of 32 lanes every eighth share each, four loads at a time.
+__global__ __launch_bounds__(256) void gate_dweight_kernel(const f32x4 *partial, f32x4 *dw, int shares, int64_t n)
 {
     __shared__ f32x4 part[8][32];
     const int c = threadIdx.x % 32, r = threadIdx.x / 32;
     const int64_t i = (int64_t)blockIdx.x * 32 + c;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (i < n)
-        for (int q = r; q < runs; q += 4 * 8) {
+        for (int q = r; q < shares; q += 4 * 8) {
             f32x4 p[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) p[u] = q + u * 8 < runs ? partial[(int64_t)(q + u * 8) * n + i] : (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < 4; ++u) p[u] = q + u * 8 < shares ? partial[(int64_t)(q + u * 8) * n + i] : (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int u = 0; u < 4; ++u) v += p[u];
         }
@@ -460,14 +477,14 @@ __global__ __launch_bounds__(256) void gate_dweight_kernel(const f32x4 *partial,
 
 // --------------------------------------------------------------------------------------------- host
 
-template <int EB, int CT, int NST>
-int launch_split(const GateGradArgs &a, int runs, hipStream_t st)
+template <int EB, int CT, int NW, int NST>
+int launch_split(const GateGradArgs &a, hipStream_t st)
 {
-    using G = GateShape<EB, CT, NST>;
-    const auto kernel = gate_backward_bf16_kernel<EB, CT, NST>;
+    using G = GateShape<EB, CT, NW, NST>;
+    const auto kernel = gate_backward_bf16_kernel<EB, CT, NW, NST>;
     static LdsOptIn opted;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(kernel), G::kLdsBytes, opted)) return rc;
-    hipLaunchKernelGGL(kernel, dim3(a.each * kXcds), dim3(256), G::kLdsBytes, st, a, runs);
+    hipLaunchKernelGGL(kernel, dim3(a.blocks * a.shares), dim3(G::kThreads), G::kLdsBytes, st, a);
     return MONTA_OK;
 }
 
@@ -486,19 +503,23 @@ int with_expert_blocks(int E, F f)
 template <int EB>
 constexpr int split_tiles_of() { return EB <= 4 ? 4 : 2; }
 
+// Eight waves share the split gradients, four times more columns are waited for together: from 2^27 elements on, where splitting takes time (33 to 128 experts;
+// us, four waves twice a CU, four waves and eight: 65536 x 7168, 64 experts 368, 407 and 363; 32768 x 4096, 128 experts 198, 223 and 186;
+// 8192 x 7168, 64 experts 85, 79 and 85; 512 x 2048, 64 experts 14, 14 and 20; but 65536 x 7168, 32 experts 363, 325 and 340).
+bool eight_waves(const Call &c, int eb) { return c.bf16 && (eb == 4 || eb == 8) && (int64_t)c.s.T * c.H >= (1 << 27); }
+
 struct GatePlan {
-    int width, blocks, per, runs;
+    int blocks, shares;
 };
 
 GatePlan plan_gate_grad(const Call &c)
 {
+    const int width = with_expert_blocks(c.s.E, [&](auto eb) { constexpr int EB = decltype(eb)::value;
+        return (eight_waves(c, EB) ? 8 : 4) * 16 * (c.bf16 ? split_tiles_of<EB>() : tiles_of<EB>());
+    });
     GatePlan p;
-    p.width = with_expert_blocks(c.s.E, [&](auto eb) { return 4 * 16 * (c.bf16 ? split_tiles_of<decltype(eb)::value>() : tiles_of<decltype(eb)::value>()); });
-    p.blocks = (c.H + p.width - 1) / p.width;
-    const int64_t T = c.s.T, most = std::max<int64_t>(1, 512 / p.blocks), wanted = std::min<int64_t>(most, (T + 63) / 64);
-    const int64_t per = ((T + wanted - 1) / wanted + kSplitTokens - 1) / kSplitTokens * kSplitTokens;
-    p.per = (int)std::min<int64_t>(per, 0x7fffffe0);
-    p.runs = (int)((T + p.per - 1) / p.per);
+    p.blocks = (c.H + width - 1) / width;
+    p.shares = (int)std::min<int64_t>(std::max(1, (c.bf16 ? 256 : 512) / p.blocks), ((int64_t)c.s.T + 63) / 64);
     return p;
 }
 
@@ -518,7 +539,7 @@ int monta_gate_backward_scratch_bytes(const monta_cfg *cfg, size_t *bytes)
     if (int rc = open_call(cfg, nullptr, &c)) return rc;
     if (c.H > kGateMaxHidden) return MONTA_ERR_UNSUPPORTED;
     const GatePlan p = plan_gate_grad(c);
-    *bytes = p.runs > 1 ? (size_t)p.runs * c.s.E * c.H * 4 : 16;
+    *bytes = p.shares > 1 ? (size_t)p.shares * c.s.E * c.H * 4 : 16;
     return MONTA_OK;
 }
 
@@ -534,7 +555,7 @@ int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *
     if (dadd && !dx) return MONTA_ERR_INVALID;
     if (c.H > kGateMaxHidden) return MONTA_ERR_UNSUPPORTED;
     const GatePlan p = plan_gate_grad(c);
-    const int64_t T = c.s.T, E = c.s.E, n = T * c.row_bytes, nw = E * c.H * 4, np = p.runs > 1 ? p.runs * nw : 16;
+    const int64_t T = c.s.T, E = c.s.E, n = T * c.row_bytes, nw = E * c.H * 4, np = p.shares > 1 ? p.shares * nw : 16;
     const struct {
         const void *p;
         int64_t n;
@@ -550,24 +571,25 @@ int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *
             if (&o != &w && o.p && overlap(w.p, w.n, o.p, o.n)) return MONTA_ERR_INVALID;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int each = (p.blocks * p.runs + kXcds - 1) / kXcds;
-    const GateGradArgs a = {dlogits, x, w_gate, dadd, dx, dw_gate && p.runs > 1 ? static_cast<float *>(scratch) : dw_gate, T, c.s.E, c.H, p.per, p.blocks, each};
+    const GateGradArgs a = {dlogits, x, w_gate, dadd, dx, dw_gate && p.shares > 1 ? static_cast<float *>(scratch) : dw_gate, T, c.s.E, c.H, p.blocks, p.shares};
     {
         LaunchTimer timer(MONTA_K_GATE_BACKWARD, st);
         const int rc = with_expert_blocks(c.s.E, [&](auto eb) {
             constexpr int EB = decltype(eb)::value;
-            if (c.bf16) return launch_split<EB, split_tiles_of<EB>(), 3>(a, p.runs, st);
-            hipLaunchKernelGGL((gate_backward_kernel<false, EB>), dim3(each * kXcds), dim3(256), 0, st, a, p.runs);
+            if constexpr (EB == 4 || EB == 8)
+                if (eight_waves(c, EB)) return launch_split<EB, split_tiles_of<EB>(), 8, 3>(a, st);
+            if (c.bf16) return launch_split<EB, split_tiles_of<EB>(), 4, 3>(a, st);
+            hipLaunchKernelGGL((gate_backward_kernel<false, EB>), dim3(p.blocks * p.shares), dim3(256), 0, st, a);
             return (int)MONTA_OK;
         });
         if (rc) return rc;
         MONTA_HIP_TRY(hipGetLastError());
     }
-    if (dw_gate && p.runs > 1) {
+    if (dw_gate && p.shares > 1) {
         LaunchTimer timer(MONTA_K_GATE_DWEIGHT, st);
         const int64_t n4 = E * c.H / 4;
         hipLaunchKernelGGL(gate_dweight_kernel, dim3((unsigned)((n4 + 31) / 32)), dim3(256), 0, st, static_cast<const f32x4 *>(scratch),
-                           reinterpret_cast<f32x4 *>(dw_gate), p.runs, n4);
+                           reinterpret_cast<f32x4 *>(dw_gate), p.shares, n4);
         MONTA_HIP_TRY(hipGetLastError());
     }
     return MONTA_OK;

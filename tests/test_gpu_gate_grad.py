@@ -4,7 +4,7 @@ Bars, with u = 2^-24 and h = eps / 2 of the activation type:
   - dx adds E products and dadd in fp32: (E + 8) u of the terms' magnitudes.  With bf16 activations a gradient of a logit is multiplied as two
     bf16 numbers: v in [2^e, 2^(e+1)) leaves at most half a step, 2^(e-8); that is a bf16 number itself or lies below it, in binades whose half
     step is at most 2^(e-9-8), so the two leave 2^-17 of v.  Rounded once: h.
-  - dw adds a run's products in fp32, then the runs: run + runs additions; three bf16 numbers leave 2^(e-18-8), 2^-26 of v, a
+  - dw adds a share of the products in fp32, every so many steps of 16 or 32 tokens, then the shares: tokens / shares + 64 + shares additions; three bf16 numbers leave 2^(e-18-8), 2^-26 of v, a
     quarter of a u.
 """
 import numpy as np
@@ -52,8 +52,8 @@ def check(m, cfg, dl, x, w, add, dx, dw):  # noqa: F811
     if add is not None:
         want, mag = want + add.double(), mag + add.double().abs()
     assert bool(((dx.double() - want).abs() <= want.abs() * half("bf16" if bf16 else "f32") + mag * ((E + 8) * U + (2.0 ** -17 if bf16 else 0))).all())
-    runs = max(1, m.monta_gate_backward_scratch_bytes(cfg) // (E * H * 4))
-    chain = -(-T // runs) + 64 + runs
+    shares = max(1, m.monta_gate_backward_scratch_bytes(cfg) // (E * H * 4))
+    chain = T // shares + 64 + shares
     assert bool(((dw.double() - d.t() @ a).abs() <= (d.abs().t() @ a.abs()) * chain * U).all())
 
 
@@ -82,6 +82,12 @@ def test_gradients(m, T, H, E, dtype):  # noqa: F811
     both = add.clone()
     m.monta_gate_backward(cfg, dl, x, w, both, both, dw2, scratch(m.monta_gate_backward_scratch_bytes(cfg)))
     assert torch.equal(both, dx)
+
+
+@pytest.mark.parametrize("T,H,E", [(32833, 4104, 40), (16400, 8200, 100)])
+def test_many_elements(m, T, H, E):  # noqa: F811
+    """From 2^27 elements of x on, 33 to 128 experts have a form of their own."""
+    test_gradients(m, T, H, E, "bf16")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -117,8 +123,8 @@ def test_rows_beyond_2gib(m):  # noqa: F811
     mag = dl[0].double().abs() @ w.double().abs() + x[0].double().abs()
     assert bool(((dx[0].double() - want).abs() <= want.abs() * 2.0 ** -8 + mag * (E + 8) * U).all()) and bool((dx == dx[0]).all())
     sums = dl.double().sum(0)[:, None] * x[0].double()
-    runs = max(1, m.monta_gate_backward_scratch_bytes(cfg) // (E * H * 4))
-    assert bool(((dw.double() - sums).abs() <= sums.abs() * (T // runs + 64 + runs) * U).all())
+    shares = max(1, m.monta_gate_backward_scratch_bytes(cfg) // (E * H * 4))
+    assert bool(((dw.double() - sums).abs() <= sums.abs() * (T // shares + 64 + shares) * U).all())
 
 
 def layer(m, dtype, T=600, H=264, E=12, k=3, seed=7):  # noqa: F811
