@@ -17,7 +17,7 @@ __device__ __forceinline__ float wave_share(int vpr, int w)
 {
     int n = 0;
 #pragma unroll
-    for (int q = 0; q < NV; ++q) n += min(max(vpr - q * L - w * kWave, 0), kWave);
+    for (int q = 0; q < NV; ++q) n += min(max(vpr - q * L - w * kWave, 0), L < kWave ? L : kWave);
     return (float)(n * EV);
 }
 
@@ -285,6 +285,57 @@ __global__ __launch_bounds__(1024) void layernorm_dparams_kernel(const float *pa
     }
 }
 
+// --------------------------------------------------------------------------------------------- host
+
+// f(lanes of a row, vectors of a lane): lanes of one wave as far as their registers go, since a row of several waves meets at a barrier, and no more
+// than the row has vectors for.  us, these forms and one vector for each of 64 or 256 lanes: norm of 16384 x 768 bf16 19.1 and 28.7, 16384 x 1024 25.8 and
+// 30.5, 65536 x 256 26.4 and 31.5; its gradient 22.5 and 55.4, 28.2 and 57.3, 28.3 and 44.9.  Beyond 128 vectors the norm has no use for it (8192 x 2048 in
+// one wave 27.1, in four 26.0), its gradient has (32.6 and 35.3; 16384 x 1536 43.1 and 61).
+template <typename F>
+int with_short_row(int vpr, F f)
+{
+    using std::integral_constant;
+    if (vpr <= 16) return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    if (vpr <= 32) return f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    if (vpr <= 64) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+}
+
+template <typename F>
+int with_norm_row(int vpr, F f)
+{
+    return vpr <= 128 ? with_short_row(vpr, f) : with_row_shape(vpr, f);
+}
+
+template <typename F>
+int with_gradient_row(int vpr, F f)
+{
+    using std::integral_constant;
+    if (vpr <= 128) return with_short_row(vpr, f);
+    if (vpr <= 256) return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    return with_row_shape(vpr, f);
+}
+
+// f(bf16, streamed, lanes of a row, vectors of a lane), all of them as types
+template <typename Row, typename F>
+int with_types(bool bf16, bool streamed, Row row, F f)
+{
+    return row([&](auto lanes, auto vecs) {
+        if (bf16) return streamed ? f(std::true_type{}, std::true_type{}, lanes, vecs) : f(std::true_type{}, std::false_type{}, lanes, vecs);
+        return streamed ? f(std::false_type{}, std::true_type{}, lanes, vecs) : f(std::false_type{}, std::false_type{}, lanes, vecs);
+    });
+}
+
+// Workgroups of the gradient, and so rows of partial sums, each of which is written and read again and costs more than a row of the norm itself.  us, 256 and
+// 512 of them: 8192 x 2048 bf16 32.6 and 37.6, 16384 x 1024 28.2 and 29.6, but 48222 x 120 13.8 and 12.8.
+int gradient_grid(const Call &c)
+{
+    return with_gradient_row(c.s.vpr, [&](auto lanes, auto vecs) {
+        constexpr int L = decltype(lanes)::value, rows = backward_threads_of<L>() / L;
+        return (int)std::min<int64_t>(((int64_t)c.s.T + rows - 1) / rows, L <= kWave && decltype(vecs)::value == 1 ? 512 : 256);
+    });
+}
+
 }  // namespace
 }  // namespace monta
 
@@ -316,10 +367,11 @@ int monta_layernorm(const monta_cfg *cfg, const void *x, const void *residual, c
     if (out && out_fp8 && overlap(out_fp8, n8, out, n)) return MONTA_ERR_INVALID;
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchTimer timer(MONTA_K_LAYERNORM, st);
-    const int wgs = (int)std::min<int64_t>(((int64_t)c.s.T + rows_per_wg(c.s.vpr) - 1) / rows_per_wg(c.s.vpr), kNormGrid);
     const int64_t touched = n * (residual ? 3 : 1) + (out ? n : 0) + (out_fp8 ? n8 : 0);
-    with_form(c.bf16, touched >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
-        constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
+    const auto row = [&](auto f) { return with_norm_row(c.s.vpr, f); };
+    with_types(c.bf16, touched >= kStreamFrom, row, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value, kRows = threads_of<L>() / L;
+        const int wgs = (int)std::min<int64_t>(((int64_t)c.s.T + kRows - 1) / kRows, kNormGrid);
         hipLaunchKernelGGL((layernorm_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(wgs), dim3(threads_of<L>()), 0, st,
                            static_cast<const u32x4 *>(x), static_cast<const u32x4 *>(residual), static_cast<const u32x4 *>(weight),
                            static_cast<const u32x4 *>(bias), static_cast<u32x4 *>(sum), static_cast<u32x4 *>(out), static_cast<unsigned char *>(out_fp8),
@@ -336,7 +388,7 @@ int monta_layernorm_scratch_bytes(const monta_cfg *cfg, size_t *bytes)
     Call c;
     if (int rc = open_call(cfg, nullptr, &c)) return rc;
     if (c.s.vpr > kMaxVecs) return MONTA_ERR_UNSUPPORTED;
-    *bytes = (size_t)backward_grid(c) * c.H * 8;
+    *bytes = (size_t)gradient_grid(c) * c.H * 8;
     return MONTA_OK;
 }
 
@@ -351,7 +403,7 @@ int monta_layernorm_backward(const monta_cfg *cfg, const void *sum, const void *
         return MONTA_ERR_ALIGN;
     if (!(eps >= 0.f) || eps > 3.4e38f) return MONTA_ERR_INVALID;
     if (c.s.vpr > kMaxVecs) return MONTA_ERR_UNSUPPORTED;
-    const int grid = backward_grid(c);
+    const int grid = gradient_grid(c);
     const int64_t n = c.s.T * c.row_bytes, np = (int64_t)grid * c.H * 8, nw = (int64_t)c.H * 4;
     const struct {
         const void *p;
@@ -371,7 +423,8 @@ int monta_layernorm_backward(const monta_cfg *cfg, const void *sum, const void *
     float *partial = static_cast<float *>(scratch);
     {
         LaunchTimer timer(MONTA_K_LAYERNORM_BACKWARD, st);
-        with_form(c.bf16, n * (dsum ? 4 : 3) >= kStreamFrom, c.s.vpr, [&](auto bf, auto streamed, auto lanes, auto vecs) {
+        const auto row = [&](auto f) { return with_gradient_row(c.s.vpr, f); };
+        with_types(c.bf16, n * (dsum ? 4 : 3) >= kStreamFrom, row, [&](auto bf, auto streamed, auto lanes, auto vecs) {
             constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
             hipLaunchKernelGGL((layernorm_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(grid), dim3(backward_threads_of<L>()), 0, st,
                                static_cast<const u32x4 *>(sum), static_cast<const u32x4 *>(weight), static_cast<const u32x4 *>(dout),

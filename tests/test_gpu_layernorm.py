@@ -66,7 +66,7 @@ def params(H, dtype, seed):
 
 # every number of lanes of a row, waves without a vector, waves with a few
 SIZES = [(1, 16), (1, 4096), (3, 128), (5, 112), (17, 256), (33, 528), (9, 1040), (7, 2048), (300, 512), (4, 5120), (3, 7168), (2, 8192), (2100, 96),
-         (4500, 16), (3, 4112), (5, 2064)]
+         (4500, 16), (3, 4112), (5, 2064), (40, 192), (9, 320), (1030, 384), (21, 768), (2000, 1024), (11, 1536)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -111,7 +111,7 @@ def test_parts(m, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("H", [80, 496, 1040, 2064, 7168, 16384])
+@pytest.mark.parametrize("H", [80, 208, 368, 496, 976, 1040, 2064, 7168, 16384])
 def test_edges(m, H, dtype):  # noqa: F811
     """Rows of equal numbers, a mean far above the spread, one large value, NaN and infinities that stay in their rows, small and large magnitudes."""
     import torch
