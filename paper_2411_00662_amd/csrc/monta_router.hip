@@ -77,7 +77,7 @@ __device__ __forceinline__ Softmax softmax(f32x4 v)
 // A workgroup sums a run of tokens; its E + 1 sums and E + 1 counts are a column each of `partial`, one word a workgroup, which
 // route_loss_join_kernel adds, a wave a column.  One workgroup alone finishes by itself.
 
-constexpr int kLossThreads = 512, kLossWaves = kLossThreads / kWave, kLossGrid = 512, kMaxExperts = 256;
+constexpr int kLossThreads = 512, kLossWaves = kLossThreads / kWave, kLossGrid = 256, kMaxExperts = 256;
 
 struct LossOut {
     float *losses;
@@ -119,6 +119,18 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
     for (int i = tid; i <= E; i += kLossThreads) cnt[i] = 0;
     __syncthreads();
     const int64_t t0 = (int64_t)blockIdx.x * per, t1 = min(t0 + per, (int64_t)T);
+    f32x4 v[kAtOnce];
+    bool live[kAtOnce];
+    auto fetch = [&](int64_t base) {
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int64_t t = base + q * kTokens + tid / L;
+            live[q] = t < t1 && (!mask || mask[t]);
+            v[q] = (f32x4){kNone, kNone, kNone, kNone};
+            if (t < t1 && exist > 0) v[q] = load_some(logits + t * E + 4 * l, exist, kNone);
+        }
+    };
+    fetch(t0);                                                     // on their way while the choices are counted
     {
         const int64_t p0 = t0 * k, pairs = (t1 - t0) * k;
         for (int64_t p = tid; p < pairs; p += kLossThreads) {
@@ -130,15 +142,7 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
     float z = 0.f;
     int n = 0;
     for (int64_t base = t0; base < t1; base += kTokens * kAtOnce) {
-        f32x4 v[kAtOnce];
-        bool live[kAtOnce];
-#pragma unroll
-        for (int q = 0; q < kAtOnce; ++q) {
-            const int64_t t = base + q * kTokens + tid / L;
-            live[q] = t < t1 && (!mask || mask[t]);
-            v[q] = (f32x4){kNone, kNone, kNone, kNone};
-            if (t < t1 && exist > 0) v[q] = load_some(logits + t * E + 4 * l, exist, kNone);
-        }
+        if (base > t0) fetch(base);
 #pragma unroll
         for (int q = 0; q < kAtOnce; ++q) {
             if (base + q * kTokens >= t1) break;                    // all lanes together
@@ -187,28 +191,37 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
     }
 }
 
+// A column is a load of a wave; nine columns' loads at a time (one at a time, 64 experts take 6.0 us, of which JJJ here).
 __global__ __launch_bounds__(1024) void route_loss_join_kernel(const float *partial, LossOut o, int G, int E, int k)
 {
+    constexpr int kWaves = 1024 / kWave, kColumns = 9;
+    static_assert(kLossGrid == 4 * kWave, "a lane has four words of a column");
     __shared__ float all[kMaxExperts + 1], part[4];
     __shared__ int32_t cnt[kMaxExperts + 1];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    for (int c = wave; c < 2 * (E + 1); c += 1024 / kWave) {
-        float v = 0.f;
-        int n = 0;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, columns = 2 * (E + 1);
+    for (int c0 = wave; c0 < columns; c0 += kColumns * kWaves) {
+        f32x4 v[kColumns];
 #pragma unroll
-        for (int i = 0; i < kLossGrid / kWave; ++i) {
-            const int at = i * kWave + lane;
-            const float p = at < G ? partial[(int64_t)c * G + at] : 0.f;
-            if (c <= E) v += p;
-            else n += __float_as_int(p);
+        for (int q = 0; q < kColumns; ++q) {
+            const int c = c0 + q * kWaves;
+            v[q] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (c < columns) v[q] = load_some(partial + (int64_t)c * G + 4 * lane, G - 4 * lane, 0.f);
         }
-        if (c <= E) {
-            v = group_sum<kWave>(v);
-            if (lane == 0) all[c] = v;
-        } else {
 #pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) n += __shfl_xor(n, d, kWave);
-            if (lane == 0) cnt[c - E - 1] = n;
+        for (int q = 0; q < kColumns; ++q) {
+            const int c = c0 + q * kWaves;
+            if (c >= columns) break;                               // the whole wave
+            if (c <= E) {
+                const float t = group_sum<kWave>((v[q][0] + v[q][1]) + (v[q][2] + v[q][3]));
+                if (lane == 0) all[c] = t;
+            } else {
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n += __float_as_int(v[q][i]);
+#pragma unroll
+                for (int d = 1; d < kWave; d <<= 1) n += __shfl_xor(n, d, kWave);
+                if (lane == 0) cnt[c - E - 1] = n;
+            }
         }
     }
     __syncthreads();
@@ -221,9 +234,10 @@ __global__ __launch_bounds__(1024) void route_loss_join_kernel(const float *part
 //   renormalised over the choices:  dl[i_j] += g_j (d_j - D);     otherwise:  dl[i_j] += g_j d_j,  dl[e] -= p[e] D.
 // The losses' part, with their gradients b and c, f and n as above:
 //   dl[e] += p[e] ( b / n (f[e] - sum_i p[i] f[i]) + 2 c / n lse ).
-// A workgroup takes 256 / L tokens.  A thread has a pair: it goes over its token's pairs in LDS for D, and puts what its expert gets (once, by the
+// A workgroup takes IT 256 / L tokens.  A thread has a pair: it goes over its token's pairs in LDS for D, and puts what its expert gets (once, by the
 // first of its pairs if an expert is named twice) into the token's row in LDS, which the token's lanes then add to what p asks for.
 
+// A thread has four experts of IT tokens: their logits come together.
 constexpr int kGradThreads = 256, kRouteGrid = 1 << 20;
 
 struct RouteGradArgs {
@@ -235,10 +249,10 @@ struct RouteGradArgs {
     FastDiv by_k;
 };
 
-template <int L, bool SOFTMAX>
+template <int L, int IT, bool SOFTMAX>
 __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradArgs a)
 {
-    constexpr int kTokens = kGradThreads / L, kPairs = 4 * kGradThreads;        // k <= E <= 4 L
+    constexpr int kGroups = kGradThreads / L, kTokens = IT * kGroups, kPairs = kTokens * (4 * L < 32 ? 4 * L : 32);      // k <= E <= 4 L, k <= 32
     __shared__ float row[kTokens][4 * L], dots[kTokens], prod[kPairs], gate[kPairs];
     __shared__ int32_t expert[kPairs];
     const int tid = threadIdx.x, l = tid % L, mine = tid / L, exist = a.E - 4 * l, k = a.k;
@@ -254,13 +268,20 @@ __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradA
     }
     const int64_t chunks = ((int64_t)a.T + kTokens - 1) / kTokens;
     for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-        const int64_t t0 = chunk * kTokens, t = t0 + mine;
+        const int64_t t0 = chunk * kTokens;
         const int tokens = (int)min((int64_t)kTokens, a.T - t0);
-        const bool there = mine < tokens, live = there && (!a.mask || a.mask[t]);
-        f32x4 v = {kNone, kNone, kNone, kNone};
-        if (SOFTMAX && there && exist > 0) v = load_some(a.logits + t * a.E + 4 * l, exist, kNone);
-        *reinterpret_cast<f32x4 *>(&row[mine][4 * l]) = (f32x4){0.f, 0.f, 0.f, 0.f};
-        if (l == 0) dots[mine] = 0.f;
+        f32x4 v[IT];
+        bool there[IT], live[IT];
+#pragma unroll
+        for (int q = 0; q < IT; ++q) {
+            const int tok = q * kGroups + mine;
+            there[q] = tok < tokens;
+            live[q] = there[q] && (!a.mask || a.mask[t0 + tok]);
+            v[q] = (f32x4){kNone, kNone, kNone, kNone};
+            if (SOFTMAX && there[q] && exist > 0) v[q] = load_some(a.logits + (t0 + tok) * a.E + 4 * l, exist, kNone);
+            *reinterpret_cast<f32x4 *>(&row[tok][4 * l]) = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (l == 0) dots[tok] = 0.f;
+        }
         if (a.dgates) {
             const int pairs = tokens * k;
             for (int p = tid; p < pairs; p += kGradThreads) {
@@ -291,20 +312,24 @@ __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradA
             }
         }
         __syncthreads();
-        f32x4 d = *reinterpret_cast<const f32x4 *>(&row[mine][4 * l]);
-        if constexpr (SOFTMAX) {
-            const Softmax s = softmax<L>(v);
-            const float dot = a.renorm ? 0.f : dots[mine];
-            float pf = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pf = __builtin_fmaf(s.p[i], f[i], pf);
-            pf = group_sum<L>(pf);
-            const float every = __builtin_fmaf(c, s.lse, -dot);
+        for (int q = 0; q < IT; ++q) {
+            const int tok = q * kGroups + mine;
+            f32x4 d = *reinterpret_cast<const f32x4 *>(&row[tok][4 * l]);
+            if constexpr (SOFTMAX) {
+                const Softmax s = softmax<L>(v[q]);
+                const float dot = a.renorm ? 0.f : dots[tok];
+                float pf = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) d[i] = __builtin_fmaf(s.p[i], __builtin_fmaf(b, f[i] - pf, every), d[i]);
+                for (int i = 0; i < 4; ++i) pf = __builtin_fmaf(s.p[i], f[i], pf);
+                pf = group_sum<L>(pf);
+                const float every = __builtin_fmaf(c, s.lse, -dot);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[i] = __builtin_fmaf(s.p[i], __builtin_fmaf(b, f[i] - pf, every), d[i]);
+            }
+            if (!live[q]) d = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (there[q] && exist > 0) store_some(a.dlogits + (t0 + tok) * a.E + 4 * l, exist, d);
         }
-        if (!live) d = (f32x4){0.f, 0.f, 0.f, 0.f};
-        if (there && exist > 0) store_some(a.dlogits + t * a.E + 4 * l, exist, d);
         __syncthreads();                                           // the next tokens' pairs take the place of these
     }
 }
@@ -414,10 +439,19 @@ int monta_route_backward(const monta_cfg *cfg, const float *logits, const int32_
     const bool softmax = dlosses || (dgates && !c.s.renorm);
     LaunchTimer timer(MONTA_K_ROUTE_BACKWARD, st);
     with_lanes(c.s.E, [&](auto lanes) {
-        constexpr int L = decltype(lanes)::value, kTokens = kGradThreads / L;
-        const int grid = (int)std::min<int64_t>((T + kTokens - 1) / kTokens, kRouteGrid);
-        if (softmax) hipLaunchKernelGGL((route_backward_kernel<L, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
-        else hipLaunchKernelGGL((route_backward_kernel<L, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
+        constexpr int L = decltype(lanes)::value;
+        auto launch = [&](auto it) {
+            constexpr int IT = decltype(it)::value, kTokens = IT * kGradThreads / L;
+            const int grid = (int)std::min<int64_t>((T + kTokens - 1) / kTokens, kRouteGrid);
+            if (softmax) hipLaunchKernelGGL((route_backward_kernel<L, IT, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
+            else hipLaunchKernelGGL((route_backward_kernel<L, IT, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
+        };
+        if constexpr (L >= 16) {
+            if (T * L >= 4 * kGradThreads * 512) launch(std::integral_constant<int, 4>{});
+            else launch(std::integral_constant<int, 1>{});
+        } else {
+            launch(std::integral_constant<int, 1>{});
+        }
         return MONTA_OK;
     });
     MONTA_HIP_TRY(hipGetLastError());
