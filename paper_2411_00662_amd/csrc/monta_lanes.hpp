@@ -39,11 +39,22 @@ __device__ __forceinline__ float group_sum(float v)
     return group_join<L>(v, [](float a, float b) { return a + b; });
 }
 
-// NaN is passed over
+// The larger of two numbers, or the one that is no NaN.  The instruction itself: around fmaxf the compiler puts others, which make a signalling NaN quiet.
+__device__ __forceinline__ float plain_max(float a, float b)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+#else
+    return a > b ? a : b;
+#endif
+}
+
 template <int L>
 __device__ __forceinline__ float group_max(float v)
 {
-    return group_join<L>(v, [](float a, float b) { return fmaxf(a, b); });
+    return group_join<L>(v, [](float a, float b) { return plain_max(a, b); });
 }
 
 }  // namespace monta

@@ -1,7 +1,8 @@
 // The router's losses, and the gradient from the gates and those losses to the logits.
 //
-// A token's E logits belong to L lanes of a wave, the least power of two with 4 L >= E; lane l has experts 4 l to 4 l + 3.  Sums over a token's
-// experts are moves between its lanes.
+// A token's E logits belong to L lanes of a wave with V vectors of four each, E <= 4 L V: vector v of lane l is that of experts 4 (v L + l) and on.  Sums over
+// a token's experts are moves between its lanes, and what they, a logarithm and a quotient cost falls with the number of lanes: the gradient of 32768 tokens
+// over 256 experts takes 21.0 us with 64 lanes, VVV with 16.
 #include "monta_internal.hpp"
 #include "monta_lanes.hpp"
 
@@ -40,34 +41,51 @@ __device__ __forceinline__ float exp_neg(float x)
 {
     constexpr double kLog2e = 1.4426950408889634074;
     constexpr float kHigh = (float)kLog2e, kLow = (float)(kLog2e - (double)kHigh);
-    x = fmaxf(x, -128.f);
+    x = plain_max(x, -128.f);
     const float h = x * kHigh, l = __builtin_fmaf(x, kLow, __builtin_fmaf(x, kHigh, -h)), p = __builtin_amdgcn_exp2f(h);
     return __builtin_fmaf(p, l * 0.69314718056f, p);
 }
 
+template <int V>
 struct Softmax {
-    f32x4 p;       // of the lane's experts; 0 past the last one
+    f32x4 p[V];    // of the lane's experts; 0 past the last one
     float lse;     // log of the sum of all exponentials
 };
 
-// of the L lanes' logits; kNone past the last expert
-template <int L>
-__device__ __forceinline__ Softmax softmax(f32x4 v)
+// of the L lanes' logits; kNone past the last expert.  A reciprocal of one step, a logarithm of base 2 of one step: the sum lies in 1 .. 256.
+template <int L, int V>
+__device__ __forceinline__ Softmax<V> softmax(const f32x4 (&v)[V])
 {
-    const float top = group_max<L>(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
-    Softmax s;
+    float top = v[0][0];
+#pragma unroll
+    for (int i = 1; i < 4 * V; ++i) top = plain_max(top, v[i / 4][i % 4]);
+    top = group_max<L>(top);
+    Softmax<V> s;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        s.p[i] = exp_neg(v[i] - top);
-        sum += s.p[i];
+    for (int i = 0; i < 4 * V; ++i) {
+        const float e = exp_neg(v[i / 4][i % 4] - top);
+        s.p[i / 4][i % 4] = e;
+        sum += e;
     }
     sum = group_sum<L>(sum);
-    s.lse = top + logf(sum);
-    const float inv = 1.f / sum;
+    s.lse = __builtin_fmaf(__builtin_amdgcn_logf(sum), 0.69314718056f, top);
+    const float inv = __builtin_amdgcn_rcpf(sum);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s.p[i] *= inv;
+    for (int i = 0; i < 4 * V; ++i) s.p[i / 4][i % 4] *= inv;
     return s;
+}
+
+// a token's logits, or others of its row
+template <int L, int V>
+__device__ __forceinline__ void load_row(f32x4 (&v)[V], const float *row, int l, int E, bool there)
+{
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+        const int e = 4 * (q * L + l);
+        v[q] = (f32x4){kNone, kNone, kNone, kNone};
+        if (there && e < E) v[q] = load_some(row + e, E - e, kNone);
+    }
 }
 
 // --------------------------------------------------------------------------------------------- losses
@@ -108,26 +126,25 @@ __device__ __forceinline__ void finish_losses(const float *sums, const int32_t *
     }
 }
 
-template <int L>
+template <int L, int V>
 __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *logits, const int32_t *idx, const uint8_t *mask, float *partial, LossOut o,
                                                                   int T, int E, int k, int per)
 {
-    constexpr int kTokens = kLossThreads / L, kAtOnce = 4;          // tokens of a round; rounds whose logits are requested together
+    constexpr int kTokens = kLossThreads / L, kAtOnce = V == 1 ? 4 : 2;         // tokens of a round; rounds whose logits are requested together
     __shared__ float sums[kLossWaves][kMaxExperts + 1], all[kMaxExperts + 1], part[4];
     __shared__ int32_t cnt[kMaxExperts + 1];
-    const int tid = threadIdx.x, l = tid % L, exist = E - 4 * l, wave = tid / kWave;
+    const int tid = threadIdx.x, l = tid % L, wave = tid / kWave;
     for (int i = tid; i <= E; i += kLossThreads) cnt[i] = 0;
     __syncthreads();
     const int64_t t0 = (int64_t)blockIdx.x * per, t1 = min(t0 + per, (int64_t)T);
-    f32x4 v[kAtOnce];
+    f32x4 v[kAtOnce][V];
     bool live[kAtOnce];
     auto fetch = [&](int64_t base) {
 #pragma unroll
         for (int q = 0; q < kAtOnce; ++q) {
             const int64_t t = base + q * kTokens + tid / L;
             live[q] = t < t1 && (!mask || mask[t]);
-            v[q] = (f32x4){kNone, kNone, kNone, kNone};
-            if (t < t1 && exist > 0) v[q] = load_some(logits + t * E + 4 * l, exist, kNone);
+            load_row<L, V>(v[q], logits + t * E, l, E, t < t1);
         }
     };
     fetch(t0);                                                     // on their way while the choices are counted
@@ -138,7 +155,9 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
             if ((uint32_t)e < (uint32_t)E && (!mask || mask[t0 + (uint32_t)p / (uint32_t)k])) atomicAdd(&cnt[e], 1);
         }
     }
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    f32x4 acc[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float z = 0.f;
     int n = 0;
     for (int64_t base = t0; base < t1; base += kTokens * kAtOnce) {
@@ -146,10 +165,10 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
 #pragma unroll
         for (int q = 0; q < kAtOnce; ++q) {
             if (base + q * kTokens >= t1) break;                    // all lanes together
-            const Softmax s = softmax<L>(v[q]);
+            const Softmax<V> s = softmax<L, V>(v[q]);
             if (live[q]) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i] += s.p[i];
+                for (int i = 0; i < V; ++i) acc[i] += s.p[i];
                 if (l == 0) {
                     z = __builtin_fmaf(s.lse, s.lse, z);
                     ++n;
@@ -160,14 +179,16 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
 #pragma unroll
     for (int d = L; d < kWave; d <<= 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], d, kWave);
+        for (int i = 0; i < 4 * V; ++i) acc[i / 4][i % 4] += __shfl_xor(acc[i / 4][i % 4], d, kWave);
         z += __shfl_xor(z, d, kWave);
         n += __shfl_xor(n, d, kWave);
     }
     if (tid % kWave < L)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < exist) sums[wave][4 * l + i] = acc[i];
+        for (int i = 0; i < 4 * V; ++i) {
+            const int e = 4 * (i / 4 * L + l) + i % 4;
+            if (e < E) sums[wave][e] = acc[i / 4][i % 4];
+        }
     if (tid % kWave == 0) {
         sums[wave][E] = z;
         atomicAdd(&cnt[E], n);
@@ -234,11 +255,10 @@ __global__ __launch_bounds__(1024) void route_loss_join_kernel(const float *part
 //   renormalised over the choices:  dl[i_j] += g_j (d_j - D);     otherwise:  dl[i_j] += g_j d_j,  dl[e] -= p[e] D.
 // The losses' part, with their gradients b and c, f and n as above:
 //   dl[e] += p[e] ( b / n (f[e] - sum_i p[i] f[i]) + 2 c / n lse ).
-// A workgroup takes IT 256 / L tokens.  A thread has a pair: it goes over its token's pairs in LDS for D, and puts what its expert gets (once, by the
+// A workgroup takes 256 / L tokens.  A thread has a pair: it goes over its token's pairs in LDS for D, and puts what its expert gets (once, by the
 // first of its pairs if an expert is named twice) into the token's row in LDS, which the token's lanes then add to what p asks for.
 
-// A thread has four experts of IT tokens: their logits come together.
-constexpr int kGradThreads = 256, kRouteGrid = 1 << 20;
+constexpr int kGradThreads = 256, kRouteGrid = 1024;
 
 struct RouteGradArgs {
     const float *logits, *gates, *dgates, *dlosses;
@@ -249,39 +269,51 @@ struct RouteGradArgs {
     FastDiv by_k;
 };
 
-template <int L, int IT, bool SOFTMAX>
+template <int L, int V>
+constexpr int grad_lds(int k)       // bytes: rows, D, and of each pair product, gate and expert
+{
+    return kGradThreads / L * (4 * L * V + 1 + 3 * k) * 4;
+}
+
+template <int L, int V, bool SOFTMAX>
 __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradArgs a)
 {
-    constexpr int kGroups = kGradThreads / L, kTokens = IT * kGroups, kPairs = kTokens * (4 * L < 32 ? 4 * L : 32);      // k <= E <= 4 L, k <= 32
-    __shared__ float row[kTokens][4 * L], dots[kTokens], prod[kPairs], gate[kPairs];
-    __shared__ int32_t expert[kPairs];
-    const int tid = threadIdx.x, l = tid % L, mine = tid / L, exist = a.E - 4 * l, k = a.k;
-    f32x4 f = {0.f, 0.f, 0.f, 0.f};
-    float b = 0.f, c = 0.f;
-    if (SOFTMAX && a.dlosses) {
-        const float n = (float)max(a.counts[a.E], 1);
-        b = a.dlosses[0] / n;
-        c = 2.f * (a.dlosses[1] / n);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < exist) f[i] = (float)a.counts[4 * l + i] * ((float)a.E / (float)k) / n;
-    }
+    constexpr int kTokens = kGradThreads / L, kRow = 4 * L * V;
+    extern __shared__ __align__(16) float route_lds[];
+    const int tid = threadIdx.x, l = tid % L, mine = tid / L, k = a.k;
+    float *const row = route_lds, *const dots = row + kTokens * kRow, *const prod = dots + kTokens, *const gate = prod + kTokens * k;
+    int32_t *const expert = reinterpret_cast<int32_t *>(gate + kTokens * k);
     const int64_t chunks = ((int64_t)a.T + kTokens - 1) / kTokens;
-    for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-        const int64_t t0 = chunk * kTokens;
-        const int tokens = (int)min((int64_t)kTokens, a.T - t0);
-        f32x4 v[IT];
-        bool there[IT], live[IT];
-#pragma unroll
-        for (int q = 0; q < IT; ++q) {
-            const int tok = q * kGroups + mine;
-            there[q] = tok < tokens;
-            live[q] = there[q] && (!a.mask || a.mask[t0 + tok]);
-            v[q] = (f32x4){kNone, kNone, kNone, kNone};
-            if (SOFTMAX && there[q] && exist > 0) v[q] = load_some(a.logits + (t0 + tok) * a.E + 4 * l, exist, kNone);
-            *reinterpret_cast<f32x4 *>(&row[tok][4 * l]) = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (l == 0) dots[tok] = 0.f;
+    f32x4 v[V], f[V];
+    bool live;
+    auto fetch = [&](int64_t chunk) {
+        const int64_t t = chunk * kTokens + mine;
+        live = t < a.T && (!a.mask || a.mask[t]);
+        if constexpr (SOFTMAX) load_row<L, V>(v, a.logits + t * a.E, l, a.E, t < a.T);
+    };
+    fetch(blockIdx.x);
+    float b = 0.f, c = 0.f;
+    if (SOFTMAX) {
+        float scale = 0.f;
+        if (a.dlosses) {
+            const float n = (float)max(a.counts[a.E], 1);
+            b = a.dlosses[0] / n;
+            c = 2.f * (a.dlosses[1] / n);
+            scale = (float)a.E / ((float)k * n);
         }
+#pragma unroll
+        for (int i = 0; i < 4 * V; ++i) {
+            const int e = 4 * (i / 4 * L + l) + i % 4;
+            f[i / 4][i % 4] = a.dlosses && e < a.E ? (float)a.counts[e] * scale : 0.f;
+        }
+    }
+    for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+        const int64_t t0 = chunk * kTokens, t = t0 + mine;
+        const int tokens = (int)min((int64_t)kTokens, a.T - t0);
+        const bool there = mine < tokens, mine_live = live;
+#pragma unroll
+        for (int q = 0; q < V; ++q) *reinterpret_cast<f32x4 *>(row + mine * kRow + 4 * (q * L + l)) = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (l == 0) dots[mine] = 0.f;
         if (a.dgates) {
             const int pairs = tokens * k;
             for (int p = tid; p < pairs; p += kGradThreads) {
@@ -307,50 +339,57 @@ __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradA
                         owner = owner && first + i >= p;
                     }
                 }
-                if (owner) row[tok][e] = a.renorm ? __builtin_fmaf(-sg, dot, sp) : sp;
+                if (owner) row[tok * kRow + e] = a.renorm ? __builtin_fmaf(-sg, dot, sp) : sp;
                 if (p == first) dots[tok] = dot;
             }
         }
         __syncthreads();
+        f32x4 d[V], now[V];
 #pragma unroll
-        for (int q = 0; q < IT; ++q) {
-            const int tok = q * kGroups + mine;
-            f32x4 d = *reinterpret_cast<const f32x4 *>(&row[tok][4 * l]);
-            if constexpr (SOFTMAX) {
-                const Softmax s = softmax<L>(v[q]);
-                const float dot = a.renorm ? 0.f : dots[tok];
-                float pf = 0.f;
+        for (int q = 0; q < V; ++q) {
+            d[q] = *reinterpret_cast<const f32x4 *>(row + mine * kRow + 4 * (q * L + l));
+            if constexpr (SOFTMAX) now[q] = v[q];
+        }
+        if (chunk + gridDim.x < chunks) fetch(chunk + gridDim.x);
+        if constexpr (SOFTMAX) {
+            const Softmax<V> s = softmax<L, V>(now);
+            const float dot = a.renorm ? 0.f : dots[mine];
+            float pf = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pf = __builtin_fmaf(s.p[i], f[i], pf);
-                pf = group_sum<L>(pf);
-                const float every = __builtin_fmaf(c, s.lse, -dot);
+            for (int i = 0; i < 4 * V; ++i) pf = __builtin_fmaf(s.p[i / 4][i % 4], f[i / 4][i % 4], pf);
+            pf = group_sum<L>(pf);
+            const float every = __builtin_fmaf(c, s.lse, -dot);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d[i] = __builtin_fmaf(s.p[i], __builtin_fmaf(b, f[i] - pf, every), d[i]);
-            }
-            if (!live[q]) d = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (there[q] && exist > 0) store_some(a.dlogits + (t0 + tok) * a.E + 4 * l, exist, d);
+            for (int i = 0; i < 4 * V; ++i)
+                d[i / 4][i % 4] = __builtin_fmaf(s.p[i / 4][i % 4], __builtin_fmaf(b, f[i / 4][i % 4] - pf, every), d[i / 4][i % 4]);
+        }
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            const int e = 4 * (q * L + l);
+            if (!mine_live) d[q] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (there && e < a.E) store_some(a.dlogits + t * a.E + e, a.E - e, d[q]);
         }
         __syncthreads();                                           // the next tokens' pairs take the place of these
     }
 }
 
-// f(lanes of a token)
+// f(lanes of a token, vectors of a lane)
 template <typename F>
 int with_lanes(int E, F f)
 {
     using std::integral_constant;
-    if (E <= 4) return f(integral_constant<int, 1>{});
-    if (E <= 8) return f(integral_constant<int, 2>{});
-    if (E <= 16) return f(integral_constant<int, 4>{});
-    if (E <= 32) return f(integral_constant<int, 8>{});
-    if (E <= 64) return f(integral_constant<int, 16>{});
-    if (E <= 128) return f(integral_constant<int, 32>{});
-    return f(integral_constant<int, 64>{});
+    if (E <= 4) return f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+    if (E <= 8) return f(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+    if (E <= 16) return f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    if (E <= 32) return f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    if (E <= 64) return f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+    if (E <= 128) return f(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+    return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
 }
 
 int lanes_of(int E)
 {
-    return with_lanes(E, [](auto lanes) { return (int)decltype(lanes)::value; });
+    return with_lanes(E, [](auto lanes, auto) { return (int)decltype(lanes)::value; });
 }
 
 // workgroups of the losses: whole rounds of tokens each
@@ -405,8 +444,8 @@ int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *t
     float *partial = static_cast<float *>(scratch);
     const LossOut o = {losses, counts, means};
     LaunchTimer timer(MONTA_K_ROUTE_LOSS, st);
-    with_lanes(c.s.E, [&](auto lanes) {
-        hipLaunchKernelGGL((route_loss_kernel<decltype(lanes)::value>), dim3(grid), dim3(kLossThreads), 0, st, logits, topk_idx, token_mask, partial, o, c.s.T,
+    with_lanes(c.s.E, [&](auto lanes, auto vecs) {
+        hipLaunchKernelGGL((route_loss_kernel<decltype(lanes)::value, decltype(vecs)::value>), dim3(grid), dim3(kLossThreads), 0, st, logits, topk_idx, token_mask, partial, o, c.s.T,
                            c.s.E, c.s.k, per);
         return MONTA_OK;
     });
@@ -438,20 +477,11 @@ int monta_route_backward(const monta_cfg *cfg, const float *logits, const int32_
     const RouteGradArgs a = {logits, gates, dgates, dlosses, topk_idx, counts, token_mask, dlogits, c.s.T, c.s.E, c.s.k, c.s.renorm, c.s.by_k};
     const bool softmax = dlosses || (dgates && !c.s.renorm);
     LaunchTimer timer(MONTA_K_ROUTE_BACKWARD, st);
-    with_lanes(c.s.E, [&](auto lanes) {
-        constexpr int L = decltype(lanes)::value;
-        auto launch = [&](auto it) {
-            constexpr int IT = decltype(it)::value, kTokens = IT * kGradThreads / L;
-            const int grid = (int)std::min<int64_t>((T + kTokens - 1) / kTokens, kRouteGrid);
-            if (softmax) hipLaunchKernelGGL((route_backward_kernel<L, IT, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
-            else hipLaunchKernelGGL((route_backward_kernel<L, IT, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
-        };
-        if constexpr (L >= 16) {
-            if (T * L >= 4 * kGradThreads * 512) launch(std::integral_constant<int, 4>{});
-            else launch(std::integral_constant<int, 1>{});
-        } else {
-            launch(std::integral_constant<int, 1>{});
-        }
+    with_lanes(c.s.E, [&](auto lanes, auto vecs) {
+        constexpr int L = decltype(lanes)::value, V = decltype(vecs)::value, kTokens = kGradThreads / L;
+        const int grid = (int)std::min<int64_t>((T + kTokens - 1) / kTokens, kRouteGrid), lds = grad_lds<L, V>(c.s.k);
+        if (softmax) hipLaunchKernelGGL((route_backward_kernel<L, V, true>), dim3(grid), dim3(kGradThreads), lds, st, a);
+        else hipLaunchKernelGGL((route_backward_kernel<L, V, false>), dim3(grid), dim3(kGradThreads), lds, st, a);
         return MONTA_OK;
     });
     MONTA_HIP_TRY(hipGetLastError());
