@@ -36,9 +36,9 @@ __device__ __forceinline__ GatePart gate_part(const GateGradArgs &a, uint32_t bl
     return p;
 }
 
-// --------------------------------------------------------------------------------------------- exact products
+// --------------------------------------------------------------------------------------------- fp32
 //
-// fp32 products on the matrix cores (16 x 16 x 4), for fp32 and for bf16 activations.  A wave has 16 CT columns of a step's 16 tokens and the
+// fp32 activations: fp32 products on the matrix cores (16 x 16 x 4).  A wave has 16 CT columns of a step's 16 tokens and the
 // weights of its columns in registers; the gradient of the logits, which all waves of the workgroup need in both orders, goes through LDS.
 //   dx: rows h, columns t, summed over e.  Row r of tile i is column 4 CT (r / 4) + 4 i + r % 4, so that a lane gets 4 CT neighbours of one token.
 //   dw: rows h, columns e, summed over t.  Row r of tile i is column CT r + i, so that a lane's elements of x are neighbours.
@@ -46,29 +46,24 @@ __device__ __forceinline__ GatePart gate_part(const GateGradArgs &a, uint32_t bl
 template <int EB>
 constexpr int tiles_of() { return EB <= 4 ? 4 : 16 / EB; }
 
-template <bool BF16, int N>
+template <int N>
 struct Piece {                  // N neighbouring elements of a row
     static_assert(N == 1 || N == 2 || N == 4, "piece: elements");
-    typedef std::conditional_t<BF16, __bf16, float> E1;
-    typedef E1 V __attribute__((ext_vector_type(N == 1 ? 2 : N)));      // one alone is kept in the first of two
+    typedef float V __attribute__((ext_vector_type(N == 1 ? 2 : N)));       // one alone is kept in the first of two
     V v;
-    __device__ __forceinline__ void clear()
+    __device__ __forceinline__ void clear() { v = (V)0.f; }
+    __device__ __forceinline__ void get(const float *p)
     {
-        v = (V)(E1)0.f;
-    }
-    __device__ __forceinline__ void get(const void *base, int64_t at)
-    {
-        const E1 *p = static_cast<const E1 *>(base) + at;
         if constexpr (N == 1) v[0] = *p;
         else v = *reinterpret_cast<const V *>(p);
     }
-    __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
 };
 
 constexpr int kStepTokens = 16;
 
-template <bool BF16, int EB>
-__global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
+template <int EB>
+__global__ __launch_bounds__(256) void gate_backward_f32_kernel(GateGradArgs a)
 {
     constexpr int CT = tiles_of<EB>(), CW = 16 * CT, kPitch = 16 * EB + 4;
     __shared__ float dlt[2][kStepTokens][kPitch];
@@ -77,6 +72,8 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
     const int64_t H = a.H;
     const int col = part.col + wave * CW;                          // first column of the wave
     const bool want_dx = a.dx != nullptr, want_dw = a.dw != nullptr;
+    const float *const in = static_cast<const float *>(a.x), *const weights = static_cast<const float *>(a.w), *const dadd = static_cast<const float *>(a.dadd);
+    float *const to_dx = static_cast<float *>(a.dx);
 
     float w[CT][4 * EB];
     if (want_dx)
@@ -85,10 +82,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
 #pragma unroll
             for (int i = 0; i < CT; ++i) {
                 const int e = 4 * kk + g, h = col + (m >> 2) * (4 * CT) + 4 * i + (m & 3);
-                Piece<BF16, 1> p;
-                p.clear();
-                if (e < a.E && h < a.H) p.get(a.w, e * H + h);
-                w[i][kk] = p[0];
+                w[i][kk] = e < a.E && h < a.H ? weights[e * H + h] : 0.f;
             }
     f32x4 sum[EB][CT];
 #pragma unroll
@@ -97,8 +91,8 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
         for (int i = 0; i < CT; ++i) sum[j][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
     float dl[EB];
-    Piece<BF16, CT> x[4];
-    Piece<BF16, 4> add[CT];
+    Piece<CT> x[4];
+    Piece<4> add[CT];
     auto fetch = [&](int64_t t0) {
         const int64_t t = t0 + (tid >> 4);
 #pragma unroll
@@ -111,14 +105,14 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
             for (int s = 0; s < 4; ++s) {
                 const int64_t at = t0 + 4 * s + g;
                 x[s].clear();
-                if (at < a.T && col + m * CT < a.H) x[s].get(a.x, at * H + col + m * CT);
+                if (at < a.T && col + m * CT < a.H) x[s].get(in + at * H + col + m * CT);
             }
         if (want_dx)
 #pragma unroll
             for (int i = 0; i < CT; ++i) {
                 const int h = col + 4 * CT * g + 4 * i;
                 add[i].clear();
-                if (a.dadd && t0 + m < a.T && h < a.H) add[i].get(a.dadd, (t0 + m) * H + h);
+                if (a.dadd && t0 + m < a.T && h < a.H) add[i].get(dadd + (t0 + m) * H + h);
             }
     };
     const int64_t first = (int64_t)part.share * kStepTokens, stride = (int64_t)a.shares * kStepTokens;
@@ -127,7 +121,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
     for (int64_t t0 = first; t0 < a.T; t0 += stride, buf ^= 1) {
 #pragma unroll
         for (int q = 0; q < EB; ++q) dlt[buf][tid >> 4][(tid & 15) + 16 * q] = dl[q];
-        Piece<BF16, CT> x0[4];
+        Piece<CT> x0[4];
         f32x4 out[CT];
 #pragma unroll
         for (int s = 0; s < 4; ++s) x0[s] = x[s];
@@ -149,15 +143,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
                 for (int i = 0; i < CT; ++i) {
                     const int h = col + 4 * CT * g + 4 * i;
                     if (h >= a.H) continue;
-                    const int64_t at = (t0 + m) * H + h;
-                    if constexpr (BF16) {
-                        bf16x4 o;
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) o[v] = (__bf16)out[i][v];
-                        *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.dx) + at) = o;
-                    } else {
-                        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.dx) + at) = out[i];
-                    }
+                    *reinterpret_cast<f32x4 *>(to_dx + (t0 + m) * H + h) = out[i];
                 }
         }
         if (want_dw)
@@ -199,7 +185,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a)
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-constexpr int kSplitTokens = 32;
+constexpr int kSplitTokens = 32, kStages = 3;      // tokens of a step; stages of x
 [[maybe_unused]] constexpr int kNt = 2;         // past the cache
 
 // Segment s of row k sits at s ^ row_swizzle<C>(k) in rows of C elements: the 8 rows (8 g + j, g = 0, 1, j = 0..3) of which half a wave reads a
@@ -225,8 +211,33 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 [[maybe_unused]] __device__ __forceinline__ bf16x8 read_along(lds_bf16x8 *__restrict__ p) { return *p; }
 [[maybe_unused]] __device__ __forceinline__ void put(lds_u32x4 *__restrict__ p, u32x4 v) { *p = v; }
 
-template <int EB, int CT, int NW, int NST>
+// Eight neighbours of dl as three bf16 numbers each, one piece `pitch` bytes behind the other.
+template <int pitch>
+[[maybe_unused]] __device__ __forceinline__ void split_eight(const f32x4 (&dl)[2], unsigned char *to)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = dl[i / 4][i % 4];
+#pragma unroll
+    for (int piece = 0; piece < 3; ++piece) {
+        u32x4 b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x2 two;
+            two[0] = (__bf16)v[2 * i];
+            two[1] = (__bf16)v[2 * i + 1];
+            b[i] = __builtin_bit_cast(uint32_t, two);
+            v[2 * i] -= __uint_as_float(b[i] << 16);
+            v[2 * i + 1] -= __uint_as_float(b[i] & 0xffff0000u);
+        }
+        put((lds_u32x4 *)(to + piece * pitch), b);
+    }
+}
+
+template <int EB, int NW>
 struct GateShape {
+    static_assert(EB <= 4, "gate gradient: experts");
+    static constexpr int CT = 4, NST = kStages;
     static constexpr int kThreads = 64 * NW, CW = 16 * CT, BC = NW * CW;        // columns of a wave, of a workgroup of NW
     static constexpr int EP = EB == 1 ? 32 : 16 * EB;               // experts, in whole steps of the sum of dx
     static constexpr int KS = EP / 32;
@@ -236,7 +247,6 @@ struct GateShape {
     static constexpr int kItems = kSplitTokens * EP / 8, kItemsEach = (kItems + kThreads - 1) / kThreads;      // 8 neighbours of dl
     static constexpr int kLoadsX = kX / 1024, kPerRowX = CW / 8;
     static constexpr int kOut = CT / 2;                             // pieces of a token's columns in a lane
-    static_assert(CT == 2 || CT == 4, "gate gradient: columns");
     // accesses that every step issues after a stage's: the stages behind it and, for two steps, dadd and stores.  (dl is waited for by its use, and a wave
     // without a part in it may skip its loads.)  Before the first step: the stages and dadd.
     static constexpr int kSurely = (NST - 2) * kLoadsX + 3 * 2 * kOut, kFirst = (NST - 2) * kLoadsX + 2 * kOut;
@@ -246,11 +256,12 @@ struct GateShape {
     static_assert(NST >= 3 && kYounger < 64, "gate gradient: stages");
 };
 
-template <int EB, int CT, int NW, int NST>
-__global__ __launch_bounds__(64 * NW, EB <= 8 ? 2 : 1) void gate_backward_bf16_kernel([[maybe_unused]] GateGradArgs a)
+template <int EB, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_unused]] GateGradArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using G = GateShape<EB, CT, NW, NST>;
+    using G = GateShape<EB, NW>;
+    constexpr int CT = G::CT, NST = kStages;
     extern __shared__ __align__(16) unsigned char gate_lds[];
     unsigned char *const lds_x = gate_lds, *const lds_dl = gate_lds + G::kLdsX;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
@@ -330,26 +341,8 @@ __global__ __launch_bounds__(64 * NW, EB <= 8 ? 2 : 1) void gate_backward_bf16_k
 #pragma unroll
         for (int n = 0; n < G::kItemsEach; ++n) {
             const int item = tid + G::kThreads * n, row = item / (G::EP / 8), p = item % (G::EP / 8);
-            if (G::kItems % G::kThreads == 0 || item < G::kItems) {
-                unsigned char *const to = to_dl + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16;
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = dl[n][i / 4][i % 4];
-#pragma unroll
-                for (int piece = 0; piece < 3; ++piece) {
-                    u32x4 b;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        bf16x2 two;
-                        two[0] = (__bf16)v[2 * i];
-                        two[1] = (__bf16)v[2 * i + 1];
-                        b[i] = __builtin_bit_cast(uint32_t, two);
-                        v[2 * i] -= __uint_as_float(b[i] << 16);
-                        v[2 * i + 1] -= __uint_as_float(b[i] & 0xffff0000u);
-                    }
-                    put((lds_u32x4 *)(to + piece * G::kPiece), b);
-                }
-            }
+            if (G::kItems % G::kThreads == 0 || item < G::kItems)
+                split_eight<G::kPiece>(dl[n], to_dl + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16);
         }
     };
 #pragma unroll
@@ -451,6 +444,204 @@ __global__ __launch_bounds__(64 * NW, EB <= 8 ? 2 : 1) void gate_backward_bf16_k
 #endif
 }
 
+// More than 64 experts: what is read from LDS for each product grows with the experts that a wave has, so eight waves share both sums another way.
+//   dw: a wave has 64 experts and 64 columns.
+//   dx: a wave has 16 tokens of the step, all experts and a quarter of the workgroup's columns; the rows leave a step later, when all waves have written
+//       their parts of them.
+template <int EB>
+struct GateWide {
+    static_assert(EB == 8 || EB == 16, "wide gate gradient: experts");
+    static constexpr int NST = kStages, kWaves = 8, kThreads = 64 * kWaves, kGroups = EB / 4, kColumnGroups = kWaves / kGroups, BC = 64 * kColumnGroups;
+    static constexpr int DC = BC / 4, CD = DC / 16, kOut = CD / 2;  // columns of a wave's part of dx, tiles, pieces of 16 bytes in a lane
+    static constexpr int EP = 16 * EB, KS = EP / 32;
+    static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece, kItemsEach = kSplitTokens * EP / 8 / kThreads;
+    static constexpr int kRowX = 2 * BC, kX = kSplitTokens * kRowX, kLoadsX = kX / 1024 / kWaves, kPerRowX = BC / 8;
+    static constexpr int kLdsX = NST * kX, kLdsOut = 2 * kX, kLdsBytes = kLdsX + kLdsOut + 2 * kDl;
+    // as in GateShape
+    static constexpr int kSurely = (NST - 2) * kLoadsX + kLoadsX + kOut, kFirst = (NST - 2) * kLoadsX + kOut;
+    static constexpr int kLate = (NST - 2) * kLoadsX + 2 * kItemsEach, kYounger = kLate < kSurely ? kLate : kSurely;
+    static constexpr int wait_for(int vmcnt) { return 0x0070 | (vmcnt & 15) | ((vmcnt >> 4) << 14); }      // and lgkmcnt(0)
+    static_assert(NST >= 3 && kLdsBytes <= 160 * 1024, "wide gate gradient: stages");
+};
+
+template <int EB>
+__global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unused]] GateGradArgs a)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    using G = GateWide<EB>;
+    constexpr int NST = kStages;
+    extern __shared__ __align__(16) unsigned char gate_lds[];
+    unsigned char *const lds_x = gate_lds, *const lds_out = lds_x + G::kLdsX, *const lds_dl = lds_out + G::kLdsOut;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int group = wave / G::kColumnGroups, column = wave % G::kColumnGroups, half = wave / 4, quarter = wave % 4;
+    const GatePart part = gate_part(a, blockIdx.x, G::BC);
+    const int H = a.H, E = a.E;
+    const uint32_t pitch = (uint32_t)H * 2;
+    const bool whole4 = (E & 3) == 0;
+    // what a descriptor may reach of `rows` rows, from the first one's column part.col on: nothing of no rows, and nothing past the last column
+    auto bytes_of = [&](int rows) { return rows > 0 ? (uint32_t)rows * pitch - (uint32_t)part.col * 2u : 0u; };
+
+    f32x4 sum[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[j][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+    uint32_t at_x[G::kLoadsX], at_o[G::kOut];
+#pragma unroll
+    for (int q = 0; q < G::kLoadsX; ++q) {                         // the place in LDS is fixed by the instruction, so the swizzle is applied here
+        const int row = ((wave * G::kLoadsX + q) * 64 + lane) / G::kPerRowX, at = lane % G::kPerRowX, p = ((at >> 1) ^ row_swizzle<G::BC>(row)) * 2 + (at & 1);
+        at_x[q] = part.col + p * 8 < H ? (uint32_t)row * pitch + (uint32_t)p * 16u : kOutOfRange;
+    }
+#pragma unroll
+    for (int q = 0; q < G::kOut; ++q) {
+        const int h = quarter * G::DC + 32 * q + 8 * g;
+        at_o[q] = part.col + h < H ? (uint32_t)(16 * half + m) * pitch + (uint32_t)h * 2u : kOutOfRange;
+    }
+    const int64_t first = (int64_t)part.share * kSplitTokens, stride = (int64_t)a.shares * kSplitTokens;
+    auto rows_at = [&](int64_t t0) { return __builtin_amdgcn_readfirstlane((int)max((int64_t)0, min((int64_t)kSplitTokens, a.T - t0))); };
+    auto issue = [&](int64_t t0, int stage) {
+        const auto from = make_rsrc(static_cast<const __bf16 *>(a.x) + (t0 * H + part.col), a.dw ? bytes_of(rows_at(t0)) : 0u);
+#pragma unroll
+        for (int q = 0; q < G::kLoadsX; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(lds_x + stage + (wave * G::kLoadsX + q) * 1024), 16, at_x[q], 0, 0, kNt);
+    };
+    u32x4 add[G::kOut];
+    f32x4 dl[G::kItemsEach][2];
+    auto fetch_dl = [&](int64_t t0) {
+        const auto from = make_rsrc(a.dl + t0 * E, (uint32_t)rows_at(t0) * (uint32_t)E * 4u);
+#pragma unroll
+        for (int n = 0; n < G::kItemsEach; ++n) {
+            const int item = tid + G::kThreads * n, row = item / (G::EP / 8), e0 = item % (G::EP / 8) * 8;
+            const uint32_t at = ((uint32_t)row * (uint32_t)E + (uint32_t)e0) * 4u;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                if (whole4) {
+                    dl[n][v] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, e0 + 4 * v < E ? at + 16u * v : kOutOfRange, 0, 0));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        dl[n][v][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, e0 + 4 * v + i < E ? at + 16u * v + 4u * i : kOutOfRange, 0, 0));
+                }
+            }
+        }
+    };
+    auto fetch_add = [&](int64_t t0) {
+        const auto from = make_rsrc(static_cast<const __bf16 *>(a.dadd) + (t0 * H + part.col), a.dadd ? bytes_of(rows_at(t0)) : 0u);
+#pragma unroll
+        for (int q = 0; q < G::kOut; ++q) add[q] = __builtin_amdgcn_raw_buffer_load_b128(from, at_o[q], 0, kNt);
+    };
+    auto split = [&](unsigned char *to_dl) {
+#pragma unroll
+        for (int n = 0; n < G::kItemsEach; ++n) {
+            const int item = tid + G::kThreads * n, row = item / (G::EP / 8), p = item % (G::EP / 8);
+            split_eight<G::kPiece>(dl[n], to_dl + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16);
+        }
+    };
+    auto leave = [&](int64_t t0, const unsigned char *from, uint32_t bytes) {
+        const auto to = make_rsrc(static_cast<__bf16 *>(a.dx) + (t0 * H + part.col), a.dx ? bytes : 0u);
+#pragma unroll
+        for (int q = 0; q < G::kLoadsX; ++q)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, read_along((lds_bf16x8 *)(from + (wave * G::kLoadsX + q) * 1024 + lane * 16))), to,
+                                                   at_x[q], 0, kNt);
+    };
+
+    const int ka = 8 * g + (m >> 2), across_x = ka * G::kRowX + (m & 3) * 8, across_dl = ka * G::kRow + (m & 3) * 8, along_dl = (16 * half + m) * G::kRow + (g & 1) * 16;
+    const int sx = row_swizzle<G::BC>(ka) * 32, sd = row_swizzle<G::EP>(ka) * 32, sl = row_swizzle<G::EP>(m) * 32, so = row_swizzle<G::BC>(m) * 32;
+
+#pragma unroll
+    for (int q = 0; q < NST - 1; ++q) {
+        if (q == NST - 2) {
+            fetch_dl(first);
+            fetch_add(first);
+        }
+        issue(first + q * stride, q * G::kX);
+    }
+    bf16x8 w[G::KS][G::CD];
+#pragma unroll
+    for (int ks = 0; ks < G::KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < G::CD; ++i) {
+            const int h = part.col + quarter * G::DC + 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int e = 32 * ks + 8 * g + j;
+                w[ks][i][j] = a.dx && e < E && h < H ? static_cast<const __bf16 *>(a.w)[(int64_t)e * H + h] : (__bf16)0.f;
+            }
+        }
+    int buf = 0, stage = 0, out_at = 0;
+    __builtin_amdgcn_s_waitcnt(G::wait_for(G::kFirst));
+    split(lds_dl);
+    fetch_dl(first + stride);
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    int64_t t0 = first;
+    for (; t0 < a.T; t0 += stride) {
+        f32x4 out[G::CD];
+#pragma unroll
+        for (int i = 0; i < G::CD; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const uint32_t word = add[i / 2][i % 2 * 2 + v / 2];
+                out[i][v] = __uint_as_float(v % 2 ? word & 0xffff0000u : word << 16);
+            }
+        __builtin_amdgcn_s_waitcnt(G::wait_for(G::kYounger));      // this step's x has landed, this wave's parts of dl and of the last rows of dx are written
+        barrier();                                                 // of two buffers of dl and dx the other one has been read by all before this
+        leave(t0 - stride, lds_out + (G::kX - out_at), t0 > first ? bytes_of(rows_at(t0 - stride)) : 0u);
+        fetch_add(t0 + stride);
+        issue(t0 + (NST - 1) * stride, stage == 0 ? (NST - 1) * G::kX : stage - G::kX);       // where the step before was
+
+        const unsigned char *const dls = lds_dl + buf, *const xs = lds_x + stage;
+        bf16x8 fx[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) fx[i] = read_across((lds_s16x4 *)(xs + across_x + (((column * 4 + i) * 32) ^ sx)), 4 * G::kRowX);
+#pragma unroll
+        for (int ks = 0; ks < G::KS; ++ks)
+#pragma unroll
+            for (int piece = 0; piece < 2; ++piece) {
+                const bf16x8 b = read_along((lds_bf16x8 *)(dls + piece * G::kPiece + along_dl + (((2 * ks + (g >> 1)) * 32) ^ sl)));
+#pragma unroll
+                for (int i = 0; i < G::CD; ++i) out[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[ks][i], b, out[i], 0, 0, 0);
+            }
+#pragma unroll
+        for (int q = 0; q < G::kOut; ++q) {
+            bf16x8 o;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) o[v] = (__bf16)out[2 * q + v / 4][v % 4];
+            const int c = quarter * (G::DC / 8) + 4 * q + g;       // its piece of the row
+            put((lds_u32x4 *)(lds_out + out_at + (16 * half + m) * G::kRowX + ((c >> 1) * 32 ^ so) + (c & 1) * 16), __builtin_bit_cast(u32x4, o));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int piece = 0; piece < 3; ++piece) {
+                const bf16x8 b = read_across((lds_s16x4 *)(dls + piece * G::kPiece + across_dl + (((group * 4 + j) * 32) ^ sd)), 4 * G::kRow);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], b, sum[j][i], 0, 0, 0);
+            }
+        buf ^= G::kDl;
+        split(lds_dl + buf);                                       // for the next step, among this one's products
+        fetch_dl(t0 + 2 * stride);
+        stage = stage == (NST - 1) * G::kX ? 0 : stage + G::kX;
+        out_at = G::kX - out_at;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);                            // the loads past the end have come back: the LDS is another workgroup's after this
+    barrier();
+    leave(t0 - stride, lds_out + (G::kX - out_at), bytes_of(rows_at(t0 - stride)));
+    if (a.dw)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 16 * (group * 4 + j) + m, h = part.col + column * 64 + 16 * i + 4 * g;
+                if (e < E && h < H) *reinterpret_cast<f32x4 *>(a.dw + ((int64_t)part.share * E + e) * H + h) = sum[j][i];
+            }
+#endif
+}
+
 // Adds the shares' sums: a workgroup takes 32 vectors of them, its eight groups of 32 lanes every eighth share each, four loads at a time.
 __global__ __launch_bounds__(256) void gate_dweight_kernel(const f32x4 *partial, f32x4 *dw, int shares, int64_t n)
 {
@@ -477,11 +668,22 @@ __global__ __launch_bounds__(256) void gate_dweight_kernel(const f32x4 *partial,
 
 // --------------------------------------------------------------------------------------------- host
 
-template <int EB, int CT, int NW, int NST>
+template <int EB>
+int launch_wide(const GateGradArgs &a, hipStream_t st)
+{
+    using G = GateWide<EB>;
+    const auto kernel = gate_backward_wide_kernel<EB>;
+    static LdsOptIn opted;
+    if (int rc = opt_in_lds(reinterpret_cast<const void *>(kernel), G::kLdsBytes, opted)) return rc;
+    hipLaunchKernelGGL(kernel, dim3(a.blocks * a.shares), dim3(G::kThreads), G::kLdsBytes, st, a);
+    return MONTA_OK;
+}
+
+template <int EB, int NW>
 int launch_split(const GateGradArgs &a, hipStream_t st)
 {
-    using G = GateShape<EB, CT, NW, NST>;
-    const auto kernel = gate_backward_bf16_kernel<EB, CT, NW, NST>;
+    using G = GateShape<EB, NW>;
+    const auto kernel = gate_backward_bf16_kernel<EB, NW>;
     static LdsOptIn opted;
     if (int rc = opt_in_lds(reinterpret_cast<const void *>(kernel), G::kLdsBytes, opted)) return rc;
     hipLaunchKernelGGL(kernel, dim3(a.blocks * a.shares), dim3(G::kThreads), G::kLdsBytes, st, a);
@@ -500,13 +702,10 @@ int with_expert_blocks(int E, F f)
     return f(integral_constant<int, 16>{});
 }
 
-template <int EB>
-constexpr int split_tiles_of() { return EB <= 4 ? 4 : 2; }
-
-// Eight waves share the split gradients, four times more columns are waited for together: from 2^27 elements on, where splitting takes time (33 to 128 experts;
-// us, four waves twice a CU, four waves and eight: 65536 x 7168, 64 experts 368, 407 and 363; 32768 x 4096, 128 experts 198, 223 and 186;
-// 8192 x 7168, 64 experts 85, 79 and 85; 512 x 2048, 64 experts 14, 14 and 20; but 65536 x 7168, 32 experts 363, 325 and 340).
-bool eight_waves(const Call &c, int eb) { return c.bf16 && (eb == 4 || eb == 8) && (int64_t)c.s.T * c.H >= (1 << 27); }
+// Eight waves share the split gradients of up to 64 experts, and twice as many columns are waited for together: from 2^27 elements on, where splitting takes time
+// (33 to 64 experts; us, four waves twice a CU, four waves and eight: 65536 x 7168 368, 407 and 363; 8192 x 7168 85, 79 and 85; 512 x 2048 14, 14 and 20;
+// but 65536 x 7168 with 32 experts 363, 325 and 340).
+bool eight_waves(const Call &c) { return (int64_t)c.s.T * c.H >= (1 << 27); }
 
 struct GatePlan {
     int blocks, shares;
@@ -514,8 +713,11 @@ struct GatePlan {
 
 GatePlan plan_gate_grad(const Call &c)
 {
-    const int width = with_expert_blocks(c.s.E, [&](auto eb) { constexpr int EB = decltype(eb)::value;
-        return (eight_waves(c, EB) ? 8 : 4) * 16 * (c.bf16 ? split_tiles_of<EB>() : tiles_of<EB>());
+    const int width = with_expert_blocks(c.s.E, [&](auto eb) {
+        constexpr int EB = decltype(eb)::value;
+        if (!c.bf16) return 64 * tiles_of<EB>();
+        if constexpr (EB > 4) return (int)GateWide<EB>::BC;
+        return EB == 4 && eight_waves(c) ? 512 : 256;
     });
     GatePlan p;
     p.blocks = (c.H + width - 1) / width;
@@ -576,10 +778,13 @@ int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *
         LaunchTimer timer(MONTA_K_GATE_BACKWARD, st);
         const int rc = with_expert_blocks(c.s.E, [&](auto eb) {
             constexpr int EB = decltype(eb)::value;
-            if constexpr (EB == 4 || EB == 8)
-                if (eight_waves(c, EB)) return launch_split<EB, split_tiles_of<EB>(), 8, 3>(a, st);
-            if (c.bf16) return launch_split<EB, split_tiles_of<EB>(), 4, 3>(a, st);
-            hipLaunchKernelGGL((gate_backward_kernel<false, EB>), dim3(p.blocks * p.shares), dim3(256), 0, st, a);
+            if (c.bf16) {
+                if constexpr (EB == 4)
+                    if (eight_waves(c)) return launch_split<EB, 8>(a, st);
+                if constexpr (EB > 4) return launch_wide<EB>(a, st);
+                else return launch_split<EB, 4>(a, st);
+            }
+            hipLaunchKernelGGL((gate_backward_f32_kernel<EB>), dim3(p.blocks * p.shares), dim3(256), 0, st, a);
             return (int)MONTA_OK;
         });
         if (rc) return rc;

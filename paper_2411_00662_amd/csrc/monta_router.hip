@@ -94,8 +94,17 @@ __device__ __forceinline__ void load_row(f32x4 (&v)[V], const float *row, int l,
 //   balance = sum_e f[e] P[e],   z = mean of lse[t]^2.
 // A workgroup sums a run of tokens; its E + 1 sums and E + 1 counts are a column each of `partial`, one word a workgroup, which
 // route_loss_join_kernel adds, a wave a column.  One workgroup alone finishes by itself.
+// A workgroup of the join has eight experts (all of them in one take 12 us for 256 experts and 4.4 for 64, which is what a CU takes to fetch the columns).
+// The balance loss is the sum of their shares, which the last one to arrive adds, in the experts' order: who that is says a counter, which the
+// kernel before has cleared.
 
-constexpr int kLossThreads = 512, kLossWaves = kLossThreads / kWave, kLossGrid = 256, kMaxExperts = 256;
+constexpr int kLossThreads = 1024, kLossWaves = kLossThreads / kWave, kLossGrid = 256, kMaxExperts = 256;
+constexpr int kJoinExperts = 8, kMostJoins = kMaxExperts / kJoinExperts;        // experts of a workgroup that joins
+static_assert(kMostJoins <= kWave, "a lane has a workgroup's share");
+
+// Words of `partial`: 2 (E + 1) columns of G, then the counter, then the joins' shares.
+__host__ __device__ constexpr int64_t loss_counter(int E, int G) { return 2 * (int64_t)(E + 1) * G; }
+inline int64_t loss_scratch(int E, int G) { return (loss_counter(E, G) + 1 + kMostJoins) * 4; }
 
 struct LossOut {
     float *losses;
@@ -103,35 +112,28 @@ struct LossOut {
     float *means;
 };
 
-// Sums and counts of all tokens, in LDS (index E: the squares of lse, the tokens), to the results; the first 256 threads of the workgroup, after
-// a barrier.  `part`: four words of LDS.
-__device__ __forceinline__ void finish_losses(const float *sums, const int32_t *cnt, float *part, const LossOut &o, int E, int k)
+// Mean probability, count and share of the balance loss of expert e, from its sums over the n tokens.
+__device__ __forceinline__ float finish_expert(const LossOut &o, int e, float sum, int count, int n, int E, int k)
 {
-    const int e = threadIdx.x;
-    const int n = cnt[E];
-    float f = 0.f;
-    if (e < E) {
-        const float mean = n > 0 ? sums[e] / (float)n : 0.f;
-        f = n > 0 ? (float)cnt[e] * ((float)E / (float)k) / (float)n * mean : 0.f;
-        o.means[e] = mean;
-        o.counts[e] = cnt[e];
-    }
-    f = group_sum<kWave>(f);
-    if (e % kWave == 0 && e < kMaxExperts) part[e / kWave] = f;
-    __syncthreads();
-    if (e == 0) {
-        o.losses[0] = (part[0] + part[1]) + (part[2] + part[3]);
-        o.losses[1] = n > 0 ? sums[E] / (float)n : 0.f;
-        o.counts[E] = n;
-    }
+    const float mean = n > 0 ? sum / (float)n : 0.f;
+    o.means[e] = mean;
+    o.counts[e] = count;
+    return n > 0 ? (float)count * ((float)E / (float)k) / (float)n * mean : 0.f;
+}
+
+__device__ __forceinline__ void finish_losses(const LossOut &o, float balance, float z, int n, int E)
+{
+    o.losses[0] = balance;
+    o.losses[1] = n > 0 ? z / (float)n : 0.f;
+    o.counts[E] = n;
 }
 
 template <int L, int V>
 __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *logits, const int32_t *idx, const uint8_t *mask, float *partial, LossOut o,
                                                                   int T, int E, int k, int per)
 {
-    constexpr int kTokens = kLossThreads / L, kAtOnce = V == 1 ? 4 : 2;         // tokens of a round; rounds whose logits are requested together
-    __shared__ float sums[kLossWaves][kMaxExperts + 1], all[kMaxExperts + 1], part[4];
+    constexpr int kTokens = kLossThreads / L, kAtOnce = V == 1 ? 2 : 1;         // tokens of a round; rounds whose logits are requested together
+    __shared__ float sums[kLossWaves][kMaxExperts + 1], all[kMaxExperts + 1], part[kMaxExperts / kWave];
     __shared__ int32_t cnt[kMaxExperts + 1];
     const int tid = threadIdx.x, l = tid % L, wave = tid / kWave;
     for (int i = tid; i <= E; i += kLossThreads) cnt[i] = 0;
@@ -206,47 +208,60 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
             reinterpret_cast<int32_t *>(partial)[(int64_t)(E + 1 + i) * gridDim.x + blockIdx.x] = cnt[i];
         }
     }
-    if (alone) {
-        __syncthreads();
-        finish_losses(all, cnt, part, o, E, k);
-    }
-}
-
-// A column is a load of a wave; nine columns' loads at a time (one at a time, 64 experts take 6.0 us, of which JJJ here).
-__global__ __launch_bounds__(1024) void route_loss_join_kernel(const float *partial, LossOut o, int G, int E, int k)
-{
-    constexpr int kWaves = 1024 / kWave, kColumns = 9;
-    static_assert(kLossGrid == 4 * kWave, "a lane has four words of a column");
-    __shared__ float all[kMaxExperts + 1], part[4];
-    __shared__ int32_t cnt[kMaxExperts + 1];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, columns = 2 * (E + 1);
-    for (int c0 = wave; c0 < columns; c0 += kColumns * kWaves) {
-        f32x4 v[kColumns];
-#pragma unroll
-        for (int q = 0; q < kColumns; ++q) {
-            const int c = c0 + q * kWaves;
-            v[q] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (c < columns) v[q] = load_some(partial + (int64_t)c * G + 4 * lane, G - 4 * lane, 0.f);
-        }
-#pragma unroll
-        for (int q = 0; q < kColumns; ++q) {
-            const int c = c0 + q * kWaves;
-            if (c >= columns) break;                               // the whole wave
-            if (c <= E) {
-                const float t = group_sum<kWave>((v[q][0] + v[q][1]) + (v[q][2] + v[q][3]));
-                if (lane == 0) all[c] = t;
-            } else {
-                int n = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) n += __float_as_int(v[q][i]);
-#pragma unroll
-                for (int d = 1; d < kWave; d <<= 1) n += __shfl_xor(n, d, kWave);
-                if (lane == 0) cnt[c - E - 1] = n;
-            }
-        }
+    if (!alone) {
+        if (blockIdx.x == 0 && tid == 0) reinterpret_cast<int32_t *>(partial)[loss_counter(E, gridDim.x)] = 0;
+        return;
     }
     __syncthreads();
-    finish_losses(all, cnt, part, o, E, k);
+    const float f = group_sum<kWave>(tid < E ? finish_expert(o, tid, all[tid], cnt[tid], cnt[E], E, k) : 0.f);
+    if (tid < kMaxExperts && tid % kWave == 0) part[tid / kWave] = f;
+    __syncthreads();
+    if (tid == 0) finish_losses(o, (part[0] + part[1]) + (part[2] + part[3]), all[E], cnt[E], E);
+}
+
+__global__ __launch_bounds__(256) void route_loss_join_kernel(float *partial, LossOut o, int G, int E, int k)
+{
+    constexpr int kWaves = 4, kEach = kJoinExperts / kWaves;        // experts of a wave
+    static_assert(kLossGrid == 4 * kWave, "a lane has four words of a column");
+    __shared__ float part[kWaves];
+    __shared__ int last;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, e0 = blockIdx.x * kJoinExperts + wave * kEach;
+    auto column = [&](int c) { return load_some(partial + (int64_t)c * G + 4 * lane, G - 4 * lane, 0.f); };
+    auto total = [](f32x4 v) { return group_sum<kWave>((v[0] + v[1]) + (v[2] + v[3])); };
+    auto count = [](f32x4 v) {
+        int n = (__float_as_int(v[0]) + __float_as_int(v[1])) + (__float_as_int(v[2]) + __float_as_int(v[3]));
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) n += __shfl_xor(n, d, kWave);
+        return n;
+    };
+    f32x4 sums[kEach], counts[kEach];
+    const f32x4 tokens = column(2 * E + 1), squares = column(E);
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        const int e = min(e0 + q, E - 1);
+        sums[q] = column(e);
+        counts[q] = column(E + 1 + e);
+    }
+    const int n = count(tokens);
+    const float z = total(squares);
+    float f = 0.f;
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        const float sum = total(sums[q]);
+        const int c = count(counts[q]);
+        if (e0 + q < E && lane == 0) f += finish_expert(o, e0 + q, sum, c, n, E, k);
+    }
+    if (lane == 0) part[wave] = f;
+    __syncthreads();
+    float *const shares = partial + loss_counter(E, G) + 1;
+    if (tid == 0) {
+        __hip_atomic_store(shares + blockIdx.x, (part[0] + part[1]) + (part[2] + part[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = __hip_atomic_fetch_add(reinterpret_cast<int32_t *>(shares - 1), 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last || wave != 0) return;
+    const float balance = group_sum<kWave>(lane < (int)gridDim.x ? __hip_atomic_load(shares + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.f);
+    if (lane == 0) finish_losses(o, balance, z, n, E);
 }
 
 // --------------------------------------------------------------------------------------------- gradient by the logits
@@ -393,10 +408,11 @@ int lanes_of(int E)
 }
 
 // workgroups of the losses: whole rounds of tokens each
+constexpr int kAlone = 4;         // up to so many one workgroup takes them alone: 256 tokens over 64 experts 5.7 us, two launches 9.0; eight rounds 12.5 and 8.8
 int loss_grid(const Shape &s, int *per)
 {
     const int64_t round = kLossThreads / lanes_of(s.E), rounds = (s.T + round - 1) / round;
-    const int64_t each = (rounds + kLossGrid - 1) / kLossGrid;
+    const int64_t each = rounds <= kAlone ? rounds : (rounds + kLossGrid - 1) / kLossGrid;
     *per = (int)std::min<int64_t>(each * round, 0x7fffffff);
     return (int)((rounds + each - 1) / each);
 }
@@ -414,7 +430,7 @@ int monta_route_loss_scratch_bytes(const monta_cfg *cfg, size_t *bytes)
     Call c;
     if (int rc = open_call(cfg, nullptr, &c)) return rc;
     int per;
-    *bytes = (size_t)loss_grid(c.s, &per) * 2 * (c.s.E + 1) * 4;
+    *bytes = (size_t)loss_scratch(c.s.E, loss_grid(c.s, &per));
     return MONTA_OK;
 }
 
@@ -433,7 +449,7 @@ int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *t
         const void *p;
         int64_t n;
     } read[] = {{logits, T * E * 4}, {topk_idx, T * c.s.k * 4}, {token_mask, T}},
-      written[] = {{losses, 8}, {counts, (E + 1) * 4}, {means, E * 4}, {scratch, (int64_t)grid * 2 * (E + 1) * 4}};
+      written[] = {{losses, 8}, {counts, (E + 1) * 4}, {means, E * 4}, {scratch, loss_scratch(c.s.E, grid)}};
     for (const auto &w : written) {
         for (const auto &r : read)
             if (r.p && overlap(w.p, w.n, r.p, r.n)) return MONTA_ERR_INVALID;
@@ -451,7 +467,7 @@ int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *t
     });
     MONTA_HIP_TRY(hipGetLastError());
     if (grid > 1) {
-        hipLaunchKernelGGL(route_loss_join_kernel, dim3(1), dim3(1024), 0, st, partial, o, grid, c.s.E, c.s.k);
+        hipLaunchKernelGGL(route_loss_join_kernel, dim3((c.s.E + kJoinExperts - 1) / kJoinExperts), dim3(256), 0, st, partial, o, grid, c.s.E, c.s.k);
         MONTA_HIP_TRY(hipGetLastError());
     }
     return MONTA_OK;

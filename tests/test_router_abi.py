@@ -78,7 +78,7 @@ def test_route_loss_sizes():
     assert B.lib().monta_route_loss_scratch_bytes(ctypes.byref(cfg()), None) == -3
     for tokens, experts in ((1, 1), (65536, 64), (2 ** 31 - 1, 256), (2 ** 31 - 1, 1), (8191, 255)):
         n = m.monta_route_loss_scratch_bytes(cfg(tokens=tokens, experts=experts, top_k=1, slices=1))
-        assert 8 * (experts + 1) <= n <= 512 * 8 * (experts + 1)
+        assert 8 * (experts + 1) <= n <= 1024 + 512 * 8 * (experts + 1)
 
 
 def route_backward(c, logits=A[0], idx=A[1], gates=A[2], dgates=A[3], mask=A[4], dlosses=A[5], counts=A[6], dlogits=A[7]):
