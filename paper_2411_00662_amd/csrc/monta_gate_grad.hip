@@ -9,7 +9,6 @@ namespace monta {
 namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 struct GateGradArgs {
     const float *dl;
@@ -234,6 +233,28 @@ template <int pitch>
     }
 }
 
+// The weights of BC columns from `col` on, rows of experts, zeros past the last expert and column, to LDS by all waves.
+template <int EP, int BC, int kThreads>
+[[maybe_unused]] __device__ __forceinline__ void fetch_weights(const GateGradArgs &a, int col, unsigned char *lds, int wave, int lane)
+{
+    constexpr int kLoads = EP * BC * 2 / 16 / kThreads, kPerRow = BC / 8;
+    const uint32_t pitch = (uint32_t)a.H * 2;
+    const auto from = make_rsrc(static_cast<const __bf16 *>(a.w) + col, a.dx ? (uint32_t)a.E * pitch - (uint32_t)col * 2u : 0u);
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) {
+        const int at = (wave * kLoads + q) * 64 + lane, row = at / kPerRow, p = at % kPerRow;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(lds + (wave * kLoads + q) * 1024), 16,
+                                                 col + p * 8 < a.H ? (uint32_t)row * pitch + (uint32_t)p * 16u : kOutOfRange, 0, 0, 0);
+    }
+}
+
+// Tile i of those, experts 32 ks to 32 ks + 31, of the columns from `first` on: row r is column 32 (i / 2) + 8 (r / 4) + 4 (i % 2) + r % 4 of them.
+template <int BC>
+[[maybe_unused]] __device__ __forceinline__ bf16x8 weight_fragment(unsigned char *lds, int first, int ks, int i, int m, int g)
+{
+    return read_across((lds_s16x4 *)(lds + (32 * ks + 8 * g + (m >> 2)) * (2 * BC) + first * 2 + i / 2 * 64 + (m & 3) * 16 + i % 2 * 8), 4 * 2 * BC);
+}
+
 template <int EB, int NW>
 struct GateShape {
     static_assert(EB <= 4, "gate gradient: experts");
@@ -244,13 +265,14 @@ struct GateShape {
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece;
     static constexpr int kRowX = 2 * CW, kX = kSplitTokens * kRowX;
     static constexpr int kLdsX = NW * NST * kX, kLdsBytes = kLdsX + 2 * kDl;
+    static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // at the end, before the first step
     static constexpr int kItems = kSplitTokens * EP / 8, kItemsEach = (kItems + kThreads - 1) / kThreads;      // 8 neighbours of dl
     static constexpr int kLoadsX = kX / 1024, kPerRowX = CW / 8;
     static constexpr int kOut = CT / 2;                             // pieces of a token's columns in a lane
-    // accesses that every step issues after a stage's: the stages behind it and, for two steps, dadd and stores.  (dl is waited for by its use, and a wave
-    // without a part in it may skip its loads.)  Before the first step: the stages and dadd.
-    static constexpr int kSurely = (NST - 2) * kLoadsX + 3 * 2 * kOut, kFirst = (NST - 2) * kLoadsX + 2 * kOut;
-    static constexpr int kLate = kFirst + 2 * kItemsEach;           // those that need not have come back: the stages, the stores, dl
+    // accesses that every step issues after a stage's: the stages behind it, dadd and stores.  (dl is waited for by its use, and a wave
+    // without a part in it may skip its loads.)  Before the first step: the stages.
+    static constexpr int kSurely = (NST - 2) * kLoadsX + 2 * 2 * kOut, kFirst = (NST - 2) * kLoadsX;
+    static constexpr int kLate = kFirst + 2 * kOut + 2 * kItemsEach;           // those that need not have come back: the stages, the stores, dl
     static constexpr int kYounger = kLate < kSurely ? kLate : kSurely;
     static constexpr int wait_for(int vmcnt) { return 0x0070 | (vmcnt & 15) | ((vmcnt >> 4) << 14); }      // and lgkmcnt(0)
     static_assert(NST >= 3 && kYounger < 64, "gate gradient: stages");
@@ -302,6 +324,11 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
 #pragma unroll
         for (int q = 0; q < G::kLoadsX; ++q) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(my_x + stage + q * 1024), 16, at_x[q], 0, 0, kNt);
     };
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
     u32x4 add[2][G::kOut];
     f32x4 dl[G::kItemsEach][2];
     auto fetch_dl = [&](int64_t t0) {
@@ -345,26 +372,20 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
                 split_eight<G::kPiece>(dl[n], to_dl + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16);
         }
     };
-#pragma unroll
-    for (int q = 0; q < NST - 1; ++q) {
-        if (q == NST - 2) {
-            fetch_dl(first);
-            fetch_add(first);
-        }
-        issue(first + q * stride, q * G::kX);
-    }
+    fetch_weights<G::EP, G::BC, G::kThreads>(a, part.col, gate_lds + G::kAtWeights, wave, lane);
+    fetch_dl(first);
+    fetch_add(first);
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    barrier();
     bf16x8 w[G::KS][CT];
 #pragma unroll
     for (int ks = 0; ks < G::KS; ++ks)
 #pragma unroll
-        for (int i = 0; i < CT; ++i) {
-            const int h = col + 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3);
+        for (int i = 0; i < CT; ++i) w[ks][i] = weight_fragment<G::BC>(gate_lds + G::kAtWeights, wave * G::CW, ks, i, m, g);
+    __builtin_amdgcn_s_waitcnt(0xc07f);                            // lgkmcnt(0): read by this wave, and behind the barrier by all
+    barrier();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int e = 32 * ks + 8 * g + j;
-                w[ks][i][j] = a.dx && e < E && h < H ? static_cast<const __bf16 *>(a.w)[(int64_t)e * H + h] : (__bf16)0.f;
-            }
-        }
+    for (int q = 0; q < NST - 1; ++q) issue(first + q * stride, q * G::kX);
     int buf = 0, stage = 0;
     __builtin_amdgcn_s_waitcnt(G::wait_for(G::kFirst));
     split(lds_dl);
@@ -381,9 +402,7 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
                     out[half][i][v] = __uint_as_float(v % 2 ? word & 0xffff0000u : word << 16);
                 }
         __builtin_amdgcn_s_waitcnt(G::wait_for(G::kYounger));                      // this step's x has landed, this wave's part of dl is written
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();                              // of two buffers of dl the other one has been read by all before this
-        asm volatile("" ::: "memory");
+        barrier();                                                 // of two buffers of dl the other one has been read by all before this
         fetch_add(t0 + stride);
         issue(t0 + (NST - 1) * stride, stage == 0 ? (NST - 1) * G::kX : stage - G::kX);       // where the step before was
 
@@ -457,9 +476,10 @@ struct GateWide {
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece, kItemsEach = kSplitTokens * EP / 8 / kThreads;
     static constexpr int kRowX = 2 * BC, kX = kSplitTokens * kRowX, kLoadsX = kX / 1024 / kWaves, kPerRowX = BC / 8;
     static constexpr int kLdsX = NST * kX, kLdsOut = 2 * kX, kLdsBytes = kLdsX + kLdsOut + 2 * kDl;
+    static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // at the end, before the first step
     // as in GateShape
-    static constexpr int kSurely = (NST - 2) * kLoadsX + kLoadsX + kOut, kFirst = (NST - 2) * kLoadsX + kOut;
-    static constexpr int kLate = (NST - 2) * kLoadsX + 2 * kItemsEach, kYounger = kLate < kSurely ? kLate : kSurely;
+    static constexpr int kSurely = (NST - 2) * kLoadsX + kLoadsX + kOut, kFirst = (NST - 2) * kLoadsX;
+    static constexpr int kLate = kFirst + 2 * kItemsEach, kYounger = kLate < kSurely ? kLate : kSurely;
     static constexpr int wait_for(int vmcnt) { return 0x0070 | (vmcnt & 15) | ((vmcnt >> 4) << 14); }      // and lgkmcnt(0)
     static_assert(NST >= 3 && kLdsBytes <= 160 * 1024, "wide gate gradient: stages");
 };
@@ -549,35 +569,29 @@ __global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unus
     const int ka = 8 * g + (m >> 2), across_x = ka * G::kRowX + (m & 3) * 8, across_dl = ka * G::kRow + (m & 3) * 8, along_dl = (16 * half + m) * G::kRow + (g & 1) * 16;
     const int sx = row_swizzle<G::BC>(ka) * 32, sd = row_swizzle<G::EP>(ka) * 32, sl = row_swizzle<G::EP>(m) * 32, so = row_swizzle<G::BC>(m) * 32;
 
-#pragma unroll
-    for (int q = 0; q < NST - 1; ++q) {
-        if (q == NST - 2) {
-            fetch_dl(first);
-            fetch_add(first);
-        }
-        issue(first + q * stride, q * G::kX);
-    }
-    bf16x8 w[G::KS][G::CD];
-#pragma unroll
-    for (int ks = 0; ks < G::KS; ++ks)
-#pragma unroll
-        for (int i = 0; i < G::CD; ++i) {
-            const int h = part.col + quarter * G::DC + 32 * (i / 2) + 8 * (m >> 2) + 4 * (i % 2) + (m & 3);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int e = 32 * ks + 8 * g + j;
-                w[ks][i][j] = a.dx && e < E && h < H ? static_cast<const __bf16 *>(a.w)[(int64_t)e * H + h] : (__bf16)0.f;
-            }
-        }
-    int buf = 0, stage = 0, out_at = 0;
-    __builtin_amdgcn_s_waitcnt(G::wait_for(G::kFirst));
-    split(lds_dl);
-    fetch_dl(first + stride);
     auto barrier = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    fetch_weights<G::EP, G::BC, G::kThreads>(a, part.col, gate_lds + G::kAtWeights, wave, lane);
+    fetch_dl(first);
+    fetch_add(first);
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    barrier();
+    bf16x8 w[G::KS][G::CD];
+#pragma unroll
+    for (int ks = 0; ks < G::KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < G::CD; ++i) w[ks][i] = weight_fragment<G::BC>(gate_lds + G::kAtWeights, quarter * G::DC, ks, i, m, g);
+    __builtin_amdgcn_s_waitcnt(0xc07f);                            // lgkmcnt(0): read by this wave, and behind the barrier by all
+    barrier();
+#pragma unroll
+    for (int q = 0; q < NST - 1; ++q) issue(first + q * stride, q * G::kX);
+    int buf = 0, stage = 0, out_at = 0;
+    __builtin_amdgcn_s_waitcnt(G::wait_for(G::kFirst));
+    split(lds_dl);
+    fetch_dl(first + stride);
     int64_t t0 = first;
     for (; t0 < a.T; t0 += stride) {
         f32x4 out[G::CD];
