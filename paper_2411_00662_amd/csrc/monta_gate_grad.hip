@@ -74,15 +74,6 @@ __global__ __launch_bounds__(256) void gate_backward_f32_kernel(GateGradArgs a)
     const float *const in = static_cast<const float *>(a.x), *const weights = static_cast<const float *>(a.w), *const dadd = static_cast<const float *>(a.dadd);
     float *const to_dx = static_cast<float *>(a.dx);
 
-    float w[CT][4 * EB];
-    if (want_dx)
-#pragma unroll
-        for (int kk = 0; kk < 4 * EB; ++kk)
-#pragma unroll
-            for (int i = 0; i < CT; ++i) {
-                const int e = 4 * kk + g, h = col + (m >> 2) * (4 * CT) + 4 * i + (m & 3);
-                w[i][kk] = e < a.E && h < a.H ? weights[e * H + h] : 0.f;
-            }
     f32x4 sum[EB][CT];
 #pragma unroll
     for (int j = 0; j < EB; ++j)
@@ -116,6 +107,15 @@ __global__ __launch_bounds__(256) void gate_backward_f32_kernel(GateGradArgs a)
     };
     const int64_t first = (int64_t)part.share * kStepTokens, stride = (int64_t)a.shares * kStepTokens;
     fetch(first);
+    float w[CT][4 * EB];
+    if (want_dx)
+#pragma unroll
+        for (int kk = 0; kk < 4 * EB; ++kk)
+#pragma unroll
+            for (int i = 0; i < CT; ++i) {
+                const int e = 4 * kk + g, h = col + (m >> 2) * (4 * CT) + 4 * i + (m & 3);
+                w[i][kk] = e < a.E && h < a.H ? weights[e * H + h] : 0.f;
+            }
     int buf = 0;
     for (int64_t t0 = first; t0 < a.T; t0 += stride, buf ^= 1) {
 #pragma unroll
@@ -264,18 +264,18 @@ struct GateShape {
     static constexpr int KS = EP / 32;
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece;
     static constexpr int kRowX = 2 * CW, kX = kSplitTokens * kRowX;
-    static constexpr int kLdsX = NW * NST * kX, kLdsBytes = kLdsX + 2 * kDl;
-    static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // at the end, before the first step
+    static constexpr int kStage = NW * kX, kLdsX = NST * kStage, kLdsBytes = kLdsX + 2 * kDl;
+    static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // before the first step, behind its stage
     static constexpr int kItems = kSplitTokens * EP / 8, kItemsEach = (kItems + kThreads - 1) / kThreads;      // 8 neighbours of dl
     static constexpr int kLoadsX = kX / 1024, kPerRowX = CW / 8;
     static constexpr int kOut = CT / 2;                             // pieces of a token's columns in a lane
     // accesses that every step issues after a stage's: the stages behind it, dadd and stores.  (dl is waited for by its use, and a wave
-    // without a part in it may skip its loads.)  Before the first step: the stages.
-    static constexpr int kSurely = (NST - 2) * kLoadsX + 2 * 2 * kOut, kFirst = (NST - 2) * kLoadsX;
-    static constexpr int kLate = kFirst + 2 * kOut + 2 * kItemsEach;           // those that need not have come back: the stages, the stores, dl
+    // without a part in it may skip its loads.)
+    static constexpr int kSurely = (NST - 2) * kLoadsX + 2 * 2 * kOut;
+    static constexpr int kLate = (NST - 2) * kLoadsX + 2 * kOut + 2 * kItemsEach;           // those that need not have come back: the stages, the stores, dl
     static constexpr int kYounger = kLate < kSurely ? kLate : kSurely;
     static constexpr int wait_for(int vmcnt) { return 0x0070 | (vmcnt & 15) | ((vmcnt >> 4) << 14); }      // and lgkmcnt(0)
-    static_assert(NST >= 3 && kYounger < 64, "gate gradient: stages");
+    static_assert(NST >= 3 && kYounger < 64 && kAtWeights >= kStage, "gate gradient: stages");
 };
 
 template <int EB, int NW>
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
             at_o[half][q] = col + h < H ? (uint32_t)(16 * half + m) * pitch + (uint32_t)h * 2u : kOutOfRange;
         }
 
-    unsigned char *const my_x = lds_x + wave * (NST * G::kX);
+    unsigned char *const my_x = lds_x + wave * G::kX;
     const int64_t first = (int64_t)part.share * kSplitTokens, stride = (int64_t)a.shares * kSplitTokens;
     auto rows_at = [&](int64_t t0) { return __builtin_amdgcn_readfirstlane((int)max((int64_t)0, min((int64_t)kSplitTokens, a.T - t0))); };
     auto issue = [&](int64_t t0, int stage) {
@@ -372,6 +372,7 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
                 split_eight<G::kPiece>(dl[n], to_dl + row * G::kRow + ((p >> 1) ^ row_swizzle<G::EP>(row)) * 32 + (p & 1) * 16);
         }
     };
+    issue(first, 0);
     fetch_weights<G::EP, G::BC, G::kThreads>(a, part.col, gate_lds + G::kAtWeights, wave, lane);
     fetch_dl(first);
     fetch_add(first);
@@ -385,9 +386,8 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
     __builtin_amdgcn_s_waitcnt(0xc07f);                            // lgkmcnt(0): read by this wave, and behind the barrier by all
     barrier();
 #pragma unroll
-    for (int q = 0; q < NST - 1; ++q) issue(first + q * stride, q * G::kX);
+    for (int q = 1; q < NST - 1; ++q) issue(first + q * stride, q * G::kStage);
     int buf = 0, stage = 0;
-    __builtin_amdgcn_s_waitcnt(G::wait_for(G::kFirst));
     split(lds_dl);
     fetch_dl(first + stride);
     for (int64_t t0 = first; t0 < a.T; t0 += stride) {
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
         __builtin_amdgcn_s_waitcnt(G::wait_for(G::kYounger));                      // this step's x has landed, this wave's part of dl is written
         barrier();                                                 // of two buffers of dl the other one has been read by all before this
         fetch_add(t0 + stride);
-        issue(t0 + (NST - 1) * stride, stage == 0 ? (NST - 1) * G::kX : stage - G::kX);       // where the step before was
+        issue(t0 + (NST - 1) * stride, stage == 0 ? (NST - 1) * G::kStage : stage - G::kStage);       // where the step before was
 
         const unsigned char *const dls = lds_dl + buf;
         unsigned char *const xs = my_x + stage;
@@ -449,7 +449,7 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
         buf ^= G::kDl;
         split(lds_dl + buf);                                       // for the next step, among this one's products
         fetch_dl(t0 + 2 * stride);
-        stage = stage == (NST - 1) * G::kX ? 0 : stage + G::kX;
+        stage = stage == (NST - 1) * G::kStage ? 0 : stage + G::kStage;
     }
     __builtin_amdgcn_s_waitcnt(0x0070);                            // the loads past the end have come back: the LDS is another workgroup's after this
     if (a.dw)
@@ -476,12 +476,12 @@ struct GateWide {
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece, kItemsEach = kSplitTokens * EP / 8 / kThreads;
     static constexpr int kRowX = 2 * BC, kX = kSplitTokens * kRowX, kLoadsX = kX / 1024 / kWaves, kPerRowX = BC / 8;
     static constexpr int kLdsX = NST * kX, kLdsOut = 2 * kX, kLdsBytes = kLdsX + kLdsOut + 2 * kDl;
-    static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // at the end, before the first step
+    static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // before the first step, behind its stage
     // as in GateShape
-    static constexpr int kSurely = (NST - 2) * kLoadsX + kLoadsX + kOut, kFirst = (NST - 2) * kLoadsX;
-    static constexpr int kLate = kFirst + 2 * kItemsEach, kYounger = kLate < kSurely ? kLate : kSurely;
+    static constexpr int kSurely = (NST - 2) * kLoadsX + kLoadsX + kOut;
+    static constexpr int kLate = (NST - 2) * kLoadsX + 2 * kItemsEach, kYounger = kLate < kSurely ? kLate : kSurely;
     static constexpr int wait_for(int vmcnt) { return 0x0070 | (vmcnt & 15) | ((vmcnt >> 4) << 14); }      // and lgkmcnt(0)
-    static_assert(NST >= 3 && kLdsBytes <= 160 * 1024, "wide gate gradient: stages");
+    static_assert(NST >= 3 && kLdsBytes <= 160 * 1024 && kAtWeights >= kX, "wide gate gradient: stages");
 };
 
 template <int EB>
@@ -574,6 +574,7 @@ __global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unus
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    issue(first, 0);
     fetch_weights<G::EP, G::BC, G::kThreads>(a, part.col, gate_lds + G::kAtWeights, wave, lane);
     fetch_dl(first);
     fetch_add(first);
@@ -587,9 +588,8 @@ __global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unus
     __builtin_amdgcn_s_waitcnt(0xc07f);                            // lgkmcnt(0): read by this wave, and behind the barrier by all
     barrier();
 #pragma unroll
-    for (int q = 0; q < NST - 1; ++q) issue(first + q * stride, q * G::kX);
+    for (int q = 1; q < NST - 1; ++q) issue(first + q * stride, q * G::kX);
     int buf = 0, stage = 0, out_at = 0;
-    __builtin_amdgcn_s_waitcnt(G::wait_for(G::kFirst));
     split(lds_dl);
     fetch_dl(first + stride);
     int64_t t0 = first;
@@ -735,7 +735,10 @@ GatePlan plan_gate_grad(const Call &c)
     });
     GatePlan p;
     p.blocks = (c.H + width - 1) / width;
-    p.shares = (int)std::min<int64_t>(std::max(1, (c.bf16 ? 256 : 512) / p.blocks), ((int64_t)c.s.T + 63) / 64);
+    // one step a share where there are few: 1155 x 516 fp32 8.6 us, with four steps 10.7; but up to 64 tokens alone, without a second launch: 64 x 4096 bf16 6.1
+    // us, in two shares 7.1
+    const int64_t T = c.s.T, step = c.bf16 ? kSplitTokens : kStepTokens;
+    p.shares = (int)std::min<int64_t>(std::max(1, (c.bf16 ? 256 : 512) / p.blocks), T <= 64 ? 1 : (T + step - 1) / step);
     return p;
 }
 
