@@ -39,7 +39,7 @@ __device__ __forceinline__ GatePart gate_part(const GateGradArgs &a, uint32_t bl
 //
 // fp32 activations: fp32 products on the matrix cores (16 x 16 x 4).  A wave has 16 CT columns of a step's 16 tokens and the
 // weights of its columns in registers; the gradient of the logits, which all waves of the workgroup need in both orders, goes through LDS.
-//   dx: rows h, columns t, summed over e.  Row r of tile i is column 4 CT (r / 4) + 4 i + r % 4, so that a lane gets 4 CT neighbours of one token.
+//   dx: rows h, columns t, summed over e: a lane gets 4 neighbours of one token, four lanes 64 bytes.
 //   dw: rows h, columns e, summed over t.  Row r of tile i is column CT r + i, so that a lane's elements of x are neighbours.
 
 template <int EB>
@@ -62,7 +62,7 @@ struct Piece {                  // N neighbouring elements of a row
 constexpr int kStepTokens = 16;
 
 template <int EB>
-__global__ __launch_bounds__(256) void gate_backward_f32_kernel(GateGradArgs a)
+__global__ __launch_bounds__(256, 2) void gate_backward_f32_kernel(GateGradArgs a)
 {
     constexpr int CT = tiles_of<EB>(), CW = 16 * CT, kPitch = 16 * EB + 4;
     __shared__ float dlt[2][kStepTokens][kPitch];
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void gate_backward_f32_kernel(GateGradArgs a)
         if (want_dx)
 #pragma unroll
             for (int i = 0; i < CT; ++i) {
-                const int h = col + 4 * CT * g + 4 * i;
+                const int h = col + 16 * i + 4 * g;
                 add[i].clear();
                 if (a.dadd && t0 + m < a.T && h < a.H) add[i].get(dadd + (t0 + m) * H + h);
             }
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void gate_backward_f32_kernel(GateGradArgs a)
         for (int kk = 0; kk < 4 * EB; ++kk)
 #pragma unroll
             for (int i = 0; i < CT; ++i) {
-                const int e = 4 * kk + g, h = col + (m >> 2) * (4 * CT) + 4 * i + (m & 3);
+                const int e = 4 * kk + g, h = col + 16 * i + m;
                 w[i][kk] = e < a.E && h < a.H ? weights[e * H + h] : 0.f;
             }
     int buf = 0;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void gate_backward_f32_kernel(GateGradArgs a)
             if (t0 + m < a.T)
 #pragma unroll
                 for (int i = 0; i < CT; ++i) {
-                    const int h = col + 4 * CT * g + 4 * i;
+                    const int h = col + 16 * i + 4 * g;
                     if (h >= a.H) continue;
                     *reinterpret_cast<f32x4 *>(to_dx + (t0 + m) * H + h) = out[i];
                 }
@@ -737,8 +737,11 @@ GatePlan plan_gate_grad(const Call &c)
     p.blocks = (c.H + width - 1) / width;
     // one step a share where there are few: 1155 x 516 fp32 8.6 us, with four steps 10.7; but up to 64 tokens alone, without a second launch: 64 x 4096 bf16 6.1
     // us, in two shares 7.1
+    // Workgroups: one a CU where memory is the bound, two where products are (fp32 from 33 experts on).  us, one and two a CU: 65536 x 7168 bf16, 32 experts 325 and
+    // 363, 8 experts 334 and 352 (but 131072 x 4096 364 and 356); 8192 x 4096 fp32, 8, 32, 64 and 128 experts 75.5, 79.8, 106, 195 and 76.9, 83.4, 107, 172.
+    const int wgs = c.bf16 || c.s.E <= 32 ? 256 : 512;
     const int64_t T = c.s.T, step = c.bf16 ? kSplitTokens : kStepTokens;
-    p.shares = (int)std::min<int64_t>(std::max(1, (c.bf16 ? 256 : 512) / p.blocks), T <= 64 ? 1 : (T + step - 1) / step);
+    p.shares = (int)std::min<int64_t>(std::max(1, wgs / p.blocks), T <= 64 ? 1 : (T + step - 1) / step);
     return p;
 }
 
