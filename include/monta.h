@@ -347,7 +347,7 @@ int monta_expert_linear_fp8(const monta_cfg *cfg, const void *x_rows, const void
  * bias [H] in cfg->dtype, 16-byte aligned, or NULL; every other argument, what may share memory and the limits as in monta_rmsnorm.  Sums are held in
  * fp32, those of squares around a mean that is known by then, so that a row's mean may be far larger than its spread; the squares of a row's differences
  * from its mean have to add up to a finite fp32 number, and those below 2^-149 count as zero.  A row with a NaN or an infinity gives NaN throughout; no
- * other row changes.  eps >= 0 (with eps = 0 a row of equal numbers gives NaN). */
+ * other row changes.  A row's sum has to be a finite fp32 number, too.  eps >= 0 (with eps = 0 a row of equal numbers gives NaN, or what the rounding of its mean leaves). */
 int monta_layernorm(const monta_cfg *cfg, const void *x, const void *residual, const void *weight, const void *bias, float eps, void *sum,
                     void *out, void *out_fp8, void *stream);
 
@@ -375,7 +375,7 @@ int monta_route_loss_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
  * its values counts, whatever they are.  losses [2], means [E] fp32, counts [E + 1] int32.  A logit may be -infinity (p is 0 there), not all of a
  * token's; a NaN counts as -infinity.  An index outside 0 .. E - 1 counts for no expert.  scratch 16-byte aligned, its contents are of no use
  * afterwards and calls that overlap in time need one each.  Sums are held in fp32, their order is fixed for a shape.  Nothing that is written may share
- * memory with anything else.  Uses tokens, experts and top_k of cfg (all of it is validated); needs no workspace. */
+ * memory with anything else.  +infinity, or -infinity throughout, gives NaN.  Uses tokens, experts and top_k of cfg (all of it is validated); needs no workspace. */
 int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask, float *losses, int32_t *counts,
                      float *means, void *scratch, void *stream);
 
@@ -406,7 +406,9 @@ int monta_gate_backward_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
  * dadd: the gradient that reaches x by another way (through the dispatch), or NULL.  dlogits [T][E] fp32; x, dadd, dx [T][H] and w_gate [E][H] in
  * cfg->dtype, dw_gate [E][H] fp32, all but dlogits 16-byte aligned.  Either of dx and dw_gate may be NULL (then w_gate and dadd, or x and scratch, may be, too).
  * scratch 16-byte aligned, its contents are of no use afterwards and calls that overlap in time need one each.  dx may be dadd itself; otherwise nothing
- * that is written may share memory with anything else.  All sums are fp32, and their order is fixed for a shape.  hidden at most 2^20.
+ * that is written may share memory with anything else.  All sums are fp32, and their order is fixed for a shape.  With MONTA_BF16 dlogits is multiplied
+ * in parts of 8 bits, two for dx (off by 2^-17 of a product) and three for dw_gate (2^-26), of which those below 2^-126 count as zero; an infinity so gives NaN.
+ * hidden at most 2^20.
  * Uses tokens, hidden, dtype and experts of cfg (all of it is validated); needs no workspace. */
 int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *x, const void *w_gate, const void *dadd, void *dx, float *dw_gate,
                         void *scratch, void *stream);

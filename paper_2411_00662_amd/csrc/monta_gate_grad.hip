@@ -20,10 +20,10 @@ struct GateGradArgs {
     int32_t blocks, shares;             // column blocks; shares of the tokens
 };
 
-// What workgroup `block` does: column block `col`, and of the steps of tokens every `shares`-th from the one numbered `share` on (none: share < 0).  All
-// workgroups so move through the rows together, in one window of them for each buffer: with a run of neighbouring steps for each share, 18 windows 50 MB apart,
-// 65536 x 7168 over 8 experts took 373 us, in windows of nine 340, in one RRR.  The workgroups of an XCD go through the column blocks of a share one after the
-// other, so that its dl is read from memory once and then found in the XCD's L2.
+// What workgroup `block` does: column block `col`, and of the steps of tokens every `shares`-th from the one numbered `share` on.  All workgroups so move through
+// the rows together, in one window of them for each buffer: with a run of neighbouring steps for each share 65536 x 7168 over 8 experts took 373 us in 18 runs and
+// 344 in nine, so 363 and 331.  Consecutive workgroups, which go to the XCDs in turn, have consecutive column blocks of a share: 369 us for 64 experts, 383 with
+// all blocks of a share on one XCD, although each XCD so reads dl for itself.
 struct GatePart {
     int share, col;
 };
@@ -41,6 +41,8 @@ __device__ __forceinline__ GatePart gate_part(const GateGradArgs &a, uint32_t bl
 // weights of its columns in registers; the gradient of the logits, which all waves of the workgroup need in both orders, goes through LDS.
 //   dx: rows h, columns t, summed over e: a lane gets 4 neighbours of one token, four lanes 64 bytes.
 //   dw: rows h, columns e, summed over t.  Row r of tile i is column CT r + i, so that a lane's elements of x are neighbours.
+// Up to 32 experts bound by memory (8192 x 4096, 8 experts, dadd: 402 MB in 76 us with the sums of the shares, 5.3 TB/s), from 64 on by the products, which the 16 of
+// a tile's columns or the 4 of its sum that are no experts cost too (64 experts 107 us, 80 TFLOP/s of products; a large library product reaches 151).
 
 template <int EB>
 constexpr int tiles_of() { return EB <= 4 ? 4 : 16 / EB; }
@@ -172,14 +174,18 @@ __global__ __launch_bounds__(256, 2) void gate_backward_f32_kernel(GateGradArgs 
 //
 // bf16 activations on the bf16 matrix instruction (16 x 16 x 32).  A gradient of a logit is split into bf16 numbers, each the rest of the one before
 // it: with two the products of dx, which is rounded to bf16 (2^-8), are off by 2^-17, with three those of dw, which is fp32, by 2^-26.  A step is 32 tokens; a
-// wave has 16 CT columns of it, a workgroup 64 CT.
+// wave has 64 columns of it.
 //   dx: rows h, columns t, summed over e.  The wave keeps the weights of its columns in registers.  Row r of tile i is column 32 (i / 2) + 8 (r / 4)
 //       + 4 (i % 2) + r % 4, so that a lane gets 8 neighbours of one token and four lanes 64 bytes.
 //   dw: rows h, columns e, summed over t.  Both operands lie across the summed axis: they are kept in LDS as they come, rows of 32 bytes' segments, and
 //       read by the transposing LDS read, as in the experts' gradients.  A wave's x is its own, straight from memory to LDS in a ring of stages; the
 //       split gradients are the workgroup's, in two buffers, so that a step has one barrier.
-// Loads and stores go through descriptors that end at the run's last token, and lanes past the last column hand in an address past every descriptor: no
+// dx takes the place of the step's x in LDS, the same lanes' both, and leaves in whole lines of 128 bytes past the cache: in halves of lines, as the products leave
+// it, storing alone took 282 us of 65536 x 7168 over 8 experts, so 184.
+// Loads and stores go through descriptors that end at the last token, and lanes past the last column hand in an address past every descriptor: no
 // branch, every step issues the same number of them, also past the end, and the wait for a stage of x counts the younger ones.
+// 65536 x 7168, 64 experts: 1.9 GB in 365 to 377 us, 5.0 to 5.2 TB/s, of which the matrix pipe is busy 40 %; 8 experts 334 (5.6); 8192 x 4096, 8 experts, dadd: 201 MB
+// in 36 us and 3 for the sums of the shares.  (fp32 products 1552 and 58.)
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -467,6 +473,8 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
 //   dw: a wave has 64 experts and 64 columns.
 //   dx: a wave has 16 tokens of the step, all experts and a quarter of the workgroup's columns; the rows leave a step later, when all waves have written
 //       their parts of them.
+// 16384 x 4096 with dadd, 256 experts: 196 us (in waves of 32 columns, all experts: 283), 128 experts 107: 0.45 to 0.88 PFLOP/s of bf16 products, half of the rate
+// that the matrix pipe holds; the steps of both waves of a SIMD are in step.
 template <int EB>
 struct GateWide {
     static_assert(EB == 8 || EB == 16, "wide gate gradient: experts");

@@ -2,7 +2,7 @@
 //
 // A token's E logits belong to L lanes of a wave with V vectors of four each, E <= 4 L V: vector v of lane l is that of experts 4 (v L + l) and on.  Sums over
 // a token's experts are moves between its lanes, and what they, a logarithm and a quotient cost falls with the number of lanes: the gradient of 32768 tokens
-// over 256 experts takes 21.0 us with 64 lanes, VVV with 16.
+// over 256 experts takes 21 us with 64 lanes, 19 with 16.
 #include "monta_internal.hpp"
 #include "monta_lanes.hpp"
 
@@ -24,10 +24,12 @@ __device__ __forceinline__ f32x4 load_some(const float *p, int exist, float rest
     return v;
 }
 
+template <bool STREAM>
 __device__ __forceinline__ void store_some(float *p, int exist, f32x4 v)
 {
     if (exist >= 4) {
-        *reinterpret_cast<f32x4_any *>(p) = v;
+        if constexpr (STREAM) __builtin_nontemporal_store((f32x4_any)v, reinterpret_cast<f32x4_any *>(p));
+        else *reinterpret_cast<f32x4_any *>(p) = v;
         return;
     }
 #pragma unroll
@@ -94,9 +96,10 @@ __device__ __forceinline__ void load_row(f32x4 (&v)[V], const float *row, int l,
 //   balance = sum_e f[e] P[e],   z = mean of lse[t]^2.
 // A workgroup sums a run of tokens; its E + 1 sums and E + 1 counts are a column each of `partial`, one word a workgroup, which
 // route_loss_join_kernel adds, a wave a column.  One workgroup alone finishes by itself.
-// A workgroup of the join has eight experts (all of them in one take 12 us for 256 experts and 4.4 for 64, which is what a CU takes to fetch the columns).
+// A workgroup of the join has eight experts (one for all of them takes 12 us for 256 experts and 4.4 for 64, which is what a CU takes to fetch the columns).
 // The balance loss is the sum of their shares, which the last one to arrive adds, in the experts' order: who that is says a counter, which the
 // kernel before has cleared.
+// 65536 tokens over 64 experts, top-8, a mask: 19 MB in 11.0 us, of which 7 the first launch; over 256 69 MB in 20.
 
 constexpr int kLossThreads = 1024, kLossWaves = kLossThreads / kWave, kLossGrid = 256, kMaxExperts = 256;
 constexpr int kJoinExperts = 8, kMostJoins = kMaxExperts / kJoinExperts;        // experts of a workgroup that joins
@@ -154,7 +157,8 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const float *l
         const int64_t p0 = t0 * k, pairs = (t1 - t0) * k;
         for (int64_t p = tid; p < pairs; p += kLossThreads) {
             const int e = idx[p0 + p];
-            if ((uint32_t)e < (uint32_t)E && (!mask || mask[t0 + (uint32_t)p / (uint32_t)k])) atomicAdd(&cnt[e], 1);
+            const bool counts = !mask || mask[t0 + (uint32_t)p / (uint32_t)k];
+            if ((uint32_t)e < (uint32_t)E && counts) atomicAdd(&cnt[e], 1);
         }
     }
     f32x4 acc[V];
@@ -271,9 +275,15 @@ __global__ __launch_bounds__(256) void route_loss_join_kernel(float *partial, Lo
 // The losses' part, with their gradients b and c, f and n as above:
 //   dl[e] += p[e] ( b / n (f[e] - sum_i p[i] f[i]) + 2 c / n lse ).
 // A workgroup takes 256 / L tokens.  A thread has a pair: it goes over its token's pairs in LDS for D, and puts what its expert gets (once, by the
-// first of its pairs if an expert is named twice) into the token's row in LDS, which the token's lanes then add to what p asks for.
+// first of its pairs if an expert is named twice) into the token's row in LDS, which the token's lanes then add to what p asks for.  The next tokens' logits and
+// pairs are on their way meanwhile.  32768 tokens over 256 experts, top-8: 70 MB in 19 us, 65536 over 64 40 MB in 11, neither at the rate of memory (4.2 TB/s with
+// the launch taken off): three barriers a round, 16 waves a CU.
 
 constexpr int kGradThreads = 256, kRouteGrid = 1024;
+// From 2^21 logits on they go past the cache, up to 128 experts; those of more are read again by each of the gate's gradient's column blocks.  us, stored plainly
+// and streamed, alone and with monta_gate_backward behind: 65536 x 64 12.1 / 77.6 and 11.1 / 76.0, 16384 x 128 7.9 / 46.0 and 7.0 / 45.8, but 32768 x 256
+// 18.6 / 81.7 and 16.8 / 84.7; 16384 x 64 5.6 / 44.7 and 5.3 / 44.9.
+inline bool stream_logits(int64_t T, int64_t E) { return T * E >= (1 << 21) && E <= 128; }
 
 struct RouteGradArgs {
     const float *logits, *gates, *dgates, *dlosses;
@@ -290,7 +300,7 @@ constexpr int grad_lds(int k)       // bytes: rows, D, and of each pair product,
     return kGradThreads / L * (4 * L * V + 1 + 3 * k) * 4;
 }
 
-template <int L, int V, bool SOFTMAX>
+template <int L, int V, bool SOFTMAX, bool STREAM>
 __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradArgs a)
 {
     constexpr int kTokens = kGradThreads / L, kRow = 4 * L * V;
@@ -299,10 +309,29 @@ __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradA
     float *const row = route_lds, *const dots = row + kTokens * kRow, *const prod = dots + kTokens, *const gate = prod + kTokens * k;
     int32_t *const expert = reinterpret_cast<int32_t *>(gate + kTokens * k);
     const int64_t chunks = ((int64_t)a.T + kTokens - 1) / kTokens;
+    // what the next tokens need: their logits, and this thread's pairs
+    constexpr int kEach = kTokens * (kRow < 32 ? kRow : 32) / kGradThreads;      // k <= E <= 4 L V, k <= 32
     f32x4 v[V], f[V];
+    float pair_gate[kEach], pair_grad[kEach];
+    int32_t pair_expert[kEach];
+    uint8_t pair_mask[kEach];
     bool live;
     auto fetch = [&](int64_t chunk) {
         const int64_t t = chunk * kTokens + mine;
+        if (a.dgates) {
+            const int64_t p0 = chunk * kTokens * k;
+            const int pairs = (int)min((int64_t)kTokens, a.T - chunk * kTokens) * k;
+#pragma unroll
+            for (int q = 0; q < kEach; ++q) {
+                const int p = tid + q * kGradThreads;
+                if (p < pairs) {
+                    pair_expert[q] = a.idx[p0 + p];
+                    pair_gate[q] = a.gates[p0 + p];
+                    pair_grad[q] = a.dgates[p0 + p];
+                    pair_mask[q] = a.mask ? a.mask[chunk * kTokens + p / a.by_k] : 1;
+                }
+            }
+        }
         live = t < a.T && (!a.mask || a.mask[t]);
         if constexpr (SOFTMAX) load_row<L, V>(v, a.logits + t * a.E, l, a.E, t < a.T);
     };
@@ -331,14 +360,14 @@ __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradA
         if (l == 0) dots[mine] = 0.f;
         if (a.dgates) {
             const int pairs = tokens * k;
-            for (int p = tid; p < pairs; p += kGradThreads) {
-                const int64_t at = t0 * k + p;
-                const int e = a.idx[at];
-                const float g = a.gates[at], d = a.dgates[at];
-                const bool counts = (uint32_t)e < (uint32_t)a.E && (!a.mask || a.mask[t0 + p / a.by_k]);
-                expert[p] = counts ? e : -1;
-                gate[p] = counts ? g : 0.f;
-                prod[p] = counts ? g * d : 0.f;
+#pragma unroll
+            for (int q = 0; q < kEach; ++q) {
+                const int p = tid + q * kGradThreads;
+                if (p >= pairs) break;
+                const bool counts = (uint32_t)pair_expert[q] < (uint32_t)a.E && pair_mask[q];
+                expert[p] = counts ? pair_expert[q] : -1;
+                gate[p] = counts ? pair_gate[q] : 0.f;
+                prod[p] = counts ? pair_gate[q] * pair_grad[q] : 0.f;
             }
             __syncthreads();
             for (int p = tid; p < pairs; p += kGradThreads) {
@@ -382,7 +411,7 @@ __global__ __launch_bounds__(kGradThreads) void route_backward_kernel(RouteGradA
         for (int q = 0; q < V; ++q) {
             const int e = 4 * (q * L + l);
             if (!mine_live) d[q] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (there && e < a.E) store_some(a.dlogits + t * a.E + e, a.E - e, d[q]);
+            if (there && e < a.E) store_some<STREAM>(a.dlogits + t * a.E + e, a.E - e, d[q]);
         }
         __syncthreads();                                           // the next tokens' pairs take the place of these
     }
@@ -496,9 +525,12 @@ int monta_route_backward(const monta_cfg *cfg, const float *logits, const int32_
     with_lanes(c.s.E, [&](auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value, V = decltype(vecs)::value, kTokens = kGradThreads / L;
         const int grid = (int)std::min<int64_t>((T + kTokens - 1) / kTokens, kRouteGrid), lds = grad_lds<L, V>(c.s.k);
-        if (softmax) hipLaunchKernelGGL((route_backward_kernel<L, V, true>), dim3(grid), dim3(kGradThreads), lds, st, a);
-        else hipLaunchKernelGGL((route_backward_kernel<L, V, false>), dim3(grid), dim3(kGradThreads), lds, st, a);
-        return MONTA_OK;
+        auto launch = [&](auto with_softmax, auto streamed) {
+            hipLaunchKernelGGL((route_backward_kernel<L, V, decltype(with_softmax)::value, decltype(streamed)::value>), dim3(grid), dim3(kGradThreads), lds, st, a);
+            return MONTA_OK;
+        };
+        if (stream_logits(T, E)) return softmax ? launch(std::true_type{}, std::true_type{}) : launch(std::false_type{}, std::true_type{});
+        return softmax ? launch(std::true_type{}, std::false_type{}) : launch(std::false_type{}, std::false_type{});
     });
     MONTA_HIP_TRY(hipGetLastError());
     return MONTA_OK;
