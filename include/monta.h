@@ -404,7 +404,7 @@ int monta_gate_backward_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
  *   dx[t][h] = sum_e dlogits[t][e] * w_gate[e][h] + dadd[t][h], rounded once to cfg->dtype;
  *   dw_gate[e][h] = sum_t dlogits[t][e] * x[t][h], fp32.
  * dadd: the gradient that reaches x by another way (through the dispatch), or NULL.  dlogits [T][E] fp32; x, dadd, dx [T][H] and w_gate [E][H] in
- * cfg->dtype, dw_gate [E][H] fp32, all but dlogits 16-byte aligned.  Either of dx and dw_gate may be NULL (then w_gate and dadd, or x and scratch, may be, too).
+ * cfg->dtype, dw_gate [E][H] fp32, all but dlogits 16-byte aligned.  Either of dx and dw_gate may be NULL (then w_gate may be, too, and dadd has to be; or x and scratch may be).
  * scratch 16-byte aligned, its contents are of no use afterwards and calls that overlap in time need one each.  dx may be dadd itself; otherwise nothing
  * that is written may share memory with anything else.  All sums are fp32, and their order is fixed for a shape.  With MONTA_BF16 dlogits is multiplied
  * in parts of 8 bits, two for dx (off by 2^-17 of a product) and three for dw_gate (2^-26), of which those below 2^-126 count as zero; an infinity so gives NaN.

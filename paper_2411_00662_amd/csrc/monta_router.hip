@@ -488,14 +488,17 @@ int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *t
     hipStream_t st = static_cast<hipStream_t>(stream);
     float *partial = static_cast<float *>(scratch);
     const LossOut o = {losses, counts, means};
-    LaunchTimer timer(MONTA_K_ROUTE_LOSS, st);
-    with_lanes(c.s.E, [&](auto lanes, auto vecs) {
-        hipLaunchKernelGGL((route_loss_kernel<decltype(lanes)::value, decltype(vecs)::value>), dim3(grid), dim3(kLossThreads), 0, st, logits, topk_idx, token_mask, partial, o, c.s.T,
-                           c.s.E, c.s.k, per);
-        return MONTA_OK;
-    });
-    MONTA_HIP_TRY(hipGetLastError());
+    {
+        LaunchTimer timer(MONTA_K_ROUTE_LOSS, st);
+        with_lanes(c.s.E, [&](auto lanes, auto vecs) {
+            hipLaunchKernelGGL((route_loss_kernel<decltype(lanes)::value, decltype(vecs)::value>), dim3(grid), dim3(kLossThreads), 0, st, logits, topk_idx,
+                               token_mask, partial, o, c.s.T, c.s.E, c.s.k, per);
+            return MONTA_OK;
+        });
+        MONTA_HIP_TRY(hipGetLastError());
+    }
     if (grid > 1) {
+        LaunchTimer timer(MONTA_K_ROUTE_LOSS, st);
         hipLaunchKernelGGL(route_loss_join_kernel, dim3((c.s.E + kJoinExperts - 1) / kJoinExperts), dim3(256), 0, st, partial, o, grid, c.s.E, c.s.k);
         MONTA_HIP_TRY(hipGetLastError());
     }

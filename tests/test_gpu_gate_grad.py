@@ -111,6 +111,22 @@ def test_what_is_not_finite(m, E, dtype):  # noqa: F811
     assert bool(torch.isfinite(dx2[torch.arange(T, device="cuda") != 77]).all())
 
 
+@pytest.mark.parametrize("E", [8, 100])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_on_4_bytes(m, E, dtype):  # noqa: F811
+    """dlogits needs no more than the alignment of its numbers."""
+    import torch
+    T, H = 70, 136
+    cfg = make(m, T, H, E, dtype)
+    dl, x, w, add = inputs(T, H, E, dtype, 11)
+    store = torch.empty(T * E + 3, device="cuda")
+    want = run(m, cfg, dl, x, w, add)
+    for at in (1, 2, 3):
+        part = store[at:at + T * E].view(T, E)
+        part.copy_(dl)
+        assert all(torch.equal(a, b) for a, b in zip(run(m, cfg, part, x, w, add), want))
+
+
 def test_rows_beyond_2gib(m):  # noqa: F811
     import torch
     T, H, E = 70003, 16384, 3                          # 2.3 GB of rows

@@ -258,6 +258,32 @@ def test_grad_of_what_routing_wrote(m):
                 diff = (whole(x + step) - whole(x - step)) / 2e-4
             assert abs(diff.item() - got[t, e].item()) <= 1e-4                # third derivatives below 100, times step^2 / 6; rounding of the sum
 
+
+def test_profile_names(m):
+    """The calls' launches by name: the losses of few tokens in one, of many in two."""
+    import torch
+    want = {"layernorm": 1, "layernorm_backward": 1, "layernorm_dparams": 1, "route_backward": 1, "gate_backward": 1}
+    for T, more in ((64, {"route_loss": 1}), (9000, {"route_loss": 2, "gate_dweight": 1})):
+        E, k, H = 8, 2, 64
+        cfg = make(m, T, E, k)
+        logits, idx, gates, dgates, _ = inputs(T, E, k, 3)
+        x = torch.randn((T, H), device="cuda").bfloat16()
+        w, wg, out = x[0].clone(), x[:E].contiguous(), torch.empty_like(x)
+        p = [torch.empty(H, device="cuda") for _ in range(2)]
+        sc = [scratch(f(cfg)) for f in (m.monta_layernorm_scratch_bytes, m.monta_gate_backward_scratch_bytes)]
+        m.monta_profile_reset()
+        m.monta_profile_enable(True)
+        m.monta_layernorm(cfg, x, None, w, w, 1e-5, None, out)
+        m.monta_layernorm_backward(cfg, x, w, 1e-5, out, None, out, p[0], p[1], sc[0])
+        counts = run_loss(m, cfg, logits, idx, None)[1]
+        d = run_grad(m, cfg, logits, idx, gates, dgates, None, torch.ones(2, device="cuda"), counts)
+        m.monta_gate_backward(cfg, d, x, wg, None, out, torch.empty((E, H), device="cuda"), sc[1])
+        m.monta_profile_enable(False)
+        got = {n: m.monta_profile_read(i)[1] for i, n in enumerate(m.KERNEL_NAMES)}
+        assert {n: c for n, c in got.items() if c} == dict(want, **more)
+    m.monta_profile_reset()
+
+
 def test_graph_and_streams(m):
     """Captured and replayed with eager work between the replays; two calls at once on streams of their own; rows beyond 2^31 bytes."""
     import torch
