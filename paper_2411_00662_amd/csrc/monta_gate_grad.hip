@@ -483,6 +483,8 @@ struct GateWide {
     static constexpr int EP = 16 * EB, KS = EP / 32;
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece, kItemsEach = kSplitTokens * EP / 8 / kThreads;
     static constexpr int kRowX = 2 * BC, kX = kSplitTokens * kRowX, kLoadsX = kX / 1024 / kWaves, kPerRowX = BC / 8;
+    // the next step's dl is split before dw's products or after them, and the one after it requested then: 16384 x 4096, 256 experts 185 us and 202, 128 experts 108 and 105
+    static constexpr bool kSplitEarly = EB == 16;
     static constexpr int kLdsX = NST * kX, kLdsOut = 2 * kX, kLdsBytes = kLdsX + kLdsOut + 2 * kDl;
     static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // before the first step, behind its stage
     // as in GateShape
@@ -616,6 +618,10 @@ __global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unus
         fetch_add(t0 + stride);
         issue(t0 + (NST - 1) * stride, stage == 0 ? (NST - 1) * G::kX : stage - G::kX);       // where the step before was
 
+        auto next_dl = [&](unsigned char *to) {                    // for the next step, among this one's products
+            split(to);
+            fetch_dl(t0 + 2 * stride);
+        };
         const unsigned char *const dls = lds_dl + buf, *const xs = lds_x + stage;
         bf16x8 fx[4];
 #pragma unroll
@@ -636,6 +642,7 @@ __global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unus
             const int c = quarter * (G::DC / 8) + 4 * q + g;       // its piece of the row
             put((lds_u32x4 *)(lds_out + out_at + (16 * half + m) * G::kRowX + ((c >> 1) * 32 ^ so) + (c & 1) * 16), __builtin_bit_cast(u32x4, o));
         }
+        if constexpr (G::kSplitEarly) next_dl(lds_dl + (buf ^ G::kDl));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -645,8 +652,7 @@ __global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unus
                 for (int i = 0; i < 4; ++i) sum[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], b, sum[j][i], 0, 0, 0);
             }
         buf ^= G::kDl;
-        split(lds_dl + buf);                                       // for the next step, among this one's products
-        fetch_dl(t0 + 2 * stride);
+        if constexpr (!G::kSplitEarly) next_dl(lds_dl + buf);
         stage = stage == (NST - 1) * G::kX ? 0 : stage + G::kX;
         out_at = G::kX - out_at;
     }
