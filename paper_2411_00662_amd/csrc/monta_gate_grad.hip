@@ -473,8 +473,8 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
 //   dw: a wave has 64 experts and 64 columns.
 //   dx: a wave has 16 tokens of the step, all experts and a quarter of the workgroup's columns; the rows leave a step later, when all waves have written
 //       their parts of them.
-// 16384 x 4096 with dadd, 256 experts: 196 us (in waves of 32 columns, all experts: 283), 128 experts 107: 0.45 to 0.88 PFLOP/s of bf16 products, half of the rate
-// that the matrix pipe holds; the steps of both waves of a SIMD are in step.
+// 16384 x 4096 with dadd, 256 experts: 183 us (in waves of 32 columns, all experts: 283), 128 experts 103: 0.94 and 0.83 PFLOP/s of bf16 products, half of the
+// rate that the matrix pipe holds; the steps of both waves of a SIMD are in step.
 template <int EB>
 struct GateWide {
     static_assert(EB == 8 || EB == 16, "wide gate gradient: experts");

@@ -125,11 +125,12 @@ __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 
 
 // With n = (s - m) r and g = dout w:  dx = r (g - mean(g) - n mean(g n)) + dsum,  dw = sum over the rows of dout n,  db = that of dout.
 // A workgroup walks over rows and keeps the weight's and the bias's shares in registers; the next row is requested before the present one's
-// sums are known.  Both gradients' partial sums, 2 H in a row per workgroup, are added by layernorm_dparams_kernel: a fixed order, no atomics.
-// 8192 x 4096 bf16 with dsum: 268 MB in 45 us and 4 for the partial sums, 5.4 TB/s.
+// sums are known.  Both gradients' partial sums, 2 H in a row per workgroup, are added by layernorm_dparams_kernel: a fixed order, no atomics.  Of few
+// rows one workgroup writes the gradients itself.  8192 x 4096 bf16 with dsum: 268 MB in 45 us and 4 for the partial sums, 5.4 TB/s.
 template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_kernel(const u32x4 *s_in, const u32x4 *w, const u32x4 *dout, const u32x4 *dsum,
-                                                                                      u32x4 *dx, float *partial, int T, int vpr, float eps)
+                                                                                      u32x4 *dx, float *partial, float *dweight, float *dbias, int T, int vpr,
+                                                                                      float eps)
 {
     constexpr int EV = Elem<BF16>::kPerVec, kRows = backward_threads_of<L>() / L, LW = L < kWave ? L : kWave, W = L > kWave ? L / kWave : 1;
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
@@ -232,15 +233,17 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
             if (live && i < vpr) dx[row * vpr + i] = pack<BF16>(o);
         }
     }
-    float *to = partial + (int64_t)blockIdx.x * 2 * H;
+    // a workgroup alone has the gradients themselves
+    const bool alone = gridDim.x == 1;
+    float *const to_w = alone ? dweight : partial + (int64_t)blockIdx.x * 2 * H, *const to_b = alone ? dbias : to_w + H;
     if constexpr (kRows == 1) {
 #pragma unroll
         for (int q = 0; q < NV; ++q)
             if (l + q * L < vpr)
 #pragma unroll
                 for (int e = 0; e < EV; ++e) {
-                    to[(l + q * L) * EV + e] = dw[q][e];
-                    to[H + (l + q * L) * EV + e] = db[q][e];
+                    to_w[(l + q * L) * EV + e] = dw[q][e];
+                    if (to_b) to_b[(l + q * L) * EV + e] = db[q][e];
                 }
     } else {
         __shared__ float cols[kRows][L * NV * EV];                  // the rows' groups, then one row of sums
@@ -256,7 +259,8 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
                 float v = 0.f;
 #pragma unroll
                 for (int g = 0; g < kRows; ++g) v += cols[g][h];
-                to[which * H + h] = v;
+                if (which == 0) to_w[h] = v;
+                else if (to_b) to_b[h] = v;
             }
         }
     }
@@ -329,12 +333,17 @@ int with_types(bool bf16, bool streamed, Row row, F f)
 }
 
 // Workgroups of the gradient, and so rows of partial sums, each of which is written and read again and costs more than a row of the norm itself.  us, 256 and
-// 512 of them: 8192 x 2048 bf16 32.6 and 37.6, 16384 x 1024 28.2 and 29.6, but 48222 x 120 13.8 and 12.8.
+// 512 of them: 8192 x 2048 bf16 32.6 and 37.6, 16384 x 1024 28.2 and 29.6, but 48222 x 120 13.8 and 12.8.  One workgroup has whole sums and needs no second
+// launch, which gains as long as its rounds take less than that one: us, one workgroup and two launches, 4 rounds of lanes with one vector 4.7 to 5.0 and 6.1
+// (128 to 512 features, bf16), 6 rounds 6.0 to 6.5 and 6.1; of more vectors, 2 rounds 4.6 and 6.1 (1024 features), 7.8 and 7.8 (2048), 6.9 and 7.4 (4096),
+// 12.0 and 12.6 (8192), 3 rounds 5.6 and 6.1, 10.0 and 7.8, 8.8 and 7.4, 13.7 and 12.7.
 int gradient_grid(const Call &c)
 {
     return with_gradient_row(c.s.vpr, [&](auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value, rows = backward_threads_of<L>() / L;
-        return (int)std::min<int64_t>(((int64_t)c.s.T + rows - 1) / rows, L <= kWave && decltype(vecs)::value == 1 ? 512 : 256);
+        constexpr bool small = L <= kWave && decltype(vecs)::value == 1;
+        const int64_t rounds = ((int64_t)c.s.T + rows - 1) / rows;
+        return rounds <= (small ? 4 : 2) ? 1 : (int)std::min<int64_t>(rounds, small ? 512 : 256);
     });
 }
 
@@ -430,11 +439,12 @@ int monta_layernorm_backward(const monta_cfg *cfg, const void *sum, const void *
             constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
             hipLaunchKernelGGL((layernorm_backward_kernel<decltype(bf)::value, L, NV, decltype(streamed)::value>), dim3(grid), dim3(backward_threads_of<L>()), 0, st,
                                static_cast<const u32x4 *>(sum), static_cast<const u32x4 *>(weight), static_cast<const u32x4 *>(dout),
-                               static_cast<const u32x4 *>(dsum), static_cast<u32x4 *>(dx), partial, c.s.T, c.s.vpr, eps);
+                               static_cast<const u32x4 *>(dsum), static_cast<u32x4 *>(dx), partial, dweight, dbias, c.s.T, c.s.vpr, eps);
             return MONTA_OK;
         });
         MONTA_HIP_TRY(hipGetLastError());
     }
+    if (grid == 1) return MONTA_OK;
     LaunchTimer timer(MONTA_K_LAYERNORM_DPARAMS, st);
     hipLaunchKernelGGL(layernorm_dparams_kernel, dim3(((dbias ? 2 : 1) * c.H + 31) / 32), dim3(1024), 0, st, partial, dweight, dbias, grid, c.H);
     MONTA_HIP_TRY(hipGetLastError());

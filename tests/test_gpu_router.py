@@ -260,10 +260,10 @@ def test_grad_of_what_routing_wrote(m):
 
 
 def test_profile_names(m):
-    """The calls' launches by name: the losses of few tokens in one, of many in two."""
+    """The calls' launches by name: the losses, the norm's gradient and the gate projection's of few tokens in one, of many in two."""
     import torch
-    want = {"layernorm": 1, "layernorm_backward": 1, "layernorm_dparams": 1, "route_backward": 1, "gate_backward": 1}
-    for T, more in ((64, {"route_loss": 1}), (9000, {"route_loss": 2, "gate_dweight": 1})):
+    want = {"layernorm": 1, "layernorm_backward": 1, "route_backward": 1, "gate_backward": 1}
+    for T, more in ((64, {"route_loss": 1}), (9000, {"route_loss": 2, "gate_dweight": 1, "layernorm_dparams": 1})):
         E, k, H = 8, 2, 64
         cfg = make(m, T, E, k)
         logits, idx, gates, dgates, _ = inputs(T, E, k, 3)
