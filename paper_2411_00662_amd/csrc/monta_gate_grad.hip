@@ -800,8 +800,8 @@ int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *
         if (!w.p) continue;
         for (const auto &r : read) {
             if (!r.p) continue;
-            // an element of dadd is read by the lane that stores dx there: dx may be dadd as a whole
-            if (w.p == dx && r.p == dadd ? !same_or_apart(dx, dadd, n) : overlap(w.p, w.n, r.p, r.n)) return MONTA_ERR_INVALID;
+            // an element of dadd is read by the lane that stores dx there: dx may be dadd as a whole, unless that is another argument, too
+            if (w.p == dx && &r == &read[3] ? !same_or_apart(dx, dadd, n) : overlap(w.p, w.n, r.p, r.n)) return MONTA_ERR_INVALID;
         }
         for (const auto &o : written)
             if (&o != &w && o.p && overlap(w.p, w.n, o.p, o.n)) return MONTA_ERR_INVALID;

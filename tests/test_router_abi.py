@@ -107,6 +107,7 @@ def gate_backward(c, dl=A[0], x=A[1], w=A[2], dadd=A[3], dx=A[4], dw=A[5], scrat
     (dict(dl=A[0] + 2), -5), (dict(x=A[1] + 8), -5), (dict(w=A[2] + 8), -5), (dict(dadd=A[3] + 8), -5), (dict(dx=A[4] + 8), -5), (dict(dw=A[5] + 4), -5),
     (dict(scratch=A[6] + 4), -5),
     (dict(dx=A[0]), -1), (dict(dx=A[1]), -1), (dict(dx=A[2]), -1), (dict(dx=A[3] + 1024), -1), (dict(dw=A[0]), -1), (dict(dw=A[1]), -1), (dict(dw=A[2]), -1),
+    (dict(x=A[3], dx=A[3]), -1), (dict(w=A[3], dx=A[3]), -1), (dict(dl=A[3], dx=A[3]), -1),          # dadd itself, but another argument, too
     (dict(dw=A[3]), -1), (dict(dw=A[4]), -1), (dict(scratch=A[0]), -1), (dict(scratch=A[4]), -1), (dict(scratch=A[5]), -1)])
 def test_gate_backward_refuses(kw, code):
     assert gate_backward(cfg(), **kw) == code
