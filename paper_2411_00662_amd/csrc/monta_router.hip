@@ -460,7 +460,9 @@ int monta_route_loss_scratch_bytes(const monta_cfg *cfg, size_t *bytes)
     Call c;
     if (int rc = open_call(cfg, nullptr, &c)) return rc;
     int per;
-    *bytes = (size_t)loss_scratch(c.s.E, loss_grid(c.s, &per));
+    // workgroups take whole rounds, so that more tokens may have fewer of them; scratch for more tokens does for fewer all the same
+    const int64_t round = kLossThreads / lanes_of(c.s.E);
+    *bytes = (size_t)loss_scratch(c.s.E, std::max(loss_grid(c.s, &per), (int)std::min<int64_t>((c.s.T + round - 1) / round, kLossGrid)));
     return MONTA_OK;
 }
 

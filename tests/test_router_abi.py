@@ -43,6 +43,17 @@ def test_layernorm_sizes():
     assert B.lib().monta_layernorm_scratch_bytes(ctypes.byref(cfg()), None) == -3
 
 
+@pytest.mark.parametrize("name", ["monta_layernorm_scratch_bytes", "monta_route_loss_scratch_bytes", "monta_gate_backward_scratch_bytes"])
+@pytest.mark.parametrize("hidden,experts", [(128, 4), (1024, 16), (1536, 64), (4096, 100), (8192, 256)])
+def test_scratch_for_more_tokens_does_for_fewer(name, hidden, experts):
+    for dtype in (m.BF16, m.FP32):
+        last = 0
+        for tokens in [*range(1, 1200), 1999, 2048, 2049, 4097, 8192, 8193, 16384, 30000, 32769, 65536, 1 << 20, 1 << 24]:
+            n = getattr(m, name)(cfg(tokens=tokens, hidden=hidden, dtype=dtype, experts=experts, top_k=1, slices=1))
+            assert n >= last, tokens
+            last = n
+
+
 def layernorm_backward(c, s=A[0], w=A[1], eps=1e-5, dout=A[2], dsum=A[3], dx=A[4], dw=A[5], db=A[6], scratch=A[7]):
     return B.lib().monta_layernorm_backward(ctypes.byref(c), s, w, eps, dout, dsum, dx, dw, db, scratch, 0)
 
