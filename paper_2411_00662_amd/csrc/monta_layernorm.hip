@@ -296,7 +296,7 @@ __global__ __launch_bounds__(1024) void layernorm_dparams_kernel(const float *pa
 // f(lanes of a row, vectors of a lane): lanes of one wave as far as their registers go, since a row of several waves meets at a barrier, and no more
 // than the row has vectors for.  us, these forms and one vector for each of 64 or 256 lanes: norm of 16384 x 768 bf16 19.1 and 28.7, 16384 x 1024 25.8 and
 // 30.5, 65536 x 256 26.4 and 31.5; its gradient 22.5 and 55.4, 28.2 and 57.3, 28.3 and 44.9.  Beyond 128 vectors the norm has no use for it (8192 x 2048 in
-// one wave 27.1, in four 26.0), its gradient has (32.6 and 35.3; 16384 x 1536 43.1 and 61).
+// one wave 27.1, in four 26.0), its gradient has (32.6 and 35.3; 16384 x 1536 42.2 and 61, with four vectors 43.9).
 template <typename F>
 int with_short_row(int vpr, F f)
 {
@@ -318,6 +318,7 @@ int with_gradient_row(int vpr, F f)
 {
     using std::integral_constant;
     if (vpr <= 128) return with_short_row(vpr, f);
+    if (vpr <= 192) return f(integral_constant<int, 64>{}, integral_constant<int, 3>{});
     if (vpr <= 256) return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     return with_row_shape(vpr, f);
 }
@@ -336,15 +337,26 @@ int with_types(bool bf16, bool streamed, Row row, F f)
 // 512 of them: 8192 x 2048 bf16 32.6 and 37.6, 16384 x 1024 28.2 and 29.6, but 48222 x 120 13.8 and 12.8.  One workgroup has whole sums and needs no second
 // launch, which gains as long as its rounds take less than that one: us, one workgroup and two launches, 4 rounds of lanes with one vector 4.7 to 5.0 and 6.1
 // (128 to 512 features, bf16), 6 rounds 6.0 to 6.5 and 6.1; of more vectors, 2 rounds 4.6 and 6.1 (1024 features), 7.8 and 7.8 (2048), 6.9 and 7.4 (4096),
-// 12.0 and 12.6 (8192), 3 rounds 5.6 and 6.1, 10.0 and 7.8, 8.8 and 7.4, 13.7 and 12.7.
-int gradient_grid(const Call &c)
+// 12.0 and 12.6 (8192), 3 rounds 5.6 and 6.1, 10.0 and 7.8, 8.8 and 7.4, 13.7 and 12.7.  Of more vectors as few as have the same number of rounds: us, 256 and
+// so many, 1155 x 516 fp32 8.2 and 7.4, 1100 x 2048 bf16 12.8 and 11.7, 600 x 4096 13.2 and 11.8, 300 x 8192 21.4 and 17.9, but with one vector 9000 x 256 8.8
+// and 9.1.
+struct GradientGrid {
+    int workgroups, most;           // the most of any call of as many tokens or fewer: scratch for more tokens does for fewer
+};
+
+GradientGrid gradient_grid(const Call &c)
 {
-    return with_gradient_row(c.s.vpr, [&](auto lanes, auto vecs) {
+    GradientGrid g;
+    with_gradient_row(c.s.vpr, [&](auto lanes, auto vecs) {
         constexpr int L = decltype(lanes)::value, rows = backward_threads_of<L>() / L;
         constexpr bool small = L <= kWave && decltype(vecs)::value == 1;
         const int64_t rounds = ((int64_t)c.s.T + rows - 1) / rows;
-        return rounds <= (small ? 4 : 2) ? 1 : (int)std::min<int64_t>(rounds, small ? 512 : 256);
+        g.most = (int)std::min<int64_t>(rounds, small ? 512 : 256);
+        const int64_t each = small ? 1 : (rounds + g.most - 1) / g.most;
+        g.workgroups = rounds <= (small ? 4 : 2) ? 1 : small ? g.most : (int)((rounds + each - 1) / each);
+        return MONTA_OK;
     });
+    return g;
 }
 
 }  // namespace
@@ -399,7 +411,7 @@ int monta_layernorm_scratch_bytes(const monta_cfg *cfg, size_t *bytes)
     Call c;
     if (int rc = open_call(cfg, nullptr, &c)) return rc;
     if (c.s.vpr > kMaxVecs) return MONTA_ERR_UNSUPPORTED;
-    *bytes = (size_t)gradient_grid(c) * c.H * 8;
+    *bytes = (size_t)gradient_grid(c).most * c.H * 8;
     return MONTA_OK;
 }
 
@@ -414,7 +426,7 @@ int monta_layernorm_backward(const monta_cfg *cfg, const void *sum, const void *
         return MONTA_ERR_ALIGN;
     if (!(eps >= 0.f) || eps > 3.4e38f) return MONTA_ERR_INVALID;
     if (c.s.vpr > kMaxVecs) return MONTA_ERR_UNSUPPORTED;
-    const int grid = gradient_grid(c);
+    const int grid = gradient_grid(c).workgroups;
     const int64_t n = c.s.T * c.row_bytes, np = (int64_t)grid * c.H * 8, nw = (int64_t)c.H * 4;
     const struct {
         const void *p;

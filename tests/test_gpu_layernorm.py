@@ -149,7 +149,7 @@ def test_edges(m, H, dtype):  # noqa: F811
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("dsum", [0, 1])
-@pytest.mark.parametrize("T,H", SIZES + [(513, 4096), (1500, 520), (2, 16384), (1, 8192), (4, 4096), (5, 4096), (8, 1024), (9, 1024), (63, 128), (65, 120)])
+@pytest.mark.parametrize("T,H", SIZES + [(513, 4096), (1500, 520), (2, 16384), (1, 8192), (4, 4096), (5, 4096), (8, 1024), (9, 1024), (63, 128), (65, 120), (1155, 1040), (1100, 1536), (600, 4096), (1030, 768)])
 def test_backward(m, T, H, dtype, dsum):  # noqa: F811
     import torch
     if dtype == "f32" and H > 8192:
