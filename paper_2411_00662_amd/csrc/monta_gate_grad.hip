@@ -172,9 +172,9 @@ __global__ __launch_bounds__(256, 2) void gate_backward_f32_kernel(GateGradArgs 
 
 // --------------------------------------------------------------------------------------------- bf16
 //
-// bf16 activations on the bf16 matrix instruction (16 x 16 x 32).  A gradient of a logit is split into bf16 numbers, each the rest of the one before
-// it: with two the products of dx, which is rounded to bf16 (2^-8), are off by 2^-17, with three those of dw, which is fp32, by 2^-26.  A step is 32 tokens; a
-// wave has 64 columns of it.
+// bf16 activations on the bf16 matrix instruction (16 x 16 x 32).  A gradient of a logit is split into three bf16 numbers, each the rest of the one before
+// it, whose products are off by 2^-26: fp32 sums of dw, and of dx until it is rounded, since experts may cancel each other, or dadd their sum (with two of the
+// three dx would be off by 2^-17 of its terms).  A step is 32 tokens; a wave has 64 columns of it.
 //   dx: rows h, columns t, summed over e.  The wave keeps the weights of its columns in registers.  Row r of tile i is column 32 (i / 2) + 8 (r / 4)
 //       + 4 (i % 2) + r % 4, so that a lane gets 8 neighbours of one token and four lanes 64 bytes.
 //   dw: rows h, columns e, summed over t.  Both operands lie across the summed axis: they are kept in LDS as they come, rows of 32 bytes' segments, and
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
 #pragma unroll
         for (int ks = 0; ks < G::KS; ++ks)
 #pragma unroll
-            for (int piece = 0; piece < 2; ++piece)
+            for (int piece = 0; piece < 3; ++piece)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const bf16x8 b = read_along((lds_bf16x8 *)(dls + piece * G::kPiece + half * 16 * G::kRow + along_dl + (((2 * ks + (g >> 1)) * 32) ^ sl)));
@@ -629,7 +629,7 @@ __global__ __launch_bounds__(512, 2) void gate_backward_wide_kernel([[maybe_unus
 #pragma unroll
         for (int ks = 0; ks < G::KS; ++ks)
 #pragma unroll
-            for (int piece = 0; piece < 2; ++piece) {
+            for (int piece = 0; piece < 3; ++piece) {
                 const bf16x8 b = read_along((lds_bf16x8 *)(dls + piece * G::kPiece + along_dl + (((2 * ks + (g >> 1)) * 32) ^ sl)));
 #pragma unroll
                 for (int i = 0; i < G::CD; ++i) out[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[ks][i], b, out[i], 0, 0, 0);

@@ -1,0 +1,31 @@
+"""GPU: the gate projection's gradients where the products cancel each other.
+
+Bars, with u = 2^-24 and h = eps / 2 of the activation type: a gradient of a logit is multiplied in three parts of 8 bits, whose products are off
+by 2^-26, and n gradients that are not zero make 3 n products and an addition each: (3 n + 8) u of the terms' magnitudes; dx is rounded once more: h.
+"""
+import pytest
+
+from test_gpu_gate_grad import inputs, make, run
+from test_gpu_norm import U, half, m  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,E", [(70, 136, 2), (333, 520, 16), (200, 264, 40), (150, 1032, 100), (257, 200, 256)])
+def test_experts_that_cancel(m, T, H, E, dtype):  # noqa: F811
+    """Two experts of a token with opposite weights, whose gradients differ by 2^-17 of them: what is left of dx is as near as fp32 products leave it."""
+    import torch
+    cfg = make(m, T, H, E, dtype)
+    _, x, w, _ = inputs(T, H, E, dtype, 7, add=False)
+    first = w[0].clone()
+    w[::2], w[1::2] = first, -first
+    g, at = torch.Generator(device="cuda").manual_seed(8), torch.arange(T, device="cuda")
+    a = torch.randint(0, (E + 1) // 2, (T,), generator=g, device="cuda") * 2
+    b = torch.randint(0, E // 2, (T,), generator=g, device="cuda") * 2 + 1
+    v = torch.randn(T, generator=g, device="cuda")
+    dl = torch.zeros((T, E), device="cuda")
+    dl[at, a], dl[at, b] = v, v * (1 + 2.0 ** -17 * torch.randn(T, generator=g, device="cuda"))
+    dx, _ = run(m, cfg, dl, x, w, None, dw=False)
+    want, mag = dl.double() @ w.double(), dl.double().abs() @ w.double().abs()
+    assert bool(((dx.double() - want).abs() <= want.abs() * half(dtype) + mag * (3 * 2 + 8) * U).all())
