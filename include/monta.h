@@ -407,7 +407,7 @@ int monta_gate_backward_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
  * cfg->dtype, dw_gate [E][H] fp32, all but dlogits 16-byte aligned.  Either of dx and dw_gate may be NULL (then w_gate may be, too, and dadd has to be; or x and scratch may be).
  * scratch 16-byte aligned, its contents are of no use afterwards and calls that overlap in time need one each.  dx may be dadd itself; otherwise nothing
  * that is written may share memory with anything else.  All sums are fp32, and their order is fixed for a shape.  With MONTA_BF16 dlogits is multiplied
- * in three parts of 8 bits (off by 2^-26 of a product), of which those below 2^-126 count as zero; an infinity so gives NaN.
+ * in three parts of 8 bits, which hold all of it, but for what lies below 2^-133; an infinity so gives NaN.
  * hidden at most 2^20.
  * Uses tokens, hidden, dtype and experts of cfg (all of it is validated); needs no workspace. */
 int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *x, const void *w_gate, const void *dadd, void *dx, float *dw_gate,

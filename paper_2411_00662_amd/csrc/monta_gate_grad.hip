@@ -8,8 +8,6 @@
 namespace monta {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 struct GateGradArgs {
     const float *dl;
     const void *x, *w, *dadd;
@@ -172,9 +170,9 @@ __global__ __launch_bounds__(256, 2) void gate_backward_f32_kernel(GateGradArgs 
 
 // --------------------------------------------------------------------------------------------- bf16
 //
-// bf16 activations on the bf16 matrix instruction (16 x 16 x 32).  A gradient of a logit is split into three bf16 numbers, each the rest of the one before
-// it, whose products are off by 2^-26: fp32 sums of dw, and of dx until it is rounded, since experts may cancel each other, or dadd their sum (with two of the
-// three dx would be off by 2^-17 of its terms).  A step is 32 tokens; a wave has 64 columns of it.
+// bf16 activations on the bf16 matrix instruction (16 x 16 x 32).  A gradient of a logit is split into three bf16 numbers
+// of 8 bits each, whose products are exact: fp32 sums of dw, and of dx until it is rounded, since experts may cancel each other, or dadd their sum (with two of the
+// three dx would be off by 2^-16 of its terms).  A step is 32 tokens; a wave has 64 columns of it.
 //   dx: rows h, columns t, summed over e.  The wave keeps the weights of its columns in registers.  Row r of tile i is column 32 (i / 2) + 8 (r / 4)
 //       + 4 (i % 2) + r % 4, so that a lane gets 8 neighbours of one token and four lanes 64 bytes.
 //   dw: rows h, columns e, summed over t.  Both operands lie across the summed axis: they are kept in LDS as they come, rows of 32 bytes' segments, and
@@ -216,25 +214,22 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 [[maybe_unused]] __device__ __forceinline__ bf16x8 read_along(lds_bf16x8 *__restrict__ p) { return *p; }
 [[maybe_unused]] __device__ __forceinline__ void put(lds_u32x4 *__restrict__ p, u32x4 v) { *p = v; }
 
-// Eight neighbours of dl as three bf16 numbers each, one piece `pitch` bytes behind the other.
+// Eight neighbours of dl as three bf16 numbers each, one piece `pitch` bytes behind the other: the upper 8 of a number's 24 bits, the next 8 and the rest.  They are
+// cut off, not rounded: no finite number becomes an infinity.
 template <int pitch>
 [[maybe_unused]] __device__ __forceinline__ void split_eight(const f32x4 (&dl)[2], unsigned char *to)
 {
-    float v[8];
+    uint32_t v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = dl[i / 4][i % 4];
+    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(dl[i / 4][i % 4]);
 #pragma unroll
     for (int piece = 0; piece < 3; ++piece) {
         u32x4 b;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bf16x2 two;
-            two[0] = (__bf16)v[2 * i];
-            two[1] = (__bf16)v[2 * i + 1];
-            b[i] = __builtin_bit_cast(uint32_t, two);
-            v[2 * i] -= __uint_as_float(b[i] << 16);
-            v[2 * i + 1] -= __uint_as_float(b[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < 4; ++i) b[i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07060302u);      // the upper halves of two
+        if (piece < 2)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) - __uint_as_float(v[i] & 0xffff0000u));
         put((lds_u32x4 *)(to + piece * pitch), b);
     }
 }

@@ -1,7 +1,7 @@
-"""GPU: the gate projection's gradients where the products cancel each other.
+"""GPU: the gate projection's gradients where the products cancel each other, and where they need the whole range of a logit's gradient.
 
-Bars, with u = 2^-24 and h = eps / 2 of the activation type: a gradient of a logit is multiplied in three parts of 8 bits, whose products are off
-by 2^-26, and n gradients that are not zero make 3 n products and an addition each: (3 n + 8) u of the terms' magnitudes; dx is rounded once more: h.
+Bars, with u = 2^-24 and h = eps / 2 of the activation type: a gradient of a logit is multiplied in three parts of 8 bits, whose products are exact,
+and n gradients that are not zero make 3 n products and an addition each: (3 n + 8) u of the terms' magnitudes; dx is rounded once more: h.
 """
 import pytest
 
@@ -29,3 +29,20 @@ def test_experts_that_cancel(m, T, H, E, dtype):  # noqa: F811
     dx, _ = run(m, cfg, dl, x, w, None, dw=False)
     want, mag = dl.double() @ w.double(), dl.double().abs() @ w.double().abs()
     assert bool(((dx.double() - want).abs() <= want.abs() * half(dtype) + mag * (3 * 2 + 8) * U).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,E", [(40, 136, 3), (150, 200, 24), (100, 264, 60), (70, 520, 100), (90, 72, 256)])
+def test_largest_numbers(m, T, H, E, dtype):  # noqa: F811
+    """Finite gradients beyond the largest bf16 number, 3.39e38, are finite in their products."""
+    import torch
+    cfg = make(m, T, H, E, dtype)
+    _, x, w, _ = inputs(T, H, E, dtype, 5, add=False)
+    x, w = x * 2.0 ** -12, w * 2.0 ** -12
+    dl, at = torch.zeros((T, E), device="cuda"), torch.arange(T, device="cuda")
+    dl[at, at % E] = torch.where(at % 2 == 0, 3.4028234663852886e38, -3.395e38)
+    dx, dw = run(m, cfg, dl, x, w, None)
+    d = dl.double()
+    for got, want, mag, h, n in ((dx, d @ w.double(), d.abs() @ w.double().abs(), half(dtype), 1),
+                                 (dw, d.t() @ x.double(), d.abs().t() @ x.double().abs(), 0, -(-T // E))):
+        assert bool(((got.double() - want).abs() <= want.abs() * h + mag * (3 * n + 8) * U).all())
