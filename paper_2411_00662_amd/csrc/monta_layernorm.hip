@@ -5,10 +5,11 @@
 namespace monta {
 namespace {
 
-// Sums around a mean that is not known yet.  A wave takes its own share's mean m_w, from a first sum, and its other sums around that;
-// the waves' shares are then joined by
+// Sums around a mean that is not known yet.  A mean is two numbers: that of a first sum, which is off by some 2^-24 of the row's magnitude and may so be further
+// from the row than the row is spread, and the mean of the differences from it, off by that of those (fp32 rows at 1e4: outputs off by 1e-5 instead of 0.5).  It
+// costs a pass over the registers, 1 to 3 us of the 50 of 8192 x 4096.  A wave takes its own share's mean m_w and its other sums around that; the waves' shares are then joined by
 //   sum (s - m)^2 = sum_w [ M2_w + n_w d_w^2 ],   sum g (s - m) = sum_w [ G1_w + d_w G0_w ],   d_w = m_w - m,
-// which has no difference of large numbers, and takes one barrier for both steps.  Means are quotients: from a product with 1 / n the compiler may make a
+// which has no difference of large numbers, and takes one barrier for all steps.  Means are quotients: from a product with 1 / n the compiler may make a
 // fused difference for some elements of a row and not for others, and a row of equal numbers would not have a spread of zero.
 //
 // Elements of a row that wave w of its L lanes holds, NV vectors of EV elements a lane.
@@ -25,14 +26,14 @@ __device__ __forceinline__ float wave_share(int vpr, int w)
 //
 //   s = x + residual, rounded to the activation type and stored; m = mean(s), r = 1 / sqrt(mean((s - m)^2) + eps); v = (s - m) r w + b
 //   out = v rounded once; codes and scales of v as in monta_rmsnorm.
-// 8192 x 4096 bf16 with a residual, both outputs: 303 MB in 50 us, 6.0 TB/s; the root-mean-square norm, with one sum and no barrier's wait less, takes 48.
+// 8192 x 4096 bf16 with a residual, both outputs: 303 MB in 52 us, 5.8 TB/s; the root-mean-square norm, with one sum and no barrier's wait less, takes 48.
 template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 *x, const u32x4 *residual, const u32x4 *w, const u32x4 *bias, u32x4 *sum,
                                                                     u32x4 *out, unsigned char *rows8, int T, int vpr, int row8_bytes, float eps)
 {
     constexpr int EV = Elem<BF16>::kPerVec, kRows = threads_of<L>() / L, LW = L < kWave ? L : kWave, W = L > kWave ? L / kWave : 1;
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
-    __shared__ float part[2][2 * W];                                // alternated, so that one barrier keeps a row's sums from the next row's
+    __shared__ float part[2][3 * W];                                // alternated, so that one barrier keeps a row's sums from the next row's
     const int l = threadIdx.x % L, wave = l / kWave;
     const uint32_t group = threadIdx.x / L;
     const int H = vpr * EV;
@@ -76,28 +77,43 @@ __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 
             for (int e = 0; e < EV; ++e) total += a[e];
         }
         total = group_sum<LW>(total);
-        float mean = total / share, m2 = 0.f;
+        float mean = total / share, rest = 0.f, m2 = 0.f;
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             float a[EV];
             unpack<BF16>(s[q], a);
             if (l + q * L < vpr)
 #pragma unroll
-                for (int e = 0; e < EV; ++e) m2 = __builtin_fmaf(a[e] - mean, a[e] - mean, m2);
+                for (int e = 0; e < EV; ++e) rest += a[e] - mean;
+        }
+        rest = group_sum<LW>(rest) / share;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            float a[EV];
+            unpack<BF16>(s[q], a);
+            if (l + q * L < vpr)
+#pragma unroll
+                for (int e = 0; e < EV; ++e) {
+                    const float c = a[e] - mean - rest;
+                    m2 = __builtin_fmaf(c, c, m2);
+                }
         }
         m2 = group_sum<LW>(m2);
         if constexpr (W > 1) {
             float *const p = part[parity];
             if (threadIdx.x % kWave == 0) {
                 p[wave] = total;
-                p[W + wave] = m2;
+                p[W + wave] = rest;
+                p[2 * W + wave] = m2;
             }
             __syncthreads();
             // lane v of each group of W joins wave v's share
             total = p[peer];
             mean = group_sum<W>(total) / (float)H;
-            const float c = total / fmaxf(of_peer, 1.f) - mean;
-            m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, p[W + peer]));
+            float c = total / fmaxf(of_peer, 1.f) - mean + p[W + peer];
+            rest = group_sum<W>(of_peer * c) / (float)H;
+            c -= rest;
+            m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, p[2 * W + peer]));
         }
         const float r = 1.f / __builtin_sqrtf(m2 / (float)H + eps);
 #pragma unroll
@@ -108,7 +124,7 @@ __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 
             unpack<BF16>(wv[q], g);
             unpack<BF16>(bv[q], b);
 #pragma unroll
-            for (int e = 0; e < EV; ++e) v[e] = __builtin_fmaf((v[e] - mean) * r, g[e], b[e]);
+            for (int e = 0; e < EV; ++e) v[e] = __builtin_fmaf((v[e] - mean - rest) * r, g[e], b[e]);
             const bool mine = live && i < vpr;
             if (mine && residual) store<STREAM>(sum + row * vpr + i, s[q]);
             if (mine && out) store<STREAM>(out + row * vpr + i, pack<BF16>(v));
@@ -135,6 +151,7 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
     constexpr int EV = Elem<BF16>::kPerVec, kRows = backward_threads_of<L>() / L, LW = L < kWave ? L : kWave, W = L > kWave ? L / kWave : 1;
     constexpr u32x4 zero = {0u, 0u, 0u, 0u};
     __shared__ f32x4 part[2][kRows][W];
+    __shared__ float rests[2][kRows][W];
     const int l = threadIdx.x % L, wave = l / kWave;
     const uint32_t group = threadIdx.x / L;
     const int H = vpr * EV;
@@ -181,7 +198,16 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
         }
         if (kAhead && base + gridDim.x * kRows < (uint32_t)T) fetch(base + gridDim.x * kRows);
         total = group_sum<LW>(total);
-        float mean = total / share, m2 = 0.f, g0 = 0.f, g1 = 0.f;
+        float mean = total / share, rest = 0.f, m2 = 0.f, g0 = 0.f, g1 = 0.f;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            float a[EV];
+            unpack<BF16>(s0[q], a);
+            if (l + q * L < vpr)
+#pragma unroll
+                for (int e = 0; e < EV; ++e) rest += a[e] - mean;
+        }
+        rest = group_sum<LW>(rest) / share;
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             float a[EV], b[EV], g[EV];
@@ -191,7 +217,7 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
             if (l + q * L < vpr)
 #pragma unroll
                 for (int e = 0; e < EV; ++e) {
-                    const float c = a[e] - mean, p = b[e] * g[e];
+                    const float c = a[e] - mean - rest, p = b[e] * g[e];
                     m2 = __builtin_fmaf(c, c, m2);
                     g0 += p;
                     g1 = __builtin_fmaf(c, p, g1);
@@ -202,11 +228,16 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
         g1 = group_sum<LW>(g1);
         if constexpr (W > 1) {
             f32x4 *const p = part[parity][group];
-            if (threadIdx.x % kWave == 0) p[wave] = (f32x4){total, m2, g0, g1};
+            if (threadIdx.x % kWave == 0) {
+                p[wave] = (f32x4){total, m2, g0, g1};
+                rests[parity][group][wave] = rest;
+            }
             __syncthreads();
             const f32x4 u = p[peer];
             mean = group_sum<W>(u[0]) / (float)H;
-            const float c = u[0] / fmaxf(of_peer, 1.f) - mean;
+            float c = u[0] / fmaxf(of_peer, 1.f) - mean + rests[parity][group][peer];
+            rest = group_sum<W>(of_peer * c) / (float)H;
+            c -= rest;
             m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, u[1]));
             g0 = group_sum<W>(u[2]);
             g1 = group_sum<W>(__builtin_fmaf(c, u[2], u[3]));
@@ -223,7 +254,7 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
             unpack<BF16>(t0[q], o);
 #pragma unroll
             for (int e = 0; e < EV; ++e) {
-                const float c = a[e] - mean;
+                const float c = a[e] - mean - rest;
                 o[e] = __builtin_fmaf(r, __builtin_fmaf(-c, c1, __builtin_fmaf(b[e], g[e], -c0)), o[e]);
                 if (live) {
                     dw[q][e] = __builtin_fmaf(b[e], c * r, dw[q][e]);
