@@ -243,7 +243,8 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
             g1 = group_sum<W>(__builtin_fmaf(c, u[2], u[3]));
         }
         const float r = 1.f / __builtin_sqrtf(m2 / (float)H + eps);
-        const float c0 = g0 / (float)H, c1 = r * r * (g1 / (float)H);       // dx = r (g - c0 - (s - m) c1) + dsum
+        // dx = r (g - c0 - (s - m) c1) + dsum; r * r is infinite where the spread is below 5e-20
+        const float c0 = g0 / (float)H, c1 = r * (r * (g1 / (float)H));
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             const int i = l + q * L;

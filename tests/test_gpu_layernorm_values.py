@@ -86,3 +86,11 @@ def check_gradient(m, x, dtype, eps, dsum, small=False):  # noqa: F811
     assert bool(((dx.double() - want).abs() <= want.abs() * half(dtype) + mag * (160 + 90 * F + 4 * S) * U).all())
     for got, terms, bar in ((dw, b * n, (b * n).abs() * (T // 256 + 120 + 30 + F + S) + b.abs() * (41 + 41 * F)), (db, b, b.abs() * (T // 256 + 120))):
         assert bool(((got.double() - terms.sum(0)).abs() <= U * bar.sum(0)).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [3e-20, 1e-10, 1e15])
+@pytest.mark.parametrize("H", [64, 768, 2064, 8192])
+def test_gradient_of_small_and_large_rows(m, H, dtype, scale):  # noqa: F811
+    """eps of zero: the square of r is no fp32 number where the spread is below 5e-20, but the gradient is."""
+    check_gradient(m, (normal(9, H, "f32", H).double() * scale).to(dt(dtype)), dtype, 0.0, 0, small=True)
