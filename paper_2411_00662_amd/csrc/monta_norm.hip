@@ -140,7 +140,8 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void rmsnorm_backward_ker
         if (kAhead && base + gridDim.x * kRows < (uint32_t)T) fetch(base + gridDim.x * kRows);
         row_sums<L>(sums, part[parity][group]);
         const float r = 1.f / __builtin_sqrtf(sums[0] / (float)H + eps);
-        const float c = r * r * (sums[1] / (float)H);               // dx = r (g - s c) + dsum
+        // dx = r (g - s c) + dsum.  r * r is infinite where the row's magnitude is below 5e-20; elsewhere the product from there keeps its rounding
+        const float rr = r * r, mean = sums[1] / (float)H, c = rr <= 3.4028234663852886e38f ? rr * mean : r * (r * mean);
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
             const int i = l + q * L;

@@ -94,3 +94,24 @@ def check_gradient(m, x, dtype, eps, dsum, small=False):  # noqa: F811
 def test_gradient_of_small_and_large_rows(m, H, dtype, scale):  # noqa: F811
     """eps of zero: the square of r is no fp32 number where the spread is below 5e-20, but the gradient is."""
     check_gradient(m, (normal(9, H, "f32", H).double() * scale).to(dt(dtype)), dtype, 0.0, 0, small=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [3e-20, 1e15])
+@pytest.mark.parametrize("H", [64, 768, 2064, 8192])
+def test_rms_gradient_of_small_and_large_rows(m, H, dtype, scale):  # noqa: F811
+    """The same of the norm without a mean, its bars as there."""
+    import torch
+    x = (normal(9, H, "f32", H).double() * scale).to(dt(dtype))
+    d, (w, _) = normal(9, H, dtype, 5), params(H, dtype, 7)
+    cfg = make(m, 9, H, dtype)
+    dx, dw = torch.empty_like(x), torch.empty(H, device="cuda")
+    m.monta_rmsnorm_backward(cfg, x, w, 0.0, d, None, dx, dw, torch.empty(m.monta_rmsnorm_scratch_bytes(cfg), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    a, b = x.double(), d.double()
+    r = 1 / (a ** 2).mean(1, keepdim=True).sqrt()
+    n, g, S = a * r, b * w.double(), r ** 2 * 2.0 ** -126
+    want = r * (g - n * (g * n).mean(1, keepdim=True))
+    mag = r * (g.abs() + n.abs() * (g * n).abs().mean(1, keepdim=True))
+    assert bool(((dx.double() - want).abs() <= want.abs() * half(dtype) + mag * (160 + 4 * S) * U).all())
+    assert bool(((dw.double() - (b * n).sum(0)).abs() <= U * ((b * n).abs() * (150 + S)).sum(0)).all())
