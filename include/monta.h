@@ -375,7 +375,7 @@ int monta_route_loss_scratch_bytes(const monta_cfg *cfg, size_t *bytes);
  * its values counts, whatever they are.  losses [2], means [E] fp32, counts [E + 1] int32.  A logit may be -infinity (p is 0 there), not all of a
  * token's; a NaN counts as -infinity.  An index outside 0 .. E - 1 counts for no expert.  scratch 16-byte aligned, its contents are of no use
  * afterwards and calls that overlap in time need one each.  Sums are held in fp32, their order is fixed for a shape.  Nothing that is written may share
- * memory with anything else.  +infinity, or -infinity throughout, gives NaN.  Uses tokens, experts and top_k of cfg (all of it is validated); needs no workspace. */
+ * memory with anything else.  +infinity, or -infinity throughout, gives NaN (both losses and all means).  Uses tokens, experts and top_k of cfg (all of it is validated); needs no workspace. */
 int monta_route_loss(const monta_cfg *cfg, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask, float *losses, int32_t *counts,
                      float *means, void *scratch, void *stream);
 

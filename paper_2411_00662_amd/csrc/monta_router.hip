@@ -71,8 +71,9 @@ __device__ __forceinline__ Softmax<V> softmax(const f32x4 (&v)[V])
         sum += e;
     }
     sum = group_sum<L>(sum);
-    s.lse = __builtin_fmaf(__builtin_amdgcn_logf(sum), 0.69314718056f, top);
     const float inv = __builtin_amdgcn_rcpf(sum);
+    // without a number, or with +infinity, the sum is 0: 0 times infinity makes that NaN as the probabilities are, and changes no other
+    s.lse = __builtin_fmaf(0.f, inv, __builtin_fmaf(__builtin_amdgcn_logf(sum), 0.69314718056f, top));
 #pragma unroll
     for (int i = 0; i < 4 * V; ++i) s.p[i / 4][i % 4] *= inv;
     return s;

@@ -1,0 +1,35 @@
+"""GPU: the router's losses and gradient of tokens that have no probabilities."""
+import pytest
+
+from test_gpu_router import inputs, m, make, run_grad, run_loss  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+# every number of lanes of a token; one workgroup, and several
+SIZES = [(3, 2, 1), (300, 4, 2), (5000, 4, 2), (300, 7, 2), (4097, 8, 2), (129, 16, 4), (2050, 33, 8), (8192, 64, 8), (100, 100, 4), (1111, 255, 8)]
+
+
+@pytest.mark.parametrize("T,E,k", SIZES)
+def test_tokens_without_probabilities(m, T, E, k):  # noqa: F811
+    """-infinity throughout, NaN throughout or +infinity give NaN in both losses, the means and the token's gradients; masked, nothing."""
+    import torch
+    logits, idx, gates, dgates, _ = inputs(T, E, k, T + E)
+    cfg, one = make(m, T, E, k), torch.ones(2, device="cuda")
+    mask = torch.ones(T, dtype=torch.uint8, device="cuda")
+    at = T // 2
+    mask[at] = 0
+    want = run_loss(m, cfg, logits, idx, mask)
+    grad = run_grad(m, cfg, logits, idx, gates, dgates, mask, one, want[1])
+    for values in (float("-inf"), float("nan"), None):
+        bad = logits.clone()
+        if values is None:
+            bad[at, E // 2] = float("inf")
+        else:
+            bad[at] = values
+        got = run_loss(m, cfg, bad, idx, None)
+        assert bool(torch.isnan(got[0]).all()) and bool(torch.isnan(got[2]).all()), (values, got[0])
+        assert got[1][E].item() == T and got[1][:E].sum().item() == T * k
+        d = run_grad(m, cfg, bad, idx, gates, dgates, None, one, got[1])
+        rest = torch.arange(T, device="cuda") != at
+        assert bool(torch.isnan(d[at]).all()) and bool(torch.isfinite(d[rest]).all())
+        assert all(torch.equal(a, b) for a, b in zip(run_loss(m, cfg, bad, idx, mask), want))
+        assert torch.equal(run_grad(m, cfg, bad, idx, gates, dgates, mask, one, want[1]), grad)
