@@ -39,7 +39,7 @@ __device__ __forceinline__ float group_sum(float v)
     return group_join<L>(v, [](float a, float b) { return a + b; });
 }
 
-// The larger of two numbers, or the one that is no NaN.  The instruction itself: around fmaxf the compiler puts others, which make a signalling NaN quiet.
+// The larger of two numbers, or the one that is no NaN; no signalling ones.  The instruction itself: around fmaxf the compiler puts others, which make those quiet.
 __device__ __forceinline__ float plain_max(float a, float b)
 {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -58,9 +58,9 @@ struct Softmax {
 template <int L, int V>
 __device__ __forceinline__ Softmax<V> softmax(const f32x4 (&v)[V])
 {
-    float top = v[0][0];
+    float top = kNone;
 #pragma unroll
-    for (int i = 1; i < 4 * V; ++i) top = plain_max(top, v[i / 4][i % 4]);
+    for (int i = 0; i < 4 * V; ++i) top = plain_max(top, __builtin_canonicalizef(v[i / 4][i % 4]));      // a NaN from memory may be a signalling one
     top = group_max<L>(top);
     Softmax<V> s;
     float sum = 0.f;
