@@ -5,8 +5,8 @@ and n gradients that are not zero make 3 n products and an addition each: (3 n +
 """
 import pytest
 
-from test_gpu_gate_grad import inputs, make, run
-from test_gpu_norm import U, half, m  # noqa: F401
+from test_gpu_gate_grad import inputs, layer, make, run, test_what_is_not_finite as what_is_not_finite
+from test_gpu_norm import U, half, m, normal  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,64 @@ def test_largest_numbers(m, T, H, E, dtype):  # noqa: F811
     for got, want, mag, h, n in ((dx, d @ w.double(), d.abs() @ w.double().abs(), half(dtype), 1),
                                  (dw, d.t() @ x.double(), d.abs().t() @ x.double().abs(), 0, -(-T // E))):
         assert bool(((got.double() - want).abs() <= want.abs() * h + mag * (3 * n + 8) * U).all())
+
+
+@pytest.mark.parametrize("E", [65, 100, 128, 129, 256])
+def test_what_is_not_finite_over_many_experts(m, E):  # noqa: F811
+    what_is_not_finite(m, E, "bf16")
+
+
+@pytest.mark.parametrize("E", [40, 100, 256])
+def test_many_experts_beyond_2gib(m, E):  # noqa: F811
+    """2.3 GB of rows over the experts' forms of their own: all rows are alike, and sums over tokens have few bits."""
+    import torch
+    T, H = 70003, 16384
+    cfg = make(m, T, H, E, "bf16")
+    dl = ((torch.arange(E, device="cuda") % 7 - 3) * 0.25).expand(T, E).contiguous()
+    x, w = normal(1, H, "bf16", 1).expand(T, H).contiguous(), normal(E, H, "bf16", 2)
+    dx, dw = run(m, cfg, dl, x, w, x)
+    d = dl[0].double()
+    want, mag = d @ w.double() + x[0].double(), d.abs() @ w.double().abs() + x[0].double().abs()
+    assert bool(((dx[0].double() - want).abs() <= want.abs() * 2.0 ** -8 + mag * (3 * E + 8) * U).all()) and bool((dx == dx[0]).all())
+    sums = T * d[:, None] * x[0].double()
+    shares = max(1, m.monta_gate_backward_scratch_bytes(cfg) // (E * H * 4))
+    assert bool(((dw.double() - sums).abs() <= sums.abs() * (T // shares + 64 + shares) * U).all())
+
+
+@pytest.mark.parametrize("E,T", [(40, 600), (100, 600), (256, 333)])
+def test_step_of_many_experts_in_a_graph_and_beside_another(m, E, T):  # noqa: F811
+    """A bf16 router's training step, captured and replayed with eager work between the replays, and two of them at once on streams of their own."""
+    import torch
+    cfg, t, o, step = layer(m, "bf16", T=T, E=E)
+    _, t2, o2, step2 = layer(m, "bf16", T=T, E=E)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (50, 51, 52):
+        for u in (t, t2):
+            u["x"].copy_(normal(cfg.tokens, cfg.hidden, "bf16", seed))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        step2()
+        torch.cuda.synchronize()
+        for name in o:
+            assert torch.equal(o[name], o2[name]), name
+            o[name].zero_()
+            o2[name].zero_()
+    del graph
+    step2()
+    pair, side = [layer(m, "bf16", T=T, E=E) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    for one in pair:
+        one[1]["x"].copy_(t2["x"])
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, one in zip(side, pair):
+            with torch.cuda.stream(s):
+                one[3]()
+    torch.cuda.synchronize()
+    for one in pair:
+        for name in o2:
+            assert torch.equal(one[2][name], o2[name]), name
