@@ -352,17 +352,7 @@ int with_gradient_row(int vpr, F f)
     if (vpr <= 128) return with_short_row(vpr, f);
     if (vpr <= 192) return f(integral_constant<int, 64>{}, integral_constant<int, 3>{});
     if (vpr <= 256) return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    return with_row_shape(vpr, f);
-}
-
-// f(bf16, streamed, lanes of a row, vectors of a lane), all of them as types
-template <typename Row, typename F>
-int with_types(bool bf16, bool streamed, Row row, F f)
-{
-    return row([&](auto lanes, auto vecs) {
-        if (bf16) return streamed ? f(std::true_type{}, std::true_type{}, lanes, vecs) : f(std::true_type{}, std::false_type{}, lanes, vecs);
-        return streamed ? f(std::false_type{}, std::true_type{}, lanes, vecs) : f(std::false_type{}, std::false_type{}, lanes, vecs);
-    });
+    return with_long_row(vpr, f);
 }
 
 // Workgroups of the gradient, and so rows of partial sums, each of which is written and read again and costs more than a row of the norm itself.  us, 256 and

@@ -145,25 +145,38 @@ __device__ __forceinline__ void clear_tail(unsigned char *row, int row8_bytes, i
 
 // f(lanes of a row, vectors of a lane): few lanes for short rows, so that no wave is mostly idle
 template <typename F>
+int with_long_row(int vpr, F f)             // more than 256 vectors
+{
+    using std::integral_constant;
+    if (vpr <= 512) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    if (vpr <= 1024) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+
+template <typename F>
 int with_row_shape(int vpr, F f)
 {
     using std::integral_constant;
     if (vpr <= 16) return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
     if (vpr <= 64) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
     if (vpr <= 256) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-    if (vpr <= 512) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    if (vpr <= 1024) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-    return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    return with_long_row(vpr, f);
 }
 
-// f(bf16, streamed, lanes of a row, vectors of a lane), all of them as types
-template <typename F>
-int with_form(bool bf16, bool streamed, int vpr, F f)
+// f(bf16, streamed, lanes of a row, vectors of a lane), all of them as types; `row` knows the last two
+template <typename Row, typename F>
+int with_types(bool bf16, bool streamed, Row row, F f)
 {
-    return with_row_shape(vpr, [&](auto lanes, auto vecs) {
+    return row([&](auto lanes, auto vecs) {
         if (bf16) return streamed ? f(std::true_type{}, std::true_type{}, lanes, vecs) : f(std::true_type{}, std::false_type{}, lanes, vecs);
         return streamed ? f(std::false_type{}, std::true_type{}, lanes, vecs) : f(std::false_type{}, std::false_type{}, lanes, vecs);
     });
+}
+
+template <typename F>
+int with_form(bool bf16, bool streamed, int vpr, F f)
+{
+    return with_types(bf16, streamed, [&](auto g) { return with_row_shape(vpr, g); }, f);
 }
 
 inline int rows_per_wg(int vpr) { return vpr <= 16 ? 16 : vpr <= 64 ? 4 : 1; }
