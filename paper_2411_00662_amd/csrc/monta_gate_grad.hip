@@ -21,7 +21,7 @@ struct GateGradArgs {
 // What workgroup `block` does: column block `col`, and of the steps of tokens every `shares`-th from the one numbered `share` on.  All workgroups so move through
 // the rows together, in one window of them for each buffer: with a run of neighbouring steps for each share 65536 x 7168 over 8 experts took 373 us in 18 runs and
 // 344 in nine, so 363 and 331.  Consecutive workgroups, which go to the XCDs in turn, have consecutive column blocks of a share: 369 us for 64 experts, 383 with
-// all blocks of a share on one XCD, although each XCD so reads dl for itself.
+// all blocks of a share on one XCD, although each XCD so reads dl for itself (both with two parts of dl for dx instead of three).
 struct GatePart {
     int share, col;
 };
@@ -182,8 +182,9 @@ __global__ __launch_bounds__(256, 2) void gate_backward_f32_kernel(GateGradArgs 
 // it, storing alone took 282 us of 65536 x 7168 over 8 experts, so 184.
 // Loads and stores go through descriptors that end at the last token, and lanes past the last column hand in an address past every descriptor: no
 // branch, every step issues the same number of them, also past the end, and the wait for a stage of x counts the younger ones.
-// 65536 x 7168, 64 experts: 1.9 GB in 365 to 377 us, 5.0 to 5.2 TB/s, of which the matrix pipe is busy 40 %; 8 experts 334 (5.6); 8192 x 4096, 8 experts, dadd: 201 MB
-// in 36 us and 3 for the sums of the shares.  (fp32 products 1552 and 58.)
+// 65536 x 7168, 64 experts: 1.9 GB in 400 to 415 us in a run of calls, 4.6 to 4.7 TB/s (the first three at the full clock 375, those after them up to 560, until the
+// clock has settled), of which the matrix pipe is busy 43 %; 8 experts 330 (5.7); 8192 x 4096, 8 experts, dadd: 201 MB in 36 us and 3 for the sums of the shares.  (fp32
+// products 1552 and 58.  With two parts of dl for dx 64 experts take 375, 32 327 for 338, 8 as long.)
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -468,8 +469,8 @@ __global__ __launch_bounds__(64 * NW, 2) void gate_backward_bf16_kernel([[maybe_
 //   dw: a wave has 64 experts and 64 columns.
 //   dx: a wave has 16 tokens of the step, all experts and a quarter of the workgroup's columns; the rows leave a step later, when all waves have written
 //       their parts of them.
-// 16384 x 4096 with dadd, 256 experts: 183 us (in waves of 32 columns, all experts: 283), 128 experts 103: 0.94 and 0.83 PFLOP/s of bf16 products, half of the
-// rate that the matrix pipe holds; the steps of both waves of a SIMD are in step.
+// 16384 x 4096 with dadd, 256 experts: 201 us, 128 experts 113: 1.03 and 0.91 PFLOP/s of bf16 products, the matrix pipe busy 49 and 43 % of the time; the steps of
+// both waves of a SIMD are in step.  (With two parts of dl for dx 183 and 103, and in waves of 32 columns, all experts, 283.)
 template <int EB>
 struct GateWide {
     static_assert(EB == 8 || EB == 16, "wide gate gradient: experts");
@@ -478,7 +479,7 @@ struct GateWide {
     static constexpr int EP = 16 * EB, KS = EP / 32;
     static constexpr int kRow = 2 * EP, kPiece = kSplitTokens * kRow, kDl = 3 * kPiece, kItemsEach = kSplitTokens * EP / 8 / kThreads;
     static constexpr int kRowX = 2 * BC, kX = kSplitTokens * kRowX, kLoadsX = kX / 1024 / kWaves, kPerRowX = BC / 8;
-    // the next step's dl is split before dw's products or after them, and the one after it requested then: 16384 x 4096, 256 experts 185 us and 202, 128 experts 108 and 105
+    // the next step's dl is split before dw's products or after them, and the one after it requested then: 16384 x 4096, 256 experts 201 us and 220, 128 experts 113.4 and 112.5
     static constexpr bool kSplitEarly = EB == 16;
     static constexpr int kLdsX = NST * kX, kLdsOut = 2 * kX, kLdsBytes = kLdsX + kLdsOut + 2 * kDl;
     static constexpr int kWeights = EP * BC * 2, kAtWeights = kLdsBytes - kWeights;      // before the first step, behind its stage
@@ -726,8 +727,8 @@ int with_expert_blocks(int E, F f)
 }
 
 // Eight waves share the split gradients of up to 64 experts, and twice as many columns are waited for together: from 2^27 elements on, where splitting takes time
-// (33 to 64 experts; us, four waves twice a CU, four waves and eight: 65536 x 7168 368, 407 and 363; 8192 x 7168 85, 79 and 85; 512 x 2048 14, 14 and 20;
-// but 65536 x 7168 with 32 experts 363, 325 and 340).
+// (33 to 64 experts; us, four waves twice a CU, four waves and eight: 65536 x 7168 406, 459 and 411, with dadd 577, 585 and 521; 32768 x 4096 with dadd 160, 170 and 158;
+// but 8192 x 7168 85, 82 and 88; 512 x 2048 14, 14 and 18; 65536 x 7168 with 32 experts 366, 339 and 340).
 bool eight_waves(const Call &c) { return (int64_t)c.s.T * c.H >= (1 << 27); }
 
 struct GatePlan {
@@ -746,8 +747,8 @@ GatePlan plan_gate_grad(const Call &c)
     p.blocks = (c.H + width - 1) / width;
     // one step a share where there are few: 1155 x 516 fp32 8.6 us, with four steps 10.7; but up to 64 tokens alone, without a second launch: 64 x 4096 bf16 6.1
     // us, in two shares 7.1
-    // Workgroups: one a CU where memory is the bound, two where products are (fp32 from 33 experts on).  us, one and two a CU: 65536 x 7168 bf16, 32 experts 325 and
-    // 363, 8 experts 334 and 352 (but 131072 x 4096 364 and 356); 8192 x 4096 fp32, 8, 32, 64 and 128 experts 75.5, 79.8, 106, 195 and 76.9, 83.4, 107, 172.
+    // Workgroups: one a CU where memory is the bound, two where products are (fp32 from 33 experts on).  us, one and two a CU: 65536 x 7168 bf16, 32 experts 339 and
+    // 366, 8 experts 330 and 352, 131072 x 4096 332 and 346, 16384 x 4096 over 256 201 and 214; 8192 x 4096 fp32, 8, 32, 64 and 128 experts 75.5, 79.8, 106, 195 and 76.9, 83.4, 107, 172.
     const int wgs = c.bf16 || c.s.E <= 32 ? 256 : 512;
     const int64_t T = c.s.T, step = c.bf16 ? kSplitTokens : kStepTokens;
     p.shares = (int)std::min<int64_t>(std::max(1, wgs / p.blocks), T <= 64 ? 1 : (T + step - 1) / step);
@@ -795,7 +796,8 @@ int monta_gate_backward(const monta_cfg *cfg, const float *dlogits, const void *
         if (!w.p) continue;
         for (const auto &r : read) {
             if (!r.p) continue;
-            // an element of dadd is read by the lane that stores dx there: dx may be dadd as a whole, unless that is another argument, too
+            // a step's part of dadd is in registers before anything of the step's dx is stored, by the same lane (fp32), the same wave or behind a
+            // barrier (bf16, more than 64 experts): dx may be dadd as a whole, unless that is another argument, too
             if (w.p == dx && &r == &read[3] ? !same_or_apart(dx, dadd, n) : overlap(w.p, w.n, r.p, r.n)) return MONTA_ERR_INVALID;
         }
         for (const auto &o : written)

@@ -142,7 +142,8 @@ __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 
 // With n = (s - m) r and g = dout w:  dx = r (g - mean(g) - n mean(g n)) + dsum,  dw = sum over the rows of dout n,  db = that of dout.
 // A workgroup walks over rows and keeps the weight's and the bias's shares in registers; the next row is requested before the present one's
 // sums are known.  Both gradients' partial sums, 2 H in a row per workgroup, are added by layernorm_dparams_kernel: a fixed order, no atomics.  Of few
-// rows one workgroup writes the gradients itself.  8192 x 4096 bf16 with dsum: 268 MB in 45 us and 4 for the partial sums, 5.4 TB/s.
+// rows one workgroup writes the gradients itself.  8192 x 4096 bf16 with dsum: 268 MB in 53 us, 4 of them for the partial sums,
+// 5.1 TB/s.
 template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_kernel(const u32x4 *s_in, const u32x4 *w, const u32x4 *dout, const u32x4 *dsum,
                                                                                       u32x4 *dx, float *partial, float *dweight, float *dbias, int T, int vpr,
@@ -326,9 +327,9 @@ __global__ __launch_bounds__(1024) void layernorm_dparams_kernel(const float *pa
 // --------------------------------------------------------------------------------------------- host
 
 // f(lanes of a row, vectors of a lane): lanes of one wave as far as their registers go, since a row of several waves meets at a barrier, and no more
-// than the row has vectors for.  us, these forms and one vector for each of 64 or 256 lanes: norm of 16384 x 768 bf16 19.1 and 28.7, 16384 x 1024 25.8 and
-// 30.5, 65536 x 256 26.4 and 31.5; its gradient 22.5 and 55.4, 28.2 and 57.3, 28.3 and 44.9.  Beyond 128 vectors the norm has no use for it (8192 x 2048 in
-// one wave 27.1, in four 26.0), its gradient has (32.6 and 35.3; 16384 x 1536 42.2 and 61, with four vectors 43.9).
+// than the row has vectors for.  us, these forms and one vector for each of 64 or 256 lanes: norm of 16384 x 768 bf16 20.7 and 34.4, 16384 x 1024 26.3 and
+// 34.6, 65536 x 256 25.9 and 32.9; its gradient 26.7 and 62.0, 29.3 and 64.0, 29.4 and 49.9.  Beyond 128 vectors the norm has no use for it (8192 x 2048 in
+// one wave 27.5, in four 26.3), its gradient has (34.0 and 38.9; 16384 x 1536 43.7 and 67.9, with four vectors 46.2).
 template <typename F>
 int with_short_row(int vpr, F f)
 {
@@ -356,12 +357,12 @@ int with_gradient_row(int vpr, F f)
 }
 
 // Workgroups of the gradient, and so rows of partial sums, each of which is written and read again and costs more than a row of the norm itself.  us, 256 and
-// 512 of them: 8192 x 2048 bf16 32.6 and 37.6, 16384 x 1024 28.2 and 29.6, but 48222 x 120 13.8 and 12.8.  One workgroup has whole sums and needs no second
-// launch, which gains as long as its rounds take less than that one: us, one workgroup and two launches, 4 rounds of lanes with one vector 4.7 to 5.0 and 6.1
-// (128 to 512 features, bf16), 6 rounds 6.0 to 6.5 and 6.1; of more vectors, 2 rounds 4.6 and 6.1 (1024 features), 7.8 and 7.8 (2048), 6.9 and 7.4 (4096),
-// 12.0 and 12.6 (8192), 3 rounds 5.6 and 6.1, 10.0 and 7.8, 8.8 and 7.4, 13.7 and 12.7.  Of more vectors as few as have the same number of rounds: us, 256 and
-// so many, 1155 x 516 fp32 8.2 and 7.4, 1100 x 2048 bf16 12.8 and 11.7, 600 x 4096 13.2 and 11.8, 300 x 8192 21.4 and 17.9, but with one vector 9000 x 256 8.8
-// and 9.1.
+// 512 of them: 8192 x 2048 bf16 34.0 and 39.0, 16384 x 1024 29.3 and 30.2 (but 16384 x 768 26.7 and 24.0, 16384 x 1536 43.7 and 40.3), of one vector 65536 x 256 34.4
+// and 29.4, 48222 x 120 15.5 and 13.7.  One workgroup has whole sums and needs no second launch, which gains as long as its rounds take less than that one: us, one
+// workgroup and two launches, 4 rounds of lanes with one vector 5.4 to 5.8 and 7.8 to 8.2 (128 and 512 features, bf16), 6 rounds 6.0 to 7.3 and 6.1 to 8.0; of more
+// vectors, 2 rounds 5.3 and 8.0 (1024 features), 8.2 and 9.1 (2048), 7.6 and 8.7 (4096), 12.6 and 13.1 (8192), 3 rounds 6.1 and 8.2, 10.6 and 9.0, 9.6 and 8.7,
+// 14.7 and 13.1.  Of more vectors as few as have the same number of rounds: us, 256 and so many, 1100 x 2048 bf16 13.3 and 12.4, 600 x 4096 13.8 and 12.5, 300 x 8192
+// 21.8 and 18.4 (1155 x 516 fp32 7.9 to 9.0 and 8.2 to 8.5, by where the library is loaded), but with one vector 9000 x 256 10.0 and 10.5.
 struct GradientGrid {
     int workgroups, most;           // the most of any call of as many tokens or fewer: scratch for more tokens does for fewer
 };
