@@ -5,12 +5,17 @@
 namespace monta {
 namespace {
 
-// Sums around a mean that is not known yet.  A mean is two numbers: that of a first sum, which is off by some 2^-24 of the row's magnitude and may so be further
-// from the row than the row is spread, and the mean of the differences from it, off by that of those (fp32 rows at 1e4: outputs off by 1e-5 instead of 0.5).  It
-// costs a pass over the registers, 1 to 3 us of the 50 of 8192 x 4096.  A wave takes its own share's mean m_w and its other sums around that; the waves' shares are then joined by
+// Sums around a mean that is not known yet.  A wave takes its own share's mean m_w, from a first sum, and its other sums around that;
+// the waves' shares are then joined by
 //   sum (s - m)^2 = sum_w [ M2_w + n_w d_w^2 ],   sum g (s - m) = sum_w [ G1_w + d_w G0_w ],   d_w = m_w - m,
-// which has no difference of large numbers, and takes one barrier for all steps.  Means are quotients: from a product with 1 / n the compiler may make a
+// which has no difference of large numbers, and takes one barrier for both steps.  Means are quotients: from a product with 1 / n the compiler may make a
 // fused difference for some elements of a row and not for others, and a row of equal numbers would not have a spread of zero.
+//
+// The first sum is off by some 2^-24 of the row's magnitude, which may be more than the row is spread: fp32 rows of equal numbers at 12345 came out as 0.5 instead of
+// 0.  So where a mean is larger than the spread around it, the mean of the differences from it, `rest`, is a second part of it, and the other sums are taken
+// again around both: off by 2^-24 of the spread, for two more passes over the registers of such rows (8192 x 4096 bf16 with a mean of 50 spreads 52.3 us instead of
+// 51.3, the gradient 57.8 instead of 52).  Elsewhere the first sum's error is one of the spread's magnitude already: a second part has as much, and for bf16 rows,
+// whose sums are mostly exact, more (codes that differ from those of 64 bits 371 for 240 of 268 million).
 //
 // Elements of a row that wave w of its L lanes holds, NV vectors of EV elements a lane.
 template <int L, int NV, int EV>
@@ -26,7 +31,7 @@ __device__ __forceinline__ float wave_share(int vpr, int w)
 //
 //   s = x + residual, rounded to the activation type and stored; m = mean(s), r = 1 / sqrt(mean((s - m)^2) + eps); v = (s - m) r w + b
 //   out = v rounded once; codes and scales of v as in monta_rmsnorm.
-// 8192 x 4096 bf16 with a residual, both outputs: 303 MB in 52 us, 5.8 TB/s; the root-mean-square norm, with one sum and no barrier's wait less, takes 48.
+// 8192 x 4096 bf16 with a residual, both outputs: 303 MB in 51 us, 5.9 TB/s; the root-mean-square norm, with one sum and no barrier's wait less, takes 48.
 template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 *x, const u32x4 *residual, const u32x4 *w, const u32x4 *bias, u32x4 *sum,
                                                                     u32x4 *out, unsigned char *rows8, int T, int vpr, int row8_bytes, float eps)
@@ -84,21 +89,38 @@ __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 
             unpack<BF16>(s[q], a);
             if (l + q * L < vpr)
 #pragma unroll
-                for (int e = 0; e < EV; ++e) rest += a[e] - mean;
-        }
-        rest = group_sum<LW>(rest) / share;
-#pragma unroll
-        for (int q = 0; q < NV; ++q) {
-            float a[EV];
-            unpack<BF16>(s[q], a);
-            if (l + q * L < vpr)
-#pragma unroll
-                for (int e = 0; e < EV; ++e) {
-                    const float c = a[e] - mean - rest;
-                    m2 = __builtin_fmaf(c, c, m2);
-                }
+                for (int e = 0; e < EV; ++e) m2 = __builtin_fmaf(a[e] - mean, a[e] - mean, m2);
         }
         m2 = group_sum<LW>(m2);
+        const bool far = share * mean * mean > m2;
+        if (__any(far)) {                                          // a wave may have several rows: each has its own sums only
+            float more = 0.f, again = 0.f;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                float a[EV];
+                unpack<BF16>(s[q], a);
+                if (l + q * L < vpr)
+#pragma unroll
+                    for (int e = 0; e < EV; ++e) more += a[e] - mean;
+            }
+            more = group_sum<LW>(more) / share;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                float a[EV];
+                unpack<BF16>(s[q], a);
+                if (l + q * L < vpr)
+#pragma unroll
+                    for (int e = 0; e < EV; ++e) {
+                        const float c = a[e] - mean - more;
+                        again = __builtin_fmaf(c, c, again);
+                    }
+            }
+            again = group_sum<LW>(again);
+            if (far) {
+                rest = more;
+                m2 = again;
+            }
+        }
         if constexpr (W > 1) {
             float *const p = part[parity];
             if (threadIdx.x % kWave == 0) {
@@ -111,9 +133,14 @@ __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 
             total = p[peer];
             mean = group_sum<W>(total) / (float)H;
             float c = total / fmaxf(of_peer, 1.f) - mean + p[W + peer];
-            rest = group_sum<W>(of_peer * c) / (float)H;
-            c -= rest;
-            m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, p[2 * W + peer]));
+            const float inside = p[2 * W + peer];
+            m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, inside));
+            rest = 0.f;
+            if ((float)H * mean * mean > m2) {
+                rest = group_sum<W>(of_peer * c) / (float)H;
+                c -= rest;
+                m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, inside));
+            }
         }
         const float r = 1.f / __builtin_sqrtf(m2 / (float)H + eps);
 #pragma unroll
@@ -142,8 +169,8 @@ __global__ __launch_bounds__(threads_of<L>()) void layernorm_kernel(const u32x4 
 // With n = (s - m) r and g = dout w:  dx = r (g - mean(g) - n mean(g n)) + dsum,  dw = sum over the rows of dout n,  db = that of dout.
 // A workgroup walks over rows and keeps the weight's and the bias's shares in registers; the next row is requested before the present one's
 // sums are known.  Both gradients' partial sums, 2 H in a row per workgroup, are added by layernorm_dparams_kernel: a fixed order, no atomics.  Of few
-// rows one workgroup writes the gradients itself.  8192 x 4096 bf16 with dsum: 268 MB in 53 us, 4 of them for the partial sums,
-// 5.1 TB/s.
+// rows one workgroup writes the gradients itself.  8192 x 4096 bf16 with dsum: 268 MB in 52 us, 4 of them for the partial sums,
+// 5.2 TB/s.
 template <bool BF16, int L, int NV, bool STREAM>
 __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_kernel(const u32x4 *s_in, const u32x4 *w, const u32x4 *dout, const u32x4 *dsum,
                                                                                       u32x4 *dx, float *partial, float *dweight, float *dbias, int T, int vpr,
@@ -202,15 +229,6 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
         float mean = total / share, rest = 0.f, m2 = 0.f, g0 = 0.f, g1 = 0.f;
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
-            float a[EV];
-            unpack<BF16>(s0[q], a);
-            if (l + q * L < vpr)
-#pragma unroll
-                for (int e = 0; e < EV; ++e) rest += a[e] - mean;
-        }
-        rest = group_sum<LW>(rest) / share;
-#pragma unroll
-        for (int q = 0; q < NV; ++q) {
             float a[EV], b[EV], g[EV];
             unpack<BF16>(s0[q], a);
             unpack<BF16>(d0[q], b);
@@ -218,7 +236,7 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
             if (l + q * L < vpr)
 #pragma unroll
                 for (int e = 0; e < EV; ++e) {
-                    const float c = a[e] - mean - rest, p = b[e] * g[e];
+                    const float c = a[e] - mean, p = b[e] * g[e];
                     m2 = __builtin_fmaf(c, c, m2);
                     g0 += p;
                     g1 = __builtin_fmaf(c, p, g1);
@@ -227,6 +245,42 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
         m2 = group_sum<LW>(m2);
         g0 = group_sum<LW>(g0);
         g1 = group_sum<LW>(g1);
+        const bool far = share * mean * mean > m2;
+        if (__any(far)) {
+            float more = 0.f, again = 0.f, again1 = 0.f;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) asm volatile("" : "+v"(s0[q]), "+v"(d0[q]));      // unpacked anew: 1024 lanes have no registers for both forms
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                float a[EV];
+                unpack<BF16>(s0[q], a);
+                if (l + q * L < vpr)
+#pragma unroll
+                    for (int e = 0; e < EV; ++e) more += a[e] - mean;
+            }
+            more = group_sum<LW>(more) / share;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                float a[EV], b[EV], g[EV];
+                unpack<BF16>(s0[q], a);
+                unpack<BF16>(d0[q], b);
+                unpack<BF16>(wv[q], g);
+                if (l + q * L < vpr)
+#pragma unroll
+                    for (int e = 0; e < EV; ++e) {
+                        const float c = a[e] - mean - more;
+                        again = __builtin_fmaf(c, c, again);
+                        again1 = __builtin_fmaf(c, b[e] * g[e], again1);
+                    }
+            }
+            again = group_sum<LW>(again);
+            again1 = group_sum<LW>(again1);
+            if (far) {
+                rest = more;
+                m2 = again;
+                g1 = again1;
+            }
+        }
         if constexpr (W > 1) {
             f32x4 *const p = part[parity][group];
             if (threadIdx.x % kWave == 0) {
@@ -237,9 +291,13 @@ __global__ __launch_bounds__(backward_threads_of<L>()) void layernorm_backward_k
             const f32x4 u = p[peer];
             mean = group_sum<W>(u[0]) / (float)H;
             float c = u[0] / fmaxf(of_peer, 1.f) - mean + rests[parity][group][peer];
-            rest = group_sum<W>(of_peer * c) / (float)H;
-            c -= rest;
             m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, u[1]));
+            rest = 0.f;
+            if ((float)H * mean * mean > m2) {
+                rest = group_sum<W>(of_peer * c) / (float)H;
+                c -= rest;
+                m2 = group_sum<W>(__builtin_fmaf(of_peer * c, c, u[1]));
+            }
             g0 = group_sum<W>(u[2]);
             g1 = group_sum<W>(__builtin_fmaf(c, u[2], u[3]));
         }
