@@ -89,6 +89,30 @@ def check_gradient(m, x, dtype, eps, dsum, small=False):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H", [16, 64, 96, 128, 256, 528, 768, 1040, 2064, 4096, 8192])
+def test_rows_keep_to_themselves(m, H, dtype):  # noqa: F811
+    """Rows with a mean far above their spread, and with a NaN, among others: those have the bits that they have among their like."""
+    import torch
+    T = 37
+    x, d = normal(T, H, dtype, 11), normal(T, H, dtype, 12)
+    w, b = params(H, dtype, 13)
+    mixed = x.clone()
+    mixed[1::4] += 1000
+    mixed[7::8, H // 2] = float("nan")
+    cfg = make(m, T, H, dtype)
+    same = torch.ones(T, dtype=torch.bool, device="cuda")
+    same[1::4] = same[7::8] = False
+    outs = []
+    for s in (x, mixed):
+        dx, dw, db = torch.empty_like(x), torch.empty(H, device="cuda"), torch.empty(H, device="cuda")
+        m.monta_layernorm_backward(cfg, s, w, 1e-5, d, None, dx, dw, db, torch.empty(m.monta_layernorm_scratch_bytes(cfg), dtype=torch.uint8, device="cuda"))
+        outs.append((run_norm(m, s, None, w, b, dtype, fp8=False)[1], dx, db))
+    for one, other in list(zip(*outs))[:2]:
+        assert torch.equal(one[same], other[same]) and bool(torch.isnan(other[7::8]).all()) and bool(torch.isfinite(other[1::4]).all())
+    assert torch.equal(outs[0][2], outs[1][2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [3e-20, 1e-10, 1e15])
 @pytest.mark.parametrize("H", [64, 768, 2064, 8192])
 def test_gradient_of_small_and_large_rows(m, H, dtype, scale):  # noqa: F811
