@@ -2,7 +2,7 @@
 //
 // A token's E logits belong to L lanes of a wave with V vectors of four each, E <= 4 L V: vector v of lane l is that of experts 4 (v L + l) and on.  Sums over
 // a token's experts are moves between its lanes, and what they, a logarithm and a quotient cost falls with the number of lanes: the gradient of 32768 tokens
-// over 256 experts takes 21 us with 64 lanes, 19 with 16.
+// over 256 experts takes 21 us with 64 lanes, 19 with 16 (both stored through the cache).
 #include "monta_internal.hpp"
 #include "monta_lanes.hpp"
 
@@ -277,15 +277,15 @@ __global__ __launch_bounds__(256) void route_loss_join_kernel(float *partial, Lo
 //   dl[e] += p[e] ( b / n (f[e] - sum_i p[i] f[i]) + 2 c / n lse ).
 // A workgroup takes 256 / L tokens.  A thread has a pair: it goes over its token's pairs in LDS for D, and puts what its expert gets (once, by the
 // first of its pairs if an expert is named twice) into the token's row in LDS, which the token's lanes then add to what p asks for.  The next tokens' logits and
-// pairs are on their way meanwhile.  32768 tokens over 256 experts, top-8: 70 MB in 19 us, 65536 over 64 40 MB in 11: 4.2 TB/s with the
-// launch taken off where the logits' gradients stay in the cache for who reads them next, 4.8 past it, beside vector instructions in half of a SIMD's cycles.  A form without barriers,
+// pairs are on their way meanwhile.  32768 tokens over 256 experts, top-8: 70 MB in 17 us, 65536 over 64 40 MB in 11: 4.8 TB/s with the
+// launch taken off, beside vector instructions in half of a SIMD's cycles.  A form without barriers,
 // each wave with rows of its own in LDS, takes as long.
 
 constexpr int kGradThreads = 256, kRouteGrid = 1024;
-// From 2^21 logits on they go past the cache, up to 128 experts; those of more are read again by each of the gate's gradient's column blocks.  us, stored plainly
-// and streamed, alone and with monta_gate_backward behind: 65536 x 64 12.1 / 77.6 and 11.1 / 76.0, 16384 x 128 7.9 / 46.0 and 7.0 / 45.8, but 32768 x 256
-// 18.6 / 81.7 and 16.8 / 84.7; 16384 x 64 5.6 / 44.7 and 5.3 / 44.9.
-inline bool stream_logits(int64_t T, int64_t E) { return T * E >= (1 << 21) && E <= 128; }
+// From 2^21 logits on their gradients go past the cache.  us, stored plainly and streamed, alone and with monta_gate_backward of so many features behind: 65536 x 64
+// 12.4 / 83.6 and 11.4 / 83.2 (1024 features), 16384 x 128 7.7 / 48.4 and 6.9 / 48.3 (1024), 8192 x 256 7.8 / 108 and 7.2 / 108 (4096), 32768 x 256 18.6 / 80.1 and 16.7 /
+// 80.1 (512), 65536 x 256 35.5 / 397 and 28.8 / 401 (2048); 16384 x 64, fewer, 5.7 / 78.6 and 5.7 / 78.8 (4096).
+inline bool stream_logits(int64_t T, int64_t E) { return T * E >= 1 << 21; }
 
 struct RouteGradArgs {
     const float *logits, *gates, *dgates, *dlosses;
