@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256, 2) void gate_backward_f32_kernel(GateGradArgs 
 // Loads and stores go through descriptors that end at the last token, and lanes past the last column hand in an address past every descriptor: no
 // branch, every step issues the same number of them, also past the end, and the wait for a stage of x counts the younger ones.
 // 65536 x 7168, 64 experts: 1.9 GB in 400 to 415 us in a run of calls, 4.6 to 4.7 TB/s (the first three at the full clock 375, those after them up to 560, until the
-// clock has settled), of which the matrix pipe is busy 43 %; 8 experts 330 (5.7); 8192 x 4096, 8 experts, dadd: 201 MB in 36 us and 3 for the sums of the shares.  (fp32
+// clock has settled), of which the matrix pipe is busy 42 %; 8 experts 330 (5.7); 8192 x 4096, 8 experts, dadd: 201 MB in 36 us and 3 for the sums of the shares.  (fp32
 // products 1552 and 58.  With two parts of dl for dx 64 experts take 375, 32 327 for 338, 8 as long.)
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
